@@ -51,8 +51,14 @@ typedef enum {
     OZIMMU_ERR_WORKSPACE = 5,      /* workspace null, misaligned or too small */
     OZIMMU_ERR_HIP = 6,            /* a HIP call or kernel launch failed */
     OZIMMU_ERR_NOT_IMPLEMENTED = 7,
-    OZIMMU_ERR_TOO_LARGE = 8       /* the product needs more scratch than ozimmu_dgemm_static holds */
+    OZIMMU_ERR_TOO_LARGE = 8,      /* the product needs more scratch than ozimmu_dgemm_static holds */
+    OZIMMU_ERR_BAD_TYPE = 9,       /* not an ozimmu_type_t */
+    OZIMMU_ERR_BAD_POLYNOMIAL = 10,/* ozimmu_orthogonalize: steps, coefficients or eps it does not take */
+    OZIMMU_ERR_MISALIGNED = 11     /* a pointer that is not aligned as its values ask for */
 } ozimmu_status_t;
+
+/* Types of the matrices that the operators on weights take (the FP64 products take doubles only). */
+typedef enum { OZIMMU_F32 = 0, OZIMMU_BF16 = 1, OZIMMU_F16 = 2 } ozimmu_type_t;
 
 #define OZIMMU_MAX_SLICES 16
 #define OZIMMU_SLICE_BITS 7          /* Table 2: INT8-INT32 keeps 7 magnitude bits per slice */
@@ -62,6 +68,8 @@ typedef enum {
 #define OZIMMU_MAX_DIM 4194304       /* largest m, n or k accepted (2^22); beyond: OZIMMU_ERR_BAD_DIM */
 #define OZIMMU_INT32_BLOCK 131072    /* at most 2^17 INT8 products go into one INT32 sum:
                                         2^17 * 127^2 < 2^31 (the exact limit is 133144) */
+#define OZIMMU_MAX_BATCH 65535       /* matrices in one ozimmu_orthogonalize */
+#define OZIMMU_MAX_STEPS 64          /* of its iteration */
 #define OZIMMU_WORKSPACE_ALIGN 256
 #define OZIMMU_STATIC_SCRATCH_BYTES 67108864   /* 64 MiB: the built-in scratch of ozimmu_dgemm_static */
 
@@ -352,6 +360,68 @@ ozimmu_status_t ozimmu_zgemm_blas_auto(char transa, char transb, int64_t m, int6
                                        int max_slices, int guess, void* workspace, size_t workspace_bytes,
                                        void* scratch, size_t scratch_bytes, int* num_slices,
                                        int* guess_confirmed, void* stream);
+
+/*
+ * Weights in four bits. A weight matrix W (n x k, row-major: n outputs, k inputs) is cut the way the FP64 operands are, into small
+ * integers under a scale, but into one slice of four bits and with a scale for every `group` (32, 64 or 128) positions
+ * of a row. For each group, with T the type of the scales and RN32 the rounding to 32-bit:
+ *     s = RN_T( RN32( max |w| / 7 ) ),   c = the integer nearest to w / s (ties to even), clamped to [-8, 7];
+ * s = 0 gives c = 0, and so does an s that is not finite (the weight s c is then NaN). Layout:
+ *   codes   c + 8 in four bits, two positions to a byte, the even one in the low half. A row has ozimmu_q4_geometry's
+ *           `row_bytes` = 16 * ceil(k / 32) bytes; ldq (bytes between rows) is at least that and a multiple of 16, and codes are
+ *           16-byte aligned. What stands beyond position k of a row is written by the cut and ignored by everything else.
+ *   scales  n x ceil(k / group), row-major, lds values between rows; the last group of a row may be a part of one.
+ *
+ * ozimmu_q4_split cuts W (type `type`, ldw >= k); ozimmu_q4_expand writes the weights s c, rounded once to `type`, which is the
+ * type of the scales too.
+ *
+ * ozimmu_q4_gemm:      Y = X W^T   (X: t x k, Y: t x n: t tokens through the layer)
+ * ozimmu_q4_gemm_grad: dX = dY W   (dY: t x n, dX: t x k: the gradient on its way back through it)
+ * X, Y, dY, dX and the scales have type `type`; the sums are formed in 32 bits and rounded once. With up to sixteen tokens ozimmu_q4_gemm
+ * multiplies the codes themselves and applies the scales to the sums, in 32 bits. All other products go through an operand of the weights in the
+ * workspace: s c rounded once to bf16 or fp16, or, for 32-bit types, both operands as two fp16 slices under a
+ * power-of-two exponent per row (22 bits and more of every value that is within 2^-17 of its row's largest; the rest to 2^-39
+ * of that; the exponent goes with the group for the columns of W). A token or gradient row that holds an infinity or a NaN gives NaN where its results are not
+ * finite; every other row is what it would be without it. Empty dimensions: t = 0 or no outputs: nothing to do; an empty inner dimension
+ * gives zeros. Outputs must not overlap inputs or the workspace.
+ * workspace: ozimmu_q4_workspace_bytes(...) bytes, OZIMMU_WORKSPACE_ALIGN-aligned; may be null where that is 0.
+ * Errors: OZIMMU_ERR_BAD_DIM (sizes or group), OZIMMU_ERR_BAD_TYPE, OZIMMU_ERR_BAD_LD (also ldq), OZIMMU_ERR_NULL, OZIMMU_ERR_MISALIGNED,
+ * OZIMMU_ERR_WORKSPACE.
+ */
+ozimmu_status_t ozimmu_q4_geometry(int64_t k, int group, int64_t* row_bytes, int64_t* groups);
+ozimmu_status_t ozimmu_q4_split(int64_t n, int64_t k, int group, ozimmu_type_t type, const void* W, int64_t ldw,
+                                uint8_t* codes, int64_t ldq, ozimmu_type_t scale_type, void* scales, int64_t lds,
+                                void* stream);
+ozimmu_status_t ozimmu_q4_expand(int64_t n, int64_t k, int group, ozimmu_type_t type, const uint8_t* codes,
+                                 int64_t ldq, const void* scales, int64_t lds, void* W, int64_t ldw, void* stream);
+ozimmu_status_t ozimmu_q4_workspace_bytes(int64_t t, int64_t n, int64_t k, int group, ozimmu_type_t type,
+                                          int gradient, size_t* bytes);
+ozimmu_status_t ozimmu_q4_gemm(int64_t t, int64_t n, int64_t k, int group, ozimmu_type_t type, const void* X,
+                               int64_t ldx, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds,
+                               void* Y, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
+ozimmu_status_t ozimmu_q4_gemm_grad(int64_t t, int64_t n, int64_t k, int group, ozimmu_type_t type, const void* dY,
+                                    int64_t lddy, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds,
+                                    void* dX, int64_t lddx, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Orthogonal update (Newton-Schulz): `batch` matrices G (m x n, row-major, ldg values between rows, stride_g between matrices) become
+ *     X_0 = G / (|G| + eps)   (Frobenius norm),   X_{i+1} = a X_i + (b A + c A^2) X_i  with  A = X_i X_i^T,   X = X_steps,
+ * where for m > n the iteration runs on the transposed matrix: every singular value s of X_0 becomes p(p(...p(s))),
+ * p(x) = a x + b x^3 + c x^5, and the singular vectors stay. (a, b, c) = (3.4445, -4.7750, 2.0315) with five steps takes
+ * what is not far below the largest into 0.7 .. 1.2; (1.5, -0.5, 0) is the plain iteration for the nearest orthogonal matrix. G and X
+ * have type `type`; X may be G (same strides), and otherwise must not overlap it. The norm is summed in 64 bits. Everything between is held as two fp16 slices under a common power of two
+ * (22 bits and more), multiplied as three products with sums in 32 bits: errors are those of an iteration in 32 bits. A matrix of zeros gives zeros; one with an infinity or a NaN
+ * gives NaN in places that are not specified, and does not touch the others of its batch.
+ * steps in 1 .. OZIMMU_MAX_STEPS, eps >= 0 and finite, a >= 1 (small singular values must not shrink: they are held to 2^-38 absolutely, or as
+ * much more as intermediate values exceed four), and the polynomial must keep [0, 1] bounded under its iteration, so that no
+ * intermediate value exceeds 4096: otherwise OZIMMU_ERR_BAD_POLYNOMIAL. batch <= OZIMMU_MAX_BATCH; matrices of X must not overlap each other.
+ * workspace: ozimmu_orthogonalize_workspace_bytes(...) bytes, OZIMMU_WORKSPACE_ALIGN-aligned. m or n or batch = 0: nothing to do.
+ */
+ozimmu_status_t ozimmu_orthogonalize_workspace_bytes(int64_t batch, int64_t m, int64_t n, size_t* bytes);
+ozimmu_status_t ozimmu_orthogonalize(int64_t batch, int64_t m, int64_t n, ozimmu_type_t type, const void* G,
+                                     int64_t ldg, int64_t stride_g, void* X, int64_t ldx, int64_t stride_x, int steps,
+                                     double a, double b, double c, double eps, void* workspace, size_t workspace_bytes,
+                                     void* stream);
 
 #ifdef __cplusplus
 }

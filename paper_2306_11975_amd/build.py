@@ -16,7 +16,8 @@ EXAMPLE = PKG / "example_dgemm"       # stand-alone C++ user of the C ABI (csrc/
 PRELOAD = PKG / "libozimmu_preload.so"  # interposer for the vendor DGEMM/ZGEMM symbols (csrc/preload.cpp)
 BLAS_CLIENT = PKG / "blas_client"     # plain rocBLAS/hipBLAS program the interposer is tried on (csrc/blas_client.cpp)
 
-SOURCES = ["split.hip", "gemm.hip", "gemm_real.hip", "gemm_dd.hip", "gemm_complex.hip", "gate.hip", "gate_many.hip", "small.hip", "small_complex.hip", "probes.hip", "static_scratch.hip", "api.cpp"]
+SOURCES = ["split.hip", "gemm.hip", "gemm_real.hip", "gemm_dd.hip", "gemm_complex.hip", "gate.hip", "gate_many.hip", "small.hip", "small_complex.hip", "probes.hip", "static_scratch.hip", "api.cpp",
+           "nt_product.hip", "nt_product_two.hip", "q4.hip", "q4_few.hip", "orthogonalize.hip", "weights.cpp"]
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-ffp-contract=off", "-Wall", f"-I{INCLUDE}", f"-I{CSRC}"]
 # device code: gfx950 only; packed-FP32 instruction selection is switched off on the test machines
 DEVICE = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
@@ -30,7 +31,9 @@ def hipcc() -> str:
 
 
 # translation units whose kernels write M0 in inline assembly (the LDS base of the direct loads)
-USES_M0 = ("gemm_real.hip", "gemm_dd.hip", "gemm_complex.hip")
+USES_M0 = ("gemm_real.hip", "gemm_dd.hip", "gemm_complex.hip", "nt_product.hip", "nt_product_two.hip")
+# of those, the ones whose MFMAs the compiler issues (and keeps apart by itself)
+PLAIN_MFMA = ("nt_product.hip", "nt_product_two.hip")
 
 
 def _check_m0(src: str) -> None:
@@ -59,6 +62,8 @@ def _check_hazards(src: str) -> None:
 
     for listing in OBJ.glob(f"{src.rsplit('.', 1)[0]}-hip-amdgcn-amd-amdhsa-gfx950*.s"):
         found = asm_check.hazards(listing.read_text().splitlines())
+        if src in PLAIN_MFMA:
+            found = [x for x in found if "direct load" in x]
         if found:
             raise RuntimeError("\n".join(f"{listing.name}:{x}" for x in found[:20]))
 

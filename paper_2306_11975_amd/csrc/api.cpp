@@ -561,6 +561,9 @@ const char* ozimmu_status_string(ozimmu_status_t status) {
         case OZIMMU_ERR_HIP: return "HIP error";
         case OZIMMU_ERR_NOT_IMPLEMENTED: return "not implemented";
         case OZIMMU_ERR_TOO_LARGE: return "product too large for the built-in scratch (use a workspace)";
+        case OZIMMU_ERR_BAD_TYPE: return "bad type";
+        case OZIMMU_ERR_BAD_POLYNOMIAL: return "bad steps, coefficients or eps of an orthogonal update";
+        case OZIMMU_ERR_MISALIGNED: return "misaligned pointer";
     }
     return "unknown status";
 }

@@ -1,0 +1,135 @@
+// The orthogonal update's own kernels: the Frobenius norm and the normalised matrix in two slices (gfx950). The products of the
+// iteration are nt_product.h's.
+#include "half_common.h"
+
+namespace ozimmu {
+namespace {
+
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ double block_sum(double x, double* shared) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = shared[0];
+#pragma unroll
+    for (int i = 1; i < kThreads / 64; ++i) x += shared[i];
+    __syncthreads();
+    return x;
+}
+
+// Sums of squares in 64 bits (squares of 32-bit values do not overflow there): workgroup b of a matrix takes rows b, b + gridDim.x, ...
+// A fixed order: the same sum on every run.
+template <int TYPE>
+__launch_bounds__(kThreads)
+__global__ void norm_partials_kernel(int64_t m, int64_t n, const void* G, int64_t ldg, int64_t stride, bool vec, double* partials) {
+    typedef Elem<TYPE> E;
+    typedef typename E::raw raw;
+    constexpr int V = 16 / sizeof(raw);
+    __shared__ double shared[kThreads / 64];
+    const raw* g = reinterpret_cast<const raw*>(G) + blockIdx.y * stride;
+    double sum = 0.0;
+    // threads over the 16-byte pieces of as many rows at a time as fill the workgroup
+    const int64_t pieces = (n + V - 1) / V;
+    int tx = 1;
+    while (tx < kThreads && tx < pieces) tx *= 2;
+    const int ty = kThreads / tx;
+    for (int64_t row = (int64_t)blockIdx.x * ty + threadIdx.x / tx; row < m; row += (int64_t)gridDim.x * ty)
+        for (int64_t p = threadIdx.x % tx; p < pieces; p += tx) {
+            const raw* at = g + row * ldg + p * V;
+            raw r[V];
+            if (vec && p * V + V <= n)
+                *reinterpret_cast<v4u*>(r) = *reinterpret_cast<const v4u*>(at);
+            else
+#pragma unroll
+                for (int e = 0; e < V; ++e) r[e] = p * V + e < n ? at[e] : raw(0);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const double x = E::load(r[e]);
+                sum = fma(x, x, sum);
+            }
+        }
+    sum = block_sum(sum, shared);
+    if (threadIdx.x == 0) partials[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = sum;
+}
+
+// A 64 x 64 tile of G, divided by its norm, in two slices: rows as they lie, and through LDS transposed. The padding of rows is written as zeros.
+template <int TYPE>
+__launch_bounds__(kThreads)
+__global__ void normalised_slices_kernel(int64_t m, int64_t n, const void* G, int64_t ldg, int64_t stride, const double* partials, int parts, double eps,
+                                         double scale, unsigned short* rows, int64_t ldr, int64_t batch_r, unsigned short* cols, int64_t ldc,
+                                         int64_t batch_c, int tiles_n) {
+    typedef Elem<TYPE> E;
+    typedef typename E::raw raw;
+    __shared__ float tile[64][65];
+    __shared__ double shared[kThreads / 64];
+    const int64_t z = blockIdx.y;
+    double sum = threadIdx.x < parts ? partials[z * parts + threadIdx.x] : 0.0;
+    sum = block_sum(sum, shared);
+    const double norm = sqrt(sum) + eps;
+    const double inv = norm > 0.0 ? scale / norm : (norm == 0.0 ? 0.0 : norm);   // (a matrix of zeros stays one; NaN stays NaN)
+    const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * 64, n0 = (int64_t)(blockIdx.x % tiles_n) * 64;
+    const raw* g = reinterpret_cast<const raw*>(G) + z * stride;
+    unsigned short* r_out = rows + z * batch_r;
+    unsigned short* c_out = cols + z * batch_c;
+    const int64_t n_pad = pad_to(n, 32), m_pad = pad_to(m, 32);
+#pragma unroll
+    for (int it = 0; it < 16; ++it) {
+        const int i = it * 4 + threadIdx.x / 64, j = threadIdx.x % 64;
+        const int64_t r = m0 + i, c = n0 + j;
+        const float x = r < m && c < n ? (float)((double)E::load(g[r * ldg + c]) * inv) : 0.f;
+        tile[i][j] = x;
+        if (r < m && c < n_pad) {
+            unsigned short h, l;
+            two_slices(x, h, l);
+            const int64_t at = r * ldr + (c >> 5) * 64 + (c & 31);
+            r_out[at] = h;
+            r_out[at + 32] = l;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int it = 0; it < 16; ++it) {
+        const int j = it * 4 + threadIdx.x / 64, i = threadIdx.x % 64;
+        const int64_t r = m0 + i, c = n0 + j;
+        if (c < n && r < m_pad) {
+            unsigned short h, l;
+            two_slices(tile[i][j], h, l);
+            const int64_t at = c * ldc + (r >> 5) * 64 + (r & 31);
+            c_out[at] = h;
+            c_out[at + 32] = l;
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_norm_partials(int64_t batch, int64_t m, int64_t n, const void* G, int type, int64_t ldg, int64_t stride, double* partials, hipStream_t st) {
+    const dim3 grid(kNormBlocks, (unsigned)batch);
+    const bool vec = rows_aligned16(G, ldg, type == OZIMMU_F32 ? 4 : 2) && rows_aligned16(G, stride, type == OZIMMU_F32 ? 4 : 2);
+    if (type == OZIMMU_F32)
+        norm_partials_kernel<OZIMMU_F32><<<grid, kThreads, 0, st>>>(m, n, G, ldg, stride, vec, partials);
+    else if (type == OZIMMU_BF16)
+        norm_partials_kernel<OZIMMU_BF16><<<grid, kThreads, 0, st>>>(m, n, G, ldg, stride, vec, partials);
+    else
+        norm_partials_kernel<OZIMMU_F16><<<grid, kThreads, 0, st>>>(m, n, G, ldg, stride, vec, partials);
+    return hipGetLastError();
+}
+
+hipError_t launch_normalised_slices(int64_t batch, int64_t m, int64_t n, const void* G, int type, int64_t ldg, int64_t stride, const double* partials,
+                                    double eps, int shift, unsigned short* rows, int64_t ldr, int64_t batch_r, unsigned short* cols, int64_t ldc,
+                                    int64_t batch_c, hipStream_t st) {
+    const int tiles_n = (int)((n + 63) / 64);
+    const dim3 grid((unsigned)((m + 63) / 64 * tiles_n), (unsigned)batch);
+    const double scale = (double)(1 << shift);
+    if (type == OZIMMU_F32)
+        normalised_slices_kernel<OZIMMU_F32><<<grid, kThreads, 0, st>>>(m, n, G, ldg, stride, partials, kNormBlocks, eps, scale, rows, ldr, batch_r, cols, ldc, batch_c, tiles_n);
+    else if (type == OZIMMU_BF16)
+        normalised_slices_kernel<OZIMMU_BF16><<<grid, kThreads, 0, st>>>(m, n, G, ldg, stride, partials, kNormBlocks, eps, scale, rows, ldr, batch_r, cols, ldc, batch_c, tiles_n);
+    else
+        normalised_slices_kernel<OZIMMU_F16><<<grid, kThreads, 0, st>>>(m, n, G, ldg, stride, partials, kNormBlocks, eps, scale, rows, ldr, batch_r, cols, ldc, batch_c, tiles_n);
+    return hipGetLastError();
+}
+
+}  // namespace ozimmu

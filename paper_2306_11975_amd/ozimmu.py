@@ -12,7 +12,8 @@ from pathlib import Path
 _LIB_PATH = Path(__file__).resolve().parent / "libozimmu.so"
 
 (OK, ERR_BAD_DIM, ERR_BAD_LD, ERR_BAD_SLICES, ERR_NULL, ERR_WORKSPACE, ERR_HIP, ERR_NOT_IMPLEMENTED,
- ERR_TOO_LARGE) = range(9)
+ ERR_TOO_LARGE, ERR_BAD_TYPE, ERR_BAD_POLYNOMIAL, ERR_MISALIGNED) = range(12)
+F32, BF16, F16 = range(3)            # ozimmu_type_t
 MAX_SLICES = 16
 ROW_ALIGN = 128
 K_ALIGN = 32
@@ -27,6 +28,8 @@ EXPORTS = (
     "ozimmu_launch_plan", "ozimmu_dgemm_dd", "ozimmu_dgemm_blas", "ozimmu_zgemm_blas_workspace_bytes", "ozimmu_zgemm_blas",
     "ozimmu_auto_scratch_bytes", "ozimmu_auto_num_slices", "ozimmu_auto_num_slices_blas", "ozimmu_zgemm_auto",
     "ozimmu_dgemm_auto", "ozimmu_dgemm_blas_auto", "ozimmu_zgemm_blas_auto",
+    "ozimmu_q4_geometry", "ozimmu_q4_split", "ozimmu_q4_expand", "ozimmu_q4_workspace_bytes", "ozimmu_q4_gemm", "ozimmu_q4_gemm_grad",
+    "ozimmu_orthogonalize_workspace_bytes", "ozimmu_orthogonalize",
 )
 PROBE_EXPORTS = ("ozimmu_probe_int8_mfma",)      # include/ozimmu_probe.h: measurement utility, not the product path
 
@@ -111,6 +114,22 @@ def lib() -> ctypes.CDLL:
         L.ozimmu_zgemm_blas_auto.argtypes = [ctypes.c_char, ctypes.c_char, i64, i64, i64, vp, vp, i64, vp, i64, vp, vp, i64,
                                              ctypes.c_double, i32, i32, vp, sz, vp, sz, ctypes.POINTER(i32),
                                              ctypes.POINTER(i32), vp]
+        L.ozimmu_q4_geometry.restype = i32
+        L.ozimmu_q4_geometry.argtypes = [i64, i32, ctypes.POINTER(i64), ctypes.POINTER(i64)]
+        L.ozimmu_q4_split.restype = i32
+        L.ozimmu_q4_split.argtypes = [i64, i64, i32, i32, vp, i64, vp, i64, i32, vp, i64, vp]
+        L.ozimmu_q4_expand.restype = i32
+        L.ozimmu_q4_expand.argtypes = [i64, i64, i32, i32, vp, i64, vp, i64, vp, i64, vp]
+        L.ozimmu_q4_workspace_bytes.restype = i32
+        L.ozimmu_q4_workspace_bytes.argtypes = [i64, i64, i64, i32, i32, i32, ctypes.POINTER(sz)]
+        for name in ("ozimmu_q4_gemm", "ozimmu_q4_gemm_grad"):
+            f = getattr(L, name)
+            f.restype = i32
+            f.argtypes = [i64, i64, i64, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, sz, vp]
+        L.ozimmu_orthogonalize_workspace_bytes.restype = i32
+        L.ozimmu_orthogonalize_workspace_bytes.argtypes = [i64, i64, i64, ctypes.POINTER(sz)]
+        L.ozimmu_orthogonalize.restype = i32
+        L.ozimmu_orthogonalize.argtypes = [i64, i64, i64, i32, vp, i64, i64, vp, i64, i64, i32] + [ctypes.c_double] * 4 + [vp, sz, vp]
         dp = ctypes.POINTER(ctypes.c_double)
         L.ozimmu_probe_int8_mfma.restype = i32
         L.ozimmu_probe_int8_mfma.argtypes = [i32, i32, i32, dp, dp]
@@ -385,6 +404,140 @@ def auto_num_slices_blas(transa: str, transb: str, m: int, n: int, k: int, A, ld
                                              int(bool(is_complex)), float(threshold), int(max_slices), _ptr(scratch),
                                              scratch.numel(), ctypes.byref(s), sums.ctypes.data, _stream(stream)))
     return s.value, sums
+
+
+def _type_of(dtype) -> int:
+    import torch
+
+    types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+    if dtype not in types:
+        raise ValueError(f"expected float32, bfloat16 or float16, got {dtype}")
+    return types[dtype]
+
+
+def _expect(condition, what: str) -> None:
+    if not condition:
+        raise ValueError(what)
+
+
+def _on_device(stream, *tensors):
+    """The device that all tensors are on, made current for the call, and the stream: torch's current one of that device unless one is
+    given, which must belong to it."""
+    import torch
+
+    device = tensors[0].device
+    _expect(all(t is None or t.device == device for t in tensors), "all tensors must be on one device")
+    _expect(device.type == "cuda", "expected tensors on a GPU")
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    _expect(stream.device == device, "the stream belongs to another device than the tensors")
+    return torch.cuda.device(device), stream.cuda_stream
+
+
+def q4_geometry(k: int, group: int):
+    """(bytes of a row of codes, scales of a row) for weights of k inputs (see ozimmu.h)."""
+    row_bytes_, groups = ctypes.c_int64(), ctypes.c_int64()
+    _check(lib().ozimmu_q4_geometry(k, group, ctypes.byref(row_bytes_), ctypes.byref(groups)))
+    return row_bytes_.value, groups.value
+
+
+def q4_row_bytes(k: int) -> int:
+    return q4_geometry(k, 32)[0]
+
+
+def _q4_weights(n: int, k: int, codes, scales, group: int):
+    """Checks the codes and scales of an n x k weight matrix; (codes' row stride in bytes, scales' row stride)."""
+    import torch
+
+    row_bytes_, groups = q4_geometry(k, group)
+    _expect(codes.dtype == torch.uint8, "codes are uint8")
+    _expect(codes.dim() == 2 and codes.shape[0] == n and codes.shape[1] >= row_bytes_, f"codes: expected {n} rows of at least {row_bytes_} bytes")
+    _expect(tuple(scales.shape) == (n, groups), f"scales: expected the shape {(n, groups)}")
+    return (_ld(codes, row_bytes_) if n > 1 else row_bytes_), _ld(scales, groups)
+
+
+def q4_split(W, group: int, codes, scales, stream=None) -> None:
+    """W (n x k; float32, bfloat16 or float16) into four-bit codes (uint8, n x q4_row_bytes(k)) and scales (n x ceil(k / group), any of
+    the three types)."""
+    n, k = W.shape
+    ldq, lds = _q4_weights(n, k, codes, scales, group)
+    device, st = _on_device(stream, W, codes, scales)
+    with device:
+        _check(lib().ozimmu_q4_split(n, k, group, _type_of(W.dtype), _ptr(W), _ld(W, k), _ptr(codes), ldq, _type_of(scales.dtype), _ptr(scales), lds, st))
+
+
+def q4_expand(codes, scales, group: int, W, stream=None) -> None:
+    """The weights that codes and scales stand for, into W (n x k, of the scales' type)."""
+    n, k = W.shape
+    ldq, lds = _q4_weights(n, k, codes, scales, group)
+    _expect(W.dtype == scales.dtype, "W and the scales must have one type")
+    device, st = _on_device(stream, W, codes, scales)
+    with device:
+        _check(lib().ozimmu_q4_expand(n, k, group, _type_of(W.dtype), _ptr(codes), ldq, _ptr(scales), lds, _ptr(W), _ld(W, k), st))
+
+
+def q4_workspace_bytes(t: int, n: int, k: int, group: int, dtype, gradient: bool = False) -> int:
+    out = ctypes.c_size_t()
+    _check(lib().ozimmu_q4_workspace_bytes(t, n, k, group, _type_of(dtype), int(bool(gradient)), ctypes.byref(out)))
+    return out.value
+
+
+def alloc_q4_workspace(t: int, n: int, k: int, group: int, dtype, gradient: bool = False, device="cuda"):
+    """A uint8 tensor of the size that q4_gemm (gradient: q4_gemm_grad) asks for; it serves fewer tokens too."""
+    import torch
+
+    return torch.empty(max(q4_workspace_bytes(t, n, k, group, dtype, gradient), WORKSPACE_ALIGN), dtype=torch.uint8, device=device)
+
+
+def _q4_product(f, V, codes, scales, group, R, n, k, workspace, stream):
+    _expect(V.dtype == scales.dtype == R.dtype, "tokens, scales and result must have one type")
+    ldq, lds = _q4_weights(n, k, codes, scales, group)
+    device, st = _on_device(stream, V, codes, scales, R, workspace)
+    with device:
+        _check(f(V.shape[0], n, k, group, _type_of(V.dtype), _ptr(V), _ld(V, V.shape[1]), _ptr(codes), ldq, _ptr(scales), lds, _ptr(R),
+                 _ld(R, R.shape[1]), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), st))
+
+
+def q4_gemm(X, codes, scales, group: int, Y, workspace=None, stream=None) -> None:
+    """Y = X W^T for weights in four bits (X: t x k, Y: t x n; X, Y and the scales of one type). The workspace may be None for
+    as few tokens as q4_workspace_bytes gives 0 for."""
+    _expect(X.dim() == 2 and Y.dim() == 2 and X.shape[0] == Y.shape[0], "X and Y must have the same number of rows")
+    _q4_product(lib().ozimmu_q4_gemm, X, codes, scales, group, Y, Y.shape[1], X.shape[1], workspace, stream)
+
+
+def q4_gemm_grad(dY, codes, scales, group: int, dX, workspace, stream=None) -> None:
+    """dX = dY W for weights in four bits (dY: t x n, dX: t x k): the gradient of q4_gemm's result, on its way to X."""
+    _expect(dY.dim() == 2 and dX.dim() == 2 and dY.shape[0] == dX.shape[0], "dY and dX must have the same number of rows")
+    _q4_product(lib().ozimmu_q4_gemm_grad, dY, codes, scales, group, dX, dY.shape[1], dX.shape[1], workspace, stream)
+
+
+def orthogonalize_workspace_bytes(batch: int, m: int, n: int) -> int:
+    out = ctypes.c_size_t()
+    _check(lib().ozimmu_orthogonalize_workspace_bytes(batch, m, n, ctypes.byref(out)))
+    return out.value
+
+
+def alloc_orthogonalize_workspace(batch: int, m: int, n: int, dtype=None, device="cuda"):
+    import torch
+
+    return torch.empty(max(orthogonalize_workspace_bytes(batch, m, n), WORKSPACE_ALIGN), dtype=torch.uint8, device=device)
+
+
+def orthogonalize(G, X, workspace, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, stream=None) -> None:
+    """X = the orthogonal update of G by `steps` Newton-Schulz steps (see ozimmu.h). G and X: m x n, or a batch of such, of one
+    type (float32, bfloat16, float16), rows with unit stride; X may be G itself."""
+    _expect(G.dim() in (2, 3) and G.shape == X.shape and G.dtype == X.dtype, "G and X must have one shape (two or three dimensions) and type")
+    m, n = G.shape[-2:]
+    batch = G.shape[0] if G.dim() == 3 else 1
+    ld = {}
+    for name, t in (("g", G), ("x", X)):
+        _expect(n <= 1 or t.stride(-1) == 1, "expected rows with unit stride")
+        ld[name] = (t.stride(-2) if m > 1 else max(n, 1), t.stride(0) if t.dim() == 3 else 0)
+    a, b, c = coefficients
+    device, st = _on_device(stream, G, X, workspace)
+    with device:
+        _check(lib().ozimmu_orthogonalize(batch, m, n, _type_of(G.dtype), _ptr(G), *ld["g"], _ptr(X), *ld["x"], int(steps), float(a), float(b),
+                                          float(c), float(eps), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), st))
 
 
 def probe_int8_mfma(pattern: int, shape: int = 0, iters: int = 200000):

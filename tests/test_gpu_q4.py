@@ -1,0 +1,323 @@
+"""Weights in four bits against plain 64-bit implementations: the cut and its inverse exactly, products and gradients within bounds that count roundings."""
+import math
+
+import pytest
+import torch
+
+from paper_2306_11975_amd import ozimmu as oz
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+TYPES = [F32, BF16, F16]
+GUARD = 0x5A
+
+
+def half_step(dt):
+    return torch.finfo(dt).eps / 2
+
+
+# ---------------------------------------------------------------- plain implementations (CPU, 64 bits)
+def plain_cut(W, group, stype):
+    """codes (int, n x k) and scales by the definition; quotients in 64 bits, where they cannot fall onto a border they only come near."""
+    n, k = W.shape
+    groups = -(-k // group)
+    codes, scales = torch.zeros(n, k, dtype=torch.int64), torch.zeros(n, groups, dtype=stype)
+    for g in range(groups):
+        w = W[:, g * group:(g + 1) * group].double()
+        top = w.abs().amax(dim=1)      # (NaN stays)
+        s = (top.float() / torch.full((n,), 7.0)).to(stype)
+        scales[:, g] = s
+        usable = (s.double() > 0) & torch.isfinite(s.double())
+        q = w / torch.where(usable, s.double(), torch.ones(n, dtype=torch.float64))[:, None]
+        c = torch.round(torch.nan_to_num(q, nan=0.0, posinf=0.0, neginf=0.0)).clamp(-8, 7)
+        codes[:, g * group:(g + 1) * group] = torch.where(usable[:, None], c, torch.zeros_like(c)).long()
+    return codes, scales
+
+
+def unpack(codes, k):
+    c = codes.cpu().long()
+    return torch.stack((c & 15, c >> 4), dim=2).view(c.shape[0], -1)[:, :k] - 8
+
+
+def pack(c):
+    c = torch.nn.functional.pad(c, (0, -c.shape[1] % 32)) + 8
+    return (c[:, 0::2] | (c[:, 1::2] << 4)).to(torch.uint8)
+
+
+def weights64(c, scales, group):
+    return c.double() * scales.cpu().double().repeat_interleave(group, dim=1)[:, :c.shape[1]]
+
+
+def padded(rows, cols, dt, extra, offset, fill=None, seed=None):
+    """A (rows x cols) view on the GPU inside a larger buffer (row stride cols + extra, `offset` values from its start), and the buffer."""
+    ld = cols + extra
+    buf = torch.full((rows * ld + offset + 64,), fill if fill is not None else 77.0, dtype=dt, device=DEV)
+    return buf[offset:offset + rows * ld].view(rows, ld)[:, :cols], buf
+
+
+def random_weights(n, k, seed):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn(n, k, generator=g) * torch.exp(torch.randn(n, 1, generator=g)) / math.sqrt(max(k, 1))
+
+
+def device_cut(W, group, stype):
+    n, k = W.shape
+    codes = torch.zeros(n, oz.q4_row_bytes(k), dtype=torch.uint8, device=DEV)
+    scales = torch.zeros(n, -(-k // group), dtype=stype, device=DEV)
+    oz.q4_split(W, group, codes, scales)
+    return codes, scales
+
+
+# ---------------------------------------------------------------- the cut
+SPLITS = [(1, 1, 32), (1, 31, 32), (3, 32, 32), (5, 33, 64), (17, 1000, 32), (64, 129, 128), (130, 257, 64), (9, 4096, 128), (2, 20000, 128), (1000, 96, 128)]
+
+
+@pytest.mark.parametrize("stype", TYPES)
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("n,k,group", SPLITS)
+def test_split_and_expand(n, k, group, dt, stype):
+    W0 = random_weights(n, k, n * 31 + k).to(dt)
+    for extra, offset in ((0, 0), (5, 3), (8, 8)):
+        W, _ = padded(n, k, dt, extra, offset)
+        W.copy_(W0)
+        rb = oz.q4_row_bytes(k)
+        codes = torch.full((n, rb + 16), GUARD, dtype=torch.uint8, device=DEV)
+        groups = -(-k // group)
+        scales, sbuf = padded(n, groups, stype, 2, 1)
+        oz.q4_split(W, group, codes, scales)
+        c, s = plain_cut(W0, group, stype)
+        assert torch.equal(scales.cpu(), s)
+        assert torch.equal(unpack(codes[:, :rb], k), c)
+        assert (codes[:, rb:] == GUARD).all()                       # what lies between rows is left alone
+        assert torch.equal(unpack(codes[:, :rb], rb * 2)[:, k:], torch.zeros(n, 2 * rb - k, dtype=torch.int64))
+        assert (sbuf.view(-1)[:1] == 77).all() and (sbuf[1:1 + n * (groups + 2)].view(n, -1)[:, groups:] == 77).all()
+        out, obuf = padded(n, k, stype, extra, offset)
+        oz.q4_expand(codes, scales, group, out)
+        # s c is exact in 64 bits; rounded once
+        assert torch.equal(out.cpu(), weights64(c, s, group).to(torch.float32).to(stype) if stype != F32 else weights64(c, s, group).to(F32))
+        assert (obuf[:offset] == 77).all() and (obuf[offset:offset + n * (k + extra)].view(n, -1)[:, k:] == 77).all()
+
+
+@pytest.mark.parametrize("stype", TYPES)
+def test_split_at_borders_and_extremes(stype):
+    """Quotients on and next to a border, groups of zeros, scales that underflow or overflow their type, infinities and NaN."""
+    group, rows = 32, []
+    g = torch.Generator().manual_seed(5)
+    for top in (7.0, 1.0, 3.3, 0.1, 1e-3, 2.0 ** -20, 2.0 ** -26, 1e-30, 1e-38, 1e-41, 2.0 ** -149, 3e38, 1e6, 5e5, 458745.0):
+        s = float((torch.tensor([top], dtype=F32) / torch.tensor([7.0])).to(stype))
+        row = torch.zeros(group, dtype=F32)
+        row[0] = top
+        for i in range(1, 16):     # (j + 1/2) s and its neighbours in 32 bits
+            mid = torch.tensor((i % 8 - 0.5) * s * (-1 if i & 1 else 1), dtype=F32).clamp(-top, top)
+            row[2 * i - 1] = mid
+            row[2 * i] = torch.nextafter(mid, torch.tensor(0.0 if i & 2 else math.copysign(math.inf, float(mid) or 1.0))).clamp(-top, top)
+        rows.append(row)
+    rows.append(torch.zeros(group))
+    rows.append(-torch.zeros(group))
+    for bad in (math.inf, -math.inf, math.nan):
+        row = torch.randn(group, generator=g)
+        row[11] = bad
+        rows.append(row)
+    W = torch.stack(rows)
+    W = torch.cat((W, torch.randn(W.shape, generator=g)), dim=1)     # the group beside it is what it would be anyway
+    codes, scales = device_cut(W.to(DEV), group, stype)
+    c, s = plain_cut(W, group, stype)
+    assert torch.equal(scales.cpu().float().nan_to_num(nan=-1.0), s.float().nan_to_num(nan=-1.0))
+    assert torch.equal(unpack(codes, 64), c)
+    out = torch.empty(W.shape, dtype=stype, device=DEV)
+    oz.q4_expand(codes, scales, group, out)
+    assert out[-1].isnan()[:32].all() and out[-2].isnan()[:32].all() and not out[:, 32:].isnan().any()
+
+
+# ---------------------------------------------------------------- products
+def tokens(t, cols, dt, seed):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(t, cols, generator=g) * torch.exp(torch.randn(1, cols, generator=g))).to(dt)
+
+
+def check(got, V, W, dt, inner, rounded_weights):
+    """|got - V W| against what roundings can do. One rounding of the result; weights rounded to a 16-bit type; 32-bit values as two slices
+    (each operand off by at most 2^-22 of itself or 2^-40 of its row's largest, a third product of 2^-22 left out); the sums in 32 bits,
+    whose terms may carry the codes' offset (up to 24 + 16 for codes up to 8: five times the largest term)."""
+    want = V.double() @ W
+    terms = V.double().abs() @ W.abs()
+    top = V.double().abs().amax(dim=1, keepdim=True) @ W.abs().amax(dim=0, keepdim=True)
+    sums = (3 if dt == F32 else 1) * (inner + 8) * 2.0 ** -24      # (32 bits: three products to a term)
+    if dt == F32:
+        bound = 3 * 2.0 ** -22 * terms + 4 * inner * 2.0 ** -40 * top + sums * terms
+    else:
+        bound = (half_step(dt) if rounded_weights else 0.0) * terms + (sums * terms if rounded_weights else (inner + 8) * 2.0 ** -24 * 40 * torch.ones_like(terms) * top)
+    bound = bound + half_step(dt) * (want.abs() + bound) + torch.finfo(dt).tiny
+    off = (got.cpu().double() - want).abs()
+    assert (off <= bound).all(), f"off by up to {(off / bound).max():.3g} times what roundings can do"
+    # and typical errors are far below the worst: in the norm, one rounding of the result and of the weights
+    if want.numel() > 64:
+        rel = float(off.norm() / want.norm())
+        assert rel <= (2e-6 if dt == F32 else 1.5 * half_step(dt)), rel
+
+
+GEMMS = [(1, 1, 1, 32), (1, 16, 128, 128), (1, 2048, 512, 64), (1, 9000, 200, 128), (2, 15, 33, 32), (3, 33, 1000, 64), (5, 100, 257, 128), (13, 4095, 500, 32),
+         (16, 64, 4096, 128), (16, 8200, 130, 64), (17, 40, 100, 32), (40, 130, 64, 64), (64, 64, 1024, 128), (65, 333, 777, 32), (129, 257, 96, 64), (300, 150, 1000, 128),
+         (1000, 700, 320, 64), (2100, 4200, 192, 128), (3800, 3700, 100, 32)]
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("t,n,k,group", GEMMS)
+def test_gemm(t, n, k, group, dt):
+    W0 = random_weights(n, k, 7 * n + k)
+    c, s = plain_cut(W0, group, dt)
+    codes, scales = pack(c).to(DEV), s.to(DEV)
+    X0 = tokens(t, k, dt, t + k)
+    W = weights64(c, s, group).t()
+    ws = oz.alloc_q4_workspace(t, n, k, group, dt)
+    ws.fill_(0xFF)     # NaN in every type: what is read has been written
+    for extra, offset in ((0, 0), (3, 1), (16, 8)):
+        X, _ = padded(t, k, dt, extra, offset, fill=float("nan"))
+        X.copy_(X0)
+        Y, ybuf = padded(t, n, dt, extra, offset)
+        oz.q4_gemm(X, codes, scales, group, Y, ws)
+        check(Y, X0, W, dt, k, oz.q4_workspace_bytes(t, n, k, group, dt) > 0)
+        assert (ybuf[:offset] == 77).all() and (ybuf[offset:offset + t * (n + extra)].view(t, -1)[:, n:] == 77).all() and (ybuf[offset + t * (n + extra):] == 77).all()
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("t,n,k,group", [(1, 1, 1, 32), (1, 500, 300, 64), (7, 64, 64, 32), (16, 100, 1000, 128), (100, 33, 257, 64), (129, 128, 96, 128), (333, 150, 1000, 32),
+                                         (1000, 320, 700, 64), (2100, 192, 4200, 128), (3800, 100, 3700, 64)])
+def test_gradient(t, n, k, group, dt):
+    c, s = plain_cut(random_weights(n, k, 3 * n + k), group, dt)
+    codes, scales = pack(c).to(DEV), s.to(DEV)
+    D0 = tokens(t, n, dt, t + n)
+    W = weights64(c, s, group)
+    ws = oz.alloc_q4_workspace(t, n, k, group, dt, gradient=True)
+    ws.fill_(0xFF)
+    for extra, offset in ((0, 0), (3, 1), (16, 8)):
+        D, _ = padded(t, n, dt, extra, offset, fill=float("nan"))
+        D.copy_(D0)
+        R, rbuf = padded(t, k, dt, extra, offset)
+        oz.q4_gemm_grad(D, codes, scales, group, R, ws)
+        check(R, D0, W, dt, n, True)
+        assert (rbuf[:offset] == 77).all() and (rbuf[offset:offset + t * (k + extra)].view(t, -1)[:, k:] == 77).all() and (rbuf[offset + t * (k + extra):] == 77).all()
+
+
+@pytest.mark.parametrize("t", [4, 50])
+def test_gradient_against_differences(t):
+    """<dY, Y(X + E) - Y(X)> = <dX, E>: the product is linear, so the difference has no higher terms. Each side is a sum of t n (t k) products that are off by at most what
+    test_gemm allows; the norms below bound it."""
+    n, k, group = 96, 160, 32
+    c, s = plain_cut(random_weights(n, k, 1), group, F32)
+    codes, scales = pack(c).to(DEV), s.to(DEV)
+    X, E, D = (tokens(t, cols, F32, seed).to(DEV) for cols, seed in ((k, 1), (k, 2), (n, 3)))
+    ws = oz.alloc_q4_workspace(t, n, k, group, F32, gradient=True)
+    wf = oz.alloc_q4_workspace(t, n, k, group, F32)
+    Y0, Y1, R = torch.empty(t, n, device=DEV), torch.empty(t, n, device=DEV), torch.empty(t, k, device=DEV)
+    oz.q4_gemm(X, codes, scales, group, Y0, wf)
+    oz.q4_gemm(X + E, codes, scales, group, Y1, wf)
+    oz.q4_gemm_grad(D, codes, scales, group, R, ws)
+    left = (D.double() * (Y1.double() - Y0.double())).sum()
+    right = (R.double() * E.double()).sum()
+    W = weights64(c, s, group).to(DEV).abs()
+    size = (D.double().abs() * ((2 * X.double().abs() + E.double().abs()) @ W.t())).sum() + ((D.double().abs() @ W) * E.double().abs()).sum()
+    assert abs(left - right) <= (max(n, k) + 16) * 2.0 ** -24 * size
+    assert abs(left) > 1e3 * (max(n, k) + 16) * 2.0 ** -24       # (there is something to compare)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("t", [3, 40])
+def test_empty_inner_dimension_gives_zeros(t, dt):
+    Y, buf = padded(t, 70, dt, 2, 1)
+    oz.q4_gemm(torch.empty(t, 0, dtype=dt, device=DEV), torch.empty(70, 0, dtype=torch.uint8, device=DEV), torch.empty(70, 0, dtype=dt, device=DEV), 32, Y)
+    assert (Y == 0).all() and int((buf == 0).sum()) == t * 70
+    R, buf = padded(t, 70, dt, 2, 1)
+    oz.q4_gemm_grad(torch.empty(t, 0, dtype=dt, device=DEV), torch.empty(0, 48, dtype=torch.uint8, device=DEV), torch.empty(0, 3, dtype=dt, device=DEV), 32, R, None)
+    assert (R == 0).all() and int((buf == 0).sum()) == t * 70
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("t", [5, 70])
+def test_a_row_that_is_not_finite_stays_alone(t, dt):
+    n, k, group = 100, 200, 64
+    c, s = plain_cut(random_weights(n, k, 9), group, dt)
+    codes, scales = pack(c).to(DEV), s.to(DEV)
+    for grad in (False, True):
+        V = tokens(t, n if grad else k, dt, 4).to(DEV)
+        ws = oz.alloc_q4_workspace(t, n, k, group, dt, gradient=grad)
+        f = oz.q4_gemm_grad if grad else oz.q4_gemm
+        clean = torch.empty(t, k if grad else n, dtype=dt, device=DEV)
+        f(V, codes, scales, group, clean, ws)
+        bad = V.clone()
+        bad[1, 17] = float("nan")
+        bad[3, 0] = float("inf")
+        out = torch.empty_like(clean)
+        f(bad, codes, scales, group, out, ws)
+        rest = [i for i in range(t) if i not in (1, 3)]
+        assert torch.equal(out[rest], clean[rest]) and out[1].isnan().all() and not out[3].isfinite().any()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_large_and_small_values(dt):
+    """Rows of tokens of very different size, up to the ends of the type's range: each keeps its relative precision."""
+    t, n, k, group = 40, 64, 256, 32
+    c, s = plain_cut(random_weights(n, k, 2), group, dt)
+    X0 = tokens(t, k, F32, 8) / 64
+    X0 = (X0 * torch.logspace(-30, 30, t)[:, None]).to(dt)
+    Y = torch.empty(t, n, dtype=dt, device=DEV)
+    oz.q4_gemm(X0.to(DEV), pack(c).to(DEV), s.to(DEV), group, Y, oz.alloc_q4_workspace(t, n, k, group, dt))
+    check(Y, X0, weights64(c, s, group).t(), dt, k, True)
+    R = torch.empty(t, k, dtype=dt, device=DEV)
+    D0 = (tokens(t, n, F32, 3) / 64 * torch.logspace(-30, 30, t)[:, None]).to(dt)
+    # columns of W of very different size: the exponent goes with the group
+    s2 = (s.float() * torch.logspace(-4, 4, s.shape[1])).to(dt)
+    oz.q4_gemm_grad(D0.to(DEV), pack(c).to(DEV), s2.to(DEV), group, R, oz.alloc_q4_workspace(t, n, k, group, dt, gradient=True))
+    check(R, D0, weights64(c, s2, group), dt, n, True)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_other_stream_and_replayed_graph(dt):
+    """One call on a stream of its own, and prompt, token, gradient and a new cut captured into one graph that shares a workspace, replayed with other inputs."""
+    t, n, k, group = 70, 300, 500, 64
+    W = random_weights(n, k, 1).to(dt).to(DEV)
+    codes, scales = device_cut(W, group, dt)
+    X, D = tokens(t, k, dt, 1).to(DEV), tokens(t, n, dt, 2).to(DEV)
+    ws = oz.alloc_q4_workspace(t, n, k, group, dt, gradient=True)
+    ws = torch.empty(max(ws.numel(), oz.q4_workspace_bytes(t, n, k, group, dt)), dtype=torch.uint8, device=DEV)
+    Y, y1, R = torch.empty(t, n, dtype=dt, device=DEV), torch.empty(1, n, dtype=dt, device=DEV), torch.empty(t, k, dtype=dt, device=DEV)
+
+    def work():
+        oz.q4_split(W, group, codes, scales)
+        oz.q4_gemm(X, codes, scales, group, Y, ws)
+        oz.q4_gemm(X[:1], codes, scales, group, y1)
+        oz.q4_gemm_grad(D, codes, scales, group, R, ws)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        work()
+    torch.cuda.current_stream().wait_stream(side)
+    eager = [x.clone() for x in (codes, scales, Y, y1, R)]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        work()
+    first = [x.clone() for x in (W, X, D)]
+    for round_ in range(3):
+        for x, f in zip((W, X, D), first):
+            x.copy_(f * (1 + round_))       # twice and three times: other inputs
+        g.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in (codes, scales, Y, y1, R)]
+        work()
+        torch.cuda.synchronize()
+        for a, b in zip(got, (codes, scales, Y, y1, R)):
+            assert torch.equal(a, b)
+        if round_ == 0:
+            for a, b in zip(got, eager):
+                assert torch.equal(a, b)
+
+
+def test_repeated_calls_give_the_same_bits():
+    t, n, k, group = 13, 1000, 3000, 32
+    c, s = plain_cut(random_weights(n, k, 1), group, F16)
+    X, Y = tokens(t, k, F16, 1).to(DEV), torch.empty(2, t, n, dtype=F16, device=DEV)
+    for i in range(2):
+        oz.q4_gemm(X, pack(c).to(DEV), s.to(DEV), group, Y[i])
+    assert torch.equal(Y[0], Y[1])
