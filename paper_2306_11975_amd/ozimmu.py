@@ -406,13 +406,17 @@ def auto_num_slices_blas(transa: str, transb: str, m: int, n: int, k: int, A, ld
     return s.value, sums
 
 
-def _type_of(dtype) -> int:
-    import torch
+_types = {}      # torch's types as ozimmu_type_t, once torch is there
 
-    types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
-    if dtype not in types:
+
+def _type_of(dtype) -> int:
+    if not _types:
+        import torch
+
+        _types.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+    if dtype not in _types:
         raise ValueError(f"expected float32, bfloat16 or float16, got {dtype}")
-    return types[dtype]
+    return _types[dtype]
 
 
 def _expect(condition, what: str) -> None:
@@ -420,18 +424,46 @@ def _expect(condition, what: str) -> None:
         raise ValueError(what)
 
 
-def _on_device(stream, *tensors):
-    """The device that all tensors are on, made current for the call, and the stream: torch's current one of that device unless one is
-    given, which must belong to it."""
-    import torch
+_torch = None
 
+
+def _call(f, stream, tensors, *args) -> None:
+    """f(*args, stream) with the tensors' device current: all must be on one GPU. Without a stream, torch's current one of that
+    device is taken. (One token's call is a few microseconds of GPU time: what happens here is kept short.)"""
+    global _torch
+    if _torch is None:
+        import torch
+
+        _torch = torch
     device = tensors[0].device
-    _expect(all(t is None or t.device == device for t in tensors), "all tensors must be on one device")
-    _expect(device.type == "cuda", "expected tensors on a GPU")
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError("all tensors must be on one device")
+    if device.type != "cuda":
+        raise ValueError("expected tensors on a GPU")
+    index = device.index
     if stream is None:
-        stream = torch.cuda.current_stream(device)
-    _expect(stream.device == device, "the stream belongs to another device than the tensors")
-    return torch.cuda.device(device), stream.cuda_stream
+        raw = _torch._C._cuda_getCurrentRawStream(index)
+    elif stream.device != device:
+        raise ValueError("the stream belongs to another device than the tensors")
+    else:
+        raw = stream.cuda_stream
+    if index == _torch._C._cuda_getDevice():
+        code = f(*args, raw)
+    else:
+        with _torch.cuda.device(index):
+            code = f(*args, raw)
+    if code:
+        _check(code)
+
+
+def _rows(t):
+    """Rows, columns and row stride of a 2-D tensor with unit stride along its rows."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
+        raise ValueError("expected a 2-D row-major tensor (unit stride along the second dimension)")
+    rows, cols = shape
+    return rows, cols, stride[0] if rows > 1 else cols or 1
 
 
 def q4_geometry(k: int, group: int):
@@ -447,33 +479,34 @@ def q4_row_bytes(k: int) -> int:
 
 def _q4_weights(n: int, k: int, codes, scales, group: int):
     """Checks the codes and scales of an n x k weight matrix; (codes' row stride in bytes, scales' row stride)."""
-    import torch
-
-    row_bytes_, groups = q4_geometry(k, group)
-    _expect(codes.dtype == torch.uint8, "codes are uint8")
-    _expect(codes.dim() == 2 and codes.shape[0] == n and codes.shape[1] >= row_bytes_, f"codes: expected {n} rows of at least {row_bytes_} bytes")
-    _expect(tuple(scales.shape) == (n, groups), f"scales: expected the shape {(n, groups)}")
-    return (_ld(codes, row_bytes_) if n > 1 else row_bytes_), _ld(scales, groups)
+    if group not in (32, 64, 128):
+        q4_geometry(k, group)       # raises
+    row_bytes_, groups = (k + 31) // 32 * 16, -(-k // group)
+    rows, cols, ldq = _rows(codes)
+    if rows != n or cols < row_bytes_ or codes.element_size() != 1 or codes.is_floating_point() or codes.is_signed():
+        raise ValueError(f"codes: expected {n} rows of at least {row_bytes_} bytes (uint8)")
+    rows, cols, lds = _rows(scales)
+    if rows != n or cols != groups:
+        raise ValueError(f"scales: expected the shape {(n, groups)}")
+    return (ldq if n > 1 else row_bytes_), lds
 
 
 def q4_split(W, group: int, codes, scales, stream=None) -> None:
     """W (n x k; float32, bfloat16 or float16) into four-bit codes (uint8, n x q4_row_bytes(k)) and scales (n x ceil(k / group), any of
     the three types)."""
-    n, k = W.shape
+    n, k, ldw = _rows(W)
     ldq, lds = _q4_weights(n, k, codes, scales, group)
-    device, st = _on_device(stream, W, codes, scales)
-    with device:
-        _check(lib().ozimmu_q4_split(n, k, group, _type_of(W.dtype), _ptr(W), _ld(W, k), _ptr(codes), ldq, _type_of(scales.dtype), _ptr(scales), lds, st))
+    _call(lib().ozimmu_q4_split, stream, (W, codes, scales), n, k, group, _type_of(W.dtype), W.data_ptr(), ldw, codes.data_ptr(), ldq,
+          _type_of(scales.dtype), scales.data_ptr(), lds)
 
 
 def q4_expand(codes, scales, group: int, W, stream=None) -> None:
     """The weights that codes and scales stand for, into W (n x k, of the scales' type)."""
-    n, k = W.shape
+    n, k, ldw = _rows(W)
     ldq, lds = _q4_weights(n, k, codes, scales, group)
     _expect(W.dtype == scales.dtype, "W and the scales must have one type")
-    device, st = _on_device(stream, W, codes, scales)
-    with device:
-        _check(lib().ozimmu_q4_expand(n, k, group, _type_of(W.dtype), _ptr(codes), ldq, _ptr(scales), lds, _ptr(W), _ld(W, k), st))
+    _call(lib().ozimmu_q4_expand, stream, (W, codes, scales), n, k, group, _type_of(W.dtype), codes.data_ptr(), ldq, scales.data_ptr(), lds, W.data_ptr(),
+          ldw)
 
 
 def q4_workspace_bytes(t: int, n: int, k: int, group: int, dtype, gradient: bool = False) -> int:
@@ -489,26 +522,33 @@ def alloc_q4_workspace(t: int, n: int, k: int, group: int, dtype, gradient: bool
     return torch.empty(max(q4_workspace_bytes(t, n, k, group, dtype, gradient), WORKSPACE_ALIGN), dtype=torch.uint8, device=device)
 
 
-def _q4_product(f, V, codes, scales, group, R, n, k, workspace, stream):
-    _expect(V.dtype == scales.dtype == R.dtype, "tokens, scales and result must have one type")
+def _size(workspace) -> int:
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def _q4_product(f, gradient, V, codes, scales, group, R, workspace, stream):
+    dtype = V.dtype
+    if dtype != scales.dtype or dtype != R.dtype:
+        raise ValueError("tokens, scales and result must have one type")
+    t, inner, ldv = _rows(V)
+    rows, outer, ldr = _rows(R)
+    if rows != t:
+        raise ValueError("tokens and result must have the same number of rows")
+    n, k = (inner, outer) if gradient else (outer, inner)
     ldq, lds = _q4_weights(n, k, codes, scales, group)
-    device, st = _on_device(stream, V, codes, scales, R, workspace)
-    with device:
-        _check(f(V.shape[0], n, k, group, _type_of(V.dtype), _ptr(V), _ld(V, V.shape[1]), _ptr(codes), ldq, _ptr(scales), lds, _ptr(R),
-                 _ld(R, R.shape[1]), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), st))
+    _call(f, stream, (V, codes, scales, R, workspace), t, n, k, group, _type_of(dtype), V.data_ptr(), ldv, codes.data_ptr(), ldq, scales.data_ptr(), lds,
+          R.data_ptr(), ldr, _ptr(workspace), _size(workspace))
 
 
 def q4_gemm(X, codes, scales, group: int, Y, workspace=None, stream=None) -> None:
     """Y = X W^T for weights in four bits (X: t x k, Y: t x n; X, Y and the scales of one type). The workspace may be None for
     as few tokens as q4_workspace_bytes gives 0 for."""
-    _expect(X.dim() == 2 and Y.dim() == 2 and X.shape[0] == Y.shape[0], "X and Y must have the same number of rows")
-    _q4_product(lib().ozimmu_q4_gemm, X, codes, scales, group, Y, Y.shape[1], X.shape[1], workspace, stream)
+    _q4_product(lib().ozimmu_q4_gemm, False, X, codes, scales, group, Y, workspace, stream)
 
 
 def q4_gemm_grad(dY, codes, scales, group: int, dX, workspace, stream=None) -> None:
     """dX = dY W for weights in four bits (dY: t x n, dX: t x k): the gradient of q4_gemm's result, on its way to X."""
-    _expect(dY.dim() == 2 and dX.dim() == 2 and dY.shape[0] == dX.shape[0], "dY and dX must have the same number of rows")
-    _q4_product(lib().ozimmu_q4_gemm_grad, dY, codes, scales, group, dX, dY.shape[1], dX.shape[1], workspace, stream)
+    _q4_product(lib().ozimmu_q4_gemm_grad, True, dY, codes, scales, group, dX, workspace, stream)
 
 
 def orthogonalize_workspace_bytes(batch: int, m: int, n: int) -> int:
@@ -534,10 +574,8 @@ def orthogonalize(G, X, workspace, steps: int = 5, coefficients=(3.4445, -4.7750
         _expect(n <= 1 or t.stride(-1) == 1, "expected rows with unit stride")
         ld[name] = (t.stride(-2) if m > 1 else max(n, 1), t.stride(0) if t.dim() == 3 else 0)
     a, b, c = coefficients
-    device, st = _on_device(stream, G, X, workspace)
-    with device:
-        _check(lib().ozimmu_orthogonalize(batch, m, n, _type_of(G.dtype), _ptr(G), *ld["g"], _ptr(X), *ld["x"], int(steps), float(a), float(b),
-                                          float(c), float(eps), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), st))
+    _call(lib().ozimmu_orthogonalize, stream, (G, X, workspace), batch, m, n, _type_of(G.dtype), G.data_ptr(), *ld["g"], X.data_ptr(), *ld["x"], int(steps),
+          float(a), float(b), float(c), float(eps), _ptr(workspace), _size(workspace))
 
 
 def probe_int8_mfma(pattern: int, shape: int = 0, iters: int = 200000):
