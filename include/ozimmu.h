@@ -68,6 +68,7 @@ typedef enum { OZIMMU_F32 = 0, OZIMMU_BF16 = 1, OZIMMU_F16 = 2 } ozimmu_type_t;
 #define OZIMMU_MAX_DIM 4194304       /* largest m, n or k accepted (2^22); beyond: OZIMMU_ERR_BAD_DIM */
 #define OZIMMU_INT32_BLOCK 131072    /* at most 2^17 INT8 products go into one INT32 sum:
                                         2^17 * 127^2 < 2^31 (the exact limit is 133144) */
+#define OZIMMU_MAX_LD 16777216       /* largest distance between rows (2^24 values, bytes of codes) that the four-bit operators take */
 #define OZIMMU_MAX_BATCH 65535       /* matrices in one ozimmu_orthogonalize */
 #define OZIMMU_MAX_STEPS 64          /* of its iteration */
 #define OZIMMU_WORKSPACE_ALIGN 256
@@ -377,15 +378,15 @@ ozimmu_status_t ozimmu_zgemm_blas_auto(char transa, char transb, int64_t m, int6
  *
  * ozimmu_q4_gemm:      Y = X W^T   (X: t x k, Y: t x n: t tokens through the layer)
  * ozimmu_q4_gemm_grad: dX = dY W   (dY: t x n, dX: t x k: the gradient on its way back through it)
- * X, Y, dY, dX and the scales have type `type`; the sums are formed in 32 bits and rounded once. With up to sixteen tokens ozimmu_q4_gemm
- * multiplies the codes themselves and applies the scales to the sums, in 32 bits. All other products go through an operand of the weights in the
- * workspace: s c rounded once to bf16 or fp16, or, for 32-bit types, both operands as two fp16 slices under a
+ * X, Y, dY, dX and the scales have type `type`; the sums are formed in 32 bits and rounded once. With few tokens (how many depends on n and
+ * k: where ozimmu_q4_workspace_bytes gives 0) ozimmu_q4_gemm multiplies the codes themselves and applies the scales to the sums, in 32 bits. All other
+ * products go through an operand of the weights in the workspace: s c rounded once to bf16 or fp16, or, for 32-bit types, both operands as two fp16 slices under a
  * power-of-two exponent per row (22 bits and more of every value that is within 2^-17 of its row's largest; the rest to 2^-39
  * of that; the exponent goes with the group for the columns of W). A token or gradient row that holds an infinity or a NaN gives NaN where its results are not
  * finite; every other row is what it would be without it. Empty dimensions: t = 0 or no outputs: nothing to do; an empty inner dimension
  * gives zeros. Outputs must not overlap inputs or the workspace.
  * workspace: ozimmu_q4_workspace_bytes(...) bytes, OZIMMU_WORKSPACE_ALIGN-aligned; may be null where that is 0.
- * Errors: OZIMMU_ERR_BAD_DIM (sizes or group), OZIMMU_ERR_BAD_TYPE, OZIMMU_ERR_BAD_LD (also ldq), OZIMMU_ERR_NULL, OZIMMU_ERR_MISALIGNED,
+ * Errors: OZIMMU_ERR_BAD_DIM (sizes or group), OZIMMU_ERR_BAD_TYPE, OZIMMU_ERR_BAD_LD (also ldq, and any beyond OZIMMU_MAX_LD), OZIMMU_ERR_NULL, OZIMMU_ERR_MISALIGNED,
  * OZIMMU_ERR_WORKSPACE.
  */
 ozimmu_status_t ozimmu_q4_geometry(int64_t k, int group, int64_t* row_bytes, int64_t* groups);

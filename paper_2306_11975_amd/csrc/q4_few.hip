@@ -2,10 +2,12 @@
 //
 // What bounds it is reading the codes; the sums go to the matrix cores (v_mfma_f32_16x16x32) although most of their rows stay empty with
 // one token, because the vector units have their hands full making 16-bit operands of the codes. A wavefront takes 16 NT rows of
-// W and a part of k; the wavefronts of a workgroup share the rows and add their parts up in LDS.
+// W, 16 TT tokens and every eighth step of k; the wavefronts of a workgroup share the rows and add their parts up in LDS.
 //
-// A step is 128 positions. A lane holds rows lane % 16 of each 16 x 128 block of codes and quarter lane / 16 of every group (so that an
-// MFMA adds up positions of one group only); its word j is MFMA j's operand, and the tokens' operand is loaded from the same positions.
+// A step is 128 positions. A lane loads 16 bytes, 32 positions, of row lane % 16 of each 16 x 128 block of codes. An MFMA adds up positions of one
+// group only: in groups of 64 and 32 the quarters of a wavefront (lane / 16) first exchange words (v_permlane32_swap, v_permlane16_swap), so that
+// word j of every lane belongs to one group, and is MFMA j's operand. (Loads of 8 and 4 bytes instead: 78 us where these take 31.) The tokens' operand
+// is loaded from the same positions.
 //
 // Codes to 16-bit values: the four bits of c + 8 go into the mantissa of 16.0 (one shift, one and-or for two codes), which
 // gives 16 + (c + 8) exactly. The 24 too much is taken out by the matrix cores: the sums start from the tokens' product with a
@@ -30,28 +32,40 @@ __device__ __forceinline__ v4u pair_by_four(const v4u& x) {
     return r;
 }
 
+// The two constants of offset_codes in registers of their own (v_and_or_b32 takes one scalar and no two literals), hidden from the optimiser, which would turn them back
+// into literals and take two instructions.
+struct CodeBits {
+    unsigned mask, one;
+    template <bool BF16>
+    static __device__ __forceinline__ CodeBits of() {
+        CodeBits c;
+        if constexpr (BF16)
+            asm("s_mov_b32 %0, 0x00780078\n\tv_mov_b32 %1, 0x41804180" : "=s"(c.mask), "=v"(c.one));
+        else
+            asm("s_mov_b32 %0, 0x03c003c0\n\tv_mov_b32 %1, 0x4c004c00" : "=s"(c.mask), "=v"(c.one));
+        return c;
+    }
+};
 // 16 + (c + 8) of the codes (0, 4), (1, 5), (2, 6), (3, 7) of a word
 template <bool BF16>
-__device__ __forceinline__ v4u offset_codes(unsigned w) {
+__device__ __forceinline__ v4u offset_codes(unsigned w, const CodeBits& b) {
     v4u r;
     if constexpr (BF16) {
-        constexpr unsigned mask = 0x00780078u, one = 0x41804180u;
-        r[0] = ((w << 3) & mask) | one;
-        r[1] = ((w >> 1) & mask) | one;
-        r[2] = ((w >> 5) & mask) | one;
-        r[3] = ((w >> 9) & mask) | one;
+        r[0] = ((w << 3) & b.mask) | b.one;
+        r[1] = ((w >> 1) & b.mask) | b.one;
+        r[2] = ((w >> 5) & b.mask) | b.one;
+        r[3] = ((w >> 9) & b.mask) | b.one;
     } else {
-        constexpr unsigned mask = 0x03c003c0u, one = 0x4c004c00u;
-        r[0] = ((w << 6) & mask) | one;
-        r[1] = ((w << 2) & mask) | one;
-        r[2] = ((w >> 2) & mask) | one;
-        r[3] = ((w >> 6) & mask) | one;
+        r[0] = ((w << 6) & b.mask) | b.one;
+        r[1] = ((w << 2) & b.mask) | b.one;
+        r[2] = ((w >> 2) & b.mask) | b.one;
+        r[3] = ((w >> 6) & b.mask) | b.one;
     }
     return r;
 }
 // the codes themselves as bf16
-__device__ __forceinline__ v4u exact_codes(unsigned w) {
-    v4u r = offset_codes<true>(w);
+__device__ __forceinline__ v4u exact_codes(unsigned w, const CodeBits& b) {
+    v4u r = offset_codes<true>(w, b);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float lo = __uint_as_float(r[i] << 16) - 24.f, hi = __uint_as_float(r[i] & 0xffff0000u) - 24.f;
@@ -60,35 +74,26 @@ __device__ __forceinline__ v4u exact_codes(unsigned w) {
     return r;
 }
 
+// Eight tokens' values as loaded, and as operands: one piece, or three bf16 pieces of 32-bit values.
 template <int TYPE>
-struct Tokens {
+struct Raw {
+    v4u v[TYPE == OZIMMU_F32 ? 2 : 1];
+};
+template <int TYPE>
+struct Operand {
     static constexpr int kPieces = TYPE == OZIMMU_F32 ? 3 : 1;
     v4u piece[kPieces];
 };
-
 template <int TYPE>
-__device__ __forceinline__ Tokens<TYPE> load_tokens(const typename Elem<TYPE>::raw* x, int64_t at, int64_t k, bool here, bool vec) {
-    typedef typename Elem<TYPE>::raw raw;
-    raw r[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = raw(0);
-    if (here) {
-        if (vec && at + 8 <= k) {
-            *reinterpret_cast<v4u*>(r) = *reinterpret_cast<const v4u*>(x + at);
-            if constexpr (TYPE == OZIMMU_F32) *reinterpret_cast<v4u*>(r + 4) = *reinterpret_cast<const v4u*>(x + at + 4);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (at + e < k) r[e] = x[at + e];
-        }
-    }
-    Tokens<TYPE> t;
+__device__ __forceinline__ Operand<TYPE> operand(const Raw<TYPE>& r) {
+    Operand<TYPE> t;
     if constexpr (TYPE == OZIMMU_F32) {
         unsigned a[8], b[8], c[8];   // the upper 8 bits of the significand, the next 8, and what is left
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            a[e] = __float_as_uint(r[e]) & 0xffff0000u;
-            const float rest = r[e] - __uint_as_float(a[e]);
+            const unsigned bits = r.v[e >> 2][e & 3];
+            a[e] = bits & 0xffff0000u;
+            const float rest = __uint_as_float(bits) - __uint_as_float(a[e]);
             b[e] = __float_as_uint(rest) & 0xffff0000u;
             c[e] = __float_as_uint(rest - __uint_as_float(b[e]));
         }
@@ -99,142 +104,243 @@ __device__ __forceinline__ Tokens<TYPE> load_tokens(const typename Elem<TYPE>::r
             t.piece[2][i] = __builtin_amdgcn_perm(c[i + 4], c[i], 0x07060302u);
         }
     } else {
-        t.piece[0] = pair_by_four(*reinterpret_cast<const v4u*>(r));
+        t.piece[0] = pair_by_four(r.v[0]);
     }
     return t;
 }
 
-template <int TYPE, int GROUP, int NT>
+// vectors at the alignment of their values: rows of tokens and scales may start anywhere
+typedef v4u v4u_any __attribute__((aligned(2)));
+typedef v2u v2u_any __attribute__((aligned(2)));
+typedef unsigned u32_any __attribute__((aligned(2)));
+
+template <int TYPE, int GROUP, int NT, int TT>
 __launch_bounds__(kWaves * 64)
-__global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_t ldx, bool vec, const uint8_t* codes, int64_t ldq, const void* scales,
+__global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_t ldx, const uint8_t* codes, int64_t ldq, const void* scales,
                               int64_t lds, void* Y, int64_t ldy) {
     typedef Elem<TYPE> E;
     typedef typename E::raw raw;
     constexpr bool BF16 = TYPE != OZIMMU_F16;
     constexpr int GW = GROUP / 32, GROUPS = 128 / GROUP;   // words of a lane per group, groups of a step
-    constexpr int DEPTH = 4;                               // steps whose codes are on their way at a time
-    __shared__ float part[kWaves][16][16 * NT + 1];
+    constexpr int DEPTH = 2;                 // steps whose codes are on their way at a time
+    extern __shared__ float part[];                        // [wave][token][row]
+    constexpr int kRow = 16 * NT + 1;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t n0 = (int64_t)blockIdx.x * (16 * NT);
-    const int steps = (int)((k + 127) / 128);
-    const int begin = (int)((int64_t)steps * wave / kWaves), end = (int)((int64_t)steps * (wave + 1) / kWaves);
-    const int quarter = lane >> 4, token = lane & 15;
-    const bool here = token < t;
-    const raw* x = reinterpret_cast<const raw*>(X) + (int64_t)(here ? token : 0) * ldx;
-    const uint8_t* q[NT];
-    const raw* s[NT];
+    const int t0 = blockIdx.y * (16 * TT);
+    // Whole steps are dealt to the wavefronts in turn (together they read lines in full); the last wavefront takes what is left of the row beyond them too.
+    const int full = (int)(k / 128);
+    const int mine = (full - wave + kWaves - 1) / kWaves;
+    const int quarter = lane >> 4;
+    // position of word j of group h in a step, for this lane (the exchange between quarters below)
+    const int at_quarter = GROUP == 128 ? 32 * quarter : GROUP == 64 ? 32 * (quarter & 1) + 16 * (quarter >> 1) : 8 * quarter;
+    // Addresses are a scalar base and a lane's 32-bit offset (rows are at most OZIMMU_MAX_LD apart). Lanes of tokens and rows that are not there repeat the last one: their
+    // results go nowhere.
+    const raw* xb = reinterpret_cast<const raw*>(X) + (int64_t)t0 * ldx;
+    const uint8_t* qb = codes + n0 * ldq;
+    const raw* sb = reinterpret_cast<const raw*>(scales) + n0 * lds;
+    unsigned xo[TT], qo[NT], so[NT];   // bytes
+#pragma unroll
+    for (int i = 0; i < TT; ++i) xo[i] = ((unsigned)min(16 * i + (lane & 15), t - 1 - t0) * (unsigned)ldx + at_quarter) * sizeof(raw);
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-        const int64_t row = min(n0 + 16 * i + (lane & 15), n - 1);
-        q[i] = codes + row * ldq;
-        s[i] = reinterpret_cast<const raw*>(scales) + row * lds;
+        const unsigned row = (unsigned)min((int64_t)(16 * i + (lane & 15)), n - 1 - n0);
+        qo[i] = row * (unsigned)ldq + quarter * 16;
+        so[i] = row * (unsigned)lds * sizeof(raw);
     }
-    const int64_t row_bytes = pad_to(k, 32) / 2;
-    const int groups = (int)((k + GROUP - 1) / GROUP);
+    auto from = [](const void* base, int64_t at, unsigned offset) { return reinterpret_cast<const uint8_t*>(base) + at + offset; };
 
-    auto load_codes = [&](int step, unsigned (&w)[NT][4], raw (&sc)[NT][GROUPS]) {
+    // 16 bytes of every row and quarter: positions 32 quarter .. + 31 of the step
+    auto load_codes = [&](int step, v4u (&w)[NT], raw (&sc)[NT][GROUPS]) {
 #pragma unroll
-        for (int h = 0; h < GROUPS; ++h) {
-            const int64_t at = (int64_t)step * 64 + h * (GROUP / 2) + quarter * (GROUP / 8);   // bytes
-            const bool in = at < row_bytes;
-            const int g = min(step * GROUPS + h, groups - 1);
+        for (int i = 0; i < NT; ++i) {
+            w[i] = *reinterpret_cast<const v4u*>(from(qb, (int64_t)step * 64, qo[i]));
+            const uint8_t* at = from(sb, (int64_t)step * GROUPS * sizeof(raw), so[i]);
+            if constexpr (GROUPS * sizeof(raw) == 16)
+                *reinterpret_cast<v4u*>(sc[i]) = *reinterpret_cast<const v4u_any*>(at);
+            else if constexpr (GROUPS * sizeof(raw) == 8)
+                *reinterpret_cast<v2u*>(sc[i]) = *reinterpret_cast<const v2u_any*>(at);
+            else if constexpr (GROUPS * sizeof(raw) == 4)
+                *reinterpret_cast<unsigned*>(sc[i]) = *reinterpret_cast<const u32_any*>(at);
+            else
+                sc[i][0] = *reinterpret_cast<const raw*>(at);
+        }
+    };
+    constexpr int kParts = TYPE == OZIMMU_F32 ? 2 : 1;
+    auto load_word = [&](int step, int j, Raw<TYPE> (&to)[TT]) {
+        const int64_t at = ((int64_t)step * 128 + (j / GW) * GROUP + 8 * (j % GW)) * sizeof(raw);
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                // (where a quarter lies beyond the row its tokens are zeros, and any finite code will do)
-                if constexpr (GW == 4) {
-                    // a row's last 16 bytes can be this quarter's only in full: rows take a multiple of 16 bytes
-                    const v4u v = in ? *reinterpret_cast<const v4u*>(q[i] + at) : v4u{0, 0, 0, 0};
+        for (int i = 0; i < TT; ++i)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) w[i][j] = v[j];
-                } else if constexpr (GW == 2) {
-                    const v2u v = in ? *reinterpret_cast<const v2u*>(q[i] + at) : v2u{0, 0};
-                    w[i][2 * h] = v[0];
-                    w[i][2 * h + 1] = v[1];
-                } else {
-                    w[i][h] = in ? *reinterpret_cast<const unsigned*>(q[i] + at) : 0u;
-                }
-                sc[i][h] = s[i][g];
+            for (int v = 0; v < kParts; ++v) to[i].v[v] = *reinterpret_cast<const v4u_any*>(from(xb, at + 16 * v, xo[i]));
+    };
+    // The same where a row ends inside the step: tokens beyond k are zeros, so any finite code will do there (rows take a multiple of 16 bytes).
+    auto load_last_codes = [&](v4u (&w)[NT], raw (&sc)[NT][GROUPS]) {
+        const int64_t last = pad_to(k, 32) / 2 - 16;
+        const int groups = (int)((k + GROUP - 1) / GROUP);
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            w[i] = *reinterpret_cast<const v4u*>(from(qb, min((int64_t)full * 64 + quarter * 16, last) - quarter * 16, qo[i]));
+#pragma unroll
+            for (int h = 0; h < GROUPS; ++h) sc[i][h] = *reinterpret_cast<const raw*>(from(sb, (int64_t)min(full * GROUPS + h, groups - 1) * sizeof(raw), so[i]));
+        }
+    };
+    auto load_last_word = [&](int j, Raw<TYPE> (&to)[TT]) {
+        const int64_t at = (int64_t)full * 128 + (j / GW) * GROUP + 8 * (j % GW);
+#pragma unroll
+        for (int i = 0; i < TT; ++i) {
+            raw r[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int64_t beyond = max(at + at_quarter + e - (k - 1), (int64_t)0);
+                const raw y = *reinterpret_cast<const raw*>(from(xb, (at + e - beyond) * (int64_t)sizeof(raw), xo[i]));
+                r[e] = beyond ? raw(0) : y;
             }
+#pragma unroll
+            for (int v = 0; v < kParts; ++v) to[i].v[v] = *reinterpret_cast<const v4u*>(r + 4 * v);
         }
     };
 
-    v4f total[NT];
-#pragma unroll
-    for (int i = 0; i < NT; ++i) total[i] = v4f{0.f, 0.f, 0.f, 0.f};
-    const unsigned minus = BF16 ? 0xc1c0c1c0u : 0xce00ce00u;   // -24, twice
-    const v4u minus24 = {minus, minus, minus, minus};
-
-    auto multiply = [&](int step, const unsigned (&w)[NT][4], const raw (&sc)[NT][GROUPS]) {
-#pragma unroll
-        for (int h = 0; h < GROUPS; ++h) {
-            v4f sum[NT];
-            v4f start = v4f{0.f, 0.f, 0.f, 0.f};
-            Tokens<TYPE> xs[GW];
-#pragma unroll
-            for (int j = 0; j < GW; ++j) {
-                const int64_t at = (int64_t)step * 128 + h * GROUP + quarter * (GROUP / 4) + 8 * j;
-                xs[j] = load_tokens<TYPE>(x, at, k, here, vec);
-                if constexpr (TYPE != OZIMMU_F32) start = mfma_half<BF16>(xs[j].piece[0], minus24, start);
-            }
-#pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                sum[i] = start;
-#pragma unroll
-                for (int j = 0; j < GW; ++j) {
-                    const unsigned word = w[i][GW * h + j];
-                    if constexpr (TYPE == OZIMMU_F32) {
-                        const v4u c = exact_codes(word);
-#pragma unroll
-                        for (int p = 2; p >= 0; --p) sum[i] = mfma_half<true>(xs[j].piece[p], c, sum[i]);
-                    } else {
-                        sum[i] = mfma_half<BF16>(xs[j].piece[0], offset_codes<BF16>(word), sum[i]);
-                    }
-                }
-                const float f = E::load(sc[i][h]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) total[i][e] = fmaf(f, sum[i][e], total[i][e]);
-            }
-        }
-    };
-
-    unsigned w[DEPTH][NT][4];
-    raw sc[DEPTH][NT][GROUPS];
-#pragma unroll
-    for (int d = 0; d < DEPTH; ++d)
-        if (begin + d < end) load_codes(begin + d, w[d], sc[d]);
-    for (int step = begin; step < end; step += DEPTH) {
-#pragma unroll
-        for (int d = 0; d < DEPTH; ++d) {
-            if (step + d < end) multiply(step + d, w[d], sc[d]);
-            if (step + d + DEPTH < end) load_codes(step + d + DEPTH, w[d], sc[d]);
-        }
-    }
-
-    // lane: tokens 4 quarter .. + 3, rows lane % 16
+    v4f total[NT][TT];
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) part[wave][4 * quarter + e][16 * i + (lane & 15)] = total[i][e];
+        for (int tt = 0; tt < TT; ++tt) total[i][tt] = v4f{0.f, 0.f, 0.f, 0.f};
+    const unsigned minus = BF16 ? 0xc1c0c1c0u : 0xce00ce00u;   // -24, twice
+    const v4u minus24 = {minus, minus, minus, minus};
+    const CodeBits bits = CodeBits::of<BF16>();
+
+    auto multiply = [&](const v4u (&w)[NT], const raw (&sc)[NT][GROUPS], const Raw<TYPE> (&xs)[4][TT]) {
+        // words by group: the quarters of a group of 64 or 32 hold positions of two or four groups each and exchange them
+        unsigned words[NT][4];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            v4u v = w[i];
+            if constexpr (GROUP < 128) {
+                const auto a = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
+                const auto b = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
+                v = v4u{a[0], b[0], a[1], b[1]};
+                if constexpr (GROUP == 32) {
+                    const auto c = __builtin_amdgcn_permlane16_swap(v[0], v[1], false, false);
+                    const auto e = __builtin_amdgcn_permlane16_swap(v[2], v[3], false, false);
+                    v = v4u{c[0], c[1], e[0], e[1]};
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) words[i][j] = v[j];
+        }
+#pragma unroll
+        for (int h = 0; h < GROUPS; ++h) {
+            v4f sum[NT][TT], offset[TT];
+#pragma unroll
+            for (int j = 0; j < GW; ++j) {
+                Operand<TYPE> o[TT];
+#pragma unroll
+                for (int tt = 0; tt < TT; ++tt) o[tt] = operand<TYPE>(xs[GW * h + j][tt]);
+                const v4f zero = v4f{0.f, 0.f, 0.f, 0.f};
+                if constexpr (TYPE != OZIMMU_F32)
+#pragma unroll
+                    for (int tt = 0; tt < TT; ++tt) offset[tt] = mfma_half<BF16>(o[tt].piece[0], minus24, j ? offset[tt] : zero);
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    const unsigned word = words[i][GW * h + j];
+                    if constexpr (TYPE == OZIMMU_F32) {
+                        const v4u c = exact_codes(word, bits);
+#pragma unroll
+                        for (int p = 2; p >= 0; --p)
+#pragma unroll
+                            for (int tt = 0; tt < TT; ++tt) sum[i][tt] = mfma_half<true>(o[tt].piece[p], c, j || p < 2 ? sum[i][tt] : zero);
+                    } else {
+                        const v4u c = offset_codes<BF16>(word, bits);
+#pragma unroll
+                        for (int tt = 0; tt < TT; ++tt) sum[i][tt] = mfma_half<BF16>(o[tt].piece[0], c, j ? sum[i][tt] : zero);
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                const float f = E::load(sc[i][h]);
+#pragma unroll
+                for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        total[i][tt][e] = fmaf(f, TYPE == OZIMMU_F32 ? sum[i][tt][e] : sum[i][tt][e] + offset[tt][e], total[i][tt][e]);
+            }
+        }
+    };
+    if (mine > 0) {
+        v4u w[DEPTH][NT];
+        raw sc[DEPTH][NT][GROUPS] __attribute__((aligned(16)));
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d)
+            if (d < mine) load_codes(d * kWaves + wave, w[d], sc[d]);
+        Raw<TYPE> xs[2][4][TT];   // this step's tokens and the next one's
+#pragma unroll
+        for (int j = 0; j < 4; ++j) load_word(wave, j, xs[0][j]);
+        for (int step0 = 0; step0 < mine; step0 += DEPTH) {
+#pragma unroll
+            for (int d = 0; d < DEPTH; ++d) {
+                const int step = step0 + d;
+                if (step >= mine) break;
+                if (step + 1 < mine)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) load_word((step + 1) * kWaves + wave, j, xs[(d + 1) & 1][j]);
+                multiply(w[d], sc[d], xs[d & 1]);
+                if (step + DEPTH < mine) load_codes((step + DEPTH) * kWaves + wave, w[d], sc[d]);
+            }
+        }
+    }
+    if (wave == kWaves - 1 && k > (int64_t)full * 128) {
+        v4u w[NT];
+        raw sc[NT][GROUPS];
+        Raw<TYPE> xs[4][TT];
+        load_last_codes(w, sc);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) load_last_word(j, xs[j]);
+        multiply(w, sc, xs);
+    }
+
+    // lane: tokens 4 quarter .. + 3 of a tile, rows lane % 16
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) part[(wave * 16 * TT + 16 * tt + 4 * quarter + e) * kRow + 16 * i + (lane & 15)] = total[i][tt][e];
     __syncthreads();
-    for (int at = threadIdx.x; at < t * 16 * NT; at += kWaves * 64) {
+    const int here = min(16 * TT, t - t0);
+    for (int at = threadIdx.x; at < here * 16 * NT; at += kWaves * 64) {
         const int tok = at / (16 * NT), col = at % (16 * NT);
         if (n0 + col >= n) continue;
-        float sum = part[0][tok][col];
+        float sum = part[tok * kRow + col];
 #pragma unroll
-        for (int i = 1; i < kWaves; ++i) sum += part[i][tok][col];
-        reinterpret_cast<raw*>(Y)[(int64_t)tok * ldy + n0 + col] = E::store(sum);
+        for (int i = 1; i < kWaves; ++i) sum += part[(i * 16 * TT + tok) * kRow + col];
+        reinterpret_cast<raw*>(Y)[(int64_t)(t0 + tok) * ldy + n0 + col] = E::store(sum);
     }
 }
 
+template <int TYPE, int GROUP, int NT, int TT>
+hipError_t launch_tiles(int64_t t, int64_t n, int64_t k, const void* X, int64_t ldx, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds,
+                        void* Y, int64_t ldy, hipStream_t st) {
+    constexpr auto kernel = q4_few_kernel<TYPE, GROUP, NT, TT>;
+    constexpr int bytes = kWaves * 16 * TT * (16 * NT + 1) * sizeof(float);
+    if (hipError_t e = allow_dynamic_lds<kernel>(bytes); e != hipSuccess) return e;
+    const dim3 grid((unsigned)((n + 16 * NT - 1) / (16 * NT)), (unsigned)((t + 16 * TT - 1) / (16 * TT)));
+    kernel<<<grid, kWaves * 64, bytes, st>>>((int)t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy);
+    return hipGetLastError();
+}
 template <int TYPE, int GROUP>
 hipError_t launch_typed(int64_t t, int64_t n, int64_t k, const void* X, int64_t ldx, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds,
                         void* Y, int64_t ldy, hipStream_t st) {
-    const bool vec = rows_aligned16(X, ldx, sizeof(typename Elem<TYPE>::raw));
-    if (n >= 32 * 256)
-        q4_few_kernel<TYPE, GROUP, 2><<<dim3((unsigned)((n + 31) / 32)), kWaves * 64, 0, st>>>((int)t, n, k, X, ldx, vec, codes, ldq, scales, lds, Y, ldy);
-    else
-        q4_few_kernel<TYPE, GROUP, 1><<<dim3((unsigned)((n + 15) / 16)), kWaves * 64, 0, st>>>((int)t, n, k, X, ldx, vec, codes, ldq, scales, lds, Y, ldy);
-    return hipGetLastError();
+    // More rows of W to a wavefront: fewer loads of tokens; more wavefronts: more codes on their way. (t = 16, n = 16384, k = 8192 with 16, 32, 64 rows: 46.9, 32.7, 25.8 us;
+    // t = 1: 27.7, 22.5, 20.9; but n = 8192, k = 4096, t = 1: 8.7, 8.0, 12.0.) Two tiles of tokens share the operands made of the codes; with
+    // 32-bit tokens the registers do not suffice.
+    if constexpr (TYPE != OZIMMU_F32) {
+        if (t > 16) return launch_tiles<TYPE, GROUP, 2, 2>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
+        if (n >= 64 * 256) return launch_tiles<TYPE, GROUP, 4, 1>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
+    }
+    if (n * ((t + 15) / 16) >= 32 * 256) return launch_tiles<TYPE, GROUP, 2, 1>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
+    return launch_tiles<TYPE, GROUP, 1, 1>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
 }
 template <int TYPE>
 hipError_t launch_grouped(int64_t t, int64_t n, int64_t k, int group, const void* X, int64_t ldx, const uint8_t* codes, int64_t ldq, const void* scales,

@@ -25,7 +25,7 @@ bool misaligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p
 
 // What every call on weights in four bits checks of them (n, k > 0).
 ozimmu_status_t check_q4(int64_t k, int group, const void* codes, int64_t ldq, const void* scales, int scale_type, int64_t lds) {
-    if (ldq < row_bytes(k) || ldq % 16 != 0 || lds < groups_of(k, group)) return OZIMMU_ERR_BAD_LD;
+    if (ldq < row_bytes(k) || ldq % 16 != 0 || lds < groups_of(k, group) || ldq > OZIMMU_MAX_LD || lds > OZIMMU_MAX_LD) return OZIMMU_ERR_BAD_LD;
     if (!codes || !scales) return OZIMMU_ERR_NULL;
     if (misaligned(codes, 16) || misaligned(scales, size_of(scale_type))) return OZIMMU_ERR_MISALIGNED;
     return OZIMMU_OK;
@@ -53,7 +53,17 @@ Operands operands(int64_t t, int64_t n, int64_t k, int group, int type, bool gra
     o.total = off;
     return o;
 }
-bool few(int64_t t, bool gradient) { return !gradient && t <= kFewTokens; }
+// Whether Y = X W^T multiplies the codes as they are, 16 or 32 tokens a pass over them, or makes an operand of the weights and runs the tiled
+// product: by an estimate of both, in us. The passes take what their matrix and vector work takes; the product a walk along k, the operand's
+// bytes and its own operations.
+bool few(int64_t t, int64_t n, int64_t k, int type, bool gradient) {
+    if (gradient || t > 65535 * 16) return false;   // (the launch's second dimension)
+    const double nk = (double)n * (double)k;
+    // (tokens by the pass in both: more of them never go back to the passes, so that a workspace serves fewer tokens too)
+    const double passes = (double)(type == OZIMMU_F32 ? (t + 15) / 16 : (t + 31) / 32);
+    if (type == OZIMMU_F32) return 3.5 + 3.7e-7 * nk * passes <= 14.0 + 0.0055 * k + 1.0e-6 * nk + 6.7e-8 * passes * nk;
+    return 3.5 + 3.85e-7 * nk * passes <= 6.0 + 0.0047 * k + 6.0e-7 * nk + 4.6e-8 * passes * nk;
+}
 
 ozimmu_status_t q4_product(bool gradient, int64_t t, int64_t n, int64_t k, int group, int type, const void* V, int64_t ldv, const uint8_t* codes,
                            int64_t ldq, const void* scales, int64_t lds, void* R, int64_t ldr, void* ws, size_t ws_bytes, void* stream) {
@@ -61,7 +71,7 @@ ozimmu_status_t q4_product(bool gradient, int64_t t, int64_t n, int64_t k, int g
     if (!type_ok(type)) return OZIMMU_ERR_BAD_TYPE;
     const int64_t inner = gradient ? n : k, outer = gradient ? k : n;
     if (t == 0 || outer == 0) return OZIMMU_OK;
-    if (ldv < inner || ldr < outer) return OZIMMU_ERR_BAD_LD;
+    if (ldv < inner || ldr < outer || ldv > OZIMMU_MAX_LD || ldr > OZIMMU_MAX_LD) return OZIMMU_ERR_BAD_LD;
     if (!R) return OZIMMU_ERR_NULL;
     if (misaligned(R, size_of(type))) return OZIMMU_ERR_MISALIGNED;
     if (inner > 0) {
@@ -71,7 +81,7 @@ ozimmu_status_t q4_product(bool gradient, int64_t t, int64_t n, int64_t k, int g
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (inner == 0) return hip_status(launch_zero_rows(t, outer, R, type, ldr, st));
-    if (few(t, gradient)) return hip_status(launch_q4_few(t, n, k, group, V, type, ldv, codes, ldq, scales, lds, R, ldr, st));
+    if (few(t, n, k, type, gradient)) return hip_status(launch_q4_few(t, n, k, group, V, type, ldv, codes, ldq, scales, lds, R, ldr, st));
     const Operands o = operands(t, n, k, group, type, gradient);
     if (!ws || misaligned(ws, OZIMMU_WORKSPACE_ALIGN) || ws_bytes < o.total) return OZIMMU_ERR_WORKSPACE;
     unsigned char* base = static_cast<unsigned char*>(ws);
@@ -192,7 +202,7 @@ ozimmu_status_t ozimmu_q4_split(int64_t n, int64_t k, int group, ozimmu_type_t t
     if (!dim_ok(n) || !dim_ok(k) || !group_ok(group)) return OZIMMU_ERR_BAD_DIM;
     if (!type_ok(type) || !type_ok(scale_type)) return OZIMMU_ERR_BAD_TYPE;
     if (n == 0 || k == 0) return OZIMMU_OK;
-    if (ldw < k) return OZIMMU_ERR_BAD_LD;
+    if (ldw < k || ldw > OZIMMU_MAX_LD) return OZIMMU_ERR_BAD_LD;
     if (!W) return OZIMMU_ERR_NULL;
     if (misaligned(W, size_of(type))) return OZIMMU_ERR_MISALIGNED;
     if (ozimmu_status_t rc = check_q4(k, group, codes, ldq, scales, scale_type, lds); rc != OZIMMU_OK) return rc;
@@ -204,7 +214,7 @@ ozimmu_status_t ozimmu_q4_expand(int64_t n, int64_t k, int group, ozimmu_type_t 
     if (!dim_ok(n) || !dim_ok(k) || !group_ok(group)) return OZIMMU_ERR_BAD_DIM;
     if (!type_ok(type)) return OZIMMU_ERR_BAD_TYPE;
     if (n == 0 || k == 0) return OZIMMU_OK;
-    if (ldw < k) return OZIMMU_ERR_BAD_LD;
+    if (ldw < k || ldw > OZIMMU_MAX_LD) return OZIMMU_ERR_BAD_LD;
     if (!W) return OZIMMU_ERR_NULL;
     if (misaligned(W, size_of(type))) return OZIMMU_ERR_MISALIGNED;
     if (ozimmu_status_t rc = check_q4(k, group, codes, ldq, scales, type, lds); rc != OZIMMU_OK) return rc;
@@ -215,7 +225,7 @@ ozimmu_status_t ozimmu_q4_workspace_bytes(int64_t t, int64_t n, int64_t k, int g
     if (!dim_ok(t) || !dim_ok(n) || !dim_ok(k) || !group_ok(group)) return OZIMMU_ERR_BAD_DIM;
     if (!type_ok(type)) return OZIMMU_ERR_BAD_TYPE;
     if (!bytes) return OZIMMU_ERR_NULL;
-    *bytes = few(t, gradient != 0) || t == 0 || n == 0 || k == 0 ? 0 : operands(t, n, k, group, type, gradient != 0).total;
+    *bytes = few(t, n, k, type, gradient != 0) || t == 0 || n == 0 || k == 0 ? 0 : operands(t, n, k, group, type, gradient != 0).total;
     return OZIMMU_OK;
 }
 

@@ -20,7 +20,10 @@ def expand(n=4, k=64, group=32, type_=0, codes=FAKE, ldq=32, scales=FAKE, lds=2,
     return oz.lib().ozimmu_q4_expand(n, k, group, type_, codes, ldq, scales, lds, W, ldw, None)
 
 
-def gemm(t=40, n=8, k=64, group=32, type_=0, V=FAKE, ldv=64, codes=FAKE, ldq=32, scales=FAKE, lds=2, R=FAKE, ldr=64, ws=FAKE, size=BIG, grad=False):
+LARGE = dict(n=4096, k=4096, ldv=4096, ldq=2048, lds=128, ldr=4096)      # a size that takes a workspace
+
+
+def gemm(t=4000, n=8, k=64, group=32, type_=0, V=FAKE, ldv=64, codes=FAKE, ldq=32, scales=FAKE, lds=2, R=FAKE, ldr=64, ws=FAKE, size=BIG, grad=False):
     f = oz.lib().ozimmu_q4_gemm_grad if grad else oz.lib().ozimmu_q4_gemm
     return f(t, n, k, group, type_, V, ldv, codes, ldq, scales, lds, R, ldr, ws, size, None)
 
@@ -49,11 +52,13 @@ def test_workspace_sizes():
     assert size(16, 4096, 4096, 128, torch.bfloat16, gradient=True) > 0
     assert size(300, 4096, 4000, 128, torch.float16) >= 2 * 4000 * 4096
     assert size(300, 4096, 4000, 128, torch.float32) >= 4 * 4000 * 4096
+    assert size(1 << 21, 1, 1, 32, torch.float32) > 0             # more tokens than a launch of passes takes
     # more tokens never ask for less: a workspace serves fewer tokens than it was made for
     for dt in (torch.float32, torch.bfloat16):
         for grad in (False, True):
-            sizes = [size(t, 1000, 3000, 64, dt, grad) for t in (0, 1, 16, 17, 64, 65, 256, 257, 4096)]
-            assert sizes == sorted(sizes)
+            for n, k in ((1000, 3000), (4096, 4096), (16384, 8192), (100, 70)):
+                sizes = [size(t, n, k, 64, dt, grad) for t in [*range(0, 1300, 3), 4096, 10 ** 5, 10 ** 6, 1 << 21]]
+                assert sizes == sorted(sizes)
     with pytest.raises(ValueError):
         size(1, 1, 1, 32, torch.float64)
     out = ctypes.c_size_t()
@@ -79,7 +84,9 @@ def test_workspace_sizes():
     (gemm, dict(ldv=63), oz.ERR_BAD_LD), (gemm, dict(ldr=7), oz.ERR_BAD_LD), (gemm, dict(ldq=0), oz.ERR_BAD_LD), (gemm, dict(lds=0), oz.ERR_BAD_LD),
     (gemm, dict(V=None), oz.ERR_NULL), (gemm, dict(R=None), oz.ERR_NULL), (gemm, dict(codes=None), oz.ERR_NULL), (gemm, dict(scales=None), oz.ERR_NULL),
     (gemm, dict(V=ODD), oz.ERR_MISALIGNED), (gemm, dict(R=ODD), oz.ERR_MISALIGNED), (gemm, dict(codes=ODD), oz.ERR_MISALIGNED),
-    (gemm, dict(ws=None), oz.ERR_WORKSPACE), (gemm, dict(ws=ctypes.c_void_p(4224)), oz.ERR_WORKSPACE), (gemm, dict(size=64), oz.ERR_WORKSPACE),
+    (gemm, dict(ws=None, **LARGE), oz.ERR_WORKSPACE), (gemm, dict(ws=ctypes.c_void_p(4224), **LARGE), oz.ERR_WORKSPACE), (gemm, dict(size=64, **LARGE), oz.ERR_WORKSPACE),
+    (gemm, dict(ldv=(1 << 24) + 1), oz.ERR_BAD_LD), (gemm, dict(ldr=(1 << 24) + 1), oz.ERR_BAD_LD), (gemm, dict(ldq=(1 << 24) + 16), oz.ERR_BAD_LD), (gemm, dict(lds=(1 << 24) + 1), oz.ERR_BAD_LD),
+    (split, dict(ldw=(1 << 24) + 1), oz.ERR_BAD_LD), (expand, dict(ldw=1 << 25), oz.ERR_BAD_LD),
     (gemm, dict(grad=True, ldv=7), oz.ERR_BAD_LD), (gemm, dict(grad=True, ldr=63), oz.ERR_BAD_LD), (gemm, dict(grad=True, ws=None), oz.ERR_WORKSPACE),
     (gemm, dict(grad=True, t=1, ws=None), oz.ERR_WORKSPACE), (gemm, dict(grad=True, type_=-1), oz.ERR_BAD_TYPE),
     (orth, dict(batch=-1), oz.ERR_BAD_DIM), (orth, dict(batch=65536), oz.ERR_BAD_DIM), (orth, dict(m=-1), oz.ERR_BAD_DIM), (orth, dict(n=MAX + 1), oz.ERR_BAD_DIM),
