@@ -416,7 +416,7 @@ ozimmu_status_t ozimmu_q4_gemm_grad(int64_t t, int64_t n, int64_t k, int group, 
  * steps in 1 .. OZIMMU_MAX_STEPS, eps >= 0 and finite, a >= 1 (small singular values must not shrink: they are held to 2^-38 absolutely, or as
  * much more as intermediate values exceed four), and the polynomial must keep [0, 1] bounded under its iteration, so that no
  * intermediate value exceeds 4096: otherwise OZIMMU_ERR_BAD_POLYNOMIAL. batch <= OZIMMU_MAX_BATCH; matrices of X must not overlap each other.
- * workspace: ozimmu_orthogonalize_workspace_bytes(...) bytes, OZIMMU_WORKSPACE_ALIGN-aligned. m or n or batch = 0: nothing to do.
+ * workspace: ozimmu_orthogonalize_workspace_bytes(...) bytes, OZIMMU_WORKSPACE_ALIGN-aligned; may be null where that is 0. m or n or batch = 0: nothing to do.
  */
 ozimmu_status_t ozimmu_orthogonalize_workspace_bytes(int64_t batch, int64_t m, int64_t n, size_t* bytes);
 ozimmu_status_t ozimmu_orthogonalize(int64_t batch, int64_t m, int64_t n, ozimmu_type_t type, const void* G,

@@ -148,6 +148,8 @@ OrthLayout orth_layout(int64_t batch, int64_t m, int64_t n) {
     return o;
 }
 
+bool small_update(int64_t m, int64_t n) { return std::min(m, n) <= kSmallShorter && std::max(m, n) <= kSmallLonger; }
+
 // The power of two that slices of fp16 hold the iterates under: the largest up to 2^14 with which nothing overflows. The singular
 // values start at most at one, p(x) = a x + b x^3 + c x^5 takes [0, r] into [0, max |p|], and no element of X, A = X X^T or a + b A + c A^2 is
 // larger than its matrix's norm. -1: there is none, or a < 1: small values would shrink towards the 2^-25 that the slices leave of it.
@@ -243,7 +245,7 @@ ozimmu_status_t ozimmu_q4_gemm_grad(int64_t t, int64_t n, int64_t k, int group, 
 ozimmu_status_t ozimmu_orthogonalize_workspace_bytes(int64_t batch, int64_t m, int64_t n, size_t* bytes) {
     if (!dim_ok(m) || !dim_ok(n) || batch < 0 || batch > OZIMMU_MAX_BATCH) return OZIMMU_ERR_BAD_DIM;
     if (!bytes) return OZIMMU_ERR_NULL;
-    *bytes = batch == 0 || m == 0 || n == 0 ? 0 : orth_layout(batch, m, n).total;
+    *bytes = batch == 0 || m == 0 || n == 0 || small_update(m, n) ? 0 : orth_layout(batch, m, n).total;
     return OZIMMU_OK;
 }
 
@@ -260,9 +262,10 @@ ozimmu_status_t ozimmu_orthogonalize(int64_t batch, int64_t m, int64_t n, ozimmu
     if (ldg < n || ldx < n || (batch > 1 && (stride_g < 0 || stride_x < (m - 1) * ldx + n))) return OZIMMU_ERR_BAD_LD;
     if (!G || !X) return OZIMMU_ERR_NULL;
     if (misaligned(G, size_of(type)) || misaligned(X, size_of(type))) return OZIMMU_ERR_MISALIGNED;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (small_update(m, n)) return hip_status(launch_orthogonalize_small(batch, m, n, G, type, ldg, stride_g, X, ldx, stride_x, steps, a, b, c, eps, shift, st));
     const OrthLayout o = orth_layout(batch, m, n);
     if (!workspace || misaligned(workspace, OZIMMU_WORKSPACE_ALIGN) || workspace_bytes < o.total) return OZIMMU_ERR_WORKSPACE;
-    hipStream_t st = static_cast<hipStream_t>(stream);
     unsigned char* base = static_cast<unsigned char*>(workspace);
     auto at = [&](size_t off) { return reinterpret_cast<unsigned short*>(base + off); };
     double* partials = reinterpret_cast<double*>(base + o.off_norm);

@@ -76,4 +76,9 @@ hipError_t launch_normalised_slices(int64_t batch, int64_t m, int64_t n, const v
                                     const double* partials, double eps, int shift, unsigned short* rows, int64_t ldr,
                                     int64_t batch_r, unsigned short* cols, int64_t ldc, int64_t batch_c, hipStream_t st);
 
+// orthogonalize_small.hip: the whole update by one workgroup per matrix
+constexpr int64_t kSmallShorter = 64, kSmallLonger = 256;
+hipError_t launch_orthogonalize_small(int64_t batch, int64_t m, int64_t n, const void* G, int type, int64_t ldg, int64_t stride_g, void* X, int64_t ldx,
+                                      int64_t stride_x, int steps, double a, double b, double c, double eps, int shift, hipStream_t st);
+
 }  // namespace ozimmu

@@ -45,7 +45,7 @@ def check(got, G, steps=5, coefficients=MUON, eps=1e-7):
     assert off <= allowed, (off, allowed)
 
 
-SHAPES = [(1, 1), (1, 7), (7, 1), (2, 2), (16, 16), (31, 33), (33, 31), (64, 64), (64, 48), (65, 64), (100, 300), (300, 100), (128, 128), (129, 520), (513, 200), (700, 700)]
+SHAPES = [(1, 1), (1, 7), (7, 1), (2, 2), (16, 16), (31, 33), (33, 31), (64, 64), (64, 48), (65, 64), (64, 256), (256, 63), (20, 257), (33, 100), (100, 300), (300, 100), (128, 128), (129, 520), (513, 200), (700, 700)]
 
 
 @pytest.mark.parametrize("dt", [F32, BF16, F16])

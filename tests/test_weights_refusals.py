@@ -28,6 +28,9 @@ def gemm(t=4000, n=8, k=64, group=32, type_=0, V=FAKE, ldv=64, codes=FAKE, ldq=3
     return f(t, n, k, group, type_, V, ldv, codes, ldq, scales, lds, R, ldr, ws, size, None)
 
 
+WIDE = dict(n=300, ldg=300, ldx=300)      # a size that takes a workspace
+
+
 def orth(batch=1, m=8, n=16, type_=0, G=FAKE, ldg=16, sg=0, X=FAKE, ldx=16, sx=0, steps=5, a=3.4445, b=-4.775, c=2.0315, eps=1e-7, ws=FAKE, size=BIG):
     return oz.lib().ozimmu_orthogonalize(batch, m, n, type_, G, ldg, sg, X, ldx, sx, steps, a, b, c, eps, ws, size, None)
 
@@ -66,6 +69,8 @@ def test_workspace_sizes():
     assert oz.lib().ozimmu_q4_workspace_bytes(1, 1, 1, 32, 0, 0, None) == oz.ERR_NULL
     assert oz.lib().ozimmu_q4_workspace_bytes(-1, 1, 1, 32, 0, 0, ctypes.byref(out)) == oz.ERR_BAD_DIM
     assert oz.orthogonalize_workspace_bytes(0, 4, 4) == 0
+    assert oz.orthogonalize_workspace_bytes(9, 64, 256) == oz.orthogonalize_workspace_bytes(9, 256, 64) == 0       # one workgroup per matrix
+    assert oz.orthogonalize_workspace_bytes(9, 64, 257) > 0 and oz.orthogonalize_workspace_bytes(9, 65, 65) > 0
     assert oz.orthogonalize_workspace_bytes(3, 100, 200) >= 3 * 4 * (100 * 200 + 2 * 100 * 200 + 2 * 100 * 100)
     assert oz.lib().ozimmu_orthogonalize_workspace_bytes(1, 4, 4, None) == oz.ERR_NULL
     assert oz.lib().ozimmu_orthogonalize_workspace_bytes(65536, 4, 4, ctypes.byref(out)) == oz.ERR_BAD_DIM
@@ -95,8 +100,8 @@ def test_workspace_sizes():
     (orth, dict(eps=float("nan")), oz.ERR_BAD_POLYNOMIAL), (orth, dict(a=0.99), oz.ERR_BAD_POLYNOMIAL), (orth, dict(a=-3.4445, b=4.775, c=-2.0315), oz.ERR_BAD_POLYNOMIAL), (orth, dict(a=5000.0), oz.ERR_BAD_POLYNOMIAL), (orth, dict(a=3.0, b=4.0, c=5.0), oz.ERR_BAD_POLYNOMIAL),
     (orth, dict(ldg=15), oz.ERR_BAD_LD), (orth, dict(ldx=15), oz.ERR_BAD_LD), (orth, dict(batch=2, sg=128, sx=127), oz.ERR_BAD_LD),
     (orth, dict(batch=2, sg=-1, sx=128), oz.ERR_BAD_LD), (orth, dict(G=None), oz.ERR_NULL), (orth, dict(X=None), oz.ERR_NULL), (orth, dict(G=ODD), oz.ERR_MISALIGNED),
-    (orth, dict(X=ODD, type_=1), oz.ERR_MISALIGNED), (orth, dict(ws=None), oz.ERR_WORKSPACE), (orth, dict(ws=ctypes.c_void_p(4352 + 16)), oz.ERR_WORKSPACE),
-    (orth, dict(size=1000), oz.ERR_WORKSPACE),
+    (orth, dict(X=ODD, type_=1), oz.ERR_MISALIGNED), (orth, dict(ws=None, **WIDE), oz.ERR_WORKSPACE), (orth, dict(ws=ctypes.c_void_p(4352 + 16), **WIDE), oz.ERR_WORKSPACE),
+    (orth, dict(size=1000, **WIDE), oz.ERR_WORKSPACE),
 ])
 def test_refusals(call, bad, code):
     assert call(**bad) == code
