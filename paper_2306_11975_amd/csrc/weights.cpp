@@ -143,7 +143,7 @@ OrthLayout orth_layout(int64_t batch, int64_t m, int64_t n) {
     o.off_t[1] = take(2 * (size_t)batch * o.size_t_);
     o.off_a = take(2 * (size_t)batch * o.size_a);
     o.off_q = take(2 * (size_t)batch * o.size_a);
-    o.off_norm = take(sizeof(double) * (size_t)batch * kNormBlocks);
+    o.off_norm = take(sizeof(double) * (size_t)batch * norm_parts(m, n));
     o.total = off;
     return o;
 }

@@ -68,7 +68,8 @@ hipError_t launch_q4_few(int64_t t, int64_t n, int64_t k, int group, const void*
                          int64_t ldq, const void* scales, int64_t lds, void* Y, int64_t ldy, hipStream_t st);
 
 // orthogonalize.hip
-constexpr int kNormBlocks = 256;   // partial sums of squares per matrix
+constexpr int kMostNormParts = 1024;   // partial sums of squares per matrix
+int norm_parts(int64_t m, int64_t n);
 hipError_t launch_norm_partials(int64_t batch, int64_t m, int64_t n, const void* G, int type, int64_t ldg, int64_t stride,
                                 double* partials, hipStream_t st);
 // G / (|G| + eps) in two slices of fp16 scaled by 2^shift, as it lies (rows of n) and transposed (rows of m)
