@@ -8,36 +8,127 @@
 // wavefront and load; the lane that fetches 16-byte piece c of row r puts it at place c ^ (r % 8), so that the 16 lanes of a
 // fragment read, ds_read_b128, meet all banks), STAGES - 1 slabs ahead of the one that is multiplied: one barrier per slab. Rows
 // beyond the last are read from the last one and their results dropped.
+// With fewer tiles than run at a time, or a last round of them that is far from full, several workgroups share a tile's inner dimension; their sums go
+// through memory and a second launch adds them up in a fixed order (4096 x 4096 symmetric, 528 tiles of 128 where 512 run at a time: 253 us whole).
 // The fragments of Q are the MFMA's first operand: a lane then holds four consecutive columns of one row of C.
 #pragma once
+
+#include <algorithm>
 
 #include "half_common.h"
 
 namespace ozimmu {
 namespace {
 
-template <int BM, int BN, int WM, int WN, int STAGES, bool PIPE, int SLICES, bool BF16, int RESULT>
+// How the tiles of all matrices (numbered through) are dealt to workgroups: the first `whole` to one each, the others to `parts` each, with
+// `part_slabs` slabs of the inner dimension.
+struct NtPlan {
+    int tiles_m, tiles_n, tiles;   // of a matrix
+    int whole, parts, part_slabs;
+};
+
+__device__ __forceinline__ void nt_tile(const NtArgs& a, const NtPlan& p, int tile, int& tm, int& tn, int& z) {
+    z = tile / p.tiles;
+    tile -= z * p.tiles;
+    if (a.symmetric) {   // tiles on and above the diagonal, row by row of tiles
+        for (tm = 0; tile >= p.tiles_m - tm; ++tm) tile -= p.tiles_m - tm;
+        tn = tm + tile;
+    } else {
+        tile_of_logical(tile, p.tiles_m, p.tiles_n, tm, tn);
+    }
+}
+
+// What becomes of the sums of four neighbouring elements C[row][col .. col + 3].
+template <int RESULT>
+__device__ __forceinline__ void nt_finish(const NtArgs& a, int z, bool mirror, int r, int c, const v4f& acc) {
+    if constexpr (RESULT == kOutSlices) {
+        const int m_pad = (a.m + 31) & ~31, n_pad = (a.n + 31) & ~31;
+        if (c >= n_pad || r >= m_pad) return;
+        unsigned short* C = a.C + z * a.batch_c;
+        const int64_t at = (int64_t)r * a.ldc + (c >> 5) * 64 + (c & 31);
+        float v[4];
+        unsigned short h[4], l[4];
+        unsigned short ih[4] = {}, il[4] = {};
+        if (a.in && r < a.m) {
+            const unsigned short* in = a.in + z * a.batch_c;
+            *reinterpret_cast<v2u*>(ih) = *reinterpret_cast<const v2u*>(in + at);
+            *reinterpret_cast<v2u*>(il) = *reinterpret_cast<const v2u*>(in + at + 32);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = a.factor * acc[e];
+            if (a.in) v[e] = fmaf(a.beta, f16_to_f32(ih[e]) + f16_to_f32(il[e]), v[e]);
+            if (r == c + e) v[e] += a.diagonal;
+            if (c + e >= a.n || r >= a.m) v[e] = 0.f;   // the padding of a row holds zeros
+            two_slices(v[e], h[e], l[e]);
+        }
+        if (r < a.m) {
+            *reinterpret_cast<v2u*>(C + at) = *reinterpret_cast<v2u*>(h);
+            *reinterpret_cast<v2u*>(C + at + 32) = *reinterpret_cast<v2u*>(l);
+        }
+        if (mirror) {
+            unsigned short* CT = a.CT + z * a.batch_ct;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (c + e >= a.n) continue;
+                const int64_t t = (int64_t)(c + e) * a.ldct + (r >> 5) * 64 + (r & 31);
+                CT[t] = h[e];
+                CT[t + 32] = l[e];
+            }
+        }
+    } else {
+        typedef Elem<RESULT == kOutF32 ? OZIMMU_F32 : RESULT == kOutBf16 ? OZIMMU_BF16 : OZIMMU_F16> E;
+        typedef typename E::raw raw;
+        typedef raw raw4 __attribute__((ext_vector_type(4)));
+        if (r >= a.m || c >= a.n) return;
+        raw* out = reinterpret_cast<raw*>(a.out) + z * a.batch_o;
+        const bool wide = (a.ldo & 3) == 0 && (a.batch_o & 3) == 0 && (reinterpret_cast<uintptr_t>(a.out) & (4 * sizeof(raw) - 1)) == 0;
+        const int ep = RESULT == kOutF32 && a.exp_p ? a.exp_p[r] : 0;
+        raw4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float x = a.factor * acc[e];
+            if (RESULT == kOutF32 && a.exp_p) x = ldexpf(x, ep + a.exp_q[min(c + e, a.n - 1) / a.q_run]);
+            v[e] = E::store(x);
+        }
+        raw* at = out + (int64_t)r * a.ldo + c;
+        if (wide && c + 4 <= a.n)
+            *reinterpret_cast<raw4*>(at) = v;
+        else
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c + e < a.n) at[e] = v[e];
+    }
+}
+
+// When a wavefront reads its fragments of a slab from LDS: in the slab, all of them in the one before, or those that its first MFMAs need in the one before.
+enum NtWalk { kReadOnTime, kReadAhead, kFirstReadsAhead };
+
+template <int BM, int BN, int WM, int WN, int STAGES, int WALK, int SLICES, bool BF16, int RESULT>
 __launch_bounds__(WM * WN * 64)
-__global__ void nt_product_kernel(NtArgs a, int tiles_m, int tiles_n) {
+__global__ void nt_product_kernel(NtArgs a, NtPlan plan) {
     constexpr int W = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
     constexpr int LP = BM / 8 / W, LQ = BN / 8 / W;   // direct loads per wavefront and slab
     constexpr unsigned kStage = (BM + BN) * 128;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int tm, tn;
-    if (a.symmetric) {   // tiles on and above the diagonal, row by row of tiles
-        int first, count;
-        xcd_tile_range(blockIdx.x & 7, tiles_m * (tiles_m + 1) / 2, first, count);
-        int left = first + (blockIdx.x >> 3);
-        for (tm = 0; left >= tiles_m - tm; ++tm) left -= tiles_m - tm;
-        tn = tm + left;
+    int tile, slab0 = 0, slabs = a.slabs;
+    const bool shared = (int)blockIdx.x >= plan.whole;
+    if (shared) {
+        const int b = blockIdx.x - plan.whole, part = b % plan.parts;
+        tile = plan.whole + b / plan.parts;
+        slab0 = part * plan.part_slabs;
+        slabs = min(plan.part_slabs, a.slabs - slab0);
     } else {
-        tile_of_block(blockIdx.x, tiles_m, tiles_n, tm, tn);
+        int first, count;
+        xcd_tile_range(blockIdx.x & 7, plan.whole, first, count);
+        tile = first + (blockIdx.x >> 3);
     }
-    const int64_t z = blockIdx.y;
+    int tm, tn, z;
+    nt_tile(a, plan, tile, tm, tn, z);
     const int row0 = tm * BM, col0 = tn * BN;
-    const unsigned char* P = reinterpret_cast<const unsigned char*>(a.P + z * a.batch_p + (int64_t)row0 * a.ldp);
-    const unsigned char* Q = reinterpret_cast<const unsigned char*>(a.Q + z * a.batch_q + (int64_t)col0 * a.ldq);
+    const unsigned char* P = reinterpret_cast<const unsigned char*>(a.P + z * a.batch_p + (int64_t)row0 * a.ldp) + (int64_t)slab0 * 128;
+    const unsigned char* Q = reinterpret_cast<const unsigned char*>(a.Q + z * a.batch_q + (int64_t)col0 * a.ldq) + (int64_t)slab0 * 128;
     const unsigned piece = ((lane & 7) ^ (lane >> 3)) * 16;
     unsigned voff_p[LP], voff_q[LQ];
 #pragma unroll
@@ -80,12 +171,12 @@ __global__ void nt_product_kernel(NtArgs a, int tiles_m, int tiles_n) {
             for (int j = 0; j < NI; ++j) acc[i][j] = mfma_half<BF16>(q0[j], a0, acc[i][j]);
         }
     };
-    constexpr int AHEAD = PIPE ? STAGES : STAGES - 1;   // slabs requested before the first is multiplied
+    constexpr int AHEAD = WALK == kReadAhead ? STAGES : STAGES - 1;   // slabs requested before the first is multiplied
     for (int i = 0; i < AHEAD; ++i)
-        if (i < a.slabs)
+        if (i < slabs)
 #pragma unroll
             for (int l = 0; l < LP + LQ; ++l) load(l, i, i);
-    if constexpr (PIPE) {
+    if constexpr (WALK == kReadAhead) {
         // The fragments of the next slab are read from LDS while this one's are multiplied; a slab's stage is requested anew as soon as its fragments are in registers.
         struct Frags {
             v4u p0[MI], p1[MI], q0[NI], q1[NI];
@@ -104,7 +195,7 @@ __global__ void nt_product_kernel(NtArgs a, int tiles_m, int tiles_n) {
                 to.p1[i] = *reinterpret_cast<const v4u*>(at_p + i * 2048 + frag1);
             }
         };
-        if (AHEAD <= a.slabs)
+        if (AHEAD <= slabs)
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((AHEAD - 1) * (LP + LQ)) : "memory");
         else
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -112,14 +203,14 @@ __global__ void nt_product_kernel(NtArgs a, int tiles_m, int tiles_n) {
         int stage = 0;
         auto step = [&](int slab, Frags& now, Frags& next) {
             // the next slab has landed and this one's fragments are in registers; behind the barrier, everyone's
-            if (slab + STAGES <= a.slabs)
+            if (slab + STAGES <= slabs)
                 asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * (LP + LQ)) : "memory");
             else
                 asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
             const int free = stage;
             stage = stage + 1 == STAGES ? 0 : stage + 1;
-            if (slab + 1 < a.slabs) read(next, stage);
-            const bool more = slab + STAGES < a.slabs;
+            if (slab + 1 < slabs) read(next, stage);
+            const bool more = slab + STAGES < slabs;
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
                 if (more)
@@ -129,17 +220,68 @@ __global__ void nt_product_kernel(NtArgs a, int tiles_m, int tiles_n) {
             }
         };
         int slab = 0;
-        for (; slab + 1 < a.slabs; slab += 2) {
+        for (; slab + 1 < slabs; slab += 2) {
             step(slab, f[0], f[1]);
             step(slab + 1, f[1], f[0]);
         }
-        if (slab < a.slabs) step(slab, f[0], f[1]);
+        if (slab < slabs) step(slab, f[0], f[1]);
+    } else if constexpr (WALK == kFirstReadsAhead) {
+        // Two stages, two barriers a slab: behind the first nobody reads the other stage any more, and its loads go out between the first rows of MFMAs; behind the
+        // second, near the end, they have landed, and the next slab's first fragments are read under the last MFMAs.
+        static_assert(STAGES == 2 && MI >= 4);
+        v4u q0[2][NI], q1[2][NI], p0[2], p1[2];
+        auto first_reads = [&](int stage, int to) {
+            const unsigned char* at_p = lds + stage * kStage + wm * (BM / WM) * 128;
+            const unsigned char* at_q = lds + stage * kStage + BM * 128 + wn * (BN / WN) * 128;
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                q0[to][j] = *reinterpret_cast<const v4u*>(at_q + j * 2048 + frag0);
+                q1[to][j] = *reinterpret_cast<const v4u*>(at_q + j * 2048 + frag1);
+            }
+            p0[0] = *reinterpret_cast<const v4u*>(at_p + frag0);
+            p1[0] = *reinterpret_cast<const v4u*>(at_p + frag1);
+        };
+        constexpr int kLoadRows = MI / 2;
+        auto step = [&](int slab, auto odd) {
+            constexpr int now = decltype(odd)::value;
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            const bool more = slab + 1 < slabs;
+            const unsigned char* at_p = lds + now * kStage + wm * (BM / WM) * 128;
+            static_for<0, MI>([&](auto row) {
+                constexpr int i = decltype(row)::value;
+                const v4u a0 = p0[i & 1], a1 = p1[i & 1];
+                if constexpr (i + 1 < MI) {
+                    p0[(i + 1) & 1] = *reinterpret_cast<const v4u*>(at_p + (i + 1) * 2048 + frag0);
+                    p1[(i + 1) & 1] = *reinterpret_cast<const v4u*>(at_p + (i + 1) * 2048 + frag1);
+                }
+                if constexpr (i < kLoadRows) {
+                    if (more)
+#pragma unroll
+                        for (int l = (LP + LQ) * i / kLoadRows; l < (LP + LQ) * (i + 1) / kLoadRows; ++l) load(l, slab + 1, now ^ 1);
+                }
+                if constexpr (i + 1 == MI) {
+                    if (more) {
+                        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+                        first_reads(now ^ 1, now ^ 1);
+                    }
+                }
+                row_of_products(i, a0, a1, q0[now], q1[now]);
+            });
+        };
+        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+        first_reads(0, 0);
+        int slab = 0;
+        for (; slab + 1 < slabs; slab += 2) {
+            step(slab, std::integral_constant<int, 0>{});
+            step(slab + 1, std::integral_constant<int, 1>{});
+        }
+        if (slab < slabs) step(slab, std::integral_constant<int, 0>{});
     } else {
         int stage = 0;
-        for (int slab = 0; slab < a.slabs; ++slab) {
+        for (int slab = 0; slab < slabs; ++slab) {
             // this wavefront's loads of the slab have landed (later ones may be on their way) and its reads of the stage that is loaded next are done;
             // behind the barrier, everyone's
-            if (slab + AHEAD <= a.slabs)
+            if (slab + AHEAD <= slabs)
                 asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((AHEAD - 1) * (LP + LQ)) : "memory");
             else
                 asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -147,7 +289,7 @@ __global__ void nt_product_kernel(NtArgs a, int tiles_m, int tiles_n) {
             const unsigned char* at_p = lds + stage * kStage + wm * (BM / WM) * 128;
             const unsigned char* at_q = lds + stage * kStage + BM * 128 + wn * (BN / WN) * 128;
             stage = stage + 1 == STAGES ? 0 : stage + 1;
-            if (slab + AHEAD < a.slabs)
+            if (slab + AHEAD < slabs)
 #pragma unroll
                 for (int l = 0; l < LP + LQ; ++l) load(l, slab + AHEAD, to);
             v4u q0[NI], q1[NI];
@@ -166,111 +308,120 @@ __global__ void nt_product_kernel(NtArgs a, int tiles_m, int tiles_n) {
     }
 
     // ---- results: lane holds C[row][col .. col + 3]
-    const int r0 = row0 + wm * (BM / WM) + (lane & 15), c0 = col0 + wn * (BN / WN) + (lane >> 4) * 4;
-    if constexpr (RESULT == kOutSlices) {
-        unsigned short* C = a.C + z * a.batch_c;
-        const unsigned short* in = a.in ? a.in + z * a.batch_c : nullptr;
-        unsigned short* CT = a.CT ? a.CT + z * a.batch_ct : nullptr;
-        const int m_pad = (a.m + 31) & ~31, n_pad = (a.n + 31) & ~31;
-        const bool mirror = CT && !(a.symmetric && tm == tn);
+    if (shared) {
+        v4f* to = reinterpret_cast<v4f*>(a.partial) + (int64_t)(blockIdx.x - plan.whole) * (MI * NI * W * 64) + threadIdx.x;
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
-            for (int j = 0; j < NI; ++j) {
-                const int r = r0 + 16 * i, c = c0 + 16 * j;
-                if (c >= n_pad || r >= m_pad) continue;
-                const int64_t at = (int64_t)r * a.ldc + (c >> 5) * 64 + (c & 31);
-                float v[4];
-                unsigned short h[4], l[4];
-                unsigned short ih[4] = {}, il[4] = {};
-                if (in && r < a.m) {
-                    *reinterpret_cast<v2u*>(ih) = *reinterpret_cast<const v2u*>(in + at);
-                    *reinterpret_cast<v2u*>(il) = *reinterpret_cast<const v2u*>(in + at + 32);
-                }
+            for (int j = 0; j < NI; ++j) to[(i * NI + j) * (W * 64)] = acc[i][j];
+        return;
+    }
+    const int r0 = row0 + wm * (BM / WM) + (lane & 15), c0 = col0 + wn * (BN / WN) + (lane >> 4) * 4;
+    const bool mirror = a.CT && !(a.symmetric && tm == tn);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    v[e] = a.factor * acc[i][j][e];
-                    if (in) v[e] = fmaf(a.beta, f16_to_f32(ih[e]) + f16_to_f32(il[e]), v[e]);
-                    if (r == c + e) v[e] += a.diagonal;
-                    if (c + e >= a.n || r >= a.m) v[e] = 0.f;   // the padding of a row holds zeros
-                    two_slices(v[e], h[e], l[e]);
-                }
-                if (r < a.m) {
-                    *reinterpret_cast<v2u*>(C + at) = *reinterpret_cast<v2u*>(h);
-                    *reinterpret_cast<v2u*>(C + at + 32) = *reinterpret_cast<v2u*>(l);
-                }
-                if (mirror) {
+    for (int i = 0; i < MI; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (c + e >= a.n) continue;
-                        const int64_t t = (int64_t)(c + e) * a.ldct + (r >> 5) * 64 + (r & 31);
-                        CT[t] = h[e];
-                        CT[t + 32] = l[e];
-                    }
-                }
-            }
-    } else {
-        typedef Elem<RESULT == kOutF32 ? OZIMMU_F32 : RESULT == kOutBf16 ? OZIMMU_BF16 : OZIMMU_F16> E;
-        typedef typename E::raw raw;
-        typedef raw raw4 __attribute__((ext_vector_type(4)));
-        raw* out = reinterpret_cast<raw*>(a.out) + z * a.batch_o;
-        const bool wide = (a.ldo & 3) == 0 && (a.batch_o & 3) == 0 && (reinterpret_cast<uintptr_t>(a.out) & (4 * sizeof(raw) - 1)) == 0;
+        for (int j = 0; j < NI; ++j) nt_finish<RESULT>(a, z, mirror, r0 + 16 * i, c0 + 16 * j, acc[i][j]);
+}
+
+// The shared tiles: parts added up in order, a workgroup per 16 x 16 result of its wavefronts.
+template <int BM, int BN, int WM, int WN, int RESULT>
+__launch_bounds__(WM * WN * 64)
+__global__ void nt_join_kernel(NtArgs a, NtPlan plan) {
+    constexpr int W = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
+    const int i = blockIdx.y / NI, j = blockIdx.y % NI;
+    int tm, tn, z;
+    nt_tile(a, plan, plan.whole + blockIdx.x, tm, tn, z);
+    const v4f* from = reinterpret_cast<const v4f*>(a.partial) + ((int64_t)blockIdx.x * plan.parts * (MI * NI) + blockIdx.y) * (W * 64) + threadIdx.x;
+    v4f sum = from[0];
+    for (int p = 1; p < plan.parts; ++p) {
+        const v4f x = from[(int64_t)p * (MI * NI * W * 64)];
 #pragma unroll
-        for (int i = 0; i < MI; ++i) {
-            const int r = r0 + 16 * i;
-            if (r >= a.m) continue;
-            const int ep = a.exp_p ? a.exp_p[r] : 0;
-#pragma unroll
-            for (int j = 0; j < NI; ++j) {
-                const int c = c0 + 16 * j;
-                if (c >= a.n) continue;
-                raw4 v;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float x = a.factor * acc[i][j][e];
-                    if (RESULT == kOutF32 && a.exp_p) x = ldexpf(x, ep + a.exp_q[min(c + e, a.n - 1) / a.q_run]);
-                    v[e] = E::store(x);
-                }
-                raw* at = out + (int64_t)r * a.ldo + c;
-                if (wide && c + 4 <= a.n)
-                    *reinterpret_cast<raw4*>(at) = v;
-                else
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (c + e < a.n) at[e] = v[e];
+        for (int e = 0; e < 4; ++e) sum[e] += x[e];
+    }
+    nt_finish<RESULT>(a, z, a.CT && !(a.symmetric && tm == tn), tm * BM + wm * (BM / WM) + (lane & 15) + 16 * i, tn * BN + wn * (BN / WN) + (lane >> 4) * 4 + 16 * j, sum);
+}
+
+// A tile shape as the choice sees it: how many workgroups run at a time, and what a slab takes then and with one workgroup to a compute unit (us).
+struct NtShape {
+    int tile, slots;
+    double full, alone;
+};
+struct NtChoice {
+    NtPlan plan;
+    double us;
+};
+inline NtChoice nt_choose(const NtArgs& a, const NtShape& s, size_t part_bytes) {
+    NtChoice c{};
+    c.plan.tiles_m = (a.m + s.tile - 1) / s.tile;
+    c.plan.tiles_n = (a.n + s.tile - 1) / s.tile;
+    const int64_t one = a.symmetric ? (int64_t)c.plan.tiles_m * (c.plan.tiles_m + 1) / 2 : (int64_t)c.plan.tiles_m * c.plan.tiles_n, all = one * a.batch;
+    c.us = 1e30;
+    if (all > INT32_MAX / 64) return c;
+    c.plan.tiles = (int)one;
+    auto round_us = [&](int64_t workgroups, int64_t slabs) {   // of a round of at most s.slots
+        const double load = std::max(0.0, (double)(workgroups - kComputeUnits) / std::max(1, s.slots - kComputeUnits));
+        return (double)slabs * (s.alone + (s.full - s.alone) * std::min(1.0, load));
+    };
+    const int64_t rounds = all / s.slots, rest = all % s.slots;
+    c.plan.whole = (int)all;
+    c.plan.parts = 1;
+    c.plan.part_slabs = a.slabs;
+    c.us = rounds * round_us(s.slots, a.slabs) + (rest ? round_us(rest, a.slabs) : 0.0);
+    // the tiles of a last round that is not full may be shared, at the price of their sums' way through memory and of a launch
+    if (rest && a.partial) {
+        for (int64_t parts = 2; parts <= 32 && rest * parts <= s.slots && parts * 4 <= a.slabs; ++parts) {
+            const int64_t slabs = (a.slabs + parts - 1) / parts, used = (a.slabs + slabs - 1) / slabs;
+            const double bytes = (double)(rest * used) * s.tile * s.tile * sizeof(float);
+            if (used != parts || bytes > (double)part_bytes) continue;
+            const double us = rounds * round_us(s.slots, a.slabs) + round_us(rest * parts, slabs) + 5.0 + 2.0 * bytes / 4.0e6;
+            if (us < c.us) {
+                c.us = us;
+                c.plan.whole = (int)(all - rest);
+                c.plan.parts = (int)parts;
+                c.plan.part_slabs = (int)slabs;
             }
         }
     }
+    return c;
 }
 
-template <int BM, int BN, int WM, int WN, int STAGES, bool PIPE, int SLICES, bool BF16, int RESULT>
-hipError_t launch_nt_tile(const NtArgs& a, hipStream_t st) {
-    constexpr auto kernel = nt_product_kernel<BM, BN, WM, WN, STAGES, PIPE, SLICES, BF16, RESULT>;
+template <int BM, int BN, int WM, int WN, int STAGES, int WALK, int SLICES, bool BF16, int RESULT>
+hipError_t launch_nt_tile(const NtArgs& a, const NtPlan& plan, hipStream_t st) {
+    constexpr auto kernel = nt_product_kernel<BM, BN, WM, WN, STAGES, WALK, SLICES, BF16, RESULT>;
     constexpr int bytes = STAGES * (BM + BN) * 128;
     if (hipError_t e = allow_dynamic_lds<kernel>(bytes); e != hipSuccess) return e;
-    if (a.m <= 0 || a.n <= 0 || a.slabs <= 0 || (a.symmetric && (BM != BN || a.m != a.n))) return hipErrorInvalidValue;
-    const int tiles_m = (a.m + BM - 1) / BM, tiles_n = (a.n + BN - 1) / BN;
-    const int64_t tiles = a.symmetric ? (int64_t)tiles_m * (tiles_m + 1) / 2 : (int64_t)tiles_m * tiles_n;
-    if (tiles > INT32_MAX || a.batch > 65535) return hipErrorInvalidConfiguration;
-    kernel<<<dim3((unsigned)tiles, a.batch), dim3(WM * WN * 64), bytes, st>>>(a, tiles_m, tiles_n);
+    const int rest = plan.tiles * a.batch - plan.whole;
+    kernel<<<dim3((unsigned)(plan.whole + rest * plan.parts)), dim3(WM * WN * 64), bytes, st>>>(a, plan);
+    if (rest) nt_join_kernel<BM, BN, WM, WN, RESULT><<<dim3((unsigned)rest, BM / WM / 16 * (BN / WN / 16)), dim3(WM * WN * 64), 0, st>>>(a, plan);
     return hipGetLastError();
 }
 
+// A larger tile moves fewer bytes through LDS per product, a smaller one keeps more compute units busy: by an estimate from what a slab takes each shape (two slices, one
+// slice; measured with products of one to four rounds). 64 x 64 tiles come in two forms: with about one workgroup to a compute unit nothing else hides a wavefront's
+// LDS reads, and they run a slab ahead; with more, the registers and LDS of that cost the co-residents that do (2048 x 2048 x 8192, 528 tiles, 131 us against 162).
 template <int SLICES, bool BF16, int RESULT>
 hipError_t launch_nt(const NtArgs& a, hipStream_t st) {
-    auto tiles = [&](int64_t b) {
-        const int64_t x = (a.m + b - 1) / b, y = (a.n + b - 1) / b;
-        return (a.symmetric ? x * (x + 1) / 2 : x * y) * a.batch;
-    };
-    // A larger tile moves fewer bytes through LDS per product, a smaller one keeps more compute units busy. Measured, two slices, us: 4096^3 on tiles of 256, 128, 64
-    // 309, 336, 412; 2048 x 4096 x 4096 (128, 512, 2048 tiles) 247, 167, 206; 1024 x 1024 x 4096 (16, 64, 256) 250, 86, 42. One slice: 1024 x 4096 x 4096
-    // (64, 256, 1024 tiles) 98, 44, 47.
-    if (tiles(256) >= 200) return launch_nt_tile<256, 256, 2, 4, 2, false, SLICES, BF16, RESULT>(a, st);
-    if (tiles(128) >= 256) return launch_nt_tile<128, 128, 2, 2, 2, false, SLICES, BF16, RESULT>(a, st);
-    // With about one workgroup to a compute unit nothing else hides a wavefront's LDS reads: they run a slab ahead (1024 x 1024 x 4096 56 -> 42, 6 x 520 x 520 x 1024 21.1 -> 17.6).
-    // With more, their registers and LDS cost the co-residents that do (2048 x 2048 x 8192, 528 tiles, 131 against 162).
-    if (tiles(64) <= 320) return launch_nt_tile<64, 64, 2, 2, 3, true, SLICES, BF16, RESULT>(a, st);
-    return launch_nt_tile<64, 64, 2, 2, 2, false, SLICES, BF16, RESULT>(a, st);
+    if (a.m <= 0 || a.n <= 0 || a.slabs <= 0 || a.batch <= 0 || (a.symmetric && a.m != a.n)) return hipErrorInvalidValue;
+    constexpr bool two = SLICES == 2;
+    const NtShape shapes[] = {{256, 256, two ? 2.41 : 1.73, two ? 2.41 : 1.73}, {128, 512, two ? 1.31 : 0.95, two ? 0.92 : 0.62}, {64, 1280, two ? 1.0 : 0.9, two ? 0.40 : 0.37}, {64, 768, two ? 1.0 : 0.9, two ? 0.31 : 0.27}};
+    NtChoice best{};
+    int which = -1;
+    for (int i = 0; i < 4; ++i) {
+        const NtChoice c = nt_choose(a, shapes[i], a.partial_bytes);
+        if (which < 0 || c.us < best.us) {
+            best = c;
+            which = i;
+        }
+    }
+    if (best.us >= 1e30) return hipErrorInvalidConfiguration;
+    switch (which) {
+        case 0: return launch_nt_tile<256, 256, 2, 4, 2, kFirstReadsAhead, SLICES, BF16, RESULT>(a, best.plan, st);
+        case 1: return launch_nt_tile<128, 128, 2, 2, 2, kReadOnTime, SLICES, BF16, RESULT>(a, best.plan, st);
+        case 2: return launch_nt_tile<64, 64, 2, 2, 2, kReadOnTime, SLICES, BF16, RESULT>(a, best.plan, st);
+        default: return launch_nt_tile<64, 64, 2, 2, 3, kReadAhead, SLICES, BF16, RESULT>(a, best.plan, st);
+    }
 }
 
 }  // namespace

@@ -34,7 +34,7 @@ ozimmu_status_t check_q4(int64_t k, int group, const void* codes, int64_t ldq, c
 // The operands of a product with many tokens in the workspace: V (t rows of `inner` values) and the weights (`outer` rows). 32-bit types take two slices.
 struct Operands {
     int64_t inner, outer, ld;
-    size_t off_v, off_w, off_ev, off_ew, total;
+    size_t off_v, off_w, off_ev, off_ew, off_partial, total;
 };
 Operands operands(int64_t t, int64_t n, int64_t k, int group, int type, bool gradient) {
     Operands o{};
@@ -50,6 +50,8 @@ Operands operands(int64_t t, int64_t n, int64_t k, int group, int type, bool gra
     if (type == OZIMMU_F32) off = align_up(off + sizeof(int) * (size_t)(gradient ? groups_of(k, group) : n));
     o.off_ev = off;
     if (type == OZIMMU_F32) off = align_up(off + sizeof(int) * (size_t)t);
+    o.off_partial = off;
+    off = align_up(off + kPartialBytes);
     o.total = off;
     return o;
 }
@@ -107,6 +109,8 @@ ozimmu_status_t q4_product(bool gradient, int64_t t, int64_t n, int64_t k, int g
     a.n = (int)outer;
     a.batch = 1;
     a.factor = 1.0f;
+    a.partial = reinterpret_cast<float*>(base + o.off_partial);
+    a.partial_bytes = kPartialBytes;
     a.out = R;
     a.ldo = ldr;
     if (type == OZIMMU_F32) {
@@ -125,7 +129,7 @@ struct OrthLayout {
     int64_t r, l;              // shorter and longer side
     int64_t ld_x, ld_t;        // values per row: along the longer side, along the shorter one
     int64_t size_x, size_t_, size_a;
-    size_t off_x, off_t[2], off_a, off_q, off_norm, total;
+    size_t off_x, off_t[2], off_a, off_q, off_norm, off_partial, total;
 };
 OrthLayout orth_layout(int64_t batch, int64_t m, int64_t n) {
     OrthLayout o{};
@@ -144,6 +148,7 @@ OrthLayout orth_layout(int64_t batch, int64_t m, int64_t n) {
     o.off_a = take(2 * (size_t)batch * o.size_a);
     o.off_q = take(2 * (size_t)batch * o.size_a);
     o.off_norm = take(sizeof(double) * (size_t)batch * norm_parts(m, n));
+    o.off_partial = take(kPartialBytes);
     o.total = off;
     return o;
 }
@@ -281,6 +286,8 @@ ozimmu_status_t ozimmu_orthogonalize(int64_t batch, int64_t m, int64_t n, ozimmu
         unsigned short *now = at(o.off_t[i & 1]), *next = at(o.off_t[(i & 1) ^ 1]);
         NtArgs g{};
         g.batch = (int)batch;
+        g.partial = reinterpret_cast<float*>(base + o.off_partial);
+        g.partial_bytes = kPartialBytes;
         g.m = g.n = (int)o.r;
         g.symmetric = true;
         g.factor = down;
@@ -309,6 +316,8 @@ ozimmu_status_t ozimmu_orthogonalize(int64_t batch, int64_t m, int64_t n, ozimmu
         const bool last = i + 1 == steps;
         NtArgs u{};
         u.batch = (int)batch;
+        u.partial = g.partial;
+        u.partial_bytes = kPartialBytes;
         u.slabs = (int)(o.ld_t / kSlabValues);
         u.ldp = u.ldq = o.ld_t;
         if (last && tall) {   // X^T (a + b A + c A^2), as it lies in the result

@@ -24,6 +24,8 @@ struct NtArgs {
     int m, n, batch;               // rows of P, rows of Q, matrices
     bool symmetric;                // P and Q give a symmetric C: only tiles on and above the diagonal are formed, the rest mirrored
     float factor;                  // of the sums
+    float* partial;                // room for the sums of tiles whose inner dimension several workgroups share, and how much there is of it (bytes);
+    size_t partial_bytes;          // without it they do not
     // typed result, row-major
     void* out;
     int64_t ldo, batch_o;
@@ -39,6 +41,8 @@ struct NtArgs {
 };
 enum NtResult { kOutF32 = 0, kOutBf16 = 1, kOutF16 = 2, kOutSlices = 3 };
 // `slices` 1 (bf16 where `bf16`, else fp16) or 2 (fp16)
+// Room that launch_nt_product can make use of for any product (at most so many workgroups share tiles).
+constexpr size_t kPartialBytes = 512 * 128 * 128 * sizeof(float);
 hipError_t launch_nt_product(const NtArgs& a, int slices, bool bf16, NtResult result, hipStream_t st);
 
 // 16-byte accesses are possible to every row of an array of rows
