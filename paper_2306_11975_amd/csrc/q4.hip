@@ -55,41 +55,108 @@ __device__ __forceinline__ int nearest_code(float w, float s, float inv) {
     return (int)fminf(fmaxf(q, -8.f), 7.f);
 }
 
-// A thread cuts eight weights; the lanes of a group (GROUP / 8 of them, side by side) share its maximum. tx threads along a row.
-// Memory-bound: the weights are read once, 16 or 32 bytes a lane.
+// The largest magnitude of eight values, as bits: those of |w| order like the values, NaN last, so that one that is there stays visible in the scale. As integers the
+// largest is the largest positive value, as unsigned ones the largest negative one.
+__device__ __forceinline__ unsigned top_bits(const float (&w)[8]) {
+    int up = 0;
+    unsigned down = 0x80000000u;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        up = max(up, max(__float_as_int(w[e]), __float_as_int(w[e + 1])));
+        down = max(down, max(__float_as_uint(w[e]), __float_as_uint(w[e + 1])));
+    }
+    return max((unsigned)up, down & 0x7fffffffu);
+}
+// The maximum over N neighbouring lanes (4, 8 or 16), in all of them.
+template <int N>
+__device__ __forceinline__ unsigned max_of_lanes(unsigned x) {
+    x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, true));    // lanes 1, 0, 3, 2
+    x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, true));    // lanes 2, 3, 0, 1
+    if constexpr (N >= 8) x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xF, 0xF, true));   // eight mirrored
+    if constexpr (N >= 16) x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xF, 0xF, true));  // sixteen mirrored
+    return x;
+}
+
+// The codes of eight weights as a word. w * (1/s), with a reciprocal that is off by a unit, is off the quotient by less than 2e-6; adding 1.5 * 2^23 rounds it to an integer, ties to
+// even, whose low bits then stand in the low bits of the sum. That is the nearest integer to the quotient unless the product lies within 1e-5 of a border and is
+// not the quotient itself (a tie, which weights of 8 bits often are): then the remainders decide, as they do where a scale that underflowed lets codes leave their range.
+// (Both tests are asked of the wavefront: lane by lane, everyone would pay for them. 8192 x 8192 bf16: with the remainders always 62 us.)
+__device__ __forceinline__ unsigned code_word(const float (&w)[8], float s, float top) {
+    const float inv = __builtin_amdgcn_rcpf(s);
+    float t[8], far = 0.f;
+    unsigned sum[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        t[e] = w[e] * inv;
+        const float x = t[e] + 12582912.f;
+        sum[e] = __float_as_uint(x);
+        far = fmaxf(far, fabsf(t[e] - (x - 12582912.f)));
+    }
+    bool unsure = !(s >= 0x1p-60f && s <= 3.4028234664e38f) || top * inv > 7.4f;
+    if (__builtin_amdgcn_ballot_w64(far > 0.49999f)) {   // the quotients near a border once more, corrected by their remainders: then ties are exact
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float q = fmaf(fmaf(-t[e], s, w[e]), inv, t[e]), x = q + 12582912.f;
+            sum[e] = __float_as_uint(x);
+            unsure |= fabsf(q - (x - 12582912.f)) > 0.49999f && fmaf(-q, s, w[e]) != 0.f;
+        }
+    }
+    // bytes of the even positions and of the odd ones
+    const unsigned even = __builtin_amdgcn_perm(__builtin_amdgcn_perm(sum[6], sum[4], 0x0c0c0400u), __builtin_amdgcn_perm(sum[2], sum[0], 0x0c0c0400u), 0x05040100u);
+    const unsigned odd = __builtin_amdgcn_perm(__builtin_amdgcn_perm(sum[7], sum[5], 0x0c0c0400u), __builtin_amdgcn_perm(sum[3], sum[1], 0x0c0c0400u), 0x05040100u);
+    unsigned word = ((even & 0x0f0f0f0fu) | (odd & 0x0f0f0f0fu) << 4) ^ 0x88888888u;
+    if (__builtin_amdgcn_ballot_w64(unsure)) {
+        const bool usable = s > 0.f && s <= 3.4028234664e38f;
+        const float up = s < 0x1p-60f ? 0x1p64f : 1.f;   // (small scales: the reciprocal stays finite and the remainders normal)
+        unsigned exact = 0;
+#pragma unroll 1
+        for (int e = 7; e >= 0; --e) {
+            float x = w[0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) x = e == i ? w[i] : x;
+            exact = exact << 4 | (unsigned)((usable ? nearest_code(x * up, s * up, 1.0f / (s * up)) : 0) + 8);
+        }
+        if (unsure) word = exact;
+    }
+    return word;
+}
+
+// max |w| / 7, correctly rounded: the product with the rounded reciprocal, corrected by its remainder; very small ones, whose remainder would underflow, and infinities divided.
+__device__ __forceinline__ float seventh(float top) {
+    constexpr float r = 1.0f / 7.0f;
+    const float q = top * r;
+    const float exact = fmaf(fmaf(-7.0f, q, top), r, q);
+    const bool plain = top > 1e-30f && top <= 3.4028234664e38f;
+    if (__builtin_amdgcn_ballot_w64(!plain)) return plain ? exact : top / 7.0f;
+    return exact;
+}
+
+// A thread cuts eight weights of two rows; the lanes of a group (GROUP / 8 of them, side by side) share its maximum. tx threads along a row.
+// Memory-bound: the weights are read once, 16 or 32 bytes a lane, two rows on their way at a time.
 template <int TYPE, int STYPE, int GROUP>
 __launch_bounds__(kThreads)
 __global__ void q4_split_kernel(int64_t n, int64_t k, const void* W, int64_t ldw, bool vec, uint8_t* codes, int64_t ldq, void* scales,
-                                int64_t lds, int tx) {
+                                int64_t lds, int tx, unsigned across) {
     typedef Elem<TYPE> E;
     typedef Elem<STYPE> S;
-    const int64_t row = (int64_t)blockIdx.x * (kThreads / tx) + threadIdx.x / tx;
-    const int64_t at = ((int64_t)blockIdx.y * tx + threadIdx.x % tx) * 8;
-    float w[8];
-    if (row < n)
-        load8<TYPE>(reinterpret_cast<const typename E::raw*>(W) + row * ldw, at, k, vec, w);
-    else
+    constexpr int ROWS = 2;
+    const int ty = kThreads / tx;
+    const int64_t row0 = (int64_t)(blockIdx.x / across) * (ROWS * ty) + threadIdx.x / tx;
+    const int64_t at = ((int64_t)(blockIdx.x % across) * tx + threadIdx.x % tx) * 8;
+    float w[ROWS][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = 0.f;
-    unsigned top = 0;   // the bits of |w| order like the values, NaN last: one that is there stays visible in the scale
+    for (int i = 0; i < ROWS; ++i) load8<TYPE>(reinterpret_cast<const typename E::raw*>(W) + min(row0 + i * ty, n - 1) * ldw, at, k, vec, w[i]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(w[e]) & 0x7fffffffu);
-#pragma unroll
-    for (int d = 1; d < GROUP / 8; d *= 2) top = max(top, (unsigned)__shfl_xor((int)top, d));
-    const typename S::raw stored = S::store(__uint_as_float(top) / 7.0f);
-    const float s = S::load(stored);
-    const bool usable = s > 0.f && s <= 3.4028234664e38f;
-    const float up = s < 0x1p-60f ? 0x1p64f : 1.f;   // (small scales: the reciprocal stays finite and the remainders normal)
-    const float inv = 1.0f / (s * up);
-    unsigned word = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int c = usable ? nearest_code(w[e] * up, s * up, inv) : 0;
-        word |= (unsigned)(c + 8) << (4 * e);
+    for (int i = 0; i < ROWS; ++i) {
+        const int64_t row = row0 + i * ty;
+        const float top = __uint_as_float(max_of_lanes<GROUP / 8>(top_bits(w[i])));
+        const typename S::raw stored = S::store(seventh(top));
+        const unsigned word = code_word(w[i], S::load(stored), top);
+        if (row < n) {
+            if (at < pad_to(k, 32)) *reinterpret_cast<unsigned*>(codes + row * ldq + at / 2) = word;
+            if (at < k && at % GROUP == 0) reinterpret_cast<typename S::raw*>(scales)[row * lds + at / GROUP] = stored;
+        }
     }
-    if (row >= n) return;
-    if (at < pad_to(k, 32)) *reinterpret_cast<unsigned*>(codes + row * ldq + at / 2) = word;
-    if (at < k && at % GROUP == 0) reinterpret_cast<typename S::raw*>(scales)[row * lds + at / GROUP] = stored;
 }
 
 __device__ __forceinline__ float code_value(unsigned word, int e) { return (float)((int)(word >> (4 * e) & 15u) - 8); }
@@ -98,10 +165,10 @@ __device__ __forceinline__ float code_value(unsigned word, int e) { return (floa
 template <int TYPE>
 __launch_bounds__(kThreads)
 __global__ void q4_expand_kernel(int64_t n, int64_t k, int group_log2, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds,
-                                 void* W, int64_t ldw, int64_t len, bool vec, int tx) {
+                                 void* W, int64_t ldw, int64_t len, bool vec, int tx, unsigned across) {
     typedef Elem<TYPE> E;
-    const int64_t row = (int64_t)blockIdx.x * (kThreads / tx) + threadIdx.x / tx;
-    const int64_t at = ((int64_t)blockIdx.y * tx + threadIdx.x % tx) * 8;
+    const int64_t row = (int64_t)(blockIdx.x / across) * (kThreads / tx) + threadIdx.x / tx;
+    const int64_t at = ((int64_t)(blockIdx.x % across) * tx + threadIdx.x % tx) * 8;
     if (row >= n || at >= len) return;
     float x[8] = {};
     if (at < k) {
@@ -175,9 +242,9 @@ __global__ void row_slices_kernel(int64_t k, const float* X, int64_t ldx, bool v
 
 // A padded copy of rows of 16-bit values.
 __launch_bounds__(kThreads)
-__global__ void pad_rows_kernel(int64_t rows, int64_t k, const unsigned short* X, int64_t ldx, bool vec, unsigned short* out, int64_t ldo, int tx) {
-    const int64_t row = (int64_t)blockIdx.x * (kThreads / tx) + threadIdx.x / tx;
-    const int64_t at = ((int64_t)blockIdx.y * tx + threadIdx.x % tx) * 8;
+__global__ void pad_rows_kernel(int64_t rows, int64_t k, const unsigned short* X, int64_t ldx, bool vec, unsigned short* out, int64_t ldo, int tx, unsigned across) {
+    const int64_t row = (int64_t)(blockIdx.x / across) * (kThreads / tx) + threadIdx.x / tx;
+    const int64_t at = ((int64_t)(blockIdx.x % across) * tx + threadIdx.x % tx) * 8;
     if (row >= rows || at >= ldo) return;
     const unsigned short* x = X + row * ldx;
     unsigned short r[8] = {};
@@ -213,9 +280,9 @@ __global__ void scale_exponents_kernel(int64_t len, const float* scales, int64_t
 // Rows of W in two slices under the row's exponent.
 __launch_bounds__(kThreads)
 __global__ void q4_slices_kernel(int64_t n, int64_t k, int group_log2, const uint8_t* codes, int64_t ldq, const float* scales, int64_t lds,
-                                 unsigned short* out, int64_t ldo, const int* exps, int tx) {
-    const int64_t row = (int64_t)blockIdx.x * (kThreads / tx) + threadIdx.x / tx;
-    const int64_t at = ((int64_t)blockIdx.y * tx + threadIdx.x % tx) * 8;
+                                 unsigned short* out, int64_t ldo, const int* exps, int tx, unsigned across) {
+    const int64_t row = (int64_t)(blockIdx.x / across) * (kThreads / tx) + threadIdx.x / tx;
+    const int64_t at = ((int64_t)(blockIdx.x % across) * tx + threadIdx.x % tx) * 8;
     if (row >= n || at >= pad_to(k, 32)) return;
     float x[8] = {};
     if (at < k) {
@@ -272,9 +339,10 @@ int threads_along(int64_t chunks) {
     while (tx < kThreads && tx < chunks) tx *= 2;
     return tx;
 }
-dim3 grid_for(int64_t rows, int64_t chunks, int tx) {
-    return dim3((unsigned)((rows + kThreads / tx - 1) / (kThreads / tx)), (unsigned)((chunks + tx - 1) / tx));
-}
+// Workgroups over `rows` rows of `chunks` pieces, tx threads along a row: numbered along the rows, so that those that run together read memory in order (by columns first:
+// 8192 x 8192 bf16 cut in 62 us).
+unsigned across_of(int64_t chunks, int tx) { return (unsigned)((chunks + tx - 1) / tx); }
+dim3 grid_for(int64_t rows, int64_t chunks, int tx) { return dim3((unsigned)((rows + kThreads / tx - 1) / (kThreads / tx)) * across_of(chunks, tx)); }
 int log2_of(int group) { return group == 32 ? 5 : group == 64 ? 6 : 7; }
 
 template <int TYPE, int STYPE>
@@ -282,13 +350,13 @@ hipError_t split_typed(int64_t n, int64_t k, int group, const void* W, int64_t l
     const int64_t chunks = pad_to(k, group) / 8;
     const int tx = threads_along(chunks);
     const bool vec = rows_aligned16(W, ldw, sizeof(typename Elem<TYPE>::raw));
-    const dim3 grid = grid_for(n, chunks, tx);
+    const dim3 grid = grid_for((n + 1) / 2, chunks, tx);
     if (group == 32)
-        q4_split_kernel<TYPE, STYPE, 32><<<grid, kThreads, 0, st>>>(n, k, W, ldw, vec, codes, ldq, scales, lds, tx);
+        q4_split_kernel<TYPE, STYPE, 32><<<grid, kThreads, 0, st>>>(n, k, W, ldw, vec, codes, ldq, scales, lds, tx, across_of(chunks, tx));
     else if (group == 64)
-        q4_split_kernel<TYPE, STYPE, 64><<<grid, kThreads, 0, st>>>(n, k, W, ldw, vec, codes, ldq, scales, lds, tx);
+        q4_split_kernel<TYPE, STYPE, 64><<<grid, kThreads, 0, st>>>(n, k, W, ldw, vec, codes, ldq, scales, lds, tx, across_of(chunks, tx));
     else
-        q4_split_kernel<TYPE, STYPE, 128><<<grid, kThreads, 0, st>>>(n, k, W, ldw, vec, codes, ldq, scales, lds, tx);
+        q4_split_kernel<TYPE, STYPE, 128><<<grid, kThreads, 0, st>>>(n, k, W, ldw, vec, codes, ldq, scales, lds, tx, across_of(chunks, tx));
     return hipGetLastError();
 }
 template <int TYPE>
@@ -304,7 +372,7 @@ hipError_t expand_typed(int64_t n, int64_t k, int group, const uint8_t* codes, i
     const int64_t chunks = pad_to(len, 8) / 8;
     const int tx = threads_along(chunks);
     const bool vec = rows_aligned16(W, ldw, sizeof(typename Elem<TYPE>::raw));
-    q4_expand_kernel<TYPE><<<grid_for(n, chunks, tx), kThreads, 0, st>>>(n, k, log2_of(group), codes, ldq, scales, lds, W, ldw, len, vec, tx);
+    q4_expand_kernel<TYPE><<<grid_for(n, chunks, tx), kThreads, 0, st>>>(n, k, log2_of(group), codes, ldq, scales, lds, W, ldw, len, vec, tx, across_of(chunks, tx));
     return hipGetLastError();
 }
 
@@ -358,7 +426,7 @@ hipError_t launch_q4_operand(int64_t n, int64_t k, int group, const uint8_t* cod
     if (type == OZIMMU_F32) {
         const int64_t chunks = pad_to(k, 32) / 8;
         const int tx = threads_along(chunks);
-        q4_slices_kernel<<<grid_for(n, chunks, tx), kThreads, 0, st>>>(n, k, lg, codes, ldq, reinterpret_cast<const float*>(scales), lds, out, ldo, exps, tx);
+        q4_slices_kernel<<<grid_for(n, chunks, tx), kThreads, 0, st>>>(n, k, lg, codes, ldq, reinterpret_cast<const float*>(scales), lds, out, ldo, exps, tx, across_of(chunks, tx));
         return hipGetLastError();
     }
     const int64_t len = pad_to(k, 64);
@@ -373,7 +441,7 @@ hipError_t launch_row_operand(int64_t rows, int64_t k, const void* X, int type, 
     } else {
         const int64_t chunks = pad_to(k, 64) / 8;
         const int tx = threads_along(chunks);
-        pad_rows_kernel<<<grid_for(rows, chunks, tx), kThreads, 0, st>>>(rows, k, reinterpret_cast<const unsigned short*>(X), ldx, rows_aligned16(X, ldx, 2), out, ldo, tx);
+        pad_rows_kernel<<<grid_for(rows, chunks, tx), kThreads, 0, st>>>(rows, k, reinterpret_cast<const unsigned short*>(X), ldx, rows_aligned16(X, ldx, 2), out, ldo, tx, across_of(chunks, tx));
     }
     return hipGetLastError();
 }
