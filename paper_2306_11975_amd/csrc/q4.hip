@@ -165,19 +165,17 @@ __device__ __forceinline__ float code_value(unsigned word, int e) { return (floa
 template <int TYPE>
 __launch_bounds__(kThreads)
 __global__ void q4_expand_kernel(int64_t n, int64_t k, int group_log2, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds,
-                                 void* W, int64_t ldw, int64_t len, bool vec, int tx, unsigned across) {
+                                 void* W, int64_t ldw, bool vec, int tx, unsigned across) {
     typedef Elem<TYPE> E;
     const int64_t row = (int64_t)(blockIdx.x / across) * (kThreads / tx) + threadIdx.x / tx;
     const int64_t at = ((int64_t)(blockIdx.x % across) * tx + threadIdx.x % tx) * 8;
-    if (row >= n || at >= len) return;
-    float x[8] = {};
-    if (at < k) {
-        const unsigned word = *reinterpret_cast<const unsigned*>(codes + row * ldq + at / 2);
-        const float s = E::load(reinterpret_cast<const typename E::raw*>(scales)[row * lds + (at >> group_log2)]);
+    if (row >= n || at >= k) return;
+    const unsigned word = *reinterpret_cast<const unsigned*>(codes + row * ldq + at / 2);
+    const float s = E::load(reinterpret_cast<const typename E::raw*>(scales)[row * lds + (at >> group_log2)]);
+    float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = at + e < k ? s * code_value(word, e) : 0.f;
-    }
-    store8<TYPE>(reinterpret_cast<typename E::raw*>(W) + row * ldw, at, len, vec, x);
+    for (int e = 0; e < 8; ++e) x[e] = s * code_value(word, e);
+    store8<TYPE>(reinterpret_cast<typename E::raw*>(W) + row * ldw, at, k, vec, x);
 }
 
 __device__ __forceinline__ int exponent_of(float top) {   // of the power of two just above; 0 for zero
@@ -214,47 +212,203 @@ __device__ __forceinline__ void store_slices8(unsigned short* row, int64_t at, c
     *reinterpret_cast<v4u*>(to + 32) = *reinterpret_cast<const v4u*>(l);
 }
 
+// What the operands of a product are made of: weights (n x k) and rows of tokens (t x inner).
+struct OperandArgs {
+    int64_t n, k, ldq, lds;
+    int group_log2;
+    const uint8_t* codes;
+    const void* scales;
+    unsigned short* w_out;
+    int* w_exps;
+    int w_tx;
+    unsigned w_across, w_blocks;
+    int64_t t, inner, ldv, ld;   // ld: of both operands
+    const void* V;
+    bool vec;
+    unsigned short* v_out;
+    int* v_exps;
+    int v_tx;
+    unsigned v_across;
+};
+
 // Rows of 32-bit values in two slices of fp16 under a power-of-two exponent per row; a workgroup per row, which it reads twice
 // (the second time from the caches). NaN does not raise the maximum and stays in its place; so does an infinity.
-__launch_bounds__(kThreads)
-__global__ void row_slices_kernel(int64_t k, const float* X, int64_t ldx, bool vec, unsigned short* out, int64_t ldo, int* exps) {
-    __shared__ float shared[kThreads / 64];
-    const int64_t row = blockIdx.x;
-    const float* x = X + row * ldx;
+__device__ __forceinline__ void row_slices(const OperandArgs& a, unsigned block, float* shared) {
+    const int64_t row = block, k = a.inner;
+    const float* x = reinterpret_cast<const float*>(a.V) + row * a.ldv;
     float top = 0.f;
     for (int64_t at = threadIdx.x * 8; at < k; at += kThreads * 8) {
         float v[8];
-        load8<OZIMMU_F32>(x, at, k, vec, v);
+        load8<OZIMMU_F32>(x, at, k, a.vec, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
     }
     const int e0 = exponent_of(block_max(top, shared)) - kRowShift;
-    if (threadIdx.x == 0) exps[row] = e0;
+    if (threadIdx.x == 0) a.v_exps[row] = e0;
     const int64_t len = pad_to(k, 32);
     for (int64_t at = threadIdx.x * 8; at < len; at += kThreads * 8) {
         float v[8];
-        load8<OZIMMU_F32>(x, at, k, vec, v);
+        load8<OZIMMU_F32>(x, at, k, a.vec, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = ldexpf(v[e], -e0);
-        store_slices8(out + row * ldo, at, v);
+        store_slices8(a.v_out + row * a.ld, at, v);
     }
 }
 
 // A padded copy of rows of 16-bit values.
-__launch_bounds__(kThreads)
-__global__ void pad_rows_kernel(int64_t rows, int64_t k, const unsigned short* X, int64_t ldx, bool vec, unsigned short* out, int64_t ldo, int tx, unsigned across) {
-    const int64_t row = (int64_t)(blockIdx.x / across) * (kThreads / tx) + threadIdx.x / tx;
-    const int64_t at = ((int64_t)(blockIdx.x % across) * tx + threadIdx.x % tx) * 8;
-    if (row >= rows || at >= ldo) return;
-    const unsigned short* x = X + row * ldx;
+__device__ __forceinline__ void pad_rows(const OperandArgs& a, unsigned block) {
+    const int64_t row = (int64_t)(block / a.v_across) * (kThreads / a.v_tx) + threadIdx.x / a.v_tx;
+    const int64_t at = ((int64_t)(block % a.v_across) * a.v_tx + threadIdx.x % a.v_tx) * 8;
+    if (row >= a.t || at >= a.ld) return;
+    const unsigned short* x = reinterpret_cast<const unsigned short*>(a.V) + row * a.ldv;
     unsigned short r[8] = {};
-    if (vec && at + 8 <= k)
+    if (a.vec && at + 8 <= a.inner)
         *reinterpret_cast<v4u*>(r) = *reinterpret_cast<const v4u*>(x + at);
     else
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            if (at + e < k) r[e] = x[at + e];
-    *reinterpret_cast<v4u*>(out + row * ldo + at) = *reinterpret_cast<const v4u*>(r);
+            if (at + e < a.inner) r[e] = x[at + e];
+    *reinterpret_cast<v4u*>(a.v_out + row * a.ld + at) = *reinterpret_cast<const v4u*>(r);
+}
+
+// The exponent of the largest of `len` scales, `step` apart: |s c| <= 8 s.
+__device__ __forceinline__ int scale_exponent(const float* s, int64_t len, int64_t step, float* shared) {
+    float top = 0.f;
+    for (int64_t i = threadIdx.x; i < len; i += kThreads) top = fmaxf(top, fabsf(s[i * step]));
+    return exponent_of(block_max(top, shared)) + 3 - kRowShift;
+}
+
+// Rows of W in two slices under an exponent per row, which every workgroup finds for itself: alone on a row its threads share the row's scales, else (rows of less than
+// 2048 positions, at most 64 scales) sixteen lanes do.
+__device__ __forceinline__ void q4_slices(const OperandArgs& a, unsigned block, float* shared) {
+    const int64_t row = (int64_t)(block / a.w_across) * (kThreads / a.w_tx) + threadIdx.x / a.w_tx;
+    const int64_t at = ((int64_t)(block % a.w_across) * a.w_tx + threadIdx.x % a.w_tx) * 8;
+    const int64_t groups = (a.k + (1 << a.group_log2) - 1) >> a.group_log2;
+    const float* scales = reinterpret_cast<const float*>(a.scales) + min(row, a.n - 1) * a.lds;
+    int e0;
+    if (a.w_tx == kThreads) {
+        e0 = scale_exponent(scales, groups, 1, shared);
+    } else {
+        unsigned top = 0;
+        for (int64_t i = threadIdx.x % 16; i < groups; i += 16) top = max(top, __float_as_uint(scales[i]) & 0x7fffffffu);
+        e0 = exponent_of(__uint_as_float(max_of_lanes<16>(top))) + 3 - kRowShift;
+    }
+    if (row >= a.n || at >= pad_to(a.k, 32)) return;
+    if (at == 0) a.w_exps[row] = e0;
+    float x[8] = {};
+    if (at < a.k) {
+        const unsigned word = *reinterpret_cast<const unsigned*>(a.codes + row * a.ldq + at / 2);
+        const float s = ldexpf(scales[at >> a.group_log2], -e0);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = at + e < a.k ? s * code_value(word, e) : 0.f;
+    }
+    store_slices8(a.w_out + row * a.ld, at, x);
+}
+
+// Rows of W rounded to 16 bits.
+template <int TYPE>
+__device__ __forceinline__ void q4_rows(const OperandArgs& a, unsigned block) {
+    typedef Elem<TYPE> E;
+    const int64_t row = (int64_t)(block / a.w_across) * (kThreads / a.w_tx) + threadIdx.x / a.w_tx;
+    const int64_t at = ((int64_t)(block % a.w_across) * a.w_tx + threadIdx.x % a.w_tx) * 8;
+    if (row >= a.n || at >= a.ld) return;
+    float x[8] = {};
+    if (at < a.k) {
+        const unsigned word = *reinterpret_cast<const unsigned*>(a.codes + row * a.ldq + at / 2);
+        const float s = E::load(reinterpret_cast<const typename E::raw*>(a.scales)[row * a.lds + (at >> a.group_log2)]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = at + e < a.k ? s * code_value(word, e) : 0.f;
+    }
+    store8<TYPE>(a.w_out + row * a.ld, at, at + 8, true, x);
+}
+
+// Columns of W as rows along n, rounded to 16 bits or (OZIMMU_F32) in two slices under the exponent of the column's group: a tile of 64 rows and a line of codes
+// from each (two slices: half a line) through LDS, where eight values of position l lie at place (their eighth) ^ (l / 8 % 8).
+template <int TYPE>
+constexpr int kTileWidth = TYPE == OZIMMU_F32 ? 128 : 256;
+template <int TYPE>
+__device__ __forceinline__ void q4_columns(const OperandArgs& a, unsigned block, unsigned short* tile) {
+    typedef Elem<TYPE> E;
+    constexpr int kWidth = kTileWidth<TYPE>, kWords = kWidth / 8;
+    const int64_t n0 = (int64_t)(block / a.w_across) * 64, k0 = (int64_t)(block % a.w_across) * kWidth;
+    const int word_at = threadIdx.x % kWords;
+    const int64_t at = k0 + 8 * word_at;
+    constexpr int kRowsAtOnce = kThreads / kWords;
+    constexpr int kTimes = 64 / kRowsAtOnce;
+    unsigned words[kTimes];
+    float scale[kTimes];
+    const int lift = TYPE == OZIMMU_F32 && at < a.k ? -a.w_exps[at >> a.group_log2] : 0;
+#pragma unroll
+    for (int u = 0; u < kTimes; ++u) {   // all requests before the first use; rows and positions that are not there repeat the last
+        const int64_t row = min(n0 + threadIdx.x / kWords + u * kRowsAtOnce, a.n - 1), l = min(at, (a.k - 1) & ~(int64_t)7);
+        words[u] = *reinterpret_cast<const unsigned*>(a.codes + row * a.ldq + l / 2);
+        scale[u] = E::load(reinterpret_cast<const typename E::raw*>(a.scales)[row * a.lds + (l >> a.group_log2)]);
+    }
+#pragma unroll
+    for (int u = 0; u < kTimes; ++u) {
+        const int i = threadIdx.x / kWords + u * kRowsAtOnce;
+        const bool here = n0 + i < a.n && at < a.k;
+        const unsigned word = here ? words[u] : 0x88888888u;
+        const float s = !here ? 0.f : TYPE == OZIMMU_F32 ? ldexpf(scale[u], lift) : scale[u];
+        const int place = ((i >> 3) ^ (word_at & 7)) * 8 + (i & 7);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            unsigned short* to = tile + (8 * word_at + e) * 64 + place;
+            if constexpr (TYPE == OZIMMU_F32)
+                two_slices(s * code_value(word, e), to[0], to[kWidth * 64]);
+            else
+                to[0] = E::store(s * code_value(word, e));
+        }
+    }
+    __syncthreads();
+    const int eighth = threadIdx.x % 8;
+    const int64_t row = n0 + 8 * eighth;
+    if (row >= pad_to(a.n, TYPE == OZIMMU_F32 ? 32 : 64)) return;
+#pragma unroll
+    for (int l = threadIdx.x / 8; l < kWidth; l += kThreads / 8) {
+        if (k0 + l >= a.k) break;
+        const unsigned short* from = tile + l * 64 + (eighth ^ (l >> 3 & 7)) * 8;
+        unsigned short* to = a.w_out + (k0 + l) * a.ld;
+        if constexpr (TYPE == OZIMMU_F32) {
+            to += (row >> 5) * 64 + (row & 31);
+            *reinterpret_cast<v4u*>(to) = *reinterpret_cast<const v4u*>(from);
+            *reinterpret_cast<v4u*>(to + 32) = *reinterpret_cast<const v4u*>(from + kWidth * 64);
+        } else {
+            *reinterpret_cast<v4u*>(to + row) = *reinterpret_cast<const v4u*>(from);
+        }
+    }
+}
+
+// Both operands in one launch: the first workgroups make the weights', the others the tokens'.
+template <int TYPE, bool COLUMNS>
+__launch_bounds__(kThreads)
+__global__ void operands_kernel(OperandArgs a) {
+    __shared__ __attribute__((aligned(16))) unsigned short tile[COLUMNS ? 64 * 256 : 8];
+    __shared__ float shared[kThreads / 64];
+    if (blockIdx.x < a.w_blocks) {
+        if constexpr (COLUMNS)
+            q4_columns<TYPE>(a, blockIdx.x, tile);
+        else if constexpr (TYPE == OZIMMU_F32)
+            q4_slices(a, blockIdx.x, shared);
+        else
+            q4_rows<TYPE>(a, blockIdx.x);
+    } else if constexpr (TYPE == OZIMMU_F32) {
+        row_slices(a, blockIdx.x - a.w_blocks, shared);
+    } else {
+        pad_rows(a, blockIdx.x - a.w_blocks);
+    }
+}
+
+// The exponents of groups of columns, a workgroup per group (they stand before the columns' slices), beside the slices of the tokens.
+__launch_bounds__(kThreads)
+__global__ void group_exponents_kernel(OperandArgs a, unsigned groups) {
+    __shared__ float shared[kThreads / 64];
+    if (blockIdx.x < groups) {
+        const int e0 = scale_exponent(reinterpret_cast<const float*>(a.scales) + blockIdx.x, a.n, a.lds, shared);
+        if (threadIdx.x == 0) a.w_exps[blockIdx.x] = e0;
+    } else {
+        row_slices(a, blockIdx.x - groups, shared);
+    }
 }
 
 // Zeros (a product over an empty inner dimension).
@@ -263,74 +417,6 @@ __launch_bounds__(kThreads)
 __global__ void zero_rows_kernel(int64_t rows, int64_t cols, T* R, int64_t ld) {
     const int64_t row = blockIdx.x, at = (int64_t)blockIdx.y * kThreads + threadIdx.x;
     if (at < cols) R[row * ld + at] = T(0);
-}
-
-// exps[row] for the largest scale of a row of W (a workgroup per row), and exps[group] for the largest one of a group of
-// columns (a workgroup per group): |s c| <= 8 s.
-__launch_bounds__(kThreads)
-__global__ void scale_exponents_kernel(int64_t len, const float* scales, int64_t step, int64_t next, int* exps) {
-    __shared__ float shared[kThreads / 64];
-    const float* s = scales + (int64_t)blockIdx.x * next;
-    float top = 0.f;
-    for (int64_t i = threadIdx.x; i < len; i += kThreads) top = fmaxf(top, fabsf(s[i * step]));
-    const int e0 = exponent_of(block_max(top, shared)) + 3 - kRowShift;
-    if (threadIdx.x == 0) exps[blockIdx.x] = e0;
-}
-
-// Rows of W in two slices under the row's exponent.
-__launch_bounds__(kThreads)
-__global__ void q4_slices_kernel(int64_t n, int64_t k, int group_log2, const uint8_t* codes, int64_t ldq, const float* scales, int64_t lds,
-                                 unsigned short* out, int64_t ldo, const int* exps, int tx, unsigned across) {
-    const int64_t row = (int64_t)(blockIdx.x / across) * (kThreads / tx) + threadIdx.x / tx;
-    const int64_t at = ((int64_t)(blockIdx.x % across) * tx + threadIdx.x % tx) * 8;
-    if (row >= n || at >= pad_to(k, 32)) return;
-    float x[8] = {};
-    if (at < k) {
-        const unsigned word = *reinterpret_cast<const unsigned*>(codes + row * ldq + at / 2);
-        const float s = ldexpf(scales[row * lds + (at >> group_log2)], -exps[row]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = at + e < k ? s * code_value(word, e) : 0.f;
-    }
-    store_slices8(out + row * ldo, at, x);
-}
-
-// Columns of W as rows along n: a 64 x 64 tile through LDS. TYPE OZIMMU_F32: two slices under the exponent of the column's group.
-template <int TYPE>
-__launch_bounds__(kThreads)
-__global__ void q4_transposed_kernel(int64_t n, int64_t k, int group_log2, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds,
-                                     unsigned short* out, int64_t ldo, const int* exps) {
-    typedef Elem<TYPE> E;
-    __shared__ float tile[64][65];
-    const int64_t n0 = (int64_t)blockIdx.y * 64, k0 = (int64_t)blockIdx.x * 64;
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int i = half * 32 + threadIdx.x / 8, j = threadIdx.x % 8 * 8;
-        const int64_t row = n0 + i, at = k0 + j;
-        float x[8] = {};
-        if (row < n && at < k) {
-            const unsigned word = *reinterpret_cast<const unsigned*>(codes + row * ldq + at / 2);
-            float s = E::load(reinterpret_cast<const typename E::raw*>(scales)[row * lds + (at >> group_log2)]);
-            if (TYPE == OZIMMU_F32) s = ldexpf(s, -exps[at >> group_log2]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = s * code_value(word, e);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) tile[j + e][i] = x[e];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int j = half * 32 + threadIdx.x / 8, i = threadIdx.x % 8 * 8;
-        const int64_t col = k0 + j, at = n0 + i;
-        if (col >= k || at >= pad_to(n, TYPE == OZIMMU_F32 ? 32 : 64)) continue;
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = tile[j][i + e];
-        if constexpr (TYPE == OZIMMU_F32)
-            store_slices8(out + col * ldo, at, x);
-        else
-            store8<TYPE>(out + col * ldo, at, at + 8, true, x);
-    }
 }
 
 // Threads along a row of `chunks` pieces: a power of two of at least 16 (the lanes of the largest group), so that short rows share a workgroup.
@@ -368,11 +454,11 @@ hipError_t split_from(int64_t n, int64_t k, int group, const void* W, int64_t ld
 
 template <int TYPE>
 hipError_t expand_typed(int64_t n, int64_t k, int group, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds, void* W, int64_t ldw,
-                        int64_t len, hipStream_t st) {
-    const int64_t chunks = pad_to(len, 8) / 8;
+                        hipStream_t st) {
+    const int64_t chunks = pad_to(k, 8) / 8;
     const int tx = threads_along(chunks);
     const bool vec = rows_aligned16(W, ldw, sizeof(typename Elem<TYPE>::raw));
-    q4_expand_kernel<TYPE><<<grid_for(n, chunks, tx), kThreads, 0, st>>>(n, k, log2_of(group), codes, ldq, scales, lds, W, ldw, len, vec, tx, across_of(chunks, tx));
+    q4_expand_kernel<TYPE><<<grid_for(n, chunks, tx), kThreads, 0, st>>>(n, k, log2_of(group), codes, ldq, scales, lds, W, ldw, vec, tx, across_of(chunks, tx));
     return hipGetLastError();
 }
 
@@ -396,53 +482,62 @@ hipError_t launch_q4_split(int64_t n, int64_t k, int group, const void* W, int t
 
 hipError_t launch_q4_expand(int64_t n, int64_t k, int group, const uint8_t* codes, int64_t ldq, const void* scales, int type,
                             int64_t lds, void* W, int64_t ldw, hipStream_t st) {
-    if (type == OZIMMU_F32) return expand_typed<OZIMMU_F32>(n, k, group, codes, ldq, scales, lds, W, ldw, k, st);
-    if (type == OZIMMU_BF16) return expand_typed<OZIMMU_BF16>(n, k, group, codes, ldq, scales, lds, W, ldw, k, st);
-    return expand_typed<OZIMMU_F16>(n, k, group, codes, ldq, scales, lds, W, ldw, k, st);
+    if (type == OZIMMU_F32) return expand_typed<OZIMMU_F32>(n, k, group, codes, ldq, scales, lds, W, ldw, st);
+    if (type == OZIMMU_BF16) return expand_typed<OZIMMU_BF16>(n, k, group, codes, ldq, scales, lds, W, ldw, st);
+    return expand_typed<OZIMMU_F16>(n, k, group, codes, ldq, scales, lds, W, ldw, st);
 }
 
-hipError_t launch_q4_operand(int64_t n, int64_t k, int group, const uint8_t* codes, int64_t ldq, const void* scales, int type,
-                             int64_t lds, bool transposed, unsigned short* out, int64_t ldo, int* exps, hipStream_t st) {
-    const int lg = log2_of(group);
-    if (type == OZIMMU_F32) {
-        const float* s = reinterpret_cast<const float*>(scales);
-        const int64_t groups = (k + group - 1) / group;
-        if (transposed)
-            scale_exponents_kernel<<<dim3((unsigned)groups), kThreads, 0, st>>>(n, s, lds, 1, exps);
-        else
-            scale_exponents_kernel<<<dim3((unsigned)n), kThreads, 0, st>>>(groups, s, 1, lds, exps);
-        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    }
-    if (transposed) {
-        const dim3 grid((unsigned)((k + 63) / 64), (unsigned)((n + 63) / 64));
-        if (type == OZIMMU_F32)
-            q4_transposed_kernel<OZIMMU_F32><<<grid, kThreads, 0, st>>>(n, k, lg, codes, ldq, scales, lds, out, ldo, exps);
-        else if (type == OZIMMU_BF16)
-            q4_transposed_kernel<OZIMMU_BF16><<<grid, kThreads, 0, st>>>(n, k, lg, codes, ldq, scales, lds, out, ldo, exps);
-        else
-            q4_transposed_kernel<OZIMMU_F16><<<grid, kThreads, 0, st>>>(n, k, lg, codes, ldq, scales, lds, out, ldo, exps);
-        return hipGetLastError();
-    }
-    if (type == OZIMMU_F32) {
-        const int64_t chunks = pad_to(k, 32) / 8;
-        const int tx = threads_along(chunks);
-        q4_slices_kernel<<<grid_for(n, chunks, tx), kThreads, 0, st>>>(n, k, lg, codes, ldq, reinterpret_cast<const float*>(scales), lds, out, ldo, exps, tx, across_of(chunks, tx));
-        return hipGetLastError();
-    }
-    const int64_t len = pad_to(k, 64);
-    return type == OZIMMU_BF16 ? expand_typed<OZIMMU_BF16>(n, k, group, codes, ldq, scales, lds, out, ldo, len, st)
-                               : expand_typed<OZIMMU_F16>(n, k, group, codes, ldq, scales, lds, out, ldo, len, st);
-}
-
-hipError_t launch_row_operand(int64_t rows, int64_t k, const void* X, int type, int64_t ldx, unsigned short* out, int64_t ldo,
-                              int* exps, hipStream_t st) {
-    if (type == OZIMMU_F32) {
-        row_slices_kernel<<<dim3((unsigned)rows), kThreads, 0, st>>>(k, reinterpret_cast<const float*>(X), ldx, rows_aligned16(X, ldx, 4), out, ldo, exps);
+hipError_t launch_operands(int64_t t, int64_t n, int64_t k, int group, int type, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds, bool columns,
+                           unsigned short* w_out, int* w_exps, const void* V, int64_t ldv, unsigned short* v_out, int* v_exps, int64_t ld, hipStream_t st) {
+    OperandArgs a{};
+    a.n = n;
+    a.k = k;
+    a.ldq = ldq;
+    a.lds = lds;
+    a.group_log2 = log2_of(group);
+    a.codes = codes;
+    a.scales = scales;
+    a.w_out = w_out;
+    a.w_exps = w_exps;
+    a.t = t;
+    a.inner = columns ? n : k;
+    a.ldv = ldv;
+    a.ld = ld;
+    a.V = V;
+    a.v_out = v_out;
+    a.v_exps = v_exps;
+    const bool f32 = type == OZIMMU_F32;
+    a.vec = rows_aligned16(V, ldv, f32 ? 4 : 2);
+    if (columns) {
+        a.w_across = (unsigned)((k + (f32 ? kTileWidth<OZIMMU_F32> : kTileWidth<OZIMMU_BF16>) - 1) / (f32 ? kTileWidth<OZIMMU_F32> : kTileWidth<OZIMMU_BF16>));
+        a.w_blocks = (unsigned)((n + 63) / 64) * a.w_across;
     } else {
-        const int64_t chunks = pad_to(k, 64) / 8;
-        const int tx = threads_along(chunks);
-        pad_rows_kernel<<<grid_for(rows, chunks, tx), kThreads, 0, st>>>(rows, k, reinterpret_cast<const unsigned short*>(X), ldx, rows_aligned16(X, ldx, 2), out, ldo, tx, across_of(chunks, tx));
+        const int64_t chunks = pad_to(k, f32 ? 32 : 64) / 8;
+        a.w_tx = threads_along(chunks);
+        a.w_across = across_of(chunks, a.w_tx);
+        a.w_blocks = grid_for(n, chunks, a.w_tx).x;
     }
+    unsigned v_blocks = 0;
+    if (v_out && f32) {
+        v_blocks = (unsigned)t;
+    } else if (v_out) {
+        a.v_tx = threads_along(ld / 8);
+        a.v_across = across_of(ld / 8, a.v_tx);
+        v_blocks = grid_for(t, ld / 8, a.v_tx).x;
+    }
+    if (columns && f32) {
+        const unsigned groups = (unsigned)((k + group - 1) / group);
+        group_exponents_kernel<<<dim3(groups + v_blocks), kThreads, 0, st>>>(a, groups);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        v_blocks = 0;
+    }
+    const dim3 grid(a.w_blocks + v_blocks);
+    if (f32)
+        columns ? operands_kernel<OZIMMU_F32, true><<<grid, kThreads, 0, st>>>(a) : operands_kernel<OZIMMU_F32, false><<<grid, kThreads, 0, st>>>(a);
+    else if (type == OZIMMU_BF16)
+        columns ? operands_kernel<OZIMMU_BF16, true><<<grid, kThreads, 0, st>>>(a) : operands_kernel<OZIMMU_BF16, false><<<grid, kThreads, 0, st>>>(a);
+    else
+        columns ? operands_kernel<OZIMMU_F16, true><<<grid, kThreads, 0, st>>>(a) : operands_kernel<OZIMMU_F16, false><<<grid, kThreads, 0, st>>>(a);
     return hipGetLastError();
 }
 

@@ -90,18 +90,13 @@ ozimmu_status_t q4_product(bool gradient, int64_t t, int64_t n, int64_t k, int g
     unsigned short* w = reinterpret_cast<unsigned short*>(base + o.off_w);
     int* ew = reinterpret_cast<int*>(base + o.off_ew);
     int* ev = reinterpret_cast<int*>(base + o.off_ev);
-    hipError_t e = launch_q4_operand(n, k, group, codes, ldq, scales, type, lds, gradient, w, o.ld, ew, st);
     NtArgs a{};
+    unsigned short* v = reinterpret_cast<unsigned short*>(base + o.off_v);
     // rows of 16-bit values that the kernel can read as they lie need no copy
-    if (type != OZIMMU_F32 && inner % kSlabValues == 0 && ldv < kMaxInPlaceLd && rows_aligned16(V, ldv, 2)) {
-        a.P = static_cast<const unsigned short*>(V);
-        a.ldp = ldv;
-    } else {
-        unsigned short* v = reinterpret_cast<unsigned short*>(base + o.off_v);
-        if (e == hipSuccess) e = launch_row_operand(t, inner, V, type, ldv, v, o.ld, ev, st);
-        a.P = v;
-        a.ldp = o.ld;
-    }
+    const bool in_place = type != OZIMMU_F32 && inner % kSlabValues == 0 && ldv < kMaxInPlaceLd && rows_aligned16(V, ldv, 2);
+    hipError_t e = launch_operands(t, n, k, group, type, codes, ldq, scales, lds, gradient, w, ew, V, ldv, in_place ? nullptr : v, ev, o.ld, st);
+    a.P = in_place ? static_cast<const unsigned short*>(V) : v;
+    a.ldp = in_place ? ldv : o.ld;
     a.Q = w;
     a.ldq = o.ld;
     a.slabs = (int)(o.ld / kSlabValues);

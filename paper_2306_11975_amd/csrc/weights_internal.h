@@ -58,13 +58,10 @@ hipError_t launch_q4_split(int64_t n, int64_t k, int group, const void* W, int t
 // The weights s c as a typed matrix.
 hipError_t launch_q4_expand(int64_t n, int64_t k, int group, const uint8_t* codes, int64_t ldq, const void* scales, int type,
                             int64_t lds, void* W, int64_t ldw, hipStream_t st);
-// The weights as an operand of the product kernel: rows of W (transposed: columns), one slice in `type`, or, for OZIMMU_F32, two slices of fp16 scaled by
-// 2^-exps per row (transposed: per group of columns).
-hipError_t launch_q4_operand(int64_t n, int64_t k, int group, const uint8_t* codes, int64_t ldq, const void* scales, int type,
-                             int64_t lds, bool transposed, unsigned short* out, int64_t ldo, int* exps, hipStream_t st);
-// Rows of a matrix as an operand: a padded copy (16-bit types), or two slices of fp16 under an exponent per row (OZIMMU_F32).
-hipError_t launch_row_operand(int64_t rows, int64_t k, const void* X, int type, int64_t ldx, unsigned short* out, int64_t ldo,
-                              int* exps, hipStream_t st);
+// The operands of a product of many tokens, rows of ld values: the weights (`columns`: their columns) and, where v_out is not null, the rows of V. 16-bit types: one
+// slice, padded to slabs. OZIMMU_F32: two slices of fp16 scaled by 2^-exponent: one exponent per row, for columns of W one per group.
+hipError_t launch_operands(int64_t t, int64_t n, int64_t k, int group, int type, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds, bool columns,
+                           unsigned short* w_out, int* w_exps, const void* V, int64_t ldv, unsigned short* v_out, int* v_exps, int64_t ld, hipStream_t st);
 // Zeros into a typed matrix.
 hipError_t launch_zero_rows(int64_t rows, int64_t cols, void* R, int type, int64_t ld, hipStream_t st);
 // q4_few.hip: Y = X W^T for few tokens, one pass over the codes
