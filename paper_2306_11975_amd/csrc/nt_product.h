@@ -38,15 +38,15 @@ __device__ __forceinline__ void nt_tile(const NtArgs& a, const NtPlan& p, int ti
     }
 }
 
-// What becomes of the sums of four neighbouring elements C[row][col .. col + 3].
+// What becomes of the sums of four neighbouring elements C[row][col .. col + 3]. Two slices: `both` receives them, the first in the low half; the transposed
+// matrix is the caller's.
 template <int RESULT>
-__device__ __forceinline__ void nt_finish(const NtArgs& a, int z, bool mirror, int r, int c, const v4f& acc) {
+__device__ __forceinline__ void nt_finish(const NtArgs& a, int z, int r, int c, const v4f& acc, unsigned (&both)[4]) {
     if constexpr (RESULT == kOutSlices) {
         const int m_pad = (a.m + 31) & ~31, n_pad = (a.n + 31) & ~31;
         if (c >= n_pad || r >= m_pad) return;
         unsigned short* C = a.C + z * a.batch_c;
         const int64_t at = (int64_t)r * a.ldc + (c >> 5) * 64 + (c & 31);
-        float v[4];
         unsigned short h[4], l[4];
         unsigned short ih[4] = {}, il[4] = {};
         if (a.in && r < a.m) {
@@ -56,25 +56,16 @@ __device__ __forceinline__ void nt_finish(const NtArgs& a, int z, bool mirror, i
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            v[e] = a.factor * acc[e];
-            if (a.in) v[e] = fmaf(a.beta, f16_to_f32(ih[e]) + f16_to_f32(il[e]), v[e]);
-            if (r == c + e) v[e] += a.diagonal;
-            if (c + e >= a.n || r >= a.m) v[e] = 0.f;   // the padding of a row holds zeros
-            two_slices(v[e], h[e], l[e]);
+            float v = a.factor * acc[e];
+            if (a.in) v = fmaf(a.beta, f16_to_f32(ih[e]) + f16_to_f32(il[e]), v);
+            if (r == c + e) v += a.diagonal;
+            if (c + e >= a.n || r >= a.m) v = 0.f;   // the padding of a row holds zeros
+            two_slices(v, h[e], l[e]);
+            both[e] = (unsigned)h[e] | (unsigned)l[e] << 16;
         }
         if (r < a.m) {
             *reinterpret_cast<v2u*>(C + at) = *reinterpret_cast<v2u*>(h);
             *reinterpret_cast<v2u*>(C + at + 32) = *reinterpret_cast<v2u*>(l);
-        }
-        if (mirror) {
-            unsigned short* CT = a.CT + z * a.batch_ct;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (c + e >= a.n) continue;
-                const int64_t t = (int64_t)(c + e) * a.ldct + (r >> 5) * 64 + (r & 31);
-                CT[t] = h[e];
-                CT[t + 32] = l[e];
-            }
         }
     } else {
         typedef Elem<RESULT == kOutF32 ? OZIMMU_F32 : RESULT == kOutBf16 ? OZIMMU_BF16 : OZIMMU_F16> E;
@@ -316,12 +307,48 @@ __global__ void nt_product_kernel(NtArgs a, NtPlan plan) {
             for (int j = 0; j < NI; ++j) to[(i * NI + j) * (W * 64)] = acc[i][j];
         return;
     }
-    const int r0 = row0 + wm * (BM / WM) + (lane & 15), c0 = col0 + wn * (BN / WN) + (lane >> 4) * 4;
-    const bool mirror = a.CT && !(a.symmetric && tm == tn);
+    const int r0 = wm * (BM / WM) + (lane & 15), c0 = wn * (BN / WN) + (lane >> 4) * 4;   // in the tile
+    // The transposed tile goes through LDS, which nobody reads any more: stored from the registers it would be two bytes at a time (4096 x 4096: 27 us of 323). kAtOnce columns of
+    // it fit; value (row, col) lies at row ^ 16 (col / 4 % 4) of its column, so that the four quarters of a wavefront meet different banks.
+    constexpr int kAtOnce = STAGES * (BM + BN) * 128 / (BM * 4) < BN ? BN / 2 : BN;
+    static_assert(kAtOnce * BM * 4 <= STAGES * (BM + BN) * 128 && kAtOnce % (BN / WN) == 0);
+    unsigned* const turned = reinterpret_cast<unsigned*>(lds);
+    const bool mirror = RESULT == kOutSlices && a.CT && !(a.symmetric && tm == tn);
+#pragma unroll 1
+    for (int part = 0; part < BN / kAtOnce; ++part) {
+        if (mirror) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (wn / (kAtOnce / (BN / WN)) == part) {
 #pragma unroll
-    for (int i = 0; i < MI; ++i)
+            for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int j = 0; j < NI; ++j) nt_finish<RESULT>(a, z, mirror, r0 + 16 * i, c0 + 16 * j, acc[i][j]);
+                for (int j = 0; j < NI; ++j) {
+                    unsigned both[4] = {};
+                    const int r = r0 + 16 * i, c = c0 + 16 * j;
+                    nt_finish<RESULT>(a, z, row0 + r, col0 + c, acc[i][j], both);
+                    if (mirror) {
+                        const int here = c - part * kAtOnce;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) turned[(here + e) * BM + (r ^ ((here >> 2 & 3) << 4))] = both[e];
+                    }
+                }
+        }
+        if (!mirror) continue;
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        unsigned short* CT = a.CT + z * a.batch_ct;
+        const int m_pad = (a.m + 31) & ~31;
+        for (int piece = threadIdx.x; piece < kAtOnce * BM / 8; piece += W * 64) {
+            const int here = piece / (BM / 8), r = piece % (BM / 8) * 8;
+            const int64_t col = col0 + part * kAtOnce + here, row = row0 + r;
+            if (col >= a.n || row >= m_pad) continue;
+            const unsigned* from = turned + here * BM + (r ^ ((here >> 2 & 3) << 4));
+            const v4u x = reinterpret_cast<const v4u*>(from)[0], y = reinterpret_cast<const v4u*>(from)[1];
+            unsigned short* to = CT + col * a.ldct + (row >> 5) * 64 + (row & 31);
+            *reinterpret_cast<v4u*>(to) = v4u{__builtin_amdgcn_perm(x[1], x[0], 0x05040100u), __builtin_amdgcn_perm(x[3], x[2], 0x05040100u),
+                                              __builtin_amdgcn_perm(y[1], y[0], 0x05040100u), __builtin_amdgcn_perm(y[3], y[2], 0x05040100u)};
+            *reinterpret_cast<v4u*>(to + 32) = v4u{__builtin_amdgcn_perm(x[1], x[0], 0x07060302u), __builtin_amdgcn_perm(x[3], x[2], 0x07060302u),
+                                                   __builtin_amdgcn_perm(y[1], y[0], 0x07060302u), __builtin_amdgcn_perm(y[3], y[2], 0x07060302u)};
+        }
+    }
 }
 
 // The shared tiles: parts added up in order, a workgroup per 16 x 16 result of its wavefronts.
@@ -340,7 +367,19 @@ __global__ void nt_join_kernel(NtArgs a, NtPlan plan) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[e] += x[e];
     }
-    nt_finish<RESULT>(a, z, a.CT && !(a.symmetric && tm == tn), tm * BM + wm * (BM / WM) + (lane & 15) + 16 * i, tn * BN + wn * (BN / WN) + (lane >> 4) * 4 + 16 * j, sum);
+    const int r = tm * BM + wm * (BM / WM) + (lane & 15) + 16 * i, c = tn * BN + wn * (BN / WN) + (lane >> 4) * 4 + 16 * j;
+    unsigned both[4] = {};
+    nt_finish<RESULT>(a, z, r, c, sum, both);
+    if (RESULT == kOutSlices && a.CT && !(a.symmetric && tm == tn) && r < ((a.m + 31) & ~31)) {
+        unsigned short* CT = a.CT + z * a.batch_ct;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < a.n) {
+                const int64_t t = (int64_t)(c + e) * a.ldct + (r >> 5) * 64 + (r & 31);
+                CT[t] = (unsigned short)both[e];
+                CT[t + 32] = (unsigned short)(both[e] >> 16);
+            }
+    }
 }
 
 // A tile shape as the choice sees it: how many workgroups run at a time, and what a slab takes then and with one workgroup to a compute unit (us).
