@@ -15,6 +15,10 @@ typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 typedef unsigned v2u __attribute__((ext_vector_type(2)));
+// vectors at the alignment of 16-bit values (global memory takes them at any): rows may start anywhere
+typedef v4u v4u_any __attribute__((aligned(2)));
+typedef v2u v2u_any __attribute__((aligned(2)));
+typedef unsigned u32_any __attribute__((aligned(2)));
 
 __device__ __forceinline__ float f16_to_f32(unsigned short b) { return (float)__builtin_bit_cast(_Float16, b); }
 __device__ __forceinline__ unsigned short f32_to_f16(float x) { return __builtin_bit_cast(unsigned short, (_Float16)x); }

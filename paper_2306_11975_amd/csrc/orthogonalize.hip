@@ -25,7 +25,7 @@ __device__ __forceinline__ double block_sum(double x, double* shared) {
 // A fixed order: the same sum on every run.
 template <int TYPE>
 __launch_bounds__(kThreads)
-__global__ void norm_partials_kernel(int64_t m, int64_t n, const void* G, int64_t ldg, int64_t stride, bool vec, double* partials) {
+__global__ void norm_partials_kernel(int64_t m, int64_t n, const void* G, int64_t ldg, int64_t stride, double* partials) {
     typedef Elem<TYPE> E;
     typedef typename E::raw raw;
     constexpr int V = 16 / sizeof(raw);
@@ -41,8 +41,8 @@ __global__ void norm_partials_kernel(int64_t m, int64_t n, const void* G, int64_
         for (int64_t p = threadIdx.x % tx; p < pieces; p += tx) {
             const raw* at = g + row * ldg + p * V;
             raw r[V];
-            if (vec && p * V + V <= n)
-                *reinterpret_cast<v4u*>(r) = *reinterpret_cast<const v4u*>(at);
+            if (p * V + V <= n)
+                *reinterpret_cast<v4u*>(r) = *reinterpret_cast<const v4u_any*>(at);
             else
 #pragma unroll
                 for (int e = 0; e < V; ++e) r[e] = p * V + e < n ? at[e] : raw(0);
@@ -60,7 +60,7 @@ __global__ void norm_partials_kernel(int64_t m, int64_t n, const void* G, int64_
 // takes 16 values of a row, then of a column: memory-bound, 16-byte accesses throughout.
 template <int TYPE>
 __launch_bounds__(kThreads)
-__global__ void normalised_slices_kernel(int64_t m, int64_t n, const void* G, int64_t ldg, int64_t stride, bool vec, const double* partials, int parts, double eps,
+__global__ void normalised_slices_kernel(int64_t m, int64_t n, const void* G, int64_t ldg, int64_t stride, const double* partials, int parts, double eps,
                                          double scale, unsigned short* rows, int64_t ldr, int64_t batch_r, unsigned short* cols, int64_t ldc,
                                          int64_t batch_c, int tiles_n) {
     typedef Elem<TYPE> E;
@@ -73,9 +73,9 @@ __global__ void normalised_slices_kernel(int64_t m, int64_t n, const void* G, in
     const int64_t row = m0 + across, at = n0 + along;
     const raw* g = reinterpret_cast<const raw*>(G) + z * stride + min(row, m - 1) * ldg + at;
     raw held[16];
-    if (vec && at + 16 <= n) {
+    if (at + 16 <= n) {
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(raw); ++i) reinterpret_cast<v4u*>(held)[i] = reinterpret_cast<const v4u*>(g)[i];
+        for (int i = 0; i < (int)sizeof(raw); ++i) reinterpret_cast<v4u*>(held)[i] = reinterpret_cast<const v4u_any*>(g)[i];
     } else {
 #pragma unroll
         for (int e = 0; e < 16; ++e) held[e] = at + e < n ? g[e] : raw(0);
@@ -117,13 +117,12 @@ int norm_parts(int64_t m, int64_t n) { return (int)std::min<int64_t>(kMostNormPa
 
 hipError_t launch_norm_partials(int64_t batch, int64_t m, int64_t n, const void* G, int type, int64_t ldg, int64_t stride, double* partials, hipStream_t st) {
     const dim3 grid((unsigned)norm_parts(m, n), (unsigned)batch);
-    const bool vec = rows_aligned16(G, ldg, type == OZIMMU_F32 ? 4 : 2) && rows_aligned16(G, stride, type == OZIMMU_F32 ? 4 : 2);
     if (type == OZIMMU_F32)
-        norm_partials_kernel<OZIMMU_F32><<<grid, kThreads, 0, st>>>(m, n, G, ldg, stride, vec, partials);
+        norm_partials_kernel<OZIMMU_F32><<<grid, kThreads, 0, st>>>(m, n, G, ldg, stride, partials);
     else if (type == OZIMMU_BF16)
-        norm_partials_kernel<OZIMMU_BF16><<<grid, kThreads, 0, st>>>(m, n, G, ldg, stride, vec, partials);
+        norm_partials_kernel<OZIMMU_BF16><<<grid, kThreads, 0, st>>>(m, n, G, ldg, stride, partials);
     else
-        norm_partials_kernel<OZIMMU_F16><<<grid, kThreads, 0, st>>>(m, n, G, ldg, stride, vec, partials);
+        norm_partials_kernel<OZIMMU_F16><<<grid, kThreads, 0, st>>>(m, n, G, ldg, stride, partials);
     return hipGetLastError();
 }
 
@@ -134,13 +133,12 @@ hipError_t launch_normalised_slices(int64_t batch, int64_t m, int64_t n, const v
     const dim3 grid((unsigned)((m + 63) / 64 * tiles_n), (unsigned)batch);
     const double scale = (double)(1 << shift);
     const int parts = norm_parts(m, n);
-    const bool vec = rows_aligned16(G, ldg, type == OZIMMU_F32 ? 4 : 2) && rows_aligned16(G, stride, type == OZIMMU_F32 ? 4 : 2);
     if (type == OZIMMU_F32)
-        normalised_slices_kernel<OZIMMU_F32><<<grid, kThreads, 0, st>>>(m, n, G, ldg, stride, vec, partials, parts, eps, scale, rows, ldr, batch_r, cols, ldc, batch_c, tiles_n);
+        normalised_slices_kernel<OZIMMU_F32><<<grid, kThreads, 0, st>>>(m, n, G, ldg, stride, partials, parts, eps, scale, rows, ldr, batch_r, cols, ldc, batch_c, tiles_n);
     else if (type == OZIMMU_BF16)
-        normalised_slices_kernel<OZIMMU_BF16><<<grid, kThreads, 0, st>>>(m, n, G, ldg, stride, vec, partials, parts, eps, scale, rows, ldr, batch_r, cols, ldc, batch_c, tiles_n);
+        normalised_slices_kernel<OZIMMU_BF16><<<grid, kThreads, 0, st>>>(m, n, G, ldg, stride, partials, parts, eps, scale, rows, ldr, batch_r, cols, ldc, batch_c, tiles_n);
     else
-        normalised_slices_kernel<OZIMMU_F16><<<grid, kThreads, 0, st>>>(m, n, G, ldg, stride, vec, partials, parts, eps, scale, rows, ldr, batch_r, cols, ldc, batch_c, tiles_n);
+        normalised_slices_kernel<OZIMMU_F16><<<grid, kThreads, 0, st>>>(m, n, G, ldg, stride, partials, parts, eps, scale, rows, ldr, batch_r, cols, ldc, batch_c, tiles_n);
     return hipGetLastError();
 }
 

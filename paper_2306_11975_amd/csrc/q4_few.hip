@@ -2,7 +2,8 @@
 //
 // What bounds it is reading the codes; the sums go to the matrix cores (v_mfma_f32_16x16x32) although most of their rows stay empty with
 // one token, because the vector units have their hands full making 16-bit operands of the codes. A wavefront takes 16 NT rows of
-// W, 16 TT tokens and every eighth step of k; the wavefronts of a workgroup share the rows and add their parts up in LDS.
+// W, 16 TT tokens and every eighth step of k (every second, with TW = 4 wavefronts along the tokens); the wavefronts of a workgroup share the rows and
+// add their parts up in LDS.
 //
 // A step is 128 positions. A lane loads 16 bytes, 32 positions, of row lane % 16 of each 16 x 128 block of codes. An MFMA adds up positions of one
 // group only: in groups of 64 and 32 the quarters of a wavefront (lane / 16) first exchange words (v_permlane32_swap, v_permlane16_swap), so that
@@ -109,12 +110,7 @@ __device__ __forceinline__ Operand<TYPE> operand(const Raw<TYPE>& r) {
     return t;
 }
 
-// vectors at the alignment of their values: rows of tokens and scales may start anywhere
-typedef v4u v4u_any __attribute__((aligned(2)));
-typedef v2u v2u_any __attribute__((aligned(2)));
-typedef unsigned u32_any __attribute__((aligned(2)));
-
-template <int TYPE, int GROUP, int NT, int TT>
+template <int TYPE, int GROUP, int NT, int TT, int TW>
 __launch_bounds__(kWaves * 64)
 __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_t ldx, const uint8_t* codes, int64_t ldq, const void* scales,
                               int64_t lds, void* Y, int64_t ldy) {
@@ -127,21 +123,23 @@ __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_
     constexpr int kRow = 16 * NT + 1;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t n0 = (int64_t)blockIdx.x * (16 * NT);
-    const int t0 = blockIdx.y * (16 * TT);
+    constexpr int KW = kWaves / TW;                        // TW wavefronts along the tokens, KW share the steps
+    const int part_k = wave % KW, part_t = wave / KW;
+    const int t0 = (blockIdx.y * TW + part_t) * (16 * TT);
     // Whole steps are dealt to the wavefronts in turn (together they read lines in full); the last wavefront takes what is left of the row beyond them too.
     const int full = (int)(k / 128);
-    const int mine = (full - wave + kWaves - 1) / kWaves;
+    const int mine = t0 < t ? (full - part_k + KW - 1) / KW : 0;
     const int quarter = lane >> 4;
     // position of word j of group h in a step, for this lane (the exchange between quarters below)
     const int at_quarter = GROUP == 128 ? 32 * quarter : GROUP == 64 ? 32 * (quarter & 1) + 16 * (quarter >> 1) : 8 * quarter;
     // Addresses are a scalar base and a lane's 32-bit offset (rows are at most OZIMMU_MAX_LD apart). Lanes of tokens and rows that are not there repeat the last one: their
     // results go nowhere.
-    const raw* xb = reinterpret_cast<const raw*>(X) + (int64_t)t0 * ldx;
+    const raw* xb = reinterpret_cast<const raw*>(X) + (int64_t)min(t0, t - 1) * ldx;
     const uint8_t* qb = codes + n0 * ldq;
     const raw* sb = reinterpret_cast<const raw*>(scales) + n0 * lds;
     unsigned xo[TT], qo[NT], so[NT];   // bytes
 #pragma unroll
-    for (int i = 0; i < TT; ++i) xo[i] = ((unsigned)min(16 * i + (lane & 15), t - 1 - t0) * (unsigned)ldx + at_quarter) * sizeof(raw);
+    for (int i = 0; i < TT; ++i) xo[i] = ((unsigned)max(min(16 * i + (lane & 15), t - 1 - t0), 0) * (unsigned)ldx + at_quarter) * sizeof(raw);
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
         const unsigned row = (unsigned)min((int64_t)(16 * i + (lane & 15)), n - 1 - n0);
@@ -273,10 +271,10 @@ __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_
         raw sc[DEPTH][NT][GROUPS] __attribute__((aligned(16)));
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d)
-            if (d < mine) load_codes(d * kWaves + wave, w[d], sc[d]);
+            if (d < mine) load_codes(d * KW + part_k, w[d], sc[d]);
         Raw<TYPE> xs[2][4][TT];   // this step's tokens and the next one's
 #pragma unroll
-        for (int j = 0; j < 4; ++j) load_word(wave, j, xs[0][j]);
+        for (int j = 0; j < 4; ++j) load_word(part_k, j, xs[0][j]);
         for (int step0 = 0; step0 < mine; step0 += DEPTH) {
 #pragma unroll
             for (int d = 0; d < DEPTH; ++d) {
@@ -284,13 +282,13 @@ __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_
                 if (step >= mine) break;
                 if (step + 1 < mine)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) load_word((step + 1) * kWaves + wave, j, xs[(d + 1) & 1][j]);
+                    for (int j = 0; j < 4; ++j) load_word((step + 1) * KW + part_k, j, xs[(d + 1) & 1][j]);
                 multiply(w[d], sc[d], xs[d & 1]);
-                if (step + DEPTH < mine) load_codes((step + DEPTH) * kWaves + wave, w[d], sc[d]);
+                if (step + DEPTH < mine) load_codes((step + DEPTH) * KW + part_k, w[d], sc[d]);
             }
         }
     }
-    if (wave == kWaves - 1 && k > (int64_t)full * 128) {
+    if (part_k == KW - 1 && t0 < t && k > (int64_t)full * 128) {
         v4u w[NT];
         raw sc[NT][GROUPS];
         Raw<TYPE> xs[4][TT];
@@ -306,26 +304,27 @@ __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_
 #pragma unroll
         for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) part[(wave * 16 * TT + 16 * tt + 4 * quarter + e) * kRow + 16 * i + (lane & 15)] = total[i][tt][e];
+            for (int e = 0; e < 4; ++e)
+                part[((part_k * TW + part_t) * 16 * TT + 16 * tt + 4 * quarter + e) * kRow + 16 * i + (lane & 15)] = total[i][tt][e];
     __syncthreads();
-    const int here = min(16 * TT, t - t0);
+    const int first = blockIdx.y * (16 * TT * TW), here = min(16 * TT * TW, t - first);
     for (int at = threadIdx.x; at < here * 16 * NT; at += kWaves * 64) {
         const int tok = at / (16 * NT), col = at % (16 * NT);
         if (n0 + col >= n) continue;
         float sum = part[tok * kRow + col];
 #pragma unroll
-        for (int i = 1; i < kWaves; ++i) sum += part[(i * 16 * TT + tok) * kRow + col];
-        reinterpret_cast<raw*>(Y)[(int64_t)(t0 + tok) * ldy + n0 + col] = E::store(sum);
+        for (int i = 1; i < KW; ++i) sum += part[(i * 16 * TT * TW + tok) * kRow + col];
+        reinterpret_cast<raw*>(Y)[(int64_t)(first + tok) * ldy + n0 + col] = E::store(sum);
     }
 }
 
-template <int TYPE, int GROUP, int NT, int TT>
+template <int TYPE, int GROUP, int NT, int TT, int TW>
 hipError_t launch_tiles(int64_t t, int64_t n, int64_t k, const void* X, int64_t ldx, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds,
                         void* Y, int64_t ldy, hipStream_t st) {
-    constexpr auto kernel = q4_few_kernel<TYPE, GROUP, NT, TT>;
+    constexpr auto kernel = q4_few_kernel<TYPE, GROUP, NT, TT, TW>;
     constexpr int bytes = kWaves * 16 * TT * (16 * NT + 1) * sizeof(float);
     if (hipError_t e = allow_dynamic_lds<kernel>(bytes); e != hipSuccess) return e;
-    const dim3 grid((unsigned)((n + 16 * NT - 1) / (16 * NT)), (unsigned)((t + 16 * TT - 1) / (16 * TT)));
+    const dim3 grid((unsigned)((n + 16 * NT - 1) / (16 * NT)), (unsigned)((t + 16 * TT * TW - 1) / (16 * TT * TW)));
     kernel<<<grid, kWaves * 64, bytes, st>>>((int)t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy);
     return hipGetLastError();
 }
@@ -335,12 +334,19 @@ hipError_t launch_typed(int64_t t, int64_t n, int64_t k, const void* X, int64_t 
     // More rows of W to a wavefront: fewer loads of tokens; more wavefronts: more codes on their way. (t = 16, n = 16384, k = 8192 with 16, 32, 64 rows: 46.9, 32.7, 25.8 us;
     // t = 1: 27.7, 22.5, 20.9; but n = 8192, k = 4096, t = 1: 8.7, 8.0, 12.0.) Two tiles of tokens share the operands made of the codes; with
     // 32-bit tokens the registers do not suffice.
+    // Four wavefronts along the tokens instead of all along k, where that leaves enough workgroups: a part of k is longer and fewer sums meet in LDS (300 32-bit tokens, n = 1500,
+    // k = 1000: 17.9 -> 15.1 us; 512 of 16 bits, 4095, 5000: 99 -> 87).
+    constexpr int64_t kEnough = 192;
+    const int64_t rows32 = (n + 31) / 32;
     if constexpr (TYPE != OZIMMU_F32) {
-        if (t > 16) return launch_tiles<TYPE, GROUP, 2, 2>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
-        if (n >= 64 * 256) return launch_tiles<TYPE, GROUP, 4, 1>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
+        if (t > 64 && rows32 * ((t + 127) / 128) >= kEnough) return launch_tiles<TYPE, GROUP, 2, 2, 4>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
+        if (t > 16) return launch_tiles<TYPE, GROUP, 2, 2, 1>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
+        if (n >= 64 * 256) return launch_tiles<TYPE, GROUP, 4, 1, 1>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
+    } else {
+        if (t > 32 && rows32 * ((t + 63) / 64) >= kEnough) return launch_tiles<TYPE, GROUP, 2, 1, 4>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
     }
-    if (n * ((t + 15) / 16) >= 32 * 256) return launch_tiles<TYPE, GROUP, 2, 1>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
-    return launch_tiles<TYPE, GROUP, 1, 1>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
+    if (rows32 * ((t + 15) / 16) >= 256) return launch_tiles<TYPE, GROUP, 2, 1, 1>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
+    return launch_tiles<TYPE, GROUP, 1, 1, 1>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
 }
 template <int TYPE>
 hipError_t launch_grouped(int64_t t, int64_t n, int64_t k, int group, const void* X, int64_t ldx, const uint8_t* codes, int64_t ldq, const void* scales,

@@ -56,15 +56,18 @@ Operands operands(int64_t t, int64_t n, int64_t k, int group, int type, bool gra
     return o;
 }
 // Whether Y = X W^T multiplies the codes as they are, 16 or 32 tokens a pass over them, or makes an operand of the weights and runs the tiled
-// product: by an estimate of both, in us. The passes take what their matrix and vector work takes; the product a walk along k, the operand's
-// bytes and its own operations.
+// product: by an estimate of both, in us. The passes fill the chip with 256 workgroups of 32 rows, and every eighth of k takes a step's time; the product
+// takes a walk along k, the operand's bytes and its own operations. (Fitted to 1 to 2048 tokens through layers of 1000 x 1000 to 16384 x 8192. 2048 x 2048 in 16 bits,
+// passes and product: 128 tokens 9.0 and 18.7, 256 16.6 and 18.8, 512 26.6 and 19.7; 8192 x 4096: 64 28.0 and 37.7, 128 47.5 and 44.5.)
 bool few(int64_t t, int64_t n, int64_t k, int type, bool gradient) {
     if (gradient || t > 65535 * 16) return false;   // (the launch's second dimension)
     const double nk = (double)n * (double)k;
-    // (tokens by the pass in both: more of them never go back to the passes, so that a workspace serves fewer tokens too)
+    // Tokens by the pass in both, and the passes never behind while they leave the chip partly idle: with more tokens the answer changes once, so that a
+    // workspace serves fewer tokens too.
     const double passes = (double)(type == OZIMMU_F32 ? (t + 15) / 16 : (t + 31) / 32);
-    if (type == OZIMMU_F32) return 3.5 + 3.7e-7 * nk * passes <= 14.0 + 0.0055 * k + 1.0e-6 * nk + 6.7e-8 * passes * nk;
-    return 3.5 + 3.85e-7 * nk * passes <= 6.0 + 0.0047 * k + 6.0e-7 * nk + 4.6e-8 * passes * nk;
+    const double rounds = std::max(1.0, (double)((n + 31) / 32) * passes / 256.0);
+    if (type == OZIMMU_F32) return 2.8 + rounds * k * (3.1 / 1024.0) <= 8.0 + 0.0055 * k + 9.0e-7 * nk + 7.3e-8 * passes * nk;
+    return 2.8 + rounds * k * (2.6 / 1024.0) <= 5.0 + 0.0042 * k + 5.5e-7 * nk + 4.0e-8 * passes * nk;
 }
 
 ozimmu_status_t q4_product(bool gradient, int64_t t, int64_t n, int64_t k, int group, int type, const void* V, int64_t ldv, const uint8_t* codes,

@@ -160,7 +160,7 @@ def check(got, V, W, dt, inner, rounded_weights):
 GEMMS = [(1, 1, 1, 32), (1, 16, 128, 128), (1, 2048, 512, 64), (1, 9000, 200, 128), (2, 15, 33, 32), (3, 33, 1000, 64), (5, 100, 257, 128), (13, 4095, 500, 32),
          (16, 64, 4096, 128), (16, 8200, 130, 64), (17, 40, 100, 32), (40, 130, 64, 64), (64, 64, 1024, 128), (65, 333, 777, 32), (129, 257, 96, 64), (300, 150, 1000, 128),
          (1000, 700, 320, 64), (2100, 4200, 192, 128), (3800, 3700, 100, 32),
-         (400, 2500, 2570, 32), (200, 6000, 1100, 64), (33, 17000, 260, 128), (16, 16500, 1000, 64)]
+         (400, 2500, 2570, 32), (200, 6000, 1100, 64), (33, 17000, 260, 128), (16, 16500, 1000, 64), (400, 1700, 260, 64)]
 
 
 @pytest.mark.parametrize("dt", TYPES)
