@@ -383,7 +383,7 @@ ozimmu_status_t ozimmu_zgemm_blas_auto(char transa, char transb, int64_t m, int6
  * products go through an operand of the weights in the workspace: s c rounded once to bf16 or fp16, or, for 32-bit types, both operands as two fp16 slices under a
  * power-of-two exponent per row (22 bits and more of every value that is within 2^-17 of its row's largest; the rest to 2^-39
  * of that; the exponent goes with the group for the columns of W). A token or gradient row that holds an infinity or a NaN gives NaN where its results are not
- * finite; every other row is what it would be without it. Empty dimensions: t = 0 or no outputs: nothing to do; an empty inner dimension
+ * finite; every other row is what it would be without it. (16-bit tokens above 2^115 may overflow on the way: the codes are multiplied with an offset.) Empty dimensions: t = 0 or no outputs: nothing to do; an empty inner dimension
  * gives zeros. Outputs must not overlap inputs or the workspace.
  * workspace: ozimmu_q4_workspace_bytes(...) bytes, OZIMMU_WORKSPACE_ALIGN-aligned; may be null where that is 0.
  * Errors: OZIMMU_ERR_BAD_DIM (sizes or group), OZIMMU_ERR_BAD_TYPE, OZIMMU_ERR_BAD_LD (also ldq, and any beyond OZIMMU_MAX_LD), OZIMMU_ERR_NULL, OZIMMU_ERR_MISALIGNED,
@@ -411,7 +411,8 @@ ozimmu_status_t ozimmu_q4_gemm_grad(int64_t t, int64_t n, int64_t k, int group, 
  * p(x) = a x + b x^3 + c x^5, and the singular vectors stay. (a, b, c) = (3.4445, -4.7750, 2.0315) with five steps takes
  * what is not far below the largest into 0.7 .. 1.2; (1.5, -0.5, 0) is the plain iteration for the nearest orthogonal matrix. G and X
  * have type `type`; X may be G (same strides), and otherwise must not overlap it. The norm is summed in 64 bits. Everything between is held as two fp16 slices under a common power of two
- * (22 bits and more), multiplied as three products with sums in 32 bits: errors are those of an iteration in 32 bits. A matrix of zeros gives zeros; one with an infinity or a NaN
+ * (22 bits and more), multiplied as three products with sums in 32 bits: errors are those of an iteration in 32 bits. (For bf16 results the last product of a
+ * matrix beyond 64 x 256 takes the first slices alone: off by 2^-12 of its operands, below the result's own rounding.) A matrix of zeros gives zeros; one with an infinity or a NaN
  * gives NaN in places that are not specified, and does not touch the others of its batch.
  * steps in 1 .. OZIMMU_MAX_STEPS, eps >= 0 and finite, a >= 1 (small singular values must not shrink: they are held to 2^-38 absolutely, or as
  * much more as intermediate values exceed four), and the polynomial must keep [0, 1] bounded under its iteration, so that no

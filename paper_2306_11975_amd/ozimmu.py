@@ -523,7 +523,11 @@ def alloc_q4_workspace(t: int, n: int, k: int, group: int, dtype, gradient: bool
 
 
 def _size(workspace) -> int:
-    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+    if workspace is None:
+        return 0
+    if not workspace.is_contiguous():
+        raise ValueError("expected a contiguous workspace")
+    return workspace.numel() * workspace.element_size()
 
 
 def _q4_product(f, gradient, V, codes, scales, group, R, workspace, stream):

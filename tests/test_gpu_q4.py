@@ -273,6 +273,27 @@ def test_large_and_small_values(dt):
     check(R, D0, weights64(c, s2, group), dt, n, True)
 
 
+@pytest.mark.parametrize("t,n,k", [(3, 50, 300), (2100, 4200, 192)])
+def test_subnormal_values_of_sixteen_bits(t, n, k):
+    """Tokens below 2^-14 and weights below it too are not normal in fp16: their bits count all the same. (Results are exact multiples of 2^-48 near 2^-24 and come out as multiples of
+    2^-24: the bound is half of that, and what check counts for normal values.)"""
+    c, s = plain_cut(random_weights(n, k, 3) * 2.0 ** -9, 64, F16)
+    X0 = (tokens(t, k, F32, 2) * 2.0 ** -10).to(F16)
+    D0 = (tokens(t, n, F32, 3) * 2.0 ** -10).to(F16)
+    assert (X0.abs() < 2.0 ** -14).any() and (s < 2.0 ** -14).any()
+    W = weights64(c, s, 64)
+    W16 = W.to(F16).double()     # (a weight that is not normal is off by up to half of 2^-24)
+    for V, M, M16, grad in ((X0, W.t(), W16.t(), False), (D0, W, W16, True)):
+        R = torch.empty(t, M.shape[1], dtype=F16, device=DEV)
+        (oz.q4_gemm_grad if grad else oz.q4_gemm)(V.to(DEV), pack(c).to(DEV), s.to(DEV), 64, R, oz.alloc_q4_workspace(t, n, k, 64, F16, gradient=grad))
+        want, terms = V.double() @ M, V.double().abs() @ M.abs()
+        # weights rounded to 16 bits where there is a workspace (their own difference, exactly), sums in 32 bits with the codes' offset, one rounding
+        rounded = grad or oz.q4_workspace_bytes(t, n, k, 64, F16) > 0
+        near = V.double() @ M16 if rounded else want
+        bound = (M.shape[0] + 8) * 2.0 ** -24 * 6 * terms + 2.0 ** -25 + half_step(F16) * near.abs()
+        assert ((R.cpu().double() - near).abs() <= bound * (1 + 1e-6)).all()
+
+
 @pytest.mark.parametrize("dt", TYPES)
 def test_other_stream_and_replayed_graph(dt):
     """One call on a stream of its own, and prompt, token, gradient and a new cut captured into one graph that shares a workspace, replayed with other inputs."""
