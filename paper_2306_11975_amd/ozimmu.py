@@ -406,17 +406,25 @@ def auto_num_slices_blas(transa: str, transb: str, m: int, n: int, k: int, A, ld
     return s.value, sums
 
 
+_torch = None
 _types = {}      # torch's types as ozimmu_type_t, once torch is there
 
 
-def _type_of(dtype) -> int:
-    if not _types:
-        import torch
+def _load_torch():
+    global _torch
+    import torch
 
-        _types.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
-    if dtype not in _types:
+    _types.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+    _torch = torch
+
+
+def _type_of(dtype) -> int:
+    if _torch is None:
+        _load_torch()
+    t = _types.get(dtype)
+    if t is None:
         raise ValueError(f"expected float32, bfloat16 or float16, got {dtype}")
-    return _types[dtype]
+    return t
 
 
 def _expect(condition, what: str) -> None:
@@ -424,27 +432,20 @@ def _expect(condition, what: str) -> None:
         raise ValueError(what)
 
 
-_torch = None
-
-
 def _call(f, stream, tensors, *args) -> None:
     """f(*args, stream) with the tensors' device current: all must be on one GPU. Without a stream, torch's current one of that
     device is taken. (One token's call is a few microseconds of GPU time: what happens here is kept short.)"""
-    global _torch
     if _torch is None:
-        import torch
-
-        _torch = torch
-    device = tensors[0].device
+        _load_torch()
+    index = tensors[0].get_device()
     for t in tensors:
-        if t is not None and t.device != device:
+        if t is not None and t.get_device() != index:
             raise ValueError("all tensors must be on one device")
-    if device.type != "cuda":
+    if index < 0:
         raise ValueError("expected tensors on a GPU")
-    index = device.index
     if stream is None:
         raw = _torch._C._cuda_getCurrentRawStream(index)
-    elif stream.device != device:
+    elif stream.device.index != index:
         raise ValueError("the stream belongs to another device than the tensors")
     else:
         raw = stream.cuda_stream
@@ -459,11 +460,13 @@ def _call(f, stream, tensors, *args) -> None:
 
 def _rows(t):
     """Rows, columns and row stride of a 2-D tensor with unit stride along its rows."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
-        raise ValueError("expected a 2-D row-major tensor (unit stride along the second dimension)")
-    rows, cols = shape
-    return rows, cols, stride[0] if rows > 1 else cols or 1
+    if t.dim() != 2:
+        raise ValueError("expected a 2-D tensor")
+    rows, cols = t.shape
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError("expected a row-major tensor (unit stride along the second dimension)")
+    return rows, cols, ld if rows > 1 else cols or 1
 
 
 def q4_geometry(k: int, group: int):
