@@ -402,9 +402,9 @@ inline NtChoice nt_choose(const NtArgs& a, const NtShape& s, size_t part_bytes) 
     c.us = 1e30;
     if (all > INT32_MAX / 64) return c;
     c.plan.tiles = (int)one;
-    auto round_us = [&](int64_t workgroups, int64_t slabs) {   // of a round of at most s.slots
-        const double load = std::max(0.0, (double)(workgroups - kComputeUnits) / std::max(1, s.slots - kComputeUnits));
-        return (double)slabs * (s.alone + (s.full - s.alone) * std::min(1.0, load));
+    auto round_us = [&](int64_t workgroups, int64_t slabs) {   // of a round of at most s.slots: what the fullest compute unit takes
+        const double deepest = (double)((workgroups + kComputeUnits - 1) / kComputeUnits), most = (double)(s.slots / kComputeUnits);
+        return (double)slabs * (s.alone + (s.full - s.alone) * (most > 1.0 ? (deepest - 1.0) / (most - 1.0) : 0.0));
     };
     const int64_t rounds = all / s.slots, rest = all % s.slots;
     c.plan.whole = (int)all;
@@ -447,7 +447,7 @@ template <int SLICES, bool BF16, int RESULT>
 hipError_t launch_nt(const NtArgs& a, hipStream_t st) {
     if (a.m <= 0 || a.n <= 0 || a.slabs <= 0 || a.batch <= 0 || (a.symmetric && a.m != a.n)) return hipErrorInvalidValue;
     constexpr bool two = SLICES == 2;   // (the first of two slices: as many products as with one, on half the positions a slab)
-    const NtShape shapes[] = {{256, 256, two ? 2.41 : 1.73, two ? 2.41 : 1.73}, {128, 512, two ? 1.31 : 0.95, two ? 0.92 : 0.62}, {64, 1280, two ? 1.0 : 0.9, two ? 0.40 : 0.37}, {64, 768, two ? 1.0 : 0.9, two ? 0.31 : 0.27}};
+    const NtShape shapes[] = {{256, 256, two ? 2.41 : 1.73, two ? 2.41 : 1.73}, {128, 512, two ? 1.31 : 0.95, two ? 0.92 : 0.62}, {64, 1280, two ? 1.0 : 0.9, two ? 0.40 : 0.37}, {64, 768, two ? 0.75 : 0.66, two ? 0.31 : 0.27}};
     NtChoice best{};
     int which = -1;
     for (int i = 0; i < 4; ++i) {

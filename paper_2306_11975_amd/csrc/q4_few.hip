@@ -64,12 +64,13 @@ __device__ __forceinline__ v4u offset_codes(unsigned w, const CodeBits& b) {
     }
     return r;
 }
-// the codes themselves as bf16
-__device__ __forceinline__ v4u exact_codes(unsigned w, const CodeBits& b) {
-    v4u r = offset_codes<true>(w, b);
+// the codes' sixteenths as bf16, exactly: the conversion from four signed bits gives them, and four bits fit the upper half of a 32-bit value
+__device__ __forceinline__ v4u exact_codes(unsigned w) {
+    w ^= 0x88888888u;
+    v4u r;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float lo = __uint_as_float(r[i] << 16) - 24.f, hi = __uint_as_float(r[i] & 0xffff0000u) - 24.f;
+        const float lo = __builtin_amdgcn_cvt_off_f32_i4((int)(w >> (4 * i))), hi = __builtin_amdgcn_cvt_off_f32_i4((int)(w >> (4 * i + 16)));
         r[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
     }
     return r;
@@ -243,7 +244,7 @@ __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_
                 for (int i = 0; i < NT; ++i) {
                     const unsigned word = words[i][GW * h + j];
                     if constexpr (TYPE == OZIMMU_F32) {
-                        const v4u c = exact_codes(word, bits);
+                        const v4u c = exact_codes(word);
 #pragma unroll
                         for (int p = 2; p >= 0; --p)
 #pragma unroll
@@ -314,7 +315,7 @@ __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_
         float sum = part[tok * kRow + col];
 #pragma unroll
         for (int i = 1; i < KW; ++i) sum += part[(i * 16 * TT * TW + tok) * kRow + col];
-        reinterpret_cast<raw*>(Y)[(int64_t)(first + tok) * ldy + n0 + col] = E::store(sum);
+        reinterpret_cast<raw*>(Y)[(int64_t)(first + tok) * ldy + n0 + col] = E::store(TYPE == OZIMMU_F32 ? 16.f * sum : sum);   // (the codes' sixteenths)
     }
 }
 
