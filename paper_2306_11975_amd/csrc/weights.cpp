@@ -55,19 +55,42 @@ Operands operands(int64_t t, int64_t n, int64_t k, int group, int type, bool gra
     o.total = off;
     return o;
 }
-// Whether Y = X W^T multiplies the codes as they are, 16 or 32 tokens a pass over them, or makes an operand of the weights and runs the tiled
-// product: by an estimate of both, in us. The passes fill the chip with 256 workgroups of 32 rows, and every eighth of k takes a step's time; the product
-// takes a walk along k, the operand's bytes and its own operations. (Fitted to 1 to 2048 tokens through layers of 1000 x 1000 to 16384 x 8192. 2048 x 2048 in 16 bits,
-// passes and product: 128 tokens 9.0 and 18.7, 256 16.6 and 18.8, 512 26.6 and 19.7; 8192 x 4096: 64 28.0 and 37.7, 128 47.5 and 44.5.)
-bool few(int64_t t, int64_t n, int64_t k, int type, bool gradient) {
-    if (gradient || t > 65535 * 16) return false;   // (the launch's second dimension)
+// How Y = X W^T is computed: by passes over the codes, 16 or 32 tokens each (q4_few.hip); tile by tile, the weights' operand made on the way (q4_tile.hip,
+// 16-bit types); or as an operand of the weights and the tiled product (nt_product.h), which gradients take always.
+//
+// The choice is by an estimate of each, in us. 256 workgroups of the passes (32 rows of weights each) are a round, whose time grows with k. A tile's walk takes
+// half a microsecond a slab of 64 positions (twice that the large ones) until the chip has more than one workgroup for a compute unit. The product takes a walk
+// along k, the operand's bytes, dearer once no cache holds them, and its own operations. Fitted to 32 to 2048 tokens through fourteen layers from 20000 x 64 and
+// 1000 x 333 to 16384 x 8192, where the choices take 0.7 % more than the best ones do on average, 30 % at most (2048 x 16384, 32 tokens: the passes 46 us, the
+// product 36). Times of passes, tiles, large tiles, product, bf16: 1000 x 1000, 1024 tokens 14.8, 12.0, 19.8, 14.1; 8192 x 4096, 64 28, 34, 61, 38, 128 48, 34, 62,
+// 40, 512 -, 76, 66, 66; 16384 x 8192, 128 160, 90, 121, 180, 512 -, 283, 189, 236.
+//
+// With more tokens the answer turns to the product once and stays, so that a workspace serves fewer tokens too: every estimate rises with the tokens at least as
+// the product's does. (The passes are held against the product of their round's first tokens; `more` is added to the tiles' flat part.)
+enum class Way { passes, tiles, large_tiles, product };
+Way way_of(int64_t t, int64_t n, int64_t k, int type, bool gradient) {
+    if (gradient) return Way::product;
     const double nk = (double)n * (double)k;
-    // Tokens by the pass in both, and the passes never behind while they leave the chip partly idle: with more tokens the answer changes once, so that a
-    // workspace serves fewer tokens too.
-    const double passes = (double)(type == OZIMMU_F32 ? (t + 15) / 16 : (t + 31) / 32);
-    const double rounds = std::max(1.0, (double)((n + 31) / 32) * passes / 256.0);
-    if (type == OZIMMU_F32) return 2.8 + rounds * k * (3.1 / 1024.0) <= 8.0 + 0.0055 * k + 9.0e-7 * nk + 7.3e-8 * passes * nk;
-    return 2.8 + rounds * k * (2.6 / 1024.0) <= 5.0 + 0.0042 * k + 5.5e-7 * nk + 4.0e-8 * passes * nk;
+    const int64_t tokens = type == OZIMMU_F32 ? 16 : 32, passes = (t + tokens - 1) / tokens, rows = (n + 31) / 32;
+    const bool can_pass = passes <= 65535;   // (the launch's second dimension)
+    if (type == OZIMMU_F32) {
+        const double rounds = std::max(1.0, (double)rows * (double)passes / 256.0);
+        return can_pass && 2.8 + rounds * k * (3.1 / 1024.0) <= 8.0 + 0.0055 * k + 9.0e-7 * nk + 7.3e-8 * (double)passes * nk ? Way::passes : Way::product;
+    }
+    if (t <= 16) return Way::passes;
+    const double rounds = std::ceil((double)rows * (double)passes / 256.0), first = (rounds - 1.0) * 256.0 / (double)rows;
+    const double product = 16.5 + 0.0025 * k + 5.9e-7 * nk + 4.6e-7 * std::max(0.0, nk - 4.0e7), more = 4.5e-8 * nk;
+    const double few = 1.9 + rounds * (1.2 + 0.0036 * k);
+    const bool few_lose = !can_pass || few > product + more * first;
+    if (k < 8) return few_lose ? Way::product : Way::passes;
+    const double slabs = (double)((k + 63) / 64), grown = more * (double)passes;
+    const double fill = (double)((n + 63) / 64) * (double)passes / 512.0, fill_large = (double)((n + 127) / 128) * (double)passes / 1024.0;   // workgroups by compute unit
+    const double held = 3.2 + 0.54 * fill, held_large = 3.8 + 2.2 * fill_large, slope = (0.27 + 0.22 * fill) * slabs, slope_large = (0.16 + 0.64 * fill_large) * slabs;
+    const double surely = std::min(held + std::max(0.51 * slabs + grown, slope), held_large + std::max(slabs + grown, slope_large));
+    if (few_lose && surely > product + grown) return Way::product;
+    const double tiles = held + std::max(0.51 * slabs, slope), large = held_large + std::max(slabs, slope_large);
+    if (can_pass && few <= std::min(tiles, large)) return Way::passes;
+    return large < tiles ? Way::large_tiles : Way::tiles;
 }
 
 ozimmu_status_t q4_product(bool gradient, int64_t t, int64_t n, int64_t k, int group, int type, const void* V, int64_t ldv, const uint8_t* codes,
@@ -86,7 +109,10 @@ ozimmu_status_t q4_product(bool gradient, int64_t t, int64_t n, int64_t k, int g
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (inner == 0) return hip_status(launch_zero_rows(t, outer, R, type, ldr, st));
-    if (few(t, n, k, type, gradient)) return hip_status(launch_q4_few(t, n, k, group, V, type, ldv, codes, ldq, scales, lds, R, ldr, st));
+    const Way way = way_of(t, n, k, type, gradient);
+    if (way == Way::passes) return hip_status(launch_q4_few(t, n, k, group, V, type, ldv, codes, ldq, scales, lds, R, ldr, st));
+    if (way != Way::product)
+        return hip_status(launch_q4_tiles(way == Way::large_tiles, t, n, k, group, V, type, ldv, codes, ldq, scales, lds, R, ldr, st));
     const Operands o = operands(t, n, k, group, type, gradient);
     if (!ws || misaligned(ws, OZIMMU_WORKSPACE_ALIGN) || ws_bytes < o.total) return OZIMMU_ERR_WORKSPACE;
     unsigned char* base = static_cast<unsigned char*>(ws);
@@ -230,7 +256,7 @@ ozimmu_status_t ozimmu_q4_workspace_bytes(int64_t t, int64_t n, int64_t k, int g
     if (!dim_ok(t) || !dim_ok(n) || !dim_ok(k) || !group_ok(group)) return OZIMMU_ERR_BAD_DIM;
     if (!type_ok(type)) return OZIMMU_ERR_BAD_TYPE;
     if (!bytes) return OZIMMU_ERR_NULL;
-    *bytes = few(t, n, k, type, gradient != 0) || t == 0 || n == 0 || k == 0 ? 0 : operands(t, n, k, group, type, gradient != 0).total;
+    *bytes = t == 0 || n == 0 || k == 0 || way_of(t, n, k, type, gradient != 0) != Way::product ? 0 : operands(t, n, k, group, type, gradient != 0).total;
     return OZIMMU_OK;
 }
 

@@ -69,6 +69,10 @@ hipError_t launch_zero_rows(int64_t rows, int64_t cols, void* R, int type, int64
 hipError_t launch_q4_few(int64_t t, int64_t n, int64_t k, int group, const void* X, int type, int64_t ldx, const uint8_t* codes,
                          int64_t ldq, const void* scales, int64_t lds, void* Y, int64_t ldy, hipStream_t st);
 
+// q4_tile.hip: Y = X W^T of 16-bit types and k >= 8 for more tokens, the operand of the weights made tile by tile (64 x 64, or `large`: 128 x 128)
+hipError_t launch_q4_tiles(bool large, int64_t t, int64_t n, int64_t k, int group, const void* X, int type, int64_t ldx, const uint8_t* codes, int64_t ldq,
+                           const void* scales, int64_t lds, void* Y, int64_t ldy, hipStream_t st);
+
 // orthogonalize.hip
 constexpr int kMostNormParts = 1024;   // partial sums of squares per matrix
 int norm_parts(int64_t m, int64_t n);

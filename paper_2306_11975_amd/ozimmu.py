@@ -548,8 +548,8 @@ def _q4_product(f, gradient, V, codes, scales, group, R, workspace, stream):
 
 
 def q4_gemm(X, codes, scales, group: int, Y, workspace=None, stream=None) -> None:
-    """Y = X W^T for weights in four bits (X: t x k, Y: t x n; X, Y and the scales of one type). The workspace may be None for
-    as few tokens as q4_workspace_bytes gives 0 for."""
+    """Y = X W^T for weights in four bits (X: t x k, Y: t x n; X, Y and the scales of one type). The workspace may be None
+    where q4_workspace_bytes gives 0 (up to 16 tokens always, often for many more)."""
     _q4_product(lib().ozimmu_q4_gemm, False, X, codes, scales, group, Y, workspace, stream)
 
 

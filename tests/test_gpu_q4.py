@@ -137,8 +137,8 @@ def tokens(t, cols, dt, seed):
 
 
 def check(got, V, W, dt, inner, rounded_weights):
-    """|got - V W| against what roundings can do. One rounding of the result; weights rounded to a 16-bit type; 32-bit values as two slices
-    (each operand off by at most 2^-22 of itself or 2^-40 of its row's largest, a third product of 2^-22 left out); the sums in 32 bits,
+    """|got - V W| against what roundings can do. One rounding of the result; weights rounded to a 16-bit type (products of more than 16 tokens may do that,
+    gradients do); 32-bit values as two slices (each operand off by at most 2^-22 of itself or 2^-40 of its row's largest, a third product of 2^-22 left out); the sums in 32 bits,
     whose terms may carry the codes' offset (up to 24 + 16 for codes up to 8: five times the largest term)."""
     want = V.double() @ W
     terms = V.double().abs() @ W.abs()
@@ -147,7 +147,7 @@ def check(got, V, W, dt, inner, rounded_weights):
     if dt == F32:
         bound = 3 * 2.0 ** -22 * terms + 4 * inner * 2.0 ** -40 * top + sums * terms
     else:
-        bound = (half_step(dt) if rounded_weights else 0.0) * terms + (sums * terms if rounded_weights else (inner + 8) * 2.0 ** -24 * 40 * torch.ones_like(terms) * top)
+        bound = (half_step(dt) if rounded_weights else 0.0) * terms + (inner + 8) * 2.0 ** -24 * 40 * top
     bound = bound + half_step(dt) * (want.abs() + bound) + torch.finfo(dt).tiny
     off = (got.cpu().double() - want).abs()
     assert (off <= bound).all(), f"off by up to {(off / bound).max():.3g} times what roundings can do"
@@ -160,7 +160,10 @@ def check(got, V, W, dt, inner, rounded_weights):
 GEMMS = [(1, 1, 1, 32), (1, 16, 128, 128), (1, 2048, 512, 64), (1, 9000, 200, 128), (2, 15, 33, 32), (3, 33, 1000, 64), (5, 100, 257, 128), (13, 4095, 500, 32),
          (16, 64, 4096, 128), (16, 8200, 130, 64), (17, 40, 100, 32), (40, 130, 64, 64), (64, 64, 1024, 128), (65, 333, 777, 32), (129, 257, 96, 64), (300, 150, 1000, 128),
          (1000, 700, 320, 64), (2100, 4200, 192, 128), (3800, 3700, 100, 32),
-         (400, 2500, 2570, 32), (200, 6000, 1100, 64), (33, 17000, 260, 128), (16, 16500, 1000, 64), (400, 1700, 260, 64)]
+         (400, 2500, 2570, 32), (200, 6000, 1100, 64), (33, 17000, 260, 128), (16, 16500, 1000, 64), (400, 1700, 260, 64),
+         # tiles of 64 and of 128 that end in every way, with k from eight on; many tokens of few and of many positions
+         (300, 2000, 8, 32), (290, 2001, 9, 32), (310, 1987, 15, 64), (257, 2050, 63, 128), (1000, 1030, 129, 64), (64, 8200, 200, 32), (2000, 2100, 513, 64),
+         (2000, 4130, 66, 32), (2500, 4097, 60, 128), (3000, 2100, 7, 32), (2000, 2100, 2570, 32), (2048, 2048, 2560, 128)]
 
 
 @pytest.mark.parametrize("dt", TYPES)
@@ -178,7 +181,7 @@ def test_gemm(t, n, k, group, dt):
         X.copy_(X0)
         Y, ybuf = padded(t, n, dt, extra, offset)
         oz.q4_gemm(X, codes, scales, group, Y, ws)
-        check(Y, X0, W, dt, k, oz.q4_workspace_bytes(t, n, k, group, dt) > 0)
+        check(Y, X0, W, dt, k, t > 16)
         assert (ybuf[:offset] == 77).all() and (ybuf[offset:offset + t * (n + extra)].view(t, -1)[:, n:] == 77).all() and (ybuf[offset + t * (n + extra):] == 77).all()
 
 
@@ -235,9 +238,9 @@ def test_empty_inner_dimension_gives_zeros(t, dt):
 
 
 @pytest.mark.parametrize("dt", TYPES)
-@pytest.mark.parametrize("t", [5, 70])
-def test_a_row_that_is_not_finite_stays_alone(t, dt):
-    n, k, group = 100, 200, 64
+@pytest.mark.parametrize("t,n", [(5, 100), (70, 100), (300, 2000)])
+def test_a_row_that_is_not_finite_stays_alone(t, n, dt):
+    k, group = 200, 64
     c, s = plain_cut(random_weights(n, k, 9), group, dt)
     codes, scales = pack(c).to(DEV), s.to(DEV)
     for grad in (False, True):
@@ -273,7 +276,7 @@ def test_large_and_small_values(dt):
     check(R, D0, weights64(c, s2, group), dt, n, True)
 
 
-@pytest.mark.parametrize("t,n,k", [(3, 50, 300), (2100, 4200, 192)])
+@pytest.mark.parametrize("t,n,k", [(3, 50, 300), (400, 2000, 300), (2100, 4200, 192), (2000, 2100, 2570)])
 def test_subnormal_values_of_sixteen_bits(t, n, k):
     """Tokens below 2^-14 and weights below it too are not normal in fp16: their bits count all the same. (Results are exact multiples of 2^-48 near 2^-24 and come out as multiples of
     2^-24: the bound is half of that, and what check counts for normal values.)"""
@@ -287,9 +290,8 @@ def test_subnormal_values_of_sixteen_bits(t, n, k):
         R = torch.empty(t, M.shape[1], dtype=F16, device=DEV)
         (oz.q4_gemm_grad if grad else oz.q4_gemm)(V.to(DEV), pack(c).to(DEV), s.to(DEV), 64, R, oz.alloc_q4_workspace(t, n, k, 64, F16, gradient=grad))
         want, terms = V.double() @ M, V.double().abs() @ M.abs()
-        # weights rounded to 16 bits where there is a workspace (their own difference, exactly), sums in 32 bits with the codes' offset, one rounding
-        rounded = grad or oz.q4_workspace_bytes(t, n, k, 64, F16) > 0
-        near = V.double() @ M16 if rounded else want
+        # weights rounded to 16 bits with many tokens (their own difference, exactly), sums in 32 bits with the codes' offset, one rounding
+        near = V.double() @ M16 if grad or t > 16 else want
         bound = (M.shape[0] + 8) * 2.0 ** -24 * 6 * terms + 2.0 ** -25 + half_step(F16) * near.abs()
         assert ((R.cpu().double() - near).abs() <= bound * (1 + 1e-6)).all()
 
