@@ -334,17 +334,14 @@ hipError_t launch_typed(int64_t t, int64_t n, int64_t k, const void* X, int64_t 
                         void* Y, int64_t ldy, hipStream_t st) {
     // More rows of W to a wavefront: fewer loads of tokens; more wavefronts: more codes on their way. (t = 16, n = 16384, k = 8192 with 16, 32, 64 rows: 46.9, 32.7, 25.8 us;
     // t = 1: 27.7, 22.5, 20.9; but n = 8192, k = 4096, t = 1: 8.7, 8.0, 12.0.) Two tiles of tokens share the operands made of the codes; with
-    // 32-bit tokens the registers do not suffice.
-    // Four wavefronts along the tokens instead of all along k, where that leaves enough workgroups: a part of k is longer and fewer sums meet in LDS (300 32-bit tokens, n = 1500,
-    // k = 1000: 17.9 -> 15.1 us; 512 of 16 bits, 4095, 5000: 99 -> 87).
-    constexpr int64_t kEnough = 192;
+    // 32-bit tokens the registers do not suffice; those have four wavefronts along the tokens instead of all along k, where that leaves enough workgroups: a part of k is
+    // longer and fewer sums meet in LDS (300 tokens, n = 1500, k = 1000: 17.9 -> 15.1 us). (So many 16-bit tokens do not come here.)
     const int64_t rows32 = (n + 31) / 32;
     if constexpr (TYPE != OZIMMU_F32) {
-        if (t > 64 && rows32 * ((t + 127) / 128) >= kEnough) return launch_tiles<TYPE, GROUP, 2, 2, 4>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
         if (t > 16) return launch_tiles<TYPE, GROUP, 2, 2, 1>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
         if (n >= 64 * 256) return launch_tiles<TYPE, GROUP, 4, 1, 1>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
     } else {
-        if (t > 32 && rows32 * ((t + 63) / 64) >= kEnough) return launch_tiles<TYPE, GROUP, 2, 1, 4>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
+        if (t > 32 && rows32 * ((t + 63) / 64) >= 192) return launch_tiles<TYPE, GROUP, 2, 1, 4>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
     }
     if (rows32 * ((t + 15) / 16) >= 256) return launch_tiles<TYPE, GROUP, 2, 1, 1>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
     return launch_tiles<TYPE, GROUP, 1, 1, 1>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);

@@ -31,10 +31,18 @@ ozimmu_status_t check_q4(int64_t k, int group, const void* codes, int64_t ldq, c
     return OZIMMU_OK;
 }
 
+// Room for the sums of shared tiles (nt_choose): at most 32 workgroups share one, four slabs at least to each, and no product takes more than kPartialBytes.
+size_t partial_room(int64_t batch, int64_t m, int64_t n, int64_t slabs) {
+    const int64_t parts = std::min<int64_t>(32, slabs / 4);
+    if (parts < 2) return 0;
+    const double bytes = (double)batch * (double)pad_to(m, 256) * (double)pad_to(n, 256) * (double)parts * sizeof(float);
+    return bytes < (double)kPartialBytes ? (size_t)bytes : kPartialBytes;
+}
+
 // The operands of a product with many tokens in the workspace: V (t rows of `inner` values) and the weights (`outer` rows). 32-bit types take two slices.
 struct Operands {
     int64_t inner, outer, ld;
-    size_t off_v, off_w, off_ev, off_ew, off_partial, total;
+    size_t off_v, off_w, off_ev, off_ew, off_partial, partial, total;
 };
 Operands operands(int64_t t, int64_t n, int64_t k, int group, int type, bool gradient) {
     Operands o{};
@@ -51,7 +59,8 @@ Operands operands(int64_t t, int64_t n, int64_t k, int group, int type, bool gra
     o.off_ev = off;
     if (type == OZIMMU_F32) off = align_up(off + sizeof(int) * (size_t)t);
     o.off_partial = off;
-    off = align_up(off + kPartialBytes);
+    o.partial = partial_room(1, t, o.outer, o.ld / kSlabValues);
+    off = align_up(off + o.partial);
     o.total = off;
     return o;
 }
@@ -134,7 +143,7 @@ ozimmu_status_t q4_product(bool gradient, int64_t t, int64_t n, int64_t k, int g
     a.batch = 1;
     a.factor = 1.0f;
     a.partial = reinterpret_cast<float*>(base + o.off_partial);
-    a.partial_bytes = kPartialBytes;
+    a.partial_bytes = o.partial;
     a.out = R;
     a.ldo = ldr;
     if (type == OZIMMU_F32) {
@@ -153,7 +162,7 @@ struct OrthLayout {
     int64_t r, l;              // shorter and longer side
     int64_t ld_x, ld_t;        // values per row: along the longer side, along the shorter one
     int64_t size_x, size_t_, size_a;
-    size_t off_x, off_t[2], off_a, off_q, off_norm, off_partial, total;
+    size_t off_x, off_t[2], off_a, off_q, off_norm, off_partial, partial, total;
 };
 OrthLayout orth_layout(int64_t batch, int64_t m, int64_t n) {
     OrthLayout o{};
@@ -172,7 +181,8 @@ OrthLayout orth_layout(int64_t batch, int64_t m, int64_t n) {
     o.off_a = take(2 * (size_t)batch * o.size_a);
     o.off_q = take(2 * (size_t)batch * o.size_a);
     o.off_norm = take(sizeof(double) * (size_t)batch * norm_parts(m, n));
-    o.off_partial = take(kPartialBytes);
+    o.partial = std::max(partial_room(batch, o.r, o.r, std::max(o.ld_x, o.ld_t) / kSlabValues), partial_room(batch, o.r, o.l, o.ld_t / kSlabValues));
+    o.off_partial = take(o.partial);
     o.total = off;
     return o;
 }
@@ -311,7 +321,7 @@ ozimmu_status_t ozimmu_orthogonalize(int64_t batch, int64_t m, int64_t n, ozimmu
         NtArgs g{};
         g.batch = (int)batch;
         g.partial = reinterpret_cast<float*>(base + o.off_partial);
-        g.partial_bytes = kPartialBytes;
+        g.partial_bytes = o.partial;
         g.m = g.n = (int)o.r;
         g.symmetric = true;
         g.factor = down;
@@ -341,7 +351,7 @@ ozimmu_status_t ozimmu_orthogonalize(int64_t batch, int64_t m, int64_t n, ozimmu
         NtArgs u{};
         u.batch = (int)batch;
         u.partial = g.partial;
-        u.partial_bytes = kPartialBytes;
+        u.partial_bytes = o.partial;
         u.slabs = (int)(o.ld_t / kSlabValues);
         u.ldp = u.ldq = o.ld_t;
         if (last && tall) {   // X^T (a + b A + c A^2), as it lies in the result

@@ -155,6 +155,18 @@ def test_the_size_of_the_matrix_does_not_matter(scale):
     assert (X0 - X1).norm() <= 1e-4 * X0.norm()
 
 
+@pytest.mark.parametrize("batch,m,n", [(1, 65, 65), (3, 70, 1500), (1, 1500, 90), (2, 520, 1000), (1, 1100, 1100)])
+def test_nothing_beyond_the_workspace_is_written(batch, m, n):
+    need = oz.orthogonalize_workspace_bytes(batch, m, n)
+    room = torch.full((need + (1 << 20),), 0x5A, dtype=torch.uint8, device=DEV)
+    G0 = torch.stack([gradient(m, n, 3 + i) for i in range(batch)])
+    X = torch.empty(batch, m, n, device=DEV)
+    oz.orthogonalize(G0.to(DEV), X, room[:need])
+    assert (room[need:] == 0x5A).all()
+    for got, G in zip(X, G0):
+        check(got, G)
+
+
 def test_graph_shares_a_workspace_with_eager_calls():
     G = torch.stack([gradient(100, 140, i) for i in range(2)]).to(DEV)
     X = torch.empty_like(G)

@@ -345,3 +345,19 @@ def test_repeated_calls_give_the_same_bits():
     for i in range(2):
         oz.q4_gemm(X, pack(c).to(DEV), s.to(DEV), group, Y[i])
     assert torch.equal(Y[0], Y[1])
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("t,n,k", [(17, 1, 40), (300, 257, 2500), (2000, 2100, 2570), (64, 70, 9000), (700, 520, 1000)])
+def test_nothing_beyond_the_workspace_is_written(t, n, k, dt):
+    c, s = plain_cut(random_weights(n, k, 5), 32, dt)
+    codes, scales = pack(c).to(DEV), s.to(DEV)
+    for grad in (False, True):
+        need = oz.q4_workspace_bytes(t, n, k, 32, dt, gradient=grad)
+        room = torch.full((need + (1 << 20),), 0x5A, dtype=torch.uint8, device=DEV)
+        V = tokens(t, n if grad else k, dt, 2)
+        R = torch.empty(t, k if grad else n, dtype=dt, device=DEV)
+        (oz.q4_gemm_grad if grad else oz.q4_gemm)(V.to(DEV), codes, scales, 32, R, room[:need] if need else None)
+        assert (room[need:] == 0x5A).all()
+        W = weights64(c, s, 32)
+        check(R, V, W if grad else W.t(), dt, n if grad else k, True)
