@@ -17,7 +17,7 @@ PRELOAD = PKG / "libozimmu_preload.so"  # interposer for the vendor DGEMM/ZGEMM 
 BLAS_CLIENT = PKG / "blas_client"     # plain rocBLAS/hipBLAS program the interposer is tried on (csrc/blas_client.cpp)
 
 SOURCES = ["split.hip", "gemm.hip", "gemm_real.hip", "gemm_dd.hip", "gemm_complex.hip", "gate.hip", "gate_many.hip", "small.hip", "small_complex.hip", "probes.hip", "static_scratch.hip", "api.cpp",
-           "nt_product.hip", "nt_product_two.hip", "q4.hip", "q4_few.hip", "q4_tile.hip", "orthogonalize.hip", "orthogonalize_small.hip", "weights.cpp"]
+           "nt_product.hip", "nt_product_two.hip", "q4.hip", "q4_few.hip", "q4_token.hip", "q4_tile.hip", "orthogonalize.hip", "orthogonalize_small.hip", "weights.cpp"]
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-ffp-contract=off", "-Wall", f"-I{INCLUDE}", f"-I{CSRC}"]
 # device code: gfx950 only; packed-FP32 instruction selection is switched off on the test machines
 DEVICE = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

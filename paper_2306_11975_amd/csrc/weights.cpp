@@ -64,10 +64,13 @@ Operands operands(int64_t t, int64_t n, int64_t k, int group, int type, bool gra
     o.total = off;
     return o;
 }
-// How Y = X W^T is computed: by passes over the codes, 16 or 32 tokens each (q4_few.hip); tile by tile, the weights' operand made on the way (q4_tile.hip,
-// 16-bit types); or as an operand of the weights and the tiled product (nt_product.h), which gradients take always.
+// How Y = X W^T is computed: for one token or two on the vector units (q4_token.hip); by passes over the codes on the matrix cores, 16 or 32 tokens each
+// (q4_few.hip); tile by tile, the weights' operand made on the way (q4_tile.hip, 16-bit types); or as an operand of the weights and the tiled product
+// (nt_product.h), which gradients take always.
 //
-// The choice is by an estimate of each, in us. 256 workgroups of the passes (32 rows of weights each) are a round, whose time grows with k. A tile's walk takes
+// One token through rows of 512 positions and more is faster on the vector units everywhere, two tokens but for wide layers in bf16 (two, passes and vector units, us:
+// 2048 x 2048 4.1, 3.4; 4096 x 11008 bf16 10.0, 12.1, 32 bits 16.7, 12.0; 16384 x 8192 bf16 20.8, 22.7, fp16 23.5, 20.7; one through 512 x 256 2.5, 2.9). From there on
+// the choice is by an estimate of each, in us. 256 workgroups of the passes (32 rows of weights each) are a round, whose time grows with k. A tile's walk takes
 // half a microsecond a slab of 64 positions (twice that the large ones) until the chip has more than one workgroup for a compute unit. The product takes a walk
 // along k, the operand's bytes, dearer once no cache holds them, and its own operations. Fitted to 32 to 2048 tokens through fourteen layers from 20000 x 64 and
 // 1000 x 333 to 16384 x 8192, where the choices take 0.7 % more than the best ones do on average, 30 % at most (2048 x 16384, 32 tokens: the passes 46 us, the
@@ -76,9 +79,10 @@ Operands operands(int64_t t, int64_t n, int64_t k, int group, int type, bool gra
 //
 // With more tokens the answer turns to the product once and stays, so that a workspace serves fewer tokens too: every estimate rises with the tokens at least as
 // the product's does. (The passes are held against the product of their round's first tokens; `more` is added to the tiles' flat part.)
-enum class Way { passes, tiles, large_tiles, product };
+enum class Way { token, passes, tiles, large_tiles, product };
 Way way_of(int64_t t, int64_t n, int64_t k, int type, bool gradient) {
     if (gradient) return Way::product;
+    if (k >= 512 && (t == 1 || (t == 2 && (type != OZIMMU_BF16 || n < 4096)))) return Way::token;
     const double nk = (double)n * (double)k;
     const int64_t tokens = type == OZIMMU_F32 ? 16 : 32, passes = (t + tokens - 1) / tokens, rows = (n + 31) / 32;
     const bool can_pass = passes <= 65535;   // (the launch's second dimension)
@@ -119,8 +123,9 @@ ozimmu_status_t q4_product(bool gradient, int64_t t, int64_t n, int64_t k, int g
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (inner == 0) return hip_status(launch_zero_rows(t, outer, R, type, ldr, st));
     const Way way = way_of(t, n, k, type, gradient);
+    if (way == Way::token) return hip_status(launch_q4_token(t, n, k, group, V, type, ldv, codes, ldq, scales, lds, R, ldr, st));
     if (way == Way::passes) return hip_status(launch_q4_few(t, n, k, group, V, type, ldv, codes, ldq, scales, lds, R, ldr, st));
-    if (way != Way::product)
+    if (way == Way::tiles || way == Way::large_tiles)
         return hip_status(launch_q4_tiles(way == Way::large_tiles, t, n, k, group, V, type, ldv, codes, ldq, scales, lds, R, ldr, st));
     const Operands o = operands(t, n, k, group, type, gradient);
     if (!ws || misaligned(ws, OZIMMU_WORKSPACE_ALIGN) || ws_bytes < o.total) return OZIMMU_ERR_WORKSPACE;

@@ -65,6 +65,9 @@ hipError_t launch_operands(int64_t t, int64_t n, int64_t k, int group, int type,
                            unsigned short* w_out, int* w_exps, const void* V, int64_t ldv, unsigned short* v_out, int* v_exps, int64_t ld, hipStream_t st);
 // Zeros into a typed matrix.
 hipError_t launch_zero_rows(int64_t rows, int64_t cols, void* R, int type, int64_t ld, hipStream_t st);
+// q4_token.hip: Y = X W^T for one token or two
+hipError_t launch_q4_token(int64_t t, int64_t n, int64_t k, int group, const void* X, int type, int64_t ldx, const uint8_t* codes, int64_t ldq,
+                           const void* scales, int64_t lds, void* Y, int64_t ldy, hipStream_t st);
 // q4_few.hip: Y = X W^T for few tokens, one pass over the codes
 hipError_t launch_q4_few(int64_t t, int64_t n, int64_t k, int group, const void* X, int type, int64_t ldx, const uint8_t* codes,
                          int64_t ldq, const void* scales, int64_t lds, void* Y, int64_t ldy, hipStream_t st);

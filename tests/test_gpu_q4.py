@@ -163,6 +163,9 @@ GEMMS = [(1, 1, 1, 32), (1, 16, 128, 128), (1, 2048, 512, 64), (1, 9000, 200, 12
          (400, 2500, 2570, 32), (200, 6000, 1100, 64), (33, 17000, 260, 128), (16, 16500, 1000, 64), (400, 1700, 260, 64),
          # tiles of 64 and of 128 that end in every way, with k from eight on; many tokens of few and of many positions
          (300, 2000, 8, 32), (290, 2001, 9, 32), (310, 1987, 15, 64), (257, 2050, 63, 128), (1000, 1030, 129, 64), (64, 8200, 200, 32), (2000, 2100, 513, 64),
+         # one token and two, the row's end in every part of a piece
+         (1, 5, 513, 32), (1, 9, 4097, 128), (1, 2051, 1111, 32), (1, 8200, 600, 64), (1, 8193, 9000, 128), (1, 300, 20001, 64), (2, 6, 541, 32), (2, 1100, 5000, 64),
+         (2, 2500, 1537, 128), (2, 9000, 1026, 32), (2, 4, 33000, 128),
          (2000, 4130, 66, 32), (2500, 4097, 60, 128), (3000, 2100, 7, 32), (2000, 2100, 2570, 32), (2048, 2048, 2560, 128)]
 
 
@@ -256,6 +259,22 @@ def test_a_row_that_is_not_finite_stays_alone(t, n, dt):
         f(bad, codes, scales, group, out, ws)
         rest = [i for i in range(t) if i not in (1, 3)]
         assert torch.equal(out[rest], clean[rest]) and out[1].isnan().all() and not out[3].isfinite().any()
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("n,k", [(30, 700), (2100, 600), (8200, 1025)])
+def test_one_of_two_tokens_is_not_finite(n, k, dt):
+    c, s = plain_cut(random_weights(n, k, 9), 32, dt)
+    codes, scales = pack(c).to(DEV), s.to(DEV)
+    V = tokens(2, k, dt, 4).to(DEV)
+    clean, out = (torch.empty(2, n, dtype=dt, device=DEV) for _ in range(2))
+    oz.q4_gemm(V, codes, scales, 32, clean)
+    for at, value in ((0, "nan"), (k - 1, "nan"), (17, "inf")):
+        bad = V.clone()
+        bad[1, at] = float(value)
+        oz.q4_gemm(bad, codes, scales, 32, out)
+        # (an infinity times a code of zero is NaN, which the formula gives too)
+        assert torch.equal(out[0], clean[0]) and (out[1].isnan().all() if value == "nan" else not out[1].isfinite().any())
 
 
 @pytest.mark.parametrize("dt", [F32, BF16])
