@@ -1,14 +1,14 @@
 // Y = X W^T for few tokens and weights in four bits: one pass over the codes, no workspace (gfx950).
 //
-// What bounds it is reading the codes; the sums go to the matrix cores (v_mfma_f32_16x16x32) although most of their rows stay empty with
-// one token, because the vector units have their hands full making 16-bit operands of the codes. A wavefront takes 16 NT rows of
-// W, 16 TT tokens and every eighth step of k (every second, with TW = 4 wavefronts along the tokens); the wavefronts of a workgroup share the rows and
-// add their parts up in LDS.
+// What bounds it is reading the codes, and the tokens again for every 16 NT rows of them; the sums go to the matrix cores (v_mfma_f32_16x16x32) although most of
+// their rows stay empty with few tokens, because the vector units have their hands full making 16-bit operands of the codes. A wavefront takes 16 NT rows of
+// W, 16 TT tokens and every W-th step of k; the W wavefronts of a workgroup share the rows and add their parts up in LDS.
 //
-// A step is 128 positions. A lane loads 16 bytes, 32 positions, of row lane % 16 of each 16 x 128 block of codes. An MFMA adds up positions of one
-// group only: in groups of 64 and 32 the quarters of a wavefront (lane / 16) first exchange words (v_permlane32_swap, v_permlane16_swap), so that
-// word j of every lane belongs to one group, and is MFMA j's operand. (Loads of 8 and 4 bytes instead: 78 us where these take 31.) The tokens' operand
-// is loaded from the same positions.
+// A step is 128 positions. Memory is read along the rows, 16 lanes to 256 bytes of a token's row, four lanes to 64 of a row's codes, and goes through LDS (a region for
+// every wavefront, no barrier) into the operands' order; loads in that order, neighbouring lanes in different rows, look up a line for every lane (16 tokens, bf16, 16384 x
+// 8192 26.8 us where these take 19.9; 32 tokens 51.8 and 32.6; rows of tokens at odd places, 387 x 10575, 58 and 12). A lane's operand of the codes is 16 bytes,
+// 32 positions, of row lane % 16. An MFMA adds up positions of one group only: in groups of 64 and 32 the quarters of a wavefront (lane / 16) first exchange words
+// (v_permlane32_swap, v_permlane16_swap), so that word j of every lane belongs to one group, and is MFMA j's operand. The tokens' operand is read from the same positions.
 //
 // Codes to 16-bit values: the four bits of c + 8 go into the mantissa of 16.0 (one shift, one and-or for two codes), which
 // gives 16 + (c + 8) exactly. The 24 too much is taken out by the matrix cores: the sums start from the tokens' product with a
@@ -20,8 +20,6 @@
 
 namespace ozimmu {
 namespace {
-
-constexpr int kWaves = 8;
 
 // The operand of eight tokens' values is paired (0, 4), (1, 5), (2, 6), (3, 7) to match the codes' pairs.
 __device__ __forceinline__ v4u pair_by_four(const v4u& x) {
@@ -111,8 +109,8 @@ __device__ __forceinline__ Operand<TYPE> operand(const Raw<TYPE>& r) {
     return t;
 }
 
-template <int TYPE, int GROUP, int NT, int TT, int TW>
-__launch_bounds__(kWaves * 64)
+template <int TYPE, int GROUP, int NT, int TT, int W>
+__launch_bounds__(W * 64)
 __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_t ldx, const uint8_t* codes, int64_t ldq, const void* scales,
                               int64_t lds, void* Y, int64_t ldy) {
     typedef Elem<TYPE> E;
@@ -120,32 +118,37 @@ __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_
     constexpr bool BF16 = TYPE != OZIMMU_F16;
     constexpr int GW = GROUP / 32, GROUPS = 128 / GROUP;   // words of a lane per group, groups of a step
     constexpr int DEPTH = 2;                 // steps whose codes are on their way at a time
-    extern __shared__ float part[];                        // [wave][token][row]
     constexpr int kRow = 16 * NT + 1;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds_bytes[];
+    float* const part = reinterpret_cast<float*>(lds_bytes);   // [wave][token][row], when the walk is over
+    constexpr int kTokenRow = 128 * sizeof(raw), kCodes = NT * 1024;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t n0 = (int64_t)blockIdx.x * (16 * NT);
-    constexpr int KW = kWaves / TW;                        // TW wavefronts along the tokens, KW share the steps
-    const int part_k = wave % KW, part_t = wave / KW;
-    const int t0 = (blockIdx.y * TW + part_t) * (16 * TT);
+    const int t0 = blockIdx.y * (16 * TT);
     // Whole steps are dealt to the wavefronts in turn (together they read lines in full); the last wavefront takes what is left of the row beyond them too.
     const int full = (int)(k / 128);
-    const int mine = t0 < t ? (full - part_k + KW - 1) / KW : 0;
+    const int mine = (full - wave + W - 1) / W;
     const int quarter = lane >> 4;
     // position of word j of group h in a step, for this lane (the exchange between quarters below)
     const int at_quarter = GROUP == 128 ? 32 * quarter : GROUP == 64 ? 32 * (quarter & 1) + 16 * (quarter >> 1) : 8 * quarter;
-    // Addresses are a scalar base and a lane's 32-bit offset (rows are at most OZIMMU_MAX_LD apart). Lanes of tokens and rows that are not there repeat the last one: their
-    // results go nowhere.
+    // In LDS 16-byte piece p of row r lies at place p ^ r % 16 (codes: p ^ r / 4 % 4), so that the 16 rows of a fragment meet different banks.
+    // Addresses are a scalar base and a lane's 32-bit offset (rows are at most OZIMMU_MAX_LD apart). Rows of weights that are not there repeat the last one: their
+    // results go nowhere. Tokens that are not there are not loaded: neither do theirs.
     const raw* xb = reinterpret_cast<const raw*>(X) + (int64_t)min(t0, t - 1) * ldx;
     const uint8_t* qb = codes + n0 * ldq;
     const raw* sb = reinterpret_cast<const raw*>(scales) + n0 * lds;
-    unsigned xo[TT], qo[NT], so[NT];   // bytes
+    constexpr int kLanes = kTokenRow / 16, kRows = 64 / kLanes, kLoads = 16 * TT / kRows;   // of a token's row, rows of a load, loads of a step
+    constexpr int kPer = 16 / sizeof(raw);
+    const int tokens_here = min(16 * TT, t - t0);
+    unsigned char* const x_lds = lds_bytes + wave * (16 * TT * kTokenRow + kCodes);
+    unsigned char* const q_lds = x_lds + 16 * TT * kTokenRow;
+    unsigned xo[kLoads], qo[NT], so[NT];   // bytes
 #pragma unroll
-    for (int i = 0; i < TT; ++i) xo[i] = ((unsigned)max(min(16 * i + (lane & 15), t - 1 - t0), 0) * (unsigned)ldx + at_quarter) * sizeof(raw);
+    for (int i = 0; i < kLoads; ++i) xo[i] = ((unsigned)max(min(kRows * i + lane / kLanes, t - 1 - t0), 0) * (unsigned)ldx + lane % kLanes * kPer) * sizeof(raw);
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-        const unsigned row = (unsigned)min((int64_t)(16 * i + (lane & 15)), n - 1 - n0);
-        qo[i] = row * (unsigned)ldq + quarter * 16;
-        so[i] = row * (unsigned)lds * sizeof(raw);
+        qo[i] = (unsigned)min((int64_t)(16 * i + lane / 4), n - 1 - n0) * (unsigned)ldq + lane % 4 * 16;
+        so[i] = (unsigned)min((int64_t)(16 * i + (lane & 15)), n - 1 - n0) * (unsigned)lds * sizeof(raw);
     }
     auto from = [](const void* base, int64_t at, unsigned offset) { return reinterpret_cast<const uint8_t*>(base) + at + offset; };
 
@@ -165,13 +168,10 @@ __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_
                 sc[i][0] = *reinterpret_cast<const raw*>(at);
         }
     };
-    constexpr int kParts = TYPE == OZIMMU_F32 ? 2 : 1;
-    auto load_word = [&](int step, int j, Raw<TYPE> (&to)[TT]) {
-        const int64_t at = ((int64_t)step * 128 + (j / GW) * GROUP + 8 * (j % GW)) * sizeof(raw);
+    auto load_tokens = [&](int step, v4u (&to)[kLoads]) {
 #pragma unroll
-        for (int i = 0; i < TT; ++i)
-#pragma unroll
-            for (int v = 0; v < kParts; ++v) to[i].v[v] = *reinterpret_cast<const v4u_any*>(from(xb, at + 16 * v, xo[i]));
+        for (int i = 0; i < kLoads; ++i)
+            if (kRows * i < tokens_here) to[i] = *reinterpret_cast<const v4u_any*>(from(xb, (int64_t)step * kTokenRow, xo[i]));
     };
     // The same where a row ends inside the step: tokens beyond k are zeros, so any finite code will do there (rows take a multiple of 16 bytes).
     auto load_last_codes = [&](v4u (&w)[NT], raw (&sc)[NT][GROUPS]) {
@@ -179,24 +179,23 @@ __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_
         const int groups = (int)((k + GROUP - 1) / GROUP);
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
-            w[i] = *reinterpret_cast<const v4u*>(from(qb, min((int64_t)full * 64 + quarter * 16, last) - quarter * 16, qo[i]));
+            w[i] = *reinterpret_cast<const v4u*>(from(qb, min((int64_t)full * 64 + lane % 4 * 16, last) - lane % 4 * 16, qo[i]));
 #pragma unroll
             for (int h = 0; h < GROUPS; ++h) sc[i][h] = *reinterpret_cast<const raw*>(from(sb, (int64_t)min(full * GROUPS + h, groups - 1) * sizeof(raw), so[i]));
         }
     };
-    auto load_last_word = [&](int j, Raw<TYPE> (&to)[TT]) {
-        const int64_t at = (int64_t)full * 128 + (j / GW) * GROUP + 8 * (j % GW);
+    auto load_last_tokens = [&](v4u (&to)[kLoads]) {
+        const int64_t at = (int64_t)full * 128 + lane % kLanes * kPer;
 #pragma unroll
-        for (int i = 0; i < TT; ++i) {
-            raw r[8];
+        for (int i = 0; i < kLoads; ++i) {
+            raw r[kPer];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int64_t beyond = max(at + at_quarter + e - (k - 1), (int64_t)0);
-                const raw y = *reinterpret_cast<const raw*>(from(xb, (at + e - beyond) * (int64_t)sizeof(raw), xo[i]));
+            for (int e = 0; e < kPer; ++e) {
+                const int64_t beyond = max(at + e - (k - 1), (int64_t)0);
+                const raw y = *reinterpret_cast<const raw*>(from(xb, ((int64_t)full * 128 + e - beyond) * (int64_t)sizeof(raw), xo[i]));
                 r[e] = beyond ? raw(0) : y;
             }
-#pragma unroll
-            for (int v = 0; v < kParts; ++v) to[i].v[v] = *reinterpret_cast<const v4u*>(r + 4 * v);
+            to[i] = *reinterpret_cast<const v4u*>(r);
         }
     };
 
@@ -209,7 +208,23 @@ __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_
     const v4u minus24 = {minus, minus, minus, minus};
     const CodeBits bits = CodeBits::of<BF16>();
 
-    auto multiply = [&](const v4u (&w)[NT], const raw (&sc)[NT][GROUPS], const Raw<TYPE> (&xs)[4][TT]) {
+    auto in_order = [] {   // of the wavefront's own accesses to LDS
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    };
+    auto multiply = [&](const v4u (&w_read)[NT], const raw (&sc)[NT][GROUPS], const v4u (&x_read)[kLoads]) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int row = kRows * i + lane / kLanes;
+            *reinterpret_cast<v4u*>(x_lds + row * kTokenRow + (lane % kLanes ^ (row & 15)) * 16) = x_read[i];
+        }
+#pragma unroll
+        for (int i = 0; i < NT; ++i) *reinterpret_cast<v4u*>(q_lds + i * 1024 + lane / 4 * 64 + (lane % 4 ^ (lane / 16)) * 16) = w_read[i];
+        in_order();
+        v4u w[NT];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) w[i] = *reinterpret_cast<const v4u*>(q_lds + i * 1024 + (lane & 15) * 64 + (quarter ^ ((lane & 15) / 4)) * 16);
         // words by group: the quarters of a group of 64 or 32 hold positions of two or four groups each and exchange them
         unsigned words[NT][4];
 #pragma unroll
@@ -235,7 +250,14 @@ __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_
             for (int j = 0; j < GW; ++j) {
                 Operand<TYPE> o[TT];
 #pragma unroll
-                for (int tt = 0; tt < TT; ++tt) o[tt] = operand<TYPE>(xs[GW * h + j][tt]);
+                for (int tt = 0; tt < TT; ++tt) {
+                    Raw<TYPE> x;
+                    const int piece = (at_quarter + GROUP * h + 8 * j) / kPer;
+#pragma unroll
+                    for (int v = 0; v < 8 / kPer; ++v)
+                        x.v[v] = *reinterpret_cast<const v4u*>(x_lds + (16 * tt + (lane & 15)) * kTokenRow + ((piece + v) ^ (lane & 15)) * 16);
+                    o[tt] = operand<TYPE>(x);
+                }
                 const v4f zero = v4f{0.f, 0.f, 0.f, 0.f};
                 if constexpr (TYPE != OZIMMU_F32)
 #pragma unroll
@@ -270,34 +292,32 @@ __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_
     if (mine > 0) {
         v4u w[DEPTH][NT];
         raw sc[DEPTH][NT][GROUPS] __attribute__((aligned(16)));
+        v4u xs[2][kLoads] = {};   // this step's tokens and the next one's
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d)
-            if (d < mine) load_codes(d * KW + part_k, w[d], sc[d]);
-        Raw<TYPE> xs[2][4][TT];   // this step's tokens and the next one's
-#pragma unroll
-        for (int j = 0; j < 4; ++j) load_word(part_k, j, xs[0][j]);
+            if (d < mine) load_codes(d * W + wave, w[d], sc[d]);
+        load_tokens(wave, xs[0]);
         for (int step0 = 0; step0 < mine; step0 += DEPTH) {
 #pragma unroll
             for (int d = 0; d < DEPTH; ++d) {
                 const int step = step0 + d;
                 if (step >= mine) break;
-                if (step + 1 < mine)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) load_word((step + 1) * KW + part_k, j, xs[(d + 1) & 1][j]);
+                if (step + 1 < mine) load_tokens((step + 1) * W + wave, xs[(d + 1) & 1]);
                 multiply(w[d], sc[d], xs[d & 1]);
-                if (step + DEPTH < mine) load_codes((step + DEPTH) * KW + part_k, w[d], sc[d]);
+                in_order();
+                if (step + DEPTH < mine) load_codes((step + DEPTH) * W + wave, w[d], sc[d]);
             }
         }
     }
-    if (part_k == KW - 1 && t0 < t && k > (int64_t)full * 128) {
+    if (wave == W - 1 && k > (int64_t)full * 128) {
         v4u w[NT];
         raw sc[NT][GROUPS];
-        Raw<TYPE> xs[4][TT];
+        v4u xs[kLoads];
         load_last_codes(w, sc);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) load_last_word(j, xs[j]);
+        load_last_tokens(xs);
         multiply(w, sc, xs);
     }
+    __syncthreads();   // the parts take the place of the tokens and codes
 
     // lane: tokens 4 quarter .. + 3 of a tile, rows lane % 16
 #pragma unroll
@@ -306,45 +326,47 @@ __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_
         for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                part[((part_k * TW + part_t) * 16 * TT + 16 * tt + 4 * quarter + e) * kRow + 16 * i + (lane & 15)] = total[i][tt][e];
+                part[(wave * 16 * TT + 16 * tt + 4 * quarter + e) * kRow + 16 * i + (lane & 15)] = total[i][tt][e];
     __syncthreads();
-    const int first = blockIdx.y * (16 * TT * TW), here = min(16 * TT * TW, t - first);
-    for (int at = threadIdx.x; at < here * 16 * NT; at += kWaves * 64) {
+    const int here = min(16 * TT, t - t0);
+    for (int at = threadIdx.x; at < here * 16 * NT; at += W * 64) {
         const int tok = at / (16 * NT), col = at % (16 * NT);
         if (n0 + col >= n) continue;
         float sum = part[tok * kRow + col];
 #pragma unroll
-        for (int i = 1; i < KW; ++i) sum += part[(i * 16 * TT * TW + tok) * kRow + col];
-        reinterpret_cast<raw*>(Y)[(int64_t)(first + tok) * ldy + n0 + col] = E::store(TYPE == OZIMMU_F32 ? 16.f * sum : sum);   // (the codes' sixteenths)
+        for (int i = 1; i < W; ++i) sum += part[(i * 16 * TT + tok) * kRow + col];
+        reinterpret_cast<raw*>(Y)[(int64_t)(t0 + tok) * ldy + n0 + col] = E::store(TYPE == OZIMMU_F32 ? 16.f * sum : sum);   // (the codes' sixteenths)
     }
 }
 
-template <int TYPE, int GROUP, int NT, int TT, int TW>
+template <int TYPE, int GROUP, int NT, int TT, int W>
 hipError_t launch_tiles(int64_t t, int64_t n, int64_t k, const void* X, int64_t ldx, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds,
                         void* Y, int64_t ldy, hipStream_t st) {
-    constexpr auto kernel = q4_few_kernel<TYPE, GROUP, NT, TT, TW>;
-    constexpr int bytes = kWaves * 16 * TT * (16 * NT + 1) * sizeof(float);
+    constexpr auto kernel = q4_few_kernel<TYPE, GROUP, NT, TT, W>;
+    constexpr int kPart = 16 * TT * (16 * NT + 1) * sizeof(float), kWalk = 16 * TT * 128 * sizeof(typename Elem<TYPE>::raw) + NT * 1024;
+    constexpr int bytes = W * (kPart > kWalk ? kPart : kWalk);
     if (hipError_t e = allow_dynamic_lds<kernel>(bytes); e != hipSuccess) return e;
-    const dim3 grid((unsigned)((n + 16 * NT - 1) / (16 * NT)), (unsigned)((t + 16 * TT * TW - 1) / (16 * TT * TW)));
-    kernel<<<grid, kWaves * 64, bytes, st>>>((int)t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy);
+    const dim3 grid((unsigned)((n + 16 * NT - 1) / (16 * NT)), (unsigned)((t + 16 * TT - 1) / (16 * TT)));
+    kernel<<<grid, W * 64, bytes, st>>>((int)t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy);
     return hipGetLastError();
 }
 template <int TYPE, int GROUP>
 hipError_t launch_typed(int64_t t, int64_t n, int64_t k, const void* X, int64_t ldx, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds,
                         void* Y, int64_t ldy, hipStream_t st) {
-    // More rows of W to a wavefront: fewer loads of tokens; more wavefronts: more codes on their way. (t = 16, n = 16384, k = 8192 with 16, 32, 64 rows: 46.9, 32.7, 25.8 us;
-    // t = 1: 27.7, 22.5, 20.9; but n = 8192, k = 4096, t = 1: 8.7, 8.0, 12.0.) Two tiles of tokens share the operands made of the codes; with
-    // 32-bit tokens the registers do not suffice; those have four wavefronts along the tokens instead of all along k, where that leaves enough workgroups: a part of k is
-    // longer and fewer sums meet in LDS (300 tokens, n = 1500, k = 1000: 17.9 -> 15.1 us). (So many 16-bit tokens do not come here.)
-    const int64_t rows32 = (n + 31) / 32;
+    // The smallest tile with which a workgroup has a compute unit to itself: more rows of W or tokens to a wavefront share operands and loads, fewer keep more compute units busy. (bf16, us,
+    // rows x tokens 16 x 16, 32 x 16, 64 x 16, 32 x 32: 16 tokens, 4096 x 11008 13.0, 15.2, 19.0, 18.4; 16384 x 8192 27.8, 26.0, 19.9, 29.8; 64 tokens, 2048 x 16384 24.9, 22.4,
+    // 29.7, 27.0; 8192 x 4096 26.9, 28.5, 20.8, 19.0.) Two tiles of tokens take registers that 32-bit tokens do not leave. The smallest has sixteen wavefronts along a long k (2048 x
+    // 16384, 16 tokens: 14.0 against 17.6).
+    const auto fits = [&](int64_t rows, int64_t tokens) { return ((n + rows - 1) / rows) * ((t + tokens - 1) / tokens) <= kComputeUnits; };
     if constexpr (TYPE != OZIMMU_F32) {
-        if (t > 16) return launch_tiles<TYPE, GROUP, 2, 2, 1>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
-        if (n >= 64 * 256) return launch_tiles<TYPE, GROUP, 4, 1, 1>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
-    } else {
-        if (t > 32 && rows32 * ((t + 63) / 64) >= 192) return launch_tiles<TYPE, GROUP, 2, 1, 4>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
+        if (fits(16, 16) && k >= 16 * 128) return launch_tiles<TYPE, GROUP, 1, 1, 16>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
     }
-    if (rows32 * ((t + 15) / 16) >= 256) return launch_tiles<TYPE, GROUP, 2, 1, 1>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
-    return launch_tiles<TYPE, GROUP, 1, 1, 1>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
+    if (fits(16, 16)) return launch_tiles<TYPE, GROUP, 1, 1, 8>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
+    if (fits(32, 16)) return launch_tiles<TYPE, GROUP, 2, 1, 8>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
+    if constexpr (TYPE != OZIMMU_F32) {
+        if (t > 16) return launch_tiles<TYPE, GROUP, 2, 2, 8>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
+    }
+    return launch_tiles<TYPE, GROUP, 4, 1, 8>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
 }
 template <int TYPE>
 hipError_t launch_grouped(int64_t t, int64_t n, int64_t k, int group, const void* X, int64_t ldx, const uint8_t* codes, int64_t ldq, const void* scales,

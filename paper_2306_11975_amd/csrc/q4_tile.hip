@@ -7,9 +7,9 @@
 //
 // Against the passes of q4_few.hip (32 tokens each): the codes are converted once for BM tokens and take one MFMA, not two. Against a pass that writes the
 // operand and a product that reads it: four times fewer bytes of the weights come and none go; every tile of tokens converts the codes again. So it serves the
-// counts between the two through layers that no cache holds (bf16, passes or operand and product -> this): 128 tokens through 8192 x 4096 48.0 -> 34.4 us, 256
-// 48.5 -> 44.6; through 16384 x 8192 64 tokens 96 -> 72, 128 160 -> 90, 256 216 -> 127 (128 x 128), 512 236 -> 189. What bounds it is a workgroup's walk: 0.5 us a
-// slab of 64 x 64 (0.95 of 128 x 128), of which the conversion, in the same wavefronts as the MFMAs, takes more than half.
+// counts between the two. us in bf16, of the passes, here, of operand and product: 300 tokens through 8192 x 4096 82, 57, 63; 128 through 16384 x 8192 122, 86, 160, 256
+// (128 x 128 tiles from here) 247, 128, 217, 512 453, 185, 237; 128 through 5000 x 200 10.8, 5.9, 8.5; 512 through 20000 x 64 110, 11.7, 15.7. What bounds it is a
+// workgroup's walk: 0.5 us a slab of 64 x 64 (0.95 of 128 x 128), of which the conversion, in the same wavefronts as the MFMAs, takes more than half.
 // (dX = dY W, whose codes lie across the inner dimension, gains nothing so: 128 x 8192 x 4096 83 us against 38.)
 #include "half_common.h"
 

@@ -69,13 +69,13 @@ Operands operands(int64_t t, int64_t n, int64_t k, int group, int type, bool gra
 // (nt_product.h), which gradients take always.
 //
 // One token through rows of 512 positions and more is faster on the vector units everywhere, two tokens but for wide layers in bf16 (two, passes and vector units, us:
-// 2048 x 2048 4.1, 3.4; 4096 x 11008 bf16 10.0, 12.1, 32 bits 16.7, 12.0; 16384 x 8192 bf16 20.8, 22.7, fp16 23.5, 20.7; one through 512 x 256 2.5, 2.9). From there on
-// the choice is by an estimate of each, in us. 256 workgroups of the passes (32 rows of weights each) are a round, whose time grows with k. A tile's walk takes
-// half a microsecond a slab of 64 positions (twice that the large ones) until the chip has more than one workgroup for a compute unit. The product takes a walk
-// along k, the operand's bytes, dearer once no cache holds them, and its own operations. Fitted to 32 to 2048 tokens through fourteen layers from 20000 x 64 and
-// 1000 x 333 to 16384 x 8192, where the choices take 0.7 % more than the best ones do on average, 30 % at most (2048 x 16384, 32 tokens: the passes 46 us, the
-// product 36). Times of passes, tiles, large tiles, product, bf16: 1000 x 1000, 1024 tokens 14.8, 12.0, 19.8, 14.1; 8192 x 4096, 64 28, 34, 61, 38, 128 48, 34, 62,
-// 40, 512 -, 76, 66, 66; 16384 x 8192, 128 160, 90, 121, 180, 512 -, 283, 189, 236.
+// 2048 x 2048 4.5, 3.4; 4096 x 11008 bf16 8.7, 12.1, 32 bits 18.5, 12.0; 16384 x 8192 bf16 18.3, 22.7; one through 512 x 256 2.5, 2.9). From there on the choice is by
+// an estimate of each, in us. 256 workgroups of the passes (32 rows of weights and 32 tokens; 64 and 16 in 32 bits) are a round, whose time grows with k. A tile's walk
+// takes half a microsecond a slab of 64 positions (twice that the large ones) until the chip has more than one workgroup for a compute unit. The product takes a walk
+// along k, the operand's bytes, dearer once no cache holds them, and its own operations. Fitted to 24 to 2048 tokens through fifteen layers from 20000 x 64 and
+// 1000 x 333 to 16384 x 8192, where the choices take 0.6 % more than the best ones do on average, 24 % at most. Times of passes, tiles, large tiles, product:
+// bf16 2048 x 2048, 64 tokens 6.7, 18.5, 33.0, 17.0, 512 23.5, 19.4, 33.5, 20.0; 8192 x 4096, 64 19.4, 34.0, 61.9, 38.7, 256 67.5, 44.5, 62.5, 47.4, 1024 250, 137, 94,
+// 78; 16384 x 8192, 128 122, 86, 121, 160, 512 453, 278, 185, 237; 32 bits 16384 x 8192, 128 234, -, -, 316; 8192 x 4096, 384 194, -, -, 111.
 //
 // With more tokens the answer turns to the product once and stays, so that a workspace serves fewer tokens too: every estimate rises with the tokens at least as
 // the product's does. (The passes are held against the product of their round's first tokens; `more` is added to the tiles' flat part.)
@@ -83,26 +83,23 @@ enum class Way { token, passes, tiles, large_tiles, product };
 Way way_of(int64_t t, int64_t n, int64_t k, int type, bool gradient) {
     if (gradient) return Way::product;
     if (k >= 512 && (t == 1 || (t == 2 && (type != OZIMMU_BF16 || n < 4096)))) return Way::token;
-    const double nk = (double)n * (double)k;
-    const int64_t tokens = type == OZIMMU_F32 ? 16 : 32, passes = (t + tokens - 1) / tokens, rows = (n + 31) / 32;
-    const bool can_pass = passes <= 65535;   // (the launch's second dimension)
-    if (type == OZIMMU_F32) {
-        const double rounds = std::max(1.0, (double)rows * (double)passes / 256.0);
-        return can_pass && 2.8 + rounds * k * (3.1 / 1024.0) <= 8.0 + 0.0055 * k + 9.0e-7 * nk + 7.3e-8 * (double)passes * nk ? Way::passes : Way::product;
-    }
     if (t <= 16) return Way::passes;
-    const double rounds = std::ceil((double)rows * (double)passes / 256.0), first = (rounds - 1.0) * 256.0 / (double)rows;
-    const double product = 16.5 + 0.0025 * k + 5.9e-7 * nk + 4.6e-7 * std::max(0.0, nk - 4.0e7), more = 4.5e-8 * nk;
-    const double few = 1.9 + rounds * (1.2 + 0.0036 * k);
-    const bool few_lose = !can_pass || few > product + more * first;
-    if (k < 8) return few_lose ? Way::product : Way::passes;
+    const bool wide = type == OZIMMU_F32;
+    const double nk = (double)n * (double)k, beyond = std::max(0.0, nk - 4.0e7);
+    const int64_t passes = wide ? (t + 15) / 16 : (t + 31) / 32, rows = wide ? (n + 63) / 64 : (n + 31) / 32;
+    const double rounds = std::ceil((double)rows * (double)passes / 256.0), first = (rounds - 1.0) * 256.0 / (double)rows;   // tokens (passes) ahead of this round
+    const double product = wide ? 10.7 + 0.0051 * k + 8.75e-7 * nk + 5.3e-7 * beyond : 18.9 + 0.0013 * k + 5.7e-7 * nk + 3.9e-7 * beyond;
+    const double more = (wide ? 1.0e-7 : 5.0e-8) * nk;   // of a pass
+    const double few = passes > 65535 ? 1.0e300 : wide ? 0.24 + rounds * (2.25 + 0.0039 * k) : 5.0 + rounds * (0.27 + 0.00184 * k);   // (the launch's second dimension)
+    const bool few_lose = few > product + more * first;
+    if (wide || k < 8) return few_lose ? Way::product : Way::passes;
     const double slabs = (double)((k + 63) / 64), grown = more * (double)passes;
     const double fill = (double)((n + 63) / 64) * (double)passes / 512.0, fill_large = (double)((n + 127) / 128) * (double)passes / 1024.0;   // workgroups by compute unit
-    const double held = 3.2 + 0.54 * fill, held_large = 3.8 + 2.2 * fill_large, slope = (0.27 + 0.22 * fill) * slabs, slope_large = (0.16 + 0.64 * fill_large) * slabs;
+    const double held = 3.2 + 0.54 * fill, held_large = 3.8 + 2.2 * fill_large, slope = (0.23 + 0.225 * fill) * slabs, slope_large = (0.2 + 0.62 * fill_large) * slabs;
     const double surely = std::min(held + std::max(0.51 * slabs + grown, slope), held_large + std::max(slabs + grown, slope_large));
     if (few_lose && surely > product + grown) return Way::product;
     const double tiles = held + std::max(0.51 * slabs, slope), large = held_large + std::max(slabs, slope_large);
-    if (can_pass && few <= std::min(tiles, large)) return Way::passes;
+    if (few <= std::min(tiles, large)) return Way::passes;
     return large < tiles ? Way::large_tiles : Way::tiles;
 }
 
