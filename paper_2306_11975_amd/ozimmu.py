@@ -406,16 +406,16 @@ def auto_num_slices_blas(transa: str, transb: str, m: int, n: int, k: int, A, ld
     return s.value, sums
 
 
-_torch = None
+_torch = _uint8 = None
 _types = {}      # torch's types as ozimmu_type_t, once torch is there
 
 
 def _load_torch():
-    global _torch
+    global _torch, _uint8
     import torch
 
     _types.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
-    _torch = torch
+    _torch, _uint8 = torch, torch.uint8
 
 
 def _type_of(dtype) -> int:
@@ -438,7 +438,7 @@ def _call(f, stream, tensors, *args) -> None:
     if _torch is None:
         _load_torch()
     index = tensors[0].get_device()
-    for t in tensors:
+    for t in tensors[1:]:
         if t is not None and t.get_device() != index:
             raise ValueError("all tensors must be on one device")
     if index < 0:
@@ -460,9 +460,10 @@ def _call(f, stream, tensors, *args) -> None:
 
 def _rows(t):
     """Rows, columns and row stride of a 2-D tensor with unit stride along its rows."""
-    if t.dim() != 2:
-        raise ValueError("expected a 2-D tensor")
-    rows, cols = t.shape
+    try:
+        rows, cols = t.shape
+    except ValueError:
+        raise ValueError("expected a 2-D tensor") from None
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError("expected a row-major tensor (unit stride along the second dimension)")
@@ -482,11 +483,13 @@ def q4_row_bytes(k: int) -> int:
 
 def _q4_weights(n: int, k: int, codes, scales, group: int):
     """Checks the codes and scales of an n x k weight matrix; (codes' row stride in bytes, scales' row stride)."""
+    if _torch is None:
+        _load_torch()
     if group not in (32, 64, 128):
         q4_geometry(k, group)       # raises
     row_bytes_, groups = (k + 31) // 32 * 16, -(-k // group)
     rows, cols, ldq = _rows(codes)
-    if rows != n or cols < row_bytes_ or codes.element_size() != 1 or codes.is_floating_point() or codes.is_signed():
+    if rows != n or cols < row_bytes_ or codes.dtype is not _uint8:
         raise ValueError(f"codes: expected {n} rows of at least {row_bytes_} bytes (uint8)")
     rows, cols, lds = _rows(scales)
     if rows != n or cols != groups:
