@@ -382,3 +382,52 @@ def test_nothing_beyond_the_workspace_is_written(t, n, k, dt):
         assert (room[need:] == 0x5A).all()
         W = weights64(c, s, 32)
         check(R, V, W if grad else W.t(), dt, n if grad else k, True)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("t,n,k,group", [(1, 40, 700, 32), (2, 2100, 600, 64), (9, 100, 333, 128), (30, 60, 2500, 32), (300, 2000, 100, 64), (1100, 1000, 500, 32), (2000, 2100, 2570, 64)])
+def test_codes_and_scales_inside_larger_arrays(t, n, k, group, dt):
+    """Rows of codes and scales further apart than they need be; what lies between them is not read for anything and not written."""
+    W0 = random_weights(n, k, 11).to(dt)
+    rb, groups = oz.q4_geometry(k, group)
+    code_room = torch.full((n, rb + 48), 0x5A, dtype=torch.uint8, device=DEV)
+    scale_room = torch.full((n, groups + 3), float("nan"), dtype=dt, device=DEV)
+    codes, scales = code_room[:, 16:16 + rb], scale_room[:, 1:1 + groups]
+    oz.q4_split(W0.to(DEV), group, codes, scales)
+    tight_codes, tight_scales = device_cut(W0.to(DEV), group, dt)
+    assert torch.equal(codes, tight_codes[:, :rb]) and torch.equal(scales, tight_scales)
+    assert (code_room[:, :16] == 0x5A).all() and (code_room[:, 16 + rb:] == 0x5A).all() and scale_room[:, 0].isnan().all() and scale_room[:, 1 + groups:].isnan().all()
+    back, tight_back = torch.empty(n, k, dtype=dt, device=DEV), torch.empty(n, k, dtype=dt, device=DEV)
+    oz.q4_expand(codes, scales, group, back)
+    oz.q4_expand(tight_codes, tight_scales, group, tight_back)
+    assert torch.equal(back, tight_back)
+    for grad in (False, True):
+        V = tokens(t, n if grad else k, dt, 3).to(DEV)
+        R = torch.empty(2, t, k if grad else n, dtype=dt, device=DEV)
+        f, ws = oz.q4_gemm_grad if grad else oz.q4_gemm, oz.alloc_q4_workspace(t, n, k, group, dt, gradient=grad)
+        f(V, codes, scales, group, R[0], ws)
+        f(V, tight_codes, tight_scales, group, R[1], ws)
+        assert R.isfinite().all() and torch.equal(R[0], R[1])
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("t,n,k", [(2, 50, 600), (16, 50, 200), (70, 300, 90), (140, 2500, 70), (130, 1100, 400)])
+def test_rows_as_far_apart_as_allowed(t, n, k, dt):
+    """Tokens and results 2^24 values apart: the last rows lie beyond 32-bit offsets."""
+    ld = 1 << 24
+    c, s = plain_cut(random_weights(n, k, 5), 32, dt)
+    codes, scales = pack(c).to(DEV), s.to(DEV)
+    for grad in (False, True):
+        rows, cols = (n, k) if grad else (k, n)
+        V0 = tokens(t, rows, dt, 7)
+        room = torch.empty((t - 1) * ld + max(rows, cols), dtype=dt, device=DEV)
+        V, tight, R = room.as_strided((t, rows), (ld, 1)), V0.to(DEV), torch.empty(t, cols, dtype=dt, device=DEV)
+        V.copy_(V0)
+        f, ws = oz.q4_gemm_grad if grad else oz.q4_gemm, oz.alloc_q4_workspace(t, n, k, 32, dt, gradient=grad)
+        f(tight, codes, scales, 32, R, ws)
+        far = torch.empty_like(R)
+        f(V, codes, scales, 32, far, ws)
+        assert torch.equal(far, R)
+        out = room.as_strided((t, cols), (ld, 1))
+        f(tight, codes, scales, 32, out, ws)
+        assert torch.equal(out, R)
