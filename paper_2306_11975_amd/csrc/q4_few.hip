@@ -362,11 +362,17 @@ hipError_t launch_typed(int64_t t, int64_t n, int64_t k, const void* X, int64_t 
         if (fits(16, 16) && k >= 16 * 128) return launch_tiles<TYPE, GROUP, 1, 1, 16>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
     }
     if (fits(16, 16)) return launch_tiles<TYPE, GROUP, 1, 1, 8>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
-    if (fits(32, 16)) return launch_tiles<TYPE, GROUP, 2, 1, 8>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
-    if constexpr (TYPE != OZIMMU_F32) {
-        if (t > 16) return launch_tiles<TYPE, GROUP, 2, 2, 8>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
+    // (32-bit types in groups of 32 hold four scales a step and row: with four tiles of rows the registers do not suffice. 16 tokens, 16384 x 8192 47.6 and 48.2, 8192 x 4096
+    // 13.6 and 25.1.)
+    if constexpr (TYPE == OZIMMU_F32 && GROUP == 32) {
+        return launch_tiles<TYPE, GROUP, 2, 1, 8>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
+    } else {
+        if (fits(32, 16)) return launch_tiles<TYPE, GROUP, 2, 1, 8>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
+        if constexpr (TYPE != OZIMMU_F32) {
+            if (t > 16) return launch_tiles<TYPE, GROUP, 2, 2, 8>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
+        }
+        return launch_tiles<TYPE, GROUP, 4, 1, 8>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
     }
-    return launch_tiles<TYPE, GROUP, 4, 1, 8>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
 }
 template <int TYPE>
 hipError_t launch_grouped(int64_t t, int64_t n, int64_t k, int group, const void* X, int64_t ldx, const uint8_t* codes, int64_t ldq, const void* scales,

@@ -167,7 +167,7 @@ GEMMS = [(1, 1, 1, 32), (1, 16, 128, 128), (1, 2048, 512, 64), (1, 9000, 200, 12
          (1, 5, 513, 32), (1, 9, 4097, 128), (1, 2051, 1111, 32), (1, 8200, 600, 64), (1, 8193, 9000, 128), (1, 300, 20001, 64), (2, 6, 541, 32), (2, 1100, 5000, 64),
          (2, 2500, 1537, 128), (2, 9000, 1026, 32), (2, 4, 33000, 128),
          # every tile of the passes, with rows of tokens at odd places and an end inside a step
-         (20, 100, 2500, 32), (5, 387, 10575, 64), (37, 300, 2049, 128), (60, 1500, 701, 128), (33, 2500, 129, 32), (100, 2500, 1001, 64), (64, 8200, 513, 128), (9, 9000, 127, 64),
+         (20, 100, 2500, 32), (5, 387, 10575, 64), (37, 300, 2049, 128), (60, 1500, 701, 128), (33, 2500, 129, 32), (100, 2500, 1001, 64), (64, 8200, 513, 128), (9, 9000, 127, 64), (20, 9000, 300, 32),
          (2000, 4130, 66, 32), (2500, 4097, 60, 128), (3000, 2100, 7, 32), (52000, 260, 7, 32), (2000, 2100, 2570, 32), (2048, 2048, 2560, 128)]
 
 
