@@ -481,11 +481,14 @@ def q4_row_bytes(k: int) -> int:
     return q4_geometry(k, 32)[0]
 
 
+_GROUPS = (32, 64, 128)
+
+
 def _q4_weights(n: int, k: int, codes, scales, group: int):
     """Checks the codes and scales of an n x k weight matrix; (codes' row stride in bytes, scales' row stride)."""
     if _torch is None:
         _load_torch()
-    if group not in (32, 64, 128):
+    if group not in _GROUPS:
         q4_geometry(k, group)       # raises
     row_bytes_, groups = (k + 31) // 32 * 16, -(-k // group)
     rows, cols, ldq = _rows(codes)
@@ -537,17 +540,44 @@ def _size(workspace) -> int:
 
 
 def _q4_product(f, gradient, V, codes, scales, group, R, workspace, stream):
+    # (The checks of _rows and _q4_weights in one place: a token's call waits for every microsecond spent here.)
+    if _torch is None:
+        _load_torch()
     dtype = V.dtype
-    if dtype != scales.dtype or dtype != R.dtype:
+    kind = _types.get(dtype)
+    if kind is None:
+        _type_of(dtype)             # raises
+    if dtype is not scales.dtype or dtype is not R.dtype:
         raise ValueError("tokens, scales and result must have one type")
-    t, inner, ldv = _rows(V)
-    rows, outer, ldr = _rows(R)
+    try:
+        t, inner = V.shape
+        rows, outer = R.shape
+        code_rows, code_bytes = codes.shape
+        scale_rows, groups = scales.shape
+    except ValueError:
+        raise ValueError("expected 2-D tensors") from None
+    ldv, step_v = V.stride()
+    ldr, step_r = R.stride()
+    ldq, step_q = codes.stride()
+    lds, step_s = scales.stride()
+    if step_v != 1 and inner > 1 or step_r != 1 and outer > 1 or step_q != 1 and code_bytes > 1 or step_s != 1 and groups > 1:
+        raise ValueError("expected row-major tensors (unit stride along the second dimension)")
     if rows != t:
         raise ValueError("tokens and result must have the same number of rows")
     n, k = (inner, outer) if gradient else (outer, inner)
-    ldq, lds = _q4_weights(n, k, codes, scales, group)
-    _call(f, stream, (V, codes, scales, R, workspace), t, n, k, group, _type_of(dtype), V.data_ptr(), ldv, codes.data_ptr(), ldq, scales.data_ptr(), lds,
-          R.data_ptr(), ldr, _ptr(workspace), _size(workspace))
+    if group not in _GROUPS:
+        q4_geometry(k, group)       # raises
+    row_bytes_ = (k + 31) // 32 * 16
+    if code_rows != n or code_bytes < row_bytes_ or codes.dtype is not _uint8:
+        raise ValueError(f"codes: expected {n} rows of at least {row_bytes_} bytes (uint8)")
+    if scale_rows != n or groups != -(-k // group):
+        raise ValueError(f"scales: expected the shape {(n, -(-k // group))}")
+    if t <= 1:
+        ldv, ldr = inner or 1, outer or 1
+    if n <= 1:
+        ldq, lds = row_bytes_, groups or 1
+    _call(f, stream, (V, codes, scales, R, workspace), t, n, k, group, kind, V.data_ptr(), ldv, codes.data_ptr(), ldq, scales.data_ptr(), lds, R.data_ptr(),
+          ldr, None if workspace is None else workspace.data_ptr(), _size(workspace))
 
 
 def q4_gemm(X, codes, scales, group: int, Y, workspace=None, stream=None) -> None:
