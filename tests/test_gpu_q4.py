@@ -431,3 +431,24 @@ def test_rows_as_far_apart_as_allowed(t, n, k, dt):
         out = room.as_strided((t, cols), (ld, 1))
         f(tight, codes, scales, 32, out, ws)
         assert torch.equal(out, R)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("t,n,k", [(1, 90, 100), (1, 90, 700), (2, 90, 700), (5, 90, 333), (40, 90, 2300), (300, 2000, 100), (2000, 2100, 2570)])
+def test_weights_that_are_not_finite(t, n, k, dt):
+    """The weights of a group with an infinity or a NaN are NaN: so are their output and, on the way back, their group's positions; everything else is what it was."""
+    W = random_weights(n, k, 13).to(dt)
+    bad = W.clone()
+    bad[3, 10], bad[7, k - 1] = float("inf"), float("nan")
+    clean, broken = device_cut(W.to(DEV), 32, dt), device_cut(bad.to(DEV), 32, dt)
+    for grad in (False, True):
+        V = tokens(t, n if grad else k, dt, 3).to(DEV)
+        R = torch.empty(2, t, k if grad else n, dtype=dt, device=DEV)
+        for (codes, scales), out in zip((clean, broken), R):
+            (oz.q4_gemm_grad if grad else oz.q4_gemm)(V, codes, scales, 32, out, oz.alloc_q4_workspace(t, n, k, 32, dt, gradient=grad))
+        hit = torch.zeros(R.shape[2], dtype=torch.bool, device=DEV)
+        if grad:
+            hit[:32] = hit[(k - 1) // 32 * 32:] = True
+        else:
+            hit[3] = hit[7] = True
+        assert R[0].isfinite().all() and R[1][:, hit].isnan().all() and torch.equal(R[1][:, ~hit], R[0][:, ~hit])
