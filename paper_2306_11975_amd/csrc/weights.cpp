@@ -189,6 +189,25 @@ OrthLayout orth_layout(int64_t batch, int64_t m, int64_t n) {
     return o;
 }
 
+struct NarrowLayout {
+    size_t off_norm, off_images, off_factors, off_sums, total;
+};
+NarrowLayout narrow_layout(int64_t batch, int64_t m, int64_t n) {
+    NarrowLayout o{};
+    const size_t panels = (size_t)batch * ((std::max(m, n) + kNarrowPanel - 1) / kNarrowPanel);
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes); return at; };
+    o.off_norm = take(sizeof(double) * (size_t)batch * norm_parts(m, n));
+    o.off_images = take(panels * kNarrowPanel * 256);
+    o.off_factors = take((size_t)batch * 64 * 64 * 4);
+    o.off_sums = take(panels * 64 * 64 * sizeof(float));
+    o.total = off;
+    return o;
+}
+// A shorter side of up to 64: panels, two launches a step, up to the length where one workgroup's sum of their parts takes what that saves (us, products and panels: 64 x 257 82
+// and 48, 64 x 1024 90 and 56, 64 x 4096 125 and 75, 32 x 8192 122 and 99, 64 x 16384 151 and 157; 64 of 64 x 1024 157 and 100).
+bool narrow_update(int64_t m, int64_t n) { return std::min(m, n) <= kSmallShorter && std::max(m, n) <= kNarrowLonger; }
+
 bool small_update(int64_t m, int64_t n) { return std::min(m, n) <= kSmallShorter && std::max(m, n) <= kSmallLonger; }
 
 // The power of two that slices of fp16 hold the iterates under: the largest up to 2^14 with which nothing overflows. The singular
@@ -286,7 +305,7 @@ ozimmu_status_t ozimmu_q4_gemm_grad(int64_t t, int64_t n, int64_t k, int group, 
 ozimmu_status_t ozimmu_orthogonalize_workspace_bytes(int64_t batch, int64_t m, int64_t n, size_t* bytes) {
     if (!dim_ok(m) || !dim_ok(n) || batch < 0 || batch > OZIMMU_MAX_BATCH) return OZIMMU_ERR_BAD_DIM;
     if (!bytes) return OZIMMU_ERR_NULL;
-    *bytes = batch == 0 || m == 0 || n == 0 || small_update(m, n) ? 0 : orth_layout(batch, m, n).total;
+    *bytes = batch == 0 || m == 0 || n == 0 || small_update(m, n) ? 0 : narrow_update(m, n) ? narrow_layout(batch, m, n).total : orth_layout(batch, m, n).total;
     return OZIMMU_OK;
 }
 
@@ -305,6 +324,17 @@ ozimmu_status_t ozimmu_orthogonalize(int64_t batch, int64_t m, int64_t n, ozimmu
     if (misaligned(G, size_of(type)) || misaligned(X, size_of(type))) return OZIMMU_ERR_MISALIGNED;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (small_update(m, n)) return hip_status(launch_orthogonalize_small(batch, m, n, G, type, ldg, stride_g, X, ldx, stride_x, steps, a, b, c, eps, shift, st));
+    if (narrow_update(m, n)) {
+        const NarrowLayout o = narrow_layout(batch, m, n);
+        if (!workspace || misaligned(workspace, OZIMMU_WORKSPACE_ALIGN) || workspace_bytes < o.total) return OZIMMU_ERR_WORKSPACE;
+        unsigned char* base = static_cast<unsigned char*>(workspace);
+        double* norms = reinterpret_cast<double*>(base + o.off_norm);
+        hipError_t e = launch_norm_partials(batch, m, n, G, type, ldg, stride_g, norms, st);
+        if (e == hipSuccess)
+            e = launch_orthogonalize_narrow(batch, m, n, G, type, ldg, stride_g, X, ldx, stride_x, steps, a, b, c, eps, shift, norms, base + o.off_images, base + o.off_factors,
+                                            reinterpret_cast<float*>(base + o.off_sums), st);
+        return hip_status(e);
+    }
     const OrthLayout o = orth_layout(batch, m, n);
     if (!workspace || misaligned(workspace, OZIMMU_WORKSPACE_ALIGN) || workspace_bytes < o.total) return OZIMMU_ERR_WORKSPACE;
     unsigned char* base = static_cast<unsigned char*>(workspace);

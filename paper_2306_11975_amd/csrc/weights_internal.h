@@ -91,4 +91,12 @@ constexpr int64_t kSmallShorter = 64, kSmallLonger = 256;
 hipError_t launch_orthogonalize_small(int64_t batch, int64_t m, int64_t n, const void* G, int type, int64_t ldg, int64_t stride_g, void* X, int64_t ldx,
                                       int64_t stride_x, int steps, double a, double b, double c, double eps, int shift, hipStream_t st);
 
+// The same for longer ones, in panels of kNarrowPanel positions: `images` holds kNarrowPanel * 256 bytes and `sums` 64 * 64 values for every panel of every matrix, `factors` 64 * 64 * 4 bytes
+// for every matrix
+constexpr int kNarrowPanel = 128;
+constexpr int64_t kNarrowLonger = 8192;
+hipError_t launch_orthogonalize_narrow(int64_t batch, int64_t m, int64_t n, const void* G, int type, int64_t ldg, int64_t stride_g, void* X, int64_t ldx,
+                                       int64_t stride_x, int steps, double a, double b, double c, double eps, int shift, const double* norms, unsigned char* images,
+                                       unsigned char* factors, float* sums, hipStream_t st);
+
 }  // namespace ozimmu

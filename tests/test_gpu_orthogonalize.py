@@ -45,7 +45,8 @@ def check(got, G, steps=5, coefficients=MUON, eps=1e-7):
     assert off <= allowed, (off, allowed)
 
 
-SHAPES = [(1, 1), (1, 7), (7, 1), (2, 2), (16, 16), (31, 33), (33, 31), (64, 64), (64, 48), (65, 64), (64, 256), (256, 63), (20, 257), (33, 100), (100, 300), (300, 100), (128, 128), (129, 520), (513, 200), (700, 700)]
+SHAPES = [(1, 1), (1, 7), (7, 1), (2, 2), (16, 16), (31, 33), (33, 31), (64, 64), (64, 48), (65, 64), (64, 256), (256, 63), (20, 257), (33, 100), (100, 300), (300, 100), (128, 128), (129, 520), (513, 200), (700, 700),
+          (64, 1000), (1000, 64), (5, 8192), (8191, 33), (60, 8193), (1, 300)]
 
 
 @pytest.mark.parametrize("dt", [F32, BF16, F16])
@@ -80,7 +81,7 @@ def test_large(batch, m, n):
 
 
 @pytest.mark.parametrize("dt", [F32, BF16])
-@pytest.mark.parametrize("batch,m,n", [(3, 40, 50), (5, 130, 64), (70, 20, 20), (2, 300, 700)])
+@pytest.mark.parametrize("batch,m,n", [(3, 40, 50), (5, 130, 64), (70, 20, 20), (2, 300, 700), (7, 30, 400), (3, 1100, 60)])
 def test_batches(batch, m, n, dt):
     G0 = torch.stack([gradient(m, n, i) * 10.0 ** (i % 5 - 2) for i in range(batch)]).to(dt)
     G0[1] = 0
@@ -114,7 +115,7 @@ def test_one_matrix_for_a_whole_batch():
 @pytest.mark.parametrize("steps,coefficients,eps", [(1, MUON, 0.0), (1, (1.0, 0.0, 0.0), 0.5), (3, (2.0, -1.5, 0.5), 1e-7), (6, MUON, 1e-3),
                                                     (1, (30.0, -20.0, 10.0), 0.0)])
 def test_other_polynomials(steps, coefficients, eps):
-    for m, n in ((48, 80), (200, 150)):
+    for m, n in ((48, 80), (200, 150), (900, 50)):
         G = gradient(m, n, steps)
         X = torch.empty(m, n, device=DEV)
         oz.orthogonalize(G.to(DEV), X, oz.alloc_orthogonalize_workspace(1, m, n), steps=steps, coefficients=coefficients, eps=eps)
@@ -155,7 +156,7 @@ def test_the_size_of_the_matrix_does_not_matter(scale):
     assert (X0 - X1).norm() <= 1e-4 * X0.norm()
 
 
-@pytest.mark.parametrize("batch,m,n", [(1, 65, 65), (3, 70, 1500), (1, 1500, 90), (2, 520, 1000), (1, 1100, 1100)])
+@pytest.mark.parametrize("batch,m,n", [(1, 65, 65), (3, 70, 1500), (1, 1500, 90), (2, 520, 1000), (1, 1100, 1100), (3, 40, 700), (1, 2000, 64)])
 def test_nothing_beyond_the_workspace_is_written(batch, m, n):
     need = oz.orthogonalize_workspace_bytes(batch, m, n)
     room = torch.full((need + (1 << 20),), 0x5A, dtype=torch.uint8, device=DEV)
@@ -167,10 +168,21 @@ def test_nothing_beyond_the_workspace_is_written(batch, m, n):
         check(got, G)
 
 
-def test_graph_shares_a_workspace_with_eager_calls():
-    G = torch.stack([gradient(100, 140, i) for i in range(2)]).to(DEV)
+@pytest.mark.parametrize("m,n", [(40, 50), (50, 900), (300, 200)])
+def test_in_place(m, n):
+    G = torch.stack([gradient(m, n, i) for i in range(2)]).to(DEV)
     X = torch.empty_like(G)
-    ws = oz.alloc_orthogonalize_workspace(2, 100, 140)
+    ws = oz.alloc_orthogonalize_workspace(2, m, n)
+    oz.orthogonalize(G, X, ws)
+    oz.orthogonalize(G, G, ws)
+    assert torch.equal(G, X)
+
+
+@pytest.mark.parametrize("m,n", [(100, 140), (60, 700)])
+def test_graph_shares_a_workspace_with_eager_calls(m, n):
+    G = torch.stack([gradient(m, n, i) for i in range(2)]).to(DEV)
+    X = torch.empty_like(G)
+    ws = oz.alloc_orthogonalize_workspace(2, m, n)
     oz.orthogonalize(G, X, ws)
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g):
