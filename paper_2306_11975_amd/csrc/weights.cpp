@@ -70,7 +70,7 @@ Operands operands(int64_t t, int64_t n, int64_t k, int group, int type, bool gra
 //
 // One token through rows of 512 positions and more is faster on the vector units everywhere, two tokens but for wide layers in bf16 (two, passes and vector units, us:
 // 2048 x 2048 4.5, 3.4; 4096 x 11008 bf16 8.7, 12.1, 32 bits 18.5, 12.0; 16384 x 8192 bf16 18.3, 22.7; one through 512 x 256 2.5, 2.9). From there on the choice is by
-// an estimate of each, in us. 256 workgroups of the passes (32 rows of weights and 32 tokens; 64 and 16 in 32 bits) are a round, whose time grows with k. A tile's walk
+// an estimate of each, in us. 256 workgroups of the passes (32 rows of weights and 32 tokens; 64 and 16 in 32 bits, 32 and 16 with groups of 32) are a round, whose time grows with k. A tile's walk
 // takes half a microsecond a slab of 64 positions (twice that the large ones) until the chip has more than one workgroup for a compute unit. The product takes a walk
 // along k, the operand's bytes, dearer once no cache holds them, and its own operations. Fitted to 24 to 2048 tokens through fifteen layers from 20000 x 64 and
 // 1000 x 333 to 16384 x 8192, where the choices take 0.6 % more than the best ones do on average, 24 % at most. Times of passes, tiles, large tiles, product:
@@ -80,17 +80,17 @@ Operands operands(int64_t t, int64_t n, int64_t k, int group, int type, bool gra
 // With more tokens the answer turns to the product once and stays, so that a workspace serves fewer tokens too: every estimate rises with the tokens at least as
 // the product's does. (The passes are held against the product of their round's first tokens; `more` is added to the tiles' flat part.)
 enum class Way { token, passes, tiles, large_tiles, product };
-Way way_of(int64_t t, int64_t n, int64_t k, int type, bool gradient) {
+Way way_of(int64_t t, int64_t n, int64_t k, int group, int type, bool gradient) {
     if (gradient) return Way::product;
     if (k >= 512 && (t == 1 || (t == 2 && (type != OZIMMU_BF16 || n < 4096)))) return Way::token;
     if (t <= 16) return Way::passes;
-    const bool wide = type == OZIMMU_F32;
+    const bool wide = type == OZIMMU_F32, narrow = wide && group == 32;   // 64 rows a workgroup of the passes, or 32
     const double nk = (double)n * (double)k, beyond = std::max(0.0, nk - 4.0e7);
-    const int64_t passes = wide ? (t + 15) / 16 : (t + 31) / 32, rows = wide ? (n + 63) / 64 : (n + 31) / 32;
+    const int64_t passes = wide ? (t + 15) / 16 : (t + 31) / 32, rows = wide && !narrow ? (n + 63) / 64 : (n + 31) / 32;
     const double rounds = std::ceil((double)rows * (double)passes / 256.0), first = (rounds - 1.0) * 256.0 / (double)rows;   // tokens (passes) ahead of this round
     const double product = wide ? 10.7 + 0.0051 * k + 8.75e-7 * nk + 5.3e-7 * beyond : 18.9 + 0.0013 * k + 5.7e-7 * nk + 3.9e-7 * beyond;
     const double more = (wide ? 1.0e-7 : 5.0e-8) * nk;   // of a pass
-    const double few = passes > 65535 ? 1.0e300 : wide ? 0.24 + rounds * (2.25 + 0.0039 * k) : 5.0 + rounds * (0.27 + 0.00184 * k);   // (the launch's second dimension)
+    const double few = passes > 65535 ? 1.0e300 : narrow ? 0.24 + rounds * (1.6 + 0.0024 * k) : wide ? 0.24 + rounds * (2.25 + 0.0039 * k) : 5.0 + rounds * (0.27 + 0.00184 * k);   // (the launch's second dimension)
     const bool few_lose = few > product + more * first;
     if (wide || k < 8) return few_lose ? Way::product : Way::passes;
     const double slabs = (double)((k + 63) / 64), grown = more * (double)passes;
@@ -119,7 +119,7 @@ ozimmu_status_t q4_product(bool gradient, int64_t t, int64_t n, int64_t k, int g
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (inner == 0) return hip_status(launch_zero_rows(t, outer, R, type, ldr, st));
-    const Way way = way_of(t, n, k, type, gradient);
+    const Way way = way_of(t, n, k, group, type, gradient);
     if (way == Way::token) return hip_status(launch_q4_token(t, n, k, group, V, type, ldv, codes, ldq, scales, lds, R, ldr, st));
     if (way == Way::passes) return hip_status(launch_q4_few(t, n, k, group, V, type, ldv, codes, ldq, scales, lds, R, ldr, st));
     if (way == Way::tiles || way == Way::large_tiles)
@@ -287,7 +287,7 @@ ozimmu_status_t ozimmu_q4_workspace_bytes(int64_t t, int64_t n, int64_t k, int g
     if (!dim_ok(t) || !dim_ok(n) || !dim_ok(k) || !group_ok(group)) return OZIMMU_ERR_BAD_DIM;
     if (!type_ok(type)) return OZIMMU_ERR_BAD_TYPE;
     if (!bytes) return OZIMMU_ERR_NULL;
-    *bytes = t == 0 || n == 0 || k == 0 || way_of(t, n, k, type, gradient != 0) != Way::product ? 0 : operands(t, n, k, group, type, gradient != 0).total;
+    *bytes = t == 0 || n == 0 || k == 0 || way_of(t, n, k, group, type, gradient != 0) != Way::product ? 0 : operands(t, n, k, group, type, gradient != 0).total;
     return OZIMMU_OK;
 }
 
