@@ -383,7 +383,7 @@ ozimmu_status_t ozimmu_zgemm_blas_auto(char transa, char transb, int64_t m, int6
  * tokens, and gradients, may take, as n, k and t have it, the weights s c rounded once to bf16 or fp16 instead (one beyond the type's range becomes an infinity, as ozimmu_q4_expand has it), or, for
  * 32-bit types, both operands as two fp16 slices under a power-of-two exponent per row (22 bits and more of every value that is within 2^-17 of its row's largest; the rest to 2^-39
  * of that; the exponent goes with the group for the columns of W). A token or gradient row that holds an infinity or a NaN gives results that are
- * not finite (NaN, also where the formula has an infinity); every other row is what it would be without it. (16-bit tokens above 2^115 may overflow on the way: the codes are multiplied with an offset.) Empty dimensions: t = 0 or no outputs: nothing to do; an empty inner dimension
+ * not finite (NaN, also where the formula has an infinity); every other row is what it would be without it. Empty dimensions: t = 0 or no outputs: nothing to do; an empty inner dimension
  * gives zeros. Outputs must not overlap inputs or the workspace.
  * workspace: ozimmu_q4_workspace_bytes(...) bytes, OZIMMU_WORKSPACE_ALIGN-aligned; may be null where that is 0; one for t tokens serves fewer.
  * Errors: OZIMMU_ERR_BAD_DIM (sizes or group), OZIMMU_ERR_BAD_TYPE, OZIMMU_ERR_BAD_LD (also ldq, and any beyond OZIMMU_MAX_LD), OZIMMU_ERR_NULL, OZIMMU_ERR_MISALIGNED,

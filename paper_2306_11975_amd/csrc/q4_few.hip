@@ -1,27 +1,30 @@
-// Y = X W^T for few tokens and weights in four bits: one pass over the codes, no workspace (gfx950).
+// Y = X W^T for few tokens and weights in four bits: a pass over the codes for every 16 or 32 tokens, no workspace (gfx950).
 //
-// What bounds it is reading the codes, and the tokens again for every 16 NT rows of them; the sums go to the matrix cores (v_mfma_f32_16x16x32) although most of
-// their rows stay empty with few tokens, because the vector units have their hands full making 16-bit operands of the codes. A wavefront takes 16 NT rows of
-// W, 16 TT tokens and every W-th step of k; the W wavefronts of a workgroup share the rows and add their parts up in LDS.
+// What bounds it is reading the codes, and the tokens again for every 16 NT rows of them; the sums go to the matrix cores
+// (v_mfma_f32_16x16x32) although most of their rows stay empty with few tokens, because the vector units have their hands full making
+// 16-bit operands of the codes. A wavefront takes 16 NT rows of W, 16 TT tokens and every W-th step of k; the W wavefronts of a
+// workgroup share the rows and add their parts up in LDS.
 //
-// A step is 128 positions. Memory is read along the rows, 16 lanes to 256 bytes of a token's row, four lanes to 64 of a row's codes, and goes through LDS (a region for
-// every wavefront, no barrier) into the operands' order; loads in that order, neighbouring lanes in different rows, look up a line for every lane (16 tokens, bf16, 16384 x
-// 8192 26.8 us where these take 19.9; 32 tokens 51.8 and 32.6; rows of tokens at odd places, 387 x 10575, 58 and 12). A lane's operand of the codes is 16 bytes,
-// 32 positions, of row lane % 16. An MFMA adds up positions of one group only: in groups of 64 and 32 the quarters of a wavefront (lane / 16) first exchange words
-// (v_permlane32_swap, v_permlane16_swap), so that word j of every lane belongs to one group, and is MFMA j's operand. The tokens' operand is read from the same positions.
+// A step is 128 positions. Memory is read along the rows, 16 lanes to 256 bytes of a token's row, four lanes to 64 of a row's codes, and
+// goes through LDS (a region for every wavefront, no barrier) into the operands' order; loads in that order, neighbouring lanes in
+// different rows, look up a line for every lane (16 tokens, bf16, 16384 x 8192 26.8 us where these take 19.6; 32 tokens 51.8 and 30.5;
+// rows of tokens at odd places, 387 x 10575, 58 and 12). A lane's operand of the codes is 16 bytes, 32 positions, of row lane % 16. An
+// MFMA adds up positions of one group only: in groups of 64 and 32 the quarters of a wavefront (lane / 16) first exchange words
+// (v_permlane32_swap, v_permlane16_swap), so that word j of every lane belongs to one group, and is MFMA j's operand. The tokens' operand
+// is read from the same positions.
 //
-// Codes to 16-bit values: the four bits of c + 8 go into the mantissa of 16.0 (one shift, one and-or for two codes), which
-// gives 16 + (c + 8) exactly. The 24 too much is taken out by the matrix cores: the sums start from the tokens' product with a
-// constant operand of -24, formed once for all rows of the wavefront. So a group's sum is that of x (c + 24) and x (-24) in 32 bits:
-// against the terms alone it loses three bits of 24, which results of 8 or 11 bits do not see. 32-bit tokens are
-// cut into three bf16 (exactly) and multiplied by exact codes, without the detour.
-// The scale of a group is applied to its sum in 32 bits.
+// Codes become 16-bit values exactly, so that products are exact and a sum's error goes by its terms: a value far above the others under
+// a code of zero adds nothing to it. bf16: the conversion from four signed bits gives a code's sixteenth in 32 bits, whose upper half is
+// all of it; two halves make a word of the operand, and the result is multiplied by 16. fp16: the four bits of c + 8 go into the mantissa
+// of 1024, and a packed addition takes 1032 away. (With the offset left in and the tokens' product with it taken off the sums, an MFMA
+// more, sums of fp16 tokens lose half their bits next to a value of 6e4; 64 tokens, 16384 x 8192, groups of 32, 65.5 us against 60.9 here.)
+// 32-bit tokens are cut into three bf16 (exactly), three MFMAs. The scale of a group is applied to its sum in 32 bits.
 #include "half_common.h"
 
 namespace ozimmu {
 namespace {
 
-// The operand of eight tokens' values is paired (0, 4), (1, 5), (2, 6), (3, 7) to match the codes' pairs.
+// Eight fp16 tokens paired (0, 4), (1, 5), (2, 6), (3, 7) to match the codes' pairs.
 __device__ __forceinline__ v4u pair_by_four(const v4u& x) {
     v4u r;
     r[0] = __builtin_amdgcn_perm(x[2], x[0], 0x05040100u);
@@ -31,46 +34,49 @@ __device__ __forceinline__ v4u pair_by_four(const v4u& x) {
     return r;
 }
 
-// The two constants of offset_codes in registers of their own (v_and_or_b32 takes one scalar and no two literals), hidden from the optimiser, which would turn them back
-// into literals and take two instructions.
+// The two constants of fp16 codes in registers of their own (v_and_or_b32 takes one scalar and no two literals), hidden from the
+// optimiser, which would turn them back into literals and take two instructions.
 struct CodeBits {
     unsigned mask, one;
-    template <bool BF16>
     static __device__ __forceinline__ CodeBits of() {
         CodeBits c;
-        if constexpr (BF16)
-            asm("s_mov_b32 %0, 0x00780078\n\tv_mov_b32 %1, 0x41804180" : "=s"(c.mask), "=v"(c.one));
-        else
-            asm("s_mov_b32 %0, 0x03c003c0\n\tv_mov_b32 %1, 0x4c004c00" : "=s"(c.mask), "=v"(c.one));
+        asm("s_mov_b32 %0, 0x000f000f\n\tv_mov_b32 %1, 0x64006400" : "=s"(c.mask), "=v"(c.one));
         return c;
     }
 };
-// 16 + (c + 8) of the codes (0, 4), (1, 5), (2, 6), (3, 7) of a word
-template <bool BF16>
-__device__ __forceinline__ v4u offset_codes(unsigned w, const CodeBits& b) {
-    v4u r;
-    if constexpr (BF16) {
-        r[0] = ((w << 3) & b.mask) | b.one;
-        r[1] = ((w >> 1) & b.mask) | b.one;
-        r[2] = ((w >> 5) & b.mask) | b.one;
-        r[3] = ((w >> 9) & b.mask) | b.one;
-    } else {
-        r[0] = ((w << 6) & b.mask) | b.one;
-        r[1] = ((w << 2) & b.mask) | b.one;
-        r[2] = ((w >> 2) & b.mask) | b.one;
-        r[3] = ((w >> 6) & b.mask) | b.one;
-    }
-    return r;
-}
-// the codes' sixteenths as bf16, exactly: the conversion from four signed bits gives them, and four bits fit the upper half of a 32-bit value
-__device__ __forceinline__ v4u exact_codes(unsigned w) {
-    w ^= 0x88888888u;
+// The codes of a word in fp16, (0, 4), (1, 5), (2, 6), (3, 7), exactly: 1024 + (c + 8) less 1032.
+__device__ __forceinline__ v4u codes_f16(unsigned w, const CodeBits& b) {
+    typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+    const v2h less = {(_Float16)-1032.f, (_Float16)-1032.f};
     v4u r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float lo = __builtin_amdgcn_cvt_off_f32_i4((int)(w >> (4 * i))), hi = __builtin_amdgcn_cvt_off_f32_i4((int)(w >> (4 * i + 16)));
-        r[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
-    }
+    for (int i = 0; i < 4; ++i) r[i] = __builtin_bit_cast(unsigned, __builtin_bit_cast(v2h, ((w >> (4 * i)) & b.mask) | b.one) + less);
+    return r;
+}
+// The sixteenth of the code in the low half of byte BYTE. (In assembly for the choice of a byte: the compiler shifts ahead of most
+// conversions instead, up to five instructions a word; 16 tokens, 16384 x 8192, 21.0 us against 19.6.)
+template <int BYTE>
+__device__ __forceinline__ float sixteenth(unsigned w) {
+    float x;
+    if constexpr (BYTE == 0)
+        x = __builtin_amdgcn_cvt_off_f32_i4((int)w);
+    else if constexpr (BYTE == 1)
+        asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(x) : "v"(w));
+    else if constexpr (BYTE == 2)
+        asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(x) : "v"(w));
+    else
+        asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(x) : "v"(w));
+    return x;
+}
+// The codes' sixteenths in bf16, in order, exactly: the conversion from four signed bits gives them in 32 bits, and they fit the upper half.
+__device__ __forceinline__ v4u sixteenths_bf16(unsigned w) {
+    w ^= 0x88888888u;
+    const unsigned high = w >> 4;
+    v4u r;
+    static_for<0, 4>([&](auto byte) {
+        constexpr int i = decltype(byte)::value;
+        r[i] = __builtin_amdgcn_perm(__float_as_uint(sixteenth<i>(high)), __float_as_uint(sixteenth<i>(w)), 0x07060302u);
+    });
     return r;
 }
 
@@ -99,10 +105,12 @@ __device__ __forceinline__ Operand<TYPE> operand(const Raw<TYPE>& r) {
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            t.piece[0][i] = __builtin_amdgcn_perm(a[i + 4], a[i], 0x07060302u);
-            t.piece[1][i] = __builtin_amdgcn_perm(b[i + 4], b[i], 0x07060302u);
-            t.piece[2][i] = __builtin_amdgcn_perm(c[i + 4], c[i], 0x07060302u);
+            t.piece[0][i] = __builtin_amdgcn_perm(a[2 * i + 1], a[2 * i], 0x07060302u);
+            t.piece[1][i] = __builtin_amdgcn_perm(b[2 * i + 1], b[2 * i], 0x07060302u);
+            t.piece[2][i] = __builtin_amdgcn_perm(c[2 * i + 1], c[2 * i], 0x07060302u);
         }
+    } else if constexpr (TYPE == OZIMMU_BF16) {
+        t.piece[0] = r.v[0];
     } else {
         t.piece[0] = pair_by_four(r.v[0]);
     }
@@ -204,9 +212,7 @@ __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_
     for (int i = 0; i < NT; ++i)
 #pragma unroll
         for (int tt = 0; tt < TT; ++tt) total[i][tt] = v4f{0.f, 0.f, 0.f, 0.f};
-    const unsigned minus = BF16 ? 0xc1c0c1c0u : 0xce00ce00u;   // -24, twice
-    const v4u minus24 = {minus, minus, minus, minus};
-    const CodeBits bits = CodeBits::of<BF16>();
+    const CodeBits bits = CodeBits::of();
 
     auto in_order = [] {   // of the wavefront's own accesses to LDS
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -245,7 +251,7 @@ __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_
         }
 #pragma unroll
         for (int h = 0; h < GROUPS; ++h) {
-            v4f sum[NT][TT], offset[TT];
+            v4f sum[NT][TT];
 #pragma unroll
             for (int j = 0; j < GW; ++j) {
                 Operand<TYPE> o[TT];
@@ -259,23 +265,14 @@ __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_
                     o[tt] = operand<TYPE>(x);
                 }
                 const v4f zero = v4f{0.f, 0.f, 0.f, 0.f};
-                if constexpr (TYPE != OZIMMU_F32)
-#pragma unroll
-                    for (int tt = 0; tt < TT; ++tt) offset[tt] = mfma_half<BF16>(o[tt].piece[0], minus24, j ? offset[tt] : zero);
 #pragma unroll
                 for (int i = 0; i < NT; ++i) {
                     const unsigned word = words[i][GW * h + j];
-                    if constexpr (TYPE == OZIMMU_F32) {
-                        const v4u c = exact_codes(word);
+                    const v4u c = BF16 ? sixteenths_bf16(word) : codes_f16(word, bits);
 #pragma unroll
-                        for (int p = 2; p >= 0; --p)
+                    for (int p = Operand<TYPE>::kPieces - 1; p >= 0; --p)   // (of 32-bit tokens the smallest first)
 #pragma unroll
-                            for (int tt = 0; tt < TT; ++tt) sum[i][tt] = mfma_half<true>(o[tt].piece[p], c, j || p < 2 ? sum[i][tt] : zero);
-                    } else {
-                        const v4u c = offset_codes<BF16>(word, bits);
-#pragma unroll
-                        for (int tt = 0; tt < TT; ++tt) sum[i][tt] = mfma_half<BF16>(o[tt].piece[0], c, j ? sum[i][tt] : zero);
-                    }
+                        for (int tt = 0; tt < TT; ++tt) sum[i][tt] = mfma_half<BF16>(o[tt].piece[p], c, j || p + 1 < Operand<TYPE>::kPieces ? sum[i][tt] : zero);
                 }
             }
 #pragma unroll
@@ -284,8 +281,7 @@ __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_
 #pragma unroll
                 for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        total[i][tt][e] = fmaf(f, TYPE == OZIMMU_F32 ? sum[i][tt][e] : sum[i][tt][e] + offset[tt][e], total[i][tt][e]);
+                    for (int e = 0; e < 4; ++e) total[i][tt][e] = fmaf(f, sum[i][tt][e], total[i][tt][e]);
             }
         }
     };
@@ -335,7 +331,7 @@ __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_
         float sum = part[tok * kRow + col];
 #pragma unroll
         for (int i = 1; i < W; ++i) sum += part[(i * 16 * TT + tok) * kRow + col];
-        reinterpret_cast<raw*>(Y)[(int64_t)(t0 + tok) * ldy + n0 + col] = E::store(TYPE == OZIMMU_F32 ? 16.f * sum : sum);   // (the codes' sixteenths)
+        reinterpret_cast<raw*>(Y)[(int64_t)(t0 + tok) * ldy + n0 + col] = E::store(BF16 ? 16.f * sum : sum);   // (the codes' sixteenths)
     }
 }
 

@@ -68,7 +68,7 @@ hipError_t launch_zero_rows(int64_t rows, int64_t cols, void* R, int type, int64
 // q4_token.hip: Y = X W^T for one token or two
 hipError_t launch_q4_token(int64_t t, int64_t n, int64_t k, int group, const void* X, int type, int64_t ldx, const uint8_t* codes, int64_t ldq,
                            const void* scales, int64_t lds, void* Y, int64_t ldy, hipStream_t st);
-// q4_few.hip: Y = X W^T for few tokens, one pass over the codes
+// q4_few.hip: Y = X W^T for few tokens, a pass over the codes for every 16 or 32 of them
 hipError_t launch_q4_few(int64_t t, int64_t n, int64_t k, int group, const void* X, int type, int64_t ldx, const uint8_t* codes,
                          int64_t ldq, const void* scales, int64_t lds, void* Y, int64_t ldy, hipStream_t st);
 
