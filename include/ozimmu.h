@@ -411,8 +411,8 @@ ozimmu_status_t ozimmu_q4_gemm_grad(int64_t t, int64_t n, int64_t k, int group, 
  * p(x) = a x + b x^3 + c x^5, and the singular vectors stay. (a, b, c) = (3.4445, -4.7750, 2.0315) with five steps takes
  * what is not far below the largest into 0.7 .. 1.2; (1.5, -0.5, 0) is the plain iteration for the nearest orthogonal matrix. G and X
  * have type `type`; X may be G (same strides), and otherwise must not overlap it. The norm is summed in 64 bits. Everything between is held as two fp16 slices under a common power of two
- * (22 bits and more), multiplied as three products with sums in 32 bits: errors are those of an iteration in 32 bits. (For bf16 results the last product of a
- * matrix beyond 64 x 256 takes the first slices alone: off by 2^-12 of its operands, below the result's own rounding.) A matrix of zeros gives zeros; one with an infinity or a NaN
+ * (22 bits and more), multiplied as three products with sums in 32 bits: errors are those of an iteration in 32 bits. The result
+ * is rounded once. A matrix of zeros gives zeros; one with an infinity or a NaN
  * gives NaN in places that are not specified, and does not touch the others of its batch.
  * steps in 1 .. OZIMMU_MAX_STEPS, eps >= 0 and finite, a >= 1 (small singular values must not shrink: they are held to 2^-38 absolutely, or as
  * much more as intermediate values exceed four), and the polynomial must keep [0, 1] bounded under its iteration, so that no

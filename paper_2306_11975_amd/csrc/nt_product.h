@@ -2,7 +2,7 @@
 // dimension in slabs of 128 bytes (weights_internal.h). One slice: the ordinary product. Two slices of fp16 (value = first +
 // second, 22 bits and more): the products first*first, first*second and second*first of the same fragments, which leaves out
 // what is below 2^-22 of a term; a slab then holds both slices of 32 positions, so loads and shared memory are the same and only
-// the pairs differ. The first of two slices: first*first alone.
+// the pairs differ.
 //
 // A workgroup owns a BM x BN tile. A slab of its rows of P and Q is brought into LDS by direct loads (1 KiB = 8 rows a
 // wavefront and load; the lane that fetches 16-byte piece c of row r puts it at place c ^ (r % 8), so that the 16 lanes of a
@@ -148,10 +148,7 @@ __global__ void nt_product_kernel(NtArgs a, NtPlan plan) {
         for (int j = 0; j < NI; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
 
     auto row_of_products = [&](int i, const v4u& a0, const v4u& a1, const v4u (&q0)[NI], const v4u (&q1)[NI]) {
-        if constexpr (SLICES == kFirstOfTwo) {
-#pragma unroll
-            for (int j = 0; j < NI; ++j) acc[i][j] = mfma_half<BF16>(q0[j], a0, acc[i][j]);
-        } else if constexpr (SLICES == 1) {
+        if constexpr (SLICES == 1) {
 #pragma unroll
             for (int j = 0; j < NI; ++j) acc[i][j] = mfma_half<BF16>(q0[j], a0, acc[i][j]);
 #pragma unroll
@@ -446,7 +443,7 @@ hipError_t launch_nt_tile(const NtArgs& a, const NtPlan& plan, hipStream_t st) {
 template <int SLICES, bool BF16, int RESULT>
 hipError_t launch_nt(const NtArgs& a, hipStream_t st) {
     if (a.m <= 0 || a.n <= 0 || a.slabs <= 0 || a.batch <= 0 || (a.symmetric && a.m != a.n)) return hipErrorInvalidValue;
-    constexpr bool two = SLICES == 2;   // (the first of two slices: as many products as with one, on half the positions a slab)
+    constexpr bool two = SLICES == 2;
     const NtShape shapes[] = {{256, 256, two ? 2.41 : 1.73, two ? 2.41 : 1.73}, {128, 512, two ? 1.31 : 0.95, two ? 0.92 : 0.62}, {64, 1280, two ? 1.0 : 0.9, two ? 0.40 : 0.37}, {64, 768, two ? 0.75 : 0.66, two ? 0.31 : 0.27}};
     NtChoice best{};
     int which = -1;

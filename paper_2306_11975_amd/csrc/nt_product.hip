@@ -6,7 +6,6 @@ hipError_t launch_nt_two_slices(const NtArgs& a, NtResult result, hipStream_t st
 
 hipError_t launch_nt_product(const NtArgs& a, int slices, bool bf16, NtResult result, hipStream_t st) {
     if (slices == 2) return launch_nt_two_slices(a, result, st);
-    if (slices == kFirstOfTwo) return result == kOutBf16 ? launch_nt<kFirstOfTwo, false, kOutBf16>(a, st) : hipErrorInvalidValue;
     if (bf16) return result == kOutBf16 ? launch_nt<1, true, kOutBf16>(a, st) : hipErrorInvalidValue;
     return result == kOutF16 ? launch_nt<1, false, kOutF16>(a, st) : hipErrorInvalidValue;
 }

@@ -406,9 +406,7 @@ ozimmu_status_t ozimmu_orthogonalize(int64_t batch, int64_t m, int64_t n, ozimmu
             u.out = X;
             u.ldo = ldx;
             u.batch_o = stride_x;
-            // Results of eight bits: the last product, whose errors no step magnifies, takes the first slices alone. Its operands are then off by 2^-12 of themselves, the result by up
-            // to 1.25 times its own rounding (matrices of 256 to 1536 with strong directions above noise of 1e-4 to 1: 1.02 to 1.24); 4096 x 4096 saves 170 us of 3560.
-            e = launch_nt_product(u, type == OZIMMU_BF16 ? kFirstOfTwo : 2, false, type == OZIMMU_F32 ? kOutF32 : type == OZIMMU_BF16 ? kOutBf16 : kOutF16, st);
+            e = launch_nt_product(u, 2, false, type == OZIMMU_F32 ? kOutF32 : type == OZIMMU_BF16 ? kOutBf16 : kOutF16, st);
         } else {
             u.factor = down;
             u.C = x;

@@ -40,8 +40,7 @@ struct NtArgs {
     float beta, diagonal;
 };
 enum NtResult { kOutF32 = 0, kOutBf16 = 1, kOutF16 = 2, kOutSlices = 3 };
-// `slices` 1 (bf16 where `bf16`, else fp16), 2 (fp16) or kFirstOfTwo (operands of two slices of fp16, of which the first is multiplied)
-constexpr int kFirstOfTwo = 3;
+// `slices`: 1 (bf16 where `bf16`, else fp16) or 2 (fp16)
 // Room that launch_nt_product can make use of for any product (at most so many workgroups share tiles).
 constexpr size_t kPartialBytes = 512 * 128 * 128 * sizeof(float);
 hipError_t launch_nt_product(const NtArgs& a, int slices, bool bf16, NtResult result, hipStream_t st);
