@@ -2,6 +2,8 @@
 //
 // Group g of row i: s = RN_T(RN_32(max |w| / 7)), c = RNE(w / s) clamped to [-8, 7], stored as c + 8, two to a byte, the even
 // position in the low half; a row takes a multiple of 16 bytes (32 codes), what is beyond k stands for zero.
+#include <algorithm>
+
 #include "half_common.h"
 
 namespace ozimmu {
@@ -136,13 +138,14 @@ __device__ __forceinline__ float seventh(float top) {
 template <int TYPE, int STYPE, int GROUP>
 __launch_bounds__(kThreads)
 __global__ void q4_split_kernel(int64_t n, int64_t k, const void* W, int64_t ldw, uint8_t* codes, int64_t ldq, void* scales,
-                                int64_t lds, int tx, unsigned across) {
+                                int64_t lds, int tx, unsigned across, unsigned first) {
     typedef Elem<TYPE> E;
     typedef Elem<STYPE> S;
     constexpr int ROWS = 2;
     const int ty = kThreads / tx;
-    const int64_t row0 = (int64_t)(blockIdx.x / across) * (ROWS * ty) + threadIdx.x / tx;
-    const int64_t at = ((int64_t)(blockIdx.x % across) * tx + threadIdx.x % tx) * 8;
+    const unsigned block = first + blockIdx.x;
+    const int64_t row0 = (int64_t)(block / across) * (ROWS * ty) + threadIdx.x / tx;
+    const int64_t at = ((int64_t)(block % across) * tx + threadIdx.x % tx) * 8;
     float w[ROWS][8];
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) load8<TYPE>(reinterpret_cast<const typename E::raw*>(W) + min(row0 + i * ty, n - 1) * ldw, at, k, w[i]);
@@ -165,10 +168,11 @@ __device__ __forceinline__ float code_value(unsigned word, int e) { return (floa
 template <int TYPE>
 __launch_bounds__(kThreads)
 __global__ void q4_expand_kernel(int64_t n, int64_t k, int group_log2, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds,
-                                 void* W, int64_t ldw, int tx, unsigned across) {
+                                 void* W, int64_t ldw, int tx, unsigned across, unsigned first) {
     typedef Elem<TYPE> E;
-    const int64_t row = (int64_t)(blockIdx.x / across) * (kThreads / tx) + threadIdx.x / tx;
-    const int64_t at = ((int64_t)(blockIdx.x % across) * tx + threadIdx.x % tx) * 8;
+    const unsigned block = first + blockIdx.x;
+    const int64_t row = (int64_t)(block / across) * (kThreads / tx) + threadIdx.x / tx;
+    const int64_t at = ((int64_t)(block % across) * tx + threadIdx.x % tx) * 8;
     if (row >= n || at >= k) return;
     const unsigned word = *reinterpret_cast<const unsigned*>(codes + row * ldq + at / 2);
     const float s = E::load(reinterpret_cast<const typename E::raw*>(scales)[row * lds + (at >> group_log2)]);
@@ -228,6 +232,7 @@ struct OperandArgs {
     int* v_exps;
     int v_tx;
     unsigned v_across;
+    unsigned first;             // workgroup of the launch
 };
 
 // Rows of 32-bit values in two slices of fp16 under a power-of-two exponent per row; a workgroup per row, which it reads twice
@@ -393,17 +398,18 @@ __launch_bounds__(kThreads)
 __global__ void operands_kernel(OperandArgs a) {
     __shared__ __attribute__((aligned(16))) unsigned short tile[COLUMNS ? COLUMNS * 64 * (TYPE == OZIMMU_F32 ? 2 : 1) : 8];
     __shared__ float shared[kThreads / 64];
-    if (blockIdx.x < a.w_blocks) {
+    const unsigned block = a.first + blockIdx.x;
+    if (block < a.w_blocks) {
         if constexpr (COLUMNS != 0)
-            q4_columns<TYPE, COLUMNS>(a, blockIdx.x, tile);
+            q4_columns<TYPE, COLUMNS>(a, block, tile);
         else if constexpr (TYPE == OZIMMU_F32)
-            q4_slices(a, blockIdx.x, shared);
+            q4_slices(a, block, shared);
         else
-            q4_rows<TYPE>(a, blockIdx.x);
+            q4_rows<TYPE>(a, block);
     } else if constexpr (TYPE == OZIMMU_F32) {
-        row_slices(a, blockIdx.x - a.w_blocks, shared);
+        row_slices(a, block - a.w_blocks, shared);
     } else {
-        pad_rows(a, blockIdx.x - a.w_blocks);
+        pad_rows(a, block - a.w_blocks);
     }
 }
 
@@ -436,21 +442,31 @@ int threads_along(int64_t chunks) {
 // Workgroups over `rows` rows of `chunks` pieces, tx threads along a row: numbered along the rows, so that those that run together read memory in order (by columns first:
 // 8192 x 8192 bf16 cut in 62 us).
 unsigned across_of(int64_t chunks, int tx) { return (unsigned)((chunks + tx - 1) / tx); }
-dim3 grid_for(int64_t rows, int64_t chunks, int tx) { return dim3((unsigned)((rows + kThreads / tx - 1) / (kThreads / tx)) * across_of(chunks, tx)); }
+int64_t blocks_for(int64_t rows, int64_t chunks, int tx) { return (rows + kThreads / tx - 1) / (kThreads / tx) * (int64_t)across_of(chunks, tx); }
+// A launch has fewer than 2^32 threads along its first dimension, which 2^35 weights are beyond (4194304 x 8192, 16 GiB of codes): workgroups go out in launches of at
+// most kMostBlocks, of a millisecond each. launch(workgroups, the first one's number).
+constexpr int64_t kMostBlocks = 1 << 21;
+template <class F>
+hipError_t in_launches(int64_t blocks, F launch) {
+    if (blocks > UINT32_MAX) return hipErrorInvalidValue;   // (2^43 weights)
+    for (int64_t first = 0; first < blocks; first += kMostBlocks) launch(dim3((unsigned)std::min(kMostBlocks, blocks - first)), (unsigned)first);
+    return hipGetLastError();
+}
 int log2_of(int group) { return group == 32 ? 5 : group == 64 ? 6 : 7; }
 
 template <int TYPE, int STYPE>
 hipError_t split_typed(int64_t n, int64_t k, int group, const void* W, int64_t ldw, uint8_t* codes, int64_t ldq, void* scales, int64_t lds, hipStream_t st) {
     const int64_t chunks = pad_to(k, group) / 8;
     const int tx = threads_along(chunks);
-    const dim3 grid = grid_for((n + 1) / 2, chunks, tx);
-    if (group == 32)
-        q4_split_kernel<TYPE, STYPE, 32><<<grid, kThreads, 0, st>>>(n, k, W, ldw, codes, ldq, scales, lds, tx, across_of(chunks, tx));
-    else if (group == 64)
-        q4_split_kernel<TYPE, STYPE, 64><<<grid, kThreads, 0, st>>>(n, k, W, ldw, codes, ldq, scales, lds, tx, across_of(chunks, tx));
-    else
-        q4_split_kernel<TYPE, STYPE, 128><<<grid, kThreads, 0, st>>>(n, k, W, ldw, codes, ldq, scales, lds, tx, across_of(chunks, tx));
-    return hipGetLastError();
+    const unsigned across = across_of(chunks, tx);
+    return in_launches(blocks_for((n + 1) / 2, chunks, tx), [&](dim3 grid, unsigned first) {
+        if (group == 32)
+            q4_split_kernel<TYPE, STYPE, 32><<<grid, kThreads, 0, st>>>(n, k, W, ldw, codes, ldq, scales, lds, tx, across, first);
+        else if (group == 64)
+            q4_split_kernel<TYPE, STYPE, 64><<<grid, kThreads, 0, st>>>(n, k, W, ldw, codes, ldq, scales, lds, tx, across, first);
+        else
+            q4_split_kernel<TYPE, STYPE, 128><<<grid, kThreads, 0, st>>>(n, k, W, ldw, codes, ldq, scales, lds, tx, across, first);
+    });
 }
 template <int TYPE>
 hipError_t split_from(int64_t n, int64_t k, int group, const void* W, int64_t ldw, uint8_t* codes, int64_t ldq, void* scales, int stype, int64_t lds, hipStream_t st) {
@@ -464,8 +480,9 @@ hipError_t expand_typed(int64_t n, int64_t k, int group, const uint8_t* codes, i
                         hipStream_t st) {
     const int64_t chunks = pad_to(k, 8) / 8;
     const int tx = threads_along(chunks);
-    q4_expand_kernel<TYPE><<<grid_for(n, chunks, tx), kThreads, 0, st>>>(n, k, log2_of(group), codes, ldq, scales, lds, W, ldw, tx, across_of(chunks, tx));
-    return hipGetLastError();
+    return in_launches(blocks_for(n, chunks, tx), [&](dim3 grid, unsigned first) {
+        q4_expand_kernel<TYPE><<<grid, kThreads, 0, st>>>(n, k, log2_of(group), codes, ldq, scales, lds, W, ldw, tx, across_of(chunks, tx), first);
+    });
 }
 
 template <int TYPE>
@@ -526,37 +543,39 @@ hipError_t launch_operands(int64_t t, int64_t n, int64_t k, int group, int type,
     // Wide tiles read and write whole lines (8192 x 4096 in 16 bits 24 us with 64 positions, 18 with 256); narrow ones are more workgroups where there are few.
     const int most = f32 ? 128 : 256;
     const int width = (n + 63) / 64 * ((k + most - 1) / most) >= 1024 ? most : 64;
+    int64_t w_blocks, v_blocks = 0;
     if (columns) {
         a.w_across = (unsigned)((k + width - 1) / width);
-        a.w_blocks = (unsigned)((n + 63) / 64) * a.w_across;
+        w_blocks = (n + 63) / 64 * (int64_t)a.w_across;
     } else {
         const int64_t chunks = pad_to(k, f32 ? 32 : 64) / 8;
         a.w_tx = threads_along(chunks);
         a.w_across = across_of(chunks, a.w_tx);
-        a.w_blocks = grid_for(n, chunks, a.w_tx).x;
+        w_blocks = blocks_for(n, chunks, a.w_tx);
     }
-    unsigned v_blocks = 0;
+    a.w_blocks = (unsigned)w_blocks;
     if (v_out && f32) {
-        v_blocks = (unsigned)t;
+        v_blocks = t;
     } else if (v_out) {
         a.v_tx = threads_along(ld / 8);
         a.v_across = across_of(ld / 8, a.v_tx);
-        v_blocks = grid_for(t, ld / 8, a.v_tx).x;
+        v_blocks = blocks_for(t, ld / 8, a.v_tx);
     }
     if (columns && f32) {
         const unsigned groups = (unsigned)((k + group - 1) / group);
-        group_exponents_kernel<<<dim3(groups + v_blocks), kThreads, 0, st>>>(a, groups);
+        group_exponents_kernel<<<dim3(groups + (unsigned)v_blocks), kThreads, 0, st>>>(a, groups);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
         v_blocks = 0;
     }
-    const dim3 grid(a.w_blocks + v_blocks);
-    if (f32)
-        launch_operands_typed<OZIMMU_F32>(a, grid, columns ? width : 0, st);
-    else if (type == OZIMMU_BF16)
-        launch_operands_typed<OZIMMU_BF16>(a, grid, columns ? width : 0, st);
-    else
-        launch_operands_typed<OZIMMU_F16>(a, grid, columns ? width : 0, st);
-    return hipGetLastError();
+    return in_launches(w_blocks + v_blocks, [&](dim3 grid, unsigned first) {
+        a.first = first;
+        if (f32)
+            launch_operands_typed<OZIMMU_F32>(a, grid, columns ? width : 0, st);
+        else if (type == OZIMMU_BF16)
+            launch_operands_typed<OZIMMU_BF16>(a, grid, columns ? width : 0, st);
+        else
+            launch_operands_typed<OZIMMU_F16>(a, grid, columns ? width : 0, st);
+    });
 }
 
 }  // namespace ozimmu
