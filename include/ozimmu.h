@@ -378,16 +378,18 @@ ozimmu_status_t ozimmu_zgemm_blas_auto(char transa, char transb, int64_t m, int6
  *
  * ozimmu_q4_gemm:      Y = X W^T   (X: t x k, Y: t x n: t tokens through the layer)
  * ozimmu_q4_gemm_grad: dX = dY W   (dY: t x n, dX: t x k: the gradient on its way back through it)
- * X, Y, dY, dX and the scales have type `type`; the sums are formed in 32 bits and rounded once. Up to 16 tokens (and, for 32-bit types, where
- * ozimmu_q4_workspace_bytes gives 0) ozimmu_q4_gemm multiplies the codes themselves and applies the scales to the sums, in 32 bits. Products of more
- * tokens, and gradients, may take, as n, k and t have it, the weights s c rounded once to bf16 or fp16 instead (one beyond the type's range becomes an infinity, as ozimmu_q4_expand has it), or, for
- * 32-bit types, both operands as two fp16 slices under a power-of-two exponent per row (22 bits and more of every value that is within 2^-17 of its row's largest; the rest to 2^-39
- * of that; the exponent goes with the group for the columns of W). A token or gradient row that holds an infinity or a NaN gives results that are
- * not finite (NaN, also where the formula has an infinity); every other row is what it would be without it. Empty dimensions: t = 0 or no outputs: nothing to do; an empty inner dimension
- * gives zeros. Outputs must not overlap inputs or the workspace.
- * workspace: ozimmu_q4_workspace_bytes(...) bytes, OZIMMU_WORKSPACE_ALIGN-aligned; may be null where that is 0; one for t tokens serves fewer.
- * Errors: OZIMMU_ERR_BAD_DIM (sizes or group), OZIMMU_ERR_BAD_TYPE, OZIMMU_ERR_BAD_LD (also ldq, and any beyond OZIMMU_MAX_LD), OZIMMU_ERR_NULL, OZIMMU_ERR_MISALIGNED,
- * OZIMMU_ERR_WORKSPACE.
+ * X, Y, dY, dX and the scales have type `type`; the sums are formed in 32 bits and rounded once. Up to 16 tokens (and, for 32-bit types,
+ * where ozimmu_q4_workspace_bytes gives 0) ozimmu_q4_gemm multiplies the codes themselves and applies the scales to the sums, in 32 bits.
+ * Products of more tokens, and gradients, may take, as n, k and t have it, the weights s c rounded once to bf16 or fp16 instead (one
+ * beyond the type's range becomes an infinity, as ozimmu_q4_expand has it), or, for 32-bit types, both operands as two fp16 slices under a
+ * power-of-two exponent per row (22 bits and more of every value that is within 2^-17 of its row's largest; the rest to 2^-39 of that; the
+ * exponent goes with the group for the columns of W). So a token's result may differ in its last bits with the number of tokens beside it.
+ * A token or gradient row, or a weight, that is an infinity or a NaN gives results that are not finite (NaN, also where the formula has
+ * an infinity); everything else is what it would be without it. Empty dimensions: t = 0 or no outputs: nothing to do; an empty inner
+ * dimension gives zeros. Outputs must not overlap inputs or the workspace.
+ * workspace: ozimmu_q4_workspace_bytes(...) bytes, OZIMMU_WORKSPACE_ALIGN-aligned; may be null where that is 0; one for t tokens serves
+ * fewer. Errors: OZIMMU_ERR_BAD_DIM (sizes or group), OZIMMU_ERR_BAD_TYPE, OZIMMU_ERR_BAD_LD (also ldq, and any beyond OZIMMU_MAX_LD),
+ * OZIMMU_ERR_NULL, OZIMMU_ERR_MISALIGNED, OZIMMU_ERR_WORKSPACE.
  */
 ozimmu_status_t ozimmu_q4_geometry(int64_t k, int group, int64_t* row_bytes, int64_t* groups);
 ozimmu_status_t ozimmu_q4_split(int64_t n, int64_t k, int group, ozimmu_type_t type, const void* W, int64_t ldw,
@@ -410,14 +412,15 @@ ozimmu_status_t ozimmu_q4_gemm_grad(int64_t t, int64_t n, int64_t k, int group, 
  * where for m > n the iteration runs on the transposed matrix: every singular value s of X_0 becomes p(p(...p(s))),
  * p(x) = a x + b x^3 + c x^5, and the singular vectors stay. (a, b, c) = (3.4445, -4.7750, 2.0315) with five steps takes
  * what is not far below the largest into 0.7 .. 1.2; (1.5, -0.5, 0) is the plain iteration for the nearest orthogonal matrix. G and X
- * have type `type`; X may be G (same strides), and otherwise must not overlap it. The norm is summed in 64 bits. Everything between is held as two fp16 slices under a common power of two
- * (22 bits and more), multiplied as three products with sums in 32 bits: errors are those of an iteration in 32 bits. The result
- * is rounded once. A matrix of zeros gives zeros; one with an infinity or a NaN
- * gives NaN in places that are not specified, and does not touch the others of its batch.
- * steps in 1 .. OZIMMU_MAX_STEPS, eps >= 0 and finite, a >= 1 (small singular values must not shrink: they are held to 2^-38 absolutely, or as
- * much more as intermediate values exceed four), and the polynomial must keep [0, 1] bounded under its iteration, so that no
- * intermediate value exceeds 4096: otherwise OZIMMU_ERR_BAD_POLYNOMIAL. batch <= OZIMMU_MAX_BATCH; matrices of X must not overlap each other.
- * workspace: ozimmu_orthogonalize_workspace_bytes(...) bytes, OZIMMU_WORKSPACE_ALIGN-aligned; may be null where that is 0. m or n or batch = 0: nothing to do.
+ * have type `type`; X may be G (same strides), and otherwise must not overlap it. The norm is summed in 64 bits. Everything between is
+ * held as two fp16 slices under a common power of two (22 bits and more), multiplied as three products with sums in 32 bits: errors are
+ * those of an iteration in 32 bits. The result is rounded once. A matrix of zeros gives zeros; one with an infinity or a NaN gives NaN in
+ * places that are not specified, and does not touch the others of its batch.
+ * steps in 1 .. OZIMMU_MAX_STEPS, eps >= 0 and finite, a >= 1 (small singular values must not shrink: they are held to 2^-38 absolutely,
+ * or as much more as intermediate values exceed four), and the polynomial must keep [0, 1] bounded under its iteration, so that no
+ * intermediate value exceeds 4096: otherwise OZIMMU_ERR_BAD_POLYNOMIAL. batch <= OZIMMU_MAX_BATCH; matrices of X must not overlap each
+ * other. workspace: ozimmu_orthogonalize_workspace_bytes(...) bytes, OZIMMU_WORKSPACE_ALIGN-aligned; may be null where that is 0. m or n
+ * or batch = 0: nothing to do.
  */
 ozimmu_status_t ozimmu_orthogonalize_workspace_bytes(int64_t batch, int64_t m, int64_t n, size_t* bytes);
 ozimmu_status_t ozimmu_orthogonalize(int64_t batch, int64_t m, int64_t n, ozimmu_type_t type, const void* G,

@@ -4,13 +4,13 @@
 // what is below 2^-22 of a term; a slab then holds both slices of 32 positions, so loads and shared memory are the same and only
 // the pairs differ.
 //
-// A workgroup owns a BM x BN tile. A slab of its rows of P and Q is brought into LDS by direct loads (1 KiB = 8 rows a
-// wavefront and load; the lane that fetches 16-byte piece c of row r puts it at place c ^ (r % 8), so that the 16 lanes of a
-// fragment read, ds_read_b128, meet all banks), STAGES - 1 slabs ahead of the one that is multiplied: one barrier per slab. Rows
-// beyond the last are read from the last one and their results dropped.
-// With fewer tiles than run at a time, or a last round of them that is far from full, several workgroups share a tile's inner dimension; their sums go
-// through memory and a second launch adds them up in a fixed order (4096 x 4096 symmetric, 528 tiles of 128 where 512 run at a time: 253 us whole).
-// The fragments of Q are the MFMA's first operand: a lane then holds four consecutive columns of one row of C.
+// A workgroup owns a BM x BN tile. A slab of its rows of P and Q is brought into LDS by direct loads (1 KiB = 8 rows a wavefront and load;
+// the lane that fetches 16-byte piece c of row r puts it at place c ^ (r % 8), so that the 16 lanes of a fragment read, ds_read_b128, meet
+// all banks), STAGES - 1 slabs ahead of the one that is multiplied: one barrier per slab. Rows beyond the last are read from the last one
+// and their results dropped. With fewer tiles than run at a time, or a last round of them that is far from full, several workgroups share a
+// tile's inner dimension; their sums go through memory and a second launch adds them up in a fixed order (4096 x 4096 symmetric, 528 tiles
+// of 128 where 512 run at a time: 253 us whole). The fragments of Q are the MFMA's first operand: a lane then holds four consecutive
+// columns of one row of C.
 #pragma once
 
 #include <algorithm>
@@ -38,8 +38,8 @@ __device__ __forceinline__ void nt_tile(const NtArgs& a, const NtPlan& p, int ti
     }
 }
 
-// What becomes of the sums of four neighbouring elements C[row][col .. col + 3]. Two slices: `both` receives them, the first in the low half; the transposed
-// matrix is the caller's.
+// What becomes of the sums of four neighbouring elements C[row][col .. col + 3]. Two slices: `both` receives them, the first in the low
+// half; the transposed matrix is the caller's.
 template <int RESULT>
 __device__ __forceinline__ void nt_finish(const NtArgs& a, int z, int r, int c, const v4f& acc, unsigned (&both)[4]) {
     if constexpr (RESULT == kOutSlices) {
@@ -92,7 +92,8 @@ __device__ __forceinline__ void nt_finish(const NtArgs& a, int z, int r, int c, 
     }
 }
 
-// When a wavefront reads its fragments of a slab from LDS: in the slab, all of them in the one before, or those that its first MFMAs need in the one before.
+// When a wavefront reads its fragments of a slab from LDS: in the slab, all of them in the one before, or those that its first MFMAs need
+// in the one before.
 enum NtWalk { kReadOnTime, kReadAhead, kFirstReadsAhead };
 
 template <int BM, int BN, int WM, int WN, int STAGES, int WALK, int SLICES, bool BF16, int RESULT>
@@ -168,7 +169,8 @@ __global__ void nt_product_kernel(NtArgs a, NtPlan plan) {
 #pragma unroll
             for (int l = 0; l < LP + LQ; ++l) load(l, i, i);
     if constexpr (WALK == kReadAhead) {
-        // The fragments of the next slab are read from LDS while this one's are multiplied; a slab's stage is requested anew as soon as its fragments are in registers.
+        // The fragments of the next slab are read from LDS while this one's are multiplied; a slab's stage is requested anew as soon as its
+        // fragments are in registers.
         struct Frags {
             v4u p0[MI], p1[MI], q0[NI], q1[NI];
         } f[2];
@@ -217,8 +219,9 @@ __global__ void nt_product_kernel(NtArgs a, NtPlan plan) {
         }
         if (slab < slabs) step(slab, f[0], f[1]);
     } else if constexpr (WALK == kFirstReadsAhead) {
-        // Two stages, two barriers a slab: behind the first nobody reads the other stage any more, and its loads go out between the first rows of MFMAs; behind the
-        // second, near the end, they have landed, and the next slab's first fragments are read under the last MFMAs.
+        // Two stages, two barriers a slab: behind the first nobody reads the other stage any more, and its loads go out between the first
+        // rows of MFMAs; behind the second, near the end, they have landed, and the next slab's first fragments are read under the last
+        // MFMAs.
         static_assert(STAGES == 2 && MI >= 4);
         v4u q0[2][NI], q1[2][NI], p0[2], p1[2];
         auto first_reads = [&](int stage, int to) {
@@ -270,8 +273,8 @@ __global__ void nt_product_kernel(NtArgs a, NtPlan plan) {
     } else {
         int stage = 0;
         for (int slab = 0; slab < slabs; ++slab) {
-            // this wavefront's loads of the slab have landed (later ones may be on their way) and its reads of the stage that is loaded next are done;
-            // behind the barrier, everyone's
+            // this wavefront's loads of the slab have landed (later ones may be on their way) and its reads of the stage that is loaded
+            // next are done; behind the barrier, everyone's
             if (slab + AHEAD <= slabs)
                 asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((AHEAD - 1) * (LP + LQ)) : "memory");
             else
@@ -308,8 +311,9 @@ __global__ void nt_product_kernel(NtArgs a, NtPlan plan) {
         return;
     }
     const int r0 = wm * (BM / WM) + (lane & 15), c0 = wn * (BN / WN) + (lane >> 4) * 4;   // in the tile
-    // The transposed tile goes through LDS, which nobody reads any more: stored from the registers it would be two bytes at a time (4096 x 4096: 27 us of 323). kAtOnce columns of
-    // it fit; value (row, col) lies at row ^ 16 (col / 4 % 4) of its column, so that the four quarters of a wavefront meet different banks.
+    // The transposed tile goes through LDS, which nobody reads any more: stored from the registers it would be two bytes at a time (4096 x
+    // 4096: 27 us of 323). kAtOnce columns of it fit; value (row, col) lies at row ^ 16 (col / 4 % 4) of its column, so that the four
+    // quarters of a wavefront meet different banks.
     constexpr int kAtOnce = STAGES * (BM + BN) * 128 / (BM * 4) < BN ? BN / 2 : BN;
     static_assert(kAtOnce * BM * 4 <= STAGES * (BM + BN) * 128 && kAtOnce % (BN / WN) == 0);
     unsigned* const turned = reinterpret_cast<unsigned*>(lds);
@@ -382,7 +386,8 @@ __global__ void nt_join_kernel(NtArgs a, NtPlan plan) {
     }
 }
 
-// A tile shape as the choice sees it: how many workgroups run at a time, and what a slab takes then and with one workgroup to a compute unit (us).
+// A tile shape as the choice sees it: how many workgroups run at a time, and what a slab takes then and with one workgroup to a compute
+// unit (us).
 struct NtShape {
     int tile, slots;
     double full, alone;
@@ -437,9 +442,10 @@ hipError_t launch_nt_tile(const NtArgs& a, const NtPlan& plan, hipStream_t st) {
     return hipGetLastError();
 }
 
-// A larger tile moves fewer bytes through LDS per product, a smaller one keeps more compute units busy: by an estimate from what a slab takes each shape (two slices, one
-// slice; measured with products of one to four rounds). 64 x 64 tiles come in two forms: with about one workgroup to a compute unit nothing else hides a wavefront's
-// LDS reads, and they run a slab ahead; with more, the registers and LDS of that cost the co-residents that do (2048 x 2048 x 8192, 528 tiles, 131 us against 162).
+// A larger tile moves fewer bytes through LDS per product, a smaller one keeps more compute units busy: by an estimate from what a slab
+// takes each shape (two slices, one slice; measured with products of one to four rounds). 64 x 64 tiles come in two forms: with about one
+// workgroup to a compute unit nothing else hides a wavefront's LDS reads, and they run a slab ahead; with more, the registers and LDS of
+// that cost the co-residents that do (2048 x 2048 x 8192, 528 tiles, 131 us against 162).
 template <int SLICES, bool BF16, int RESULT>
 hipError_t launch_nt(const NtArgs& a, hipStream_t st) {
     if (a.m <= 0 || a.n <= 0 || a.slabs <= 0 || a.batch <= 0 || (a.symmetric && a.m != a.n)) return hipErrorInvalidValue;

@@ -56,8 +56,8 @@ __global__ void norm_partials_kernel(int64_t m, int64_t n, const void* G, int64_
     if (threadIdx.x == 0) partials[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = sum;
 }
 
-// A 64 x 64 tile of G, divided by its norm, in two slices: rows as they lie, and through LDS transposed. The padding of rows is written as zeros. A thread
-// takes 16 values of a row, then of a column: memory-bound, 16-byte accesses throughout.
+// A 64 x 64 tile of G, divided by its norm, in two slices: rows as they lie, and through LDS transposed. The padding of rows is written as
+// zeros. A thread takes 16 values of a row, then of a column: memory-bound, 16-byte accesses throughout.
 template <int TYPE>
 __launch_bounds__(kThreads)
 __global__ void normalised_slices_kernel(int64_t m, int64_t n, const void* G, int64_t ldg, int64_t stride, const double* partials, int parts, double eps,

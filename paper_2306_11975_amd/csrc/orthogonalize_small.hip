@@ -1,9 +1,9 @@
-// The orthogonal update of matrices whose shorter side is at most 64. Up to 256 along the longer one, one workgroup per matrix runs the whole iteration out of LDS; up to 8192,
-// panels (below) (gfx950).
+// The orthogonal update of matrices whose shorter side is at most 64. Up to 256 along the longer one, one workgroup per matrix runs the
+// whole iteration out of LDS; up to 8192, panels (below) (gfx950).
 //
-// As launches of the product kernel the iteration takes 17 of them, about 4 us each whatever the size; here a step is three
-// passes of MFMAs between barriers. In LDS lie, in two slices of fp16 as in nt_product.h (rows in slabs of 128 bytes: 32 positions of the first slice and of the
-// second, 16-byte piece c of row r at place c ^ (r % 8)): X (64 rows along the longer side), its transpose, and A, which the
+// As launches of the product kernel the iteration takes 17 of them, about 4 us each whatever the size; here a step is three passes of MFMAs
+// between barriers. In LDS lie, in two slices of fp16 as in nt_product.h (rows in slabs of 128 bytes: 32 positions of the first slice and
+// of the second, 16-byte piece c of row r at place c ^ (r % 8)): X (64 rows along the longer side), its transpose, and A, which the
 // polynomial of A then replaces. Every pass forms its results in registers, waits for everyone's reads, and writes.
 #include <algorithm>
 
@@ -14,7 +14,8 @@ namespace {
 
 constexpr int kWaves = 8, kThreads = kWaves * 64;
 
-// byte of position `at` in row `row` of an array of `rows` rows, first slice; the second one's piece is 4 places on: bit 6 of the byte changed
+// byte of position `at` in row `row` of an array of `rows` rows, first slice; the second one's piece is 4 places on: bit 6 of the byte
+// changed
 __device__ __forceinline__ unsigned slot(int rows, int row, int at) {
     return (unsigned)((at >> 5) * rows + row) * 128 + (((at & 31) >> 3) ^ (row & 7)) * 16 + (at & 7) * 2;
 }
@@ -63,7 +64,8 @@ __device__ __forceinline__ void gram(const Lane& me, const unsigned char* x_at, 
         for (int j = 0; j < 2; ++j) acc[j] = three(frag(x_at, 64, slab, me.aj + 16 * j, me.frag0), frag(x_at, 64, slab, me.aj + 16 * j, me.frag1), p0, p1, acc[j]);
     }
 }
-// From sums of X X^T to the polynomial of A in A's place. (Nobody reads that place any more; in the end nobody else has read the polynomial yet.)
+// From sums of X X^T to the polynomial of A in A's place. (Nobody reads that place any more; in the end nobody else has read the polynomial
+// yet.)
 __device__ __forceinline__ void polynomial(const Lane& me, unsigned char* a_at, const v4f (&acc)[2], float a, float b, float c, int shift) {
     const float down = ldexpf(1.f, -shift);
     float mine[2][4];
@@ -224,8 +226,9 @@ hipError_t launch_typed(int64_t batch, int64_t m, int64_t n, const void* G, int6
 }
 
 // ---- a longer side beyond that: panels of 128 positions along it, a workgroup each, which leave their part of A = X X^T; one workgroup adds the parts up, in order, and makes the
-// polynomial, and the next launch multiplies the panels by it: two launches a step, against three or four of the products. X (transposed) and the polynomial go through memory as they lie
-// in LDS. What bounds it is latency, 4 to 7 us a launch (64 x 1024: 90 us as products, 56 here; 64 of them 157 and 100).
+// polynomial, and the next launch multiplies the panels by it: two launches a step, against three or four of the products. X (transposed)
+// and the polynomial go through memory as they lie in LDS. What bounds it is latency, 4 to 7 us a launch (64 x 1024: 90 us as products, 56
+// here; 64 of them 157 and 100).
 enum PanelPart { kFirst, kMiddle, kLast };
 
 template <int TYPE, int PART>

@@ -57,8 +57,8 @@ __device__ __forceinline__ int nearest_code(float w, float s, float inv) {
     return (int)fminf(fmaxf(q, -8.f), 7.f);
 }
 
-// The largest magnitude of eight values, as bits: those of |w| order like the values, NaN last, so that one that is there stays visible in the scale. As integers the
-// largest is the largest positive value, as unsigned ones the largest negative one.
+// The largest magnitude of eight values, as bits: those of |w| order like the values, NaN last, so that one that is there stays visible in
+// the scale. As integers the largest is the largest positive value, as unsigned ones the largest negative one.
 __device__ __forceinline__ unsigned top_bits(const float (&w)[8]) {
     int up = 0;
     unsigned down = 0x80000000u;
@@ -79,10 +79,11 @@ __device__ __forceinline__ unsigned max_of_lanes(unsigned x) {
     return x;
 }
 
-// The codes of eight weights as a word. w * (1/s), with a reciprocal that is off by a unit, is off the quotient by less than 2e-6; adding 1.5 * 2^23 rounds it to an integer, ties to
-// even, whose low bits then stand in the low bits of the sum. That is the nearest integer to the quotient unless the product lies within 1e-5 of a border and is
-// not the quotient itself (a tie, which weights of 8 bits often are): then the remainders decide, as they do where a scale that underflowed lets codes leave their range.
-// (Both tests are asked of the wavefront: lane by lane, everyone would pay for them. 8192 x 8192 bf16: with the remainders always 62 us.)
+// The codes of eight weights as a word. w * (1/s), with a reciprocal that is off by a unit, is off the quotient by less than 2e-6; adding
+// 1.5 * 2^23 rounds it to an integer, ties to even, whose low bits then stand in the low bits of the sum. That is the nearest integer to
+// the quotient unless the product lies within 1e-5 of a border and is not the quotient itself (a tie, which weights of 8 bits often are):
+// then the remainders decide, as they do where a scale that underflowed lets codes leave their range. (Both tests are asked of the
+// wavefront: lane by lane, everyone would pay for them. 8192 x 8192 bf16: with the remainders always 62 us.)
 __device__ __forceinline__ unsigned code_word(const float (&w)[8], float s, float top) {
     const float inv = __builtin_amdgcn_rcpf(s);
     float t[8], far = 0.f;
@@ -123,7 +124,8 @@ __device__ __forceinline__ unsigned code_word(const float (&w)[8], float s, floa
     return word;
 }
 
-// max |w| / 7, correctly rounded: the product with the rounded reciprocal, corrected by its remainder; very small ones, whose remainder would underflow, and infinities divided.
+// max |w| / 7, correctly rounded: the product with the rounded reciprocal, corrected by its remainder; very small ones, whose remainder
+// would underflow, and infinities divided.
 __device__ __forceinline__ float seventh(float top) {
     constexpr float r = 1.0f / 7.0f;
     const float q = top * r;
@@ -133,8 +135,8 @@ __device__ __forceinline__ float seventh(float top) {
     return exact;
 }
 
-// A thread cuts eight weights of two rows; the lanes of a group (GROUP / 8 of them, side by side) share its maximum. tx threads along a row.
-// Memory-bound: the weights are read once, 16 or 32 bytes a lane, two rows on their way at a time.
+// A thread cuts eight weights of two rows; the lanes of a group (GROUP / 8 of them, side by side) share its maximum. tx threads along a
+// row. Memory-bound: the weights are read once, 16 or 32 bytes a lane, two rows on their way at a time.
 template <int TYPE, int STYPE, int GROUP>
 __launch_bounds__(kThreads)
 __global__ void q4_split_kernel(int64_t n, int64_t k, const void* W, int64_t ldw, uint8_t* codes, int64_t ldq, void* scales,
@@ -282,8 +284,8 @@ __device__ __forceinline__ int scale_exponent(const float* s, int64_t len, int64
     return exponent_of(block_max(top, shared)) + 3 - kRowShift;
 }
 
-// Rows of W in two slices under an exponent per row, which every workgroup finds for itself: alone on a row its threads share the row's scales, else (rows of less than
-// 2048 positions, at most 64 scales) sixteen lanes do.
+// Rows of W in two slices under an exponent per row, which every workgroup finds for itself: alone on a row its threads share the row's
+// scales, else (rows of less than 2048 positions, at most 64 scales) sixteen lanes do.
 __device__ __forceinline__ void q4_slices(const OperandArgs& a, unsigned block, float* shared) {
     const int64_t row = (int64_t)(block / a.w_across) * (kThreads / a.w_tx) + threadIdx.x / a.w_tx;
     const int64_t at = ((int64_t)(block % a.w_across) * a.w_tx + threadIdx.x % a.w_tx) * 8;
@@ -309,7 +311,10 @@ __device__ __forceinline__ void q4_slices(const OperandArgs& a, unsigned block, 
     store_slices8(a.w_out + row * a.ld, at, x);
 }
 
-// Rows of W rounded to 16 bits.
+// Rows of W rounded to 16 bits: what the matrix cores take of a weight at their full rate, and what an expanded weight is. (Scales on the
+// sums instead, as the passes have them, take a second set of sums, which the product's tiles have no registers for; a second slice of
+// every weight takes twice the products. Against results of exact weights, rounded: bf16 0.0021 and 0.0017 in the norm, fp16 0.00028 and
+// 0.00021.)
 template <int TYPE>
 __device__ __forceinline__ void q4_rows(const OperandArgs& a, unsigned block) {
     typedef Elem<TYPE> E;
@@ -326,8 +331,9 @@ __device__ __forceinline__ void q4_rows(const OperandArgs& a, unsigned block) {
     store8<TYPE>(a.w_out + row * a.ld, at, at + 8, x);
 }
 
-// Columns of W as rows along n, rounded to 16 bits or (OZIMMU_F32) in two slices under the exponent of the column's group: a tile of 64 rows and WIDTH positions
-// through LDS, where eight values of position l lie at place (their eighth) ^ (l / 8 % 8). A thread takes pairs of rows.
+// Columns of W as rows along n, rounded to 16 bits or (OZIMMU_F32) in two slices under the exponent of the column's group: a tile of 64
+// rows and WIDTH positions through LDS, where eight values of position l lie at place (their eighth) ^ (l / 8 % 8). A thread takes pairs of
+// rows.
 template <int TYPE, int WIDTH>
 __device__ __forceinline__ void q4_columns(const OperandArgs& a, unsigned block, unsigned short* tile) {
     typedef Elem<TYPE> E;
@@ -433,18 +439,20 @@ __global__ void zero_rows_kernel(int64_t rows, int64_t cols, T* R, int64_t ld) {
     if (at < cols) R[row * ld + at] = T(0);
 }
 
-// Threads along a row of `chunks` pieces: a power of two of at least 16 (the lanes of the largest group), so that short rows share a workgroup.
+// Threads along a row of `chunks` pieces: a power of two of at least 16 (the lanes of the largest group), so that short rows share a
+// workgroup.
 int threads_along(int64_t chunks) {
     int tx = 16;
     while (tx < kThreads && tx < chunks) tx *= 2;
     return tx;
 }
-// Workgroups over `rows` rows of `chunks` pieces, tx threads along a row: numbered along the rows, so that those that run together read memory in order (by columns first:
-// 8192 x 8192 bf16 cut in 62 us).
+// Workgroups over `rows` rows of `chunks` pieces, tx threads along a row: numbered along the rows, so that those that run together read
+// memory in order (by columns first: 8192 x 8192 bf16 cut in 62 us).
 unsigned across_of(int64_t chunks, int tx) { return (unsigned)((chunks + tx - 1) / tx); }
 int64_t blocks_for(int64_t rows, int64_t chunks, int tx) { return (rows + kThreads / tx - 1) / (kThreads / tx) * (int64_t)across_of(chunks, tx); }
-// A launch has fewer than 2^32 threads along its first dimension, which 2^35 weights are beyond (4194304 x 8192, 16 GiB of codes): workgroups go out in launches of at
-// most kMostBlocks, of a millisecond each. launch(workgroups, the first one's number).
+// A launch has fewer than 2^32 threads along its first dimension (of more the runtime starts a part, without an error), which 2^35 weights
+// are beyond (4194304 x 8192, 16 GiB of codes): workgroups go out in launches of at most kMostBlocks, of a millisecond each.
+// launch(workgroups, the first one's number).
 constexpr int64_t kMostBlocks = 1 << 21;
 template <class F>
 hipError_t in_launches(int64_t blocks, F launch) {
@@ -540,7 +548,8 @@ hipError_t launch_operands(int64_t t, int64_t n, int64_t k, int group, int type,
     a.v_out = v_out;
     a.v_exps = v_exps;
     const bool f32 = type == OZIMMU_F32;
-    // Wide tiles read and write whole lines (8192 x 4096 in 16 bits 24 us with 64 positions, 18 with 256); narrow ones are more workgroups where there are few.
+    // Wide tiles read and write whole lines (8192 x 4096 in 16 bits 24 us with 64 positions, 18 with 256); narrow ones are more workgroups
+    // where there are few.
     const int most = f32 ? 128 : 256;
     const int width = (n + 63) / 64 * ((k + most - 1) / most) >= 1024 ? most : 64;
     int64_t w_blocks, v_blocks = 0;

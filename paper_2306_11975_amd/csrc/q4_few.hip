@@ -17,7 +17,8 @@
 // a code of zero adds nothing to it. bf16: the conversion from four signed bits gives a code's sixteenth in 32 bits, whose upper half is
 // all of it; two halves make a word of the operand, and the result is multiplied by 16. fp16: the four bits of c + 8 go into the mantissa
 // of 1024, and a packed addition takes 1032 away. (With the offset left in and the tokens' product with it taken off the sums, an MFMA
-// more, sums of fp16 tokens lose half their bits next to a value of 6e4; 64 tokens, 16384 x 8192, groups of 32, 65.5 us against 60.9 here.)
+// more, the roundings of both sums stay behind: fp16 tokens with a value of 6e4 over a code of zero were off by several roundings of the
+// result. 64 tokens, 16384 x 8192, groups of 32, 65.5 us so, 60.9 here.)
 // 32-bit tokens are cut into three bf16 (exactly), three MFMAs. The scale of a group is applied to its sum in 32 bits.
 #include "half_common.h"
 
@@ -68,7 +69,8 @@ __device__ __forceinline__ float sixteenth(unsigned w) {
         asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(x) : "v"(w));
     return x;
 }
-// The codes' sixteenths in bf16, in order, exactly: the conversion from four signed bits gives them in 32 bits, and they fit the upper half.
+// The codes' sixteenths in bf16, in order, exactly: the conversion from four signed bits gives them in 32 bits, and they fit the upper
+// half.
 __device__ __forceinline__ v4u sixteenths_bf16(unsigned w) {
     w ^= 0x88888888u;
     const unsigned high = w >> 4;
@@ -133,15 +135,16 @@ __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t n0 = (int64_t)blockIdx.x * (16 * NT);
     const int t0 = blockIdx.y * (16 * TT);
-    // Whole steps are dealt to the wavefronts in turn (together they read lines in full); the last wavefront takes what is left of the row beyond them too.
+    // Whole steps are dealt to the wavefronts in turn (together they read lines in full); the last wavefront takes what is left of the row
+    // beyond them too.
     const int full = (int)(k / 128);
     const int mine = (full - wave + W - 1) / W;
     const int quarter = lane >> 4;
     // position of word j of group h in a step, for this lane (the exchange between quarters below)
     const int at_quarter = GROUP == 128 ? 32 * quarter : GROUP == 64 ? 32 * (quarter & 1) + 16 * (quarter >> 1) : 8 * quarter;
-    // In LDS 16-byte piece p of row r lies at place p ^ r % 16 (codes: p ^ r / 4 % 4), so that the 16 rows of a fragment meet different banks.
-    // Addresses are a scalar base and a lane's 32-bit offset (rows are at most OZIMMU_MAX_LD apart). Rows of weights that are not there repeat the last one: their
-    // results go nowhere. Tokens that are not there are not loaded: neither do theirs.
+    // In LDS 16-byte piece p of row r lies at place p ^ r % 16 (codes: p ^ r / 4 % 4), so that the 16 rows of a fragment meet different
+    // banks. Addresses are a scalar base and a lane's 32-bit offset (rows are at most OZIMMU_MAX_LD apart). Rows of weights that are not
+    // there repeat the last one: their results go nowhere. Tokens that are not there are not loaded: neither do theirs.
     const raw* xb = reinterpret_cast<const raw*>(X) + (int64_t)min(t0, t - 1) * ldx;
     const uint8_t* qb = codes + n0 * ldq;
     const raw* sb = reinterpret_cast<const raw*>(scales) + n0 * lds;
@@ -181,7 +184,8 @@ __global__ void q4_few_kernel(int t, int64_t n, int64_t k, const void* X, int64_
         for (int i = 0; i < kLoads; ++i)
             if (kRows * i < tokens_here) to[i] = *reinterpret_cast<const v4u_any*>(from(xb, (int64_t)step * kTokenRow, xo[i]));
     };
-    // The same where a row ends inside the step: tokens beyond k are zeros, so any finite code will do there (rows take a multiple of 16 bytes).
+    // The same where a row ends inside the step: tokens beyond k are zeros, so any finite code will do there (rows take a multiple of 16
+    // bytes).
     auto load_last_codes = [&](v4u (&w)[NT], raw (&sc)[NT][GROUPS]) {
         const int64_t last = pad_to(k, 32) / 2 - 16;
         const int groups = (int)((k + GROUP - 1) / GROUP);
@@ -349,17 +353,18 @@ hipError_t launch_tiles(int64_t t, int64_t n, int64_t k, const void* X, int64_t 
 template <int TYPE, int GROUP>
 hipError_t launch_typed(int64_t t, int64_t n, int64_t k, const void* X, int64_t ldx, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds,
                         void* Y, int64_t ldy, hipStream_t st) {
-    // The smallest tile with which a workgroup has a compute unit to itself: more rows of W or tokens to a wavefront share operands and loads, fewer keep more compute units busy. (bf16, us,
-    // rows x tokens 16 x 16, 32 x 16, 64 x 16, 32 x 32: 16 tokens, 4096 x 11008 13.0, 15.2, 19.0, 18.4; 16384 x 8192 27.8, 26.0, 19.9, 29.8; 64 tokens, 2048 x 16384 24.9, 22.4,
-    // 29.7, 27.0; 8192 x 4096 26.9, 28.5, 20.8, 19.0.) Two tiles of tokens take registers that 32-bit tokens do not leave. The smallest has sixteen wavefronts along a long k (2048 x
-    // 16384, 16 tokens: 14.0 against 17.6).
+    // The smallest tile with which a workgroup has a compute unit to itself: more rows of W or tokens to a wavefront share operands and
+    // loads, fewer keep more compute units busy. (bf16, us, rows x tokens 16 x 16, 32 x 16, 64 x 16, 32 x 32: 16 tokens, 4096 x 11008 13.0,
+    // 15.6, 21.2, 17.7; 16384 x 8192 27.1, 21.4, 20.3, 28.8; 64 tokens, 2048 x 16384 22.5, 21.5, 30.9, 25.8; 8192 x 4096 25.7, 21.8, 21.5,
+    // 18.0.) Two tiles of tokens take registers that 32-bit tokens do not leave. The smallest has sixteen wavefronts along a long k (2048 x
+    // 16384, 16 tokens: 12.7 against 16.4).
     const auto fits = [&](int64_t rows, int64_t tokens) { return ((n + rows - 1) / rows) * ((t + tokens - 1) / tokens) <= kComputeUnits; };
     if constexpr (TYPE != OZIMMU_F32) {
         if (fits(16, 16) && k >= 16 * 128) return launch_tiles<TYPE, GROUP, 1, 1, 16>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
     }
     if (fits(16, 16)) return launch_tiles<TYPE, GROUP, 1, 1, 8>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
-    // (32-bit types in groups of 32 hold four scales a step and row: with four tiles of rows the registers do not suffice. 16 tokens, 16384 x 8192 47.6 and 48.2, 8192 x 4096
-    // 13.6 and 25.1.)
+    // (32-bit types in groups of 32 hold four scales a step and row: with four tiles of rows the registers do not suffice. 16 tokens, 16384
+    // x 8192 42.8 and 45.5 us, 8192 x 4096 13.0 and 24.4.)
     if constexpr (TYPE == OZIMMU_F32 && GROUP == 32) {
         return launch_tiles<TYPE, GROUP, 2, 1, 8>(t, n, k, X, ldx, codes, ldq, scales, lds, Y, ldy, st);
     } else {

@@ -1,16 +1,19 @@
-// Y = X W^T of weights in four bits with 16-bit tokens, tile by tile, the operand of the weights made on the way (gfx950). One launch, no workspace.
+// Y = X W^T of weights in four bits with 16-bit tokens, tile by tile, the operand of the weights made on the way (gfx950). One launch, no
+// workspace.
 //
-// A workgroup owns BM tokens x BN outputs; a slab is 64 positions of k. What a slab takes from memory is on its way in registers several slabs ahead:
-// 16 bytes a lane of the tokens, and codes with their scales. A slab's codes become the weights s c, rounded once to 16 bits (as they are where the weights'
-// operand is made by a pass of its own), and go to LDS beside the tokens, in the layout of nt_product.h: rows of 128 bytes, 16-byte piece p of row r at place
-// p ^ (r % 8), which the fragments' reads (16 rows, one piece) meet without bank conflicts.
+// A workgroup owns BM tokens x BN outputs; a slab is 64 positions of k. What a slab takes from memory is on its way in registers several
+// slabs ahead: 16 bytes a lane of the tokens, and codes with their scales. A slab's codes become the weights s c, rounded once to 16 bits
+// (as they are where the weights' operand is made by a pass of its own), and go to LDS beside the tokens, in the layout of nt_product.h:
+// rows of 128 bytes, 16-byte piece p of row r at place p ^ (r % 8), which the fragments' reads (16 rows, one piece) meet without bank
+// conflicts.
 //
-// Against the passes of q4_few.hip (32 tokens each): the codes are converted once for BM tokens and take one MFMA, not two. Against a pass that writes the
-// operand and a product that reads it: four times fewer bytes of the weights come and none go; every tile of tokens converts the codes again. So it serves the
-// counts between the two. us in bf16, of the passes, here, of operand and product: 300 tokens through 8192 x 4096 82, 57, 63; 128 through 16384 x 8192 122, 86, 160, 256
-// (128 x 128 tiles from here) 247, 128, 217, 512 453, 185, 237; 128 through 5000 x 200 10.8, 5.9, 8.5; 512 through 20000 x 64 110, 11.7, 15.7. What bounds it is a
-// workgroup's walk: 0.5 us a slab of 64 x 64 (0.95 of 128 x 128), of which the conversion, in the same wavefronts as the MFMAs, takes more than half.
-// (dX = dY W, whose codes lie across the inner dimension, gains nothing so: 128 x 8192 x 4096 83 us against 38.)
+// Against the passes of q4_few.hip (32 tokens each): the codes are converted once for BM tokens and take one MFMA, not two. Against a pass
+// that writes the operand and a product that reads it: four times fewer bytes of the weights come and none go; every tile of tokens
+// converts the codes again. So it serves the counts between the two. us in bf16, of the passes, here, of operand and product: 300 tokens
+// through 8192 x 4096 83, 60, 65; 128 through 16384 x 8192 119, 88, 156, 256 (128 x 128 tiles from here) 234, 128, 222, 512 439, 198, 238;
+// 128 through 5000 x 200 11.2, 6.4, 8.9; 512 through 20000 x 64 109, 12.0, 16.0. What bounds it is a workgroup's walk: 0.5 us a slab of 64
+// x 64 (0.95 of 128 x 128), of which the conversion, in the same wavefronts as the MFMAs, takes more than half. (dX = dY W, whose codes lie
+// across the inner dimension, gains nothing so: 128 x 8192 x 4096 83 us against 38.)
 #include "half_common.h"
 
 namespace ozimmu {
@@ -35,7 +38,8 @@ struct TileArgs {
 // Code e of a word whose codes have been turned into signed ones (c + 8 with its highest bit changed).
 __device__ __forceinline__ float code_of(unsigned word, int e) { return (float)((int)(word << (28 - 4 * e)) >> 28); }
 
-// The eight weights s c of a word, rounded to 16 bits. bf16: in order; fp16: paired (0, 4), (1, 5), (2, 6), (3, 7).
+// The eight weights s c of a word, rounded to 16 bits (why: q4_rows of q4.hip). bf16: in order; fp16: paired (0, 4), (1, 5), (2, 6), (3,
+// 7).
 template <int TYPE>
 __device__ __forceinline__ v4u weights_of(unsigned word, unsigned short scale) {
     v4u r;

@@ -1,15 +1,16 @@
 // Y = X W^T for one token or two and weights in four bits: one pass over the codes on the vector units, no workspace (gfx950).
 //
-// What bounds it is reading the codes, half a byte for 2 T operations, so the loads come first: a row's codes are read along the row, 16 bytes a lane, 16 lanes side
-// by side, and four rows a load. (The matrix cores want neighbouring lanes in different rows, and such a load looks up a line for every lane: q4_few.hip.) A lane's
-// 32 positions lie in one group; it multiplies them itself, and lanes add up at the end, within rows of sixteen. The tokens' piece of 512 positions is loaded once a
-// wavefront, eight values a lane, and goes through LDS to the lanes that need it.
-// A wavefront takes 4 R rows and every W-th piece; the W of a workgroup add their parts up in LDS.
+// What bounds it is reading the codes, half a byte for 2 T operations, so the loads come first: a row's codes are read along the row, 16
+// bytes a lane, 16 lanes side by side, and four rows a load. (The matrix cores want neighbouring lanes in different rows, and such a load
+// looks up a line for every lane: q4_few.hip.) A lane's 32 positions lie in one group; it multiplies them itself, and lanes add up at the
+// end, within rows of sixteen. The tokens' piece of 512 positions is loaded once a wavefront, eight values a lane, and goes through LDS to
+// the lanes that need it. A wavefront takes 4 R rows and every W-th piece; the W of a workgroup add their parts up in LDS.
 //
-// A code's sixteenth is one conversion (v_cvt_off_f32_i4, exact), a product one fma in 32 bits; the scale goes on a lane's sum of 32 products. Two and a quarter
-// instructions a code with one token: 4 us of the vector units for 16384 x 8192, beside the 17.3 us that its 71 MB take (4.1 TB/s).
-// Measured (us; on the matrix cores -> here, one token, bf16): 2048 x 2048 3.9 -> 2.9, 1024 x 8192 7.7 -> 3.6, 2048 x 16384 14.5 -> 6.8, 8192 x 4096 7.4 -> 5.4,
-// 11008 x 4096 12.2 -> 6.8, 16384 x 8192 20.6 -> 17.3, 8 x 65536 34.3 -> 10.4; 32 bits 2048 x 2048 5.4 -> 2.9, 16384 x 8192 36.4 -> 15.8.
+// A code's sixteenth is one conversion (v_cvt_off_f32_i4, exact), a product one fma in 32 bits; the scale goes on a lane's sum of 32
+// products. Two and a quarter instructions a code with one token: 4 us of the vector units for 16384 x 8192, beside the 17.3 us that its 71
+// MB take (4.1 TB/s). Measured (us; on the matrix cores -> here, one token, bf16): 2048 x 2048 3.9 -> 2.9, 1024 x 8192 7.7 -> 3.6, 2048 x
+// 16384 14.5 -> 6.8, 8192 x 4096 7.4 -> 5.4, 11008 x 4096 12.2 -> 6.8, 16384 x 8192 20.6 -> 17.3, 8 x 65536 34.3 -> 10.4; 32 bits 2048 x
+// 2048 5.4 -> 2.9, 16384 x 8192 36.4 -> 15.8.
 #include <type_traits>
 
 #include "half_common.h"
@@ -94,7 +95,8 @@ __global__ void q4_token_kernel(int t, int64_t n, int64_t k, const void* X, int6
 #pragma unroll
         for (int r = 0; r < R; ++r) total[i][r] = 0.f;
     auto multiply = [&](const Step& s) {
-        // the tokens to the lanes that multiply them: chunk c of eight values, from lane c, is word c % 4 of lane c / 4 (of sixteen), at place 16 (c % 4) + c / 4
+        // the tokens to the lanes that multiply them: chunk c of eight values, from lane c, is word c % 4 of lane c / 4 (of sixteen), at
+        // place 16 (c % 4) + c / 4
 #pragma unroll
         for (int i = 0; i < T; ++i)
 #pragma unroll
@@ -176,8 +178,9 @@ hipError_t launch_rows(int64_t t, int64_t n, int64_t k, int group, const void* X
                                                                                                     group == 32 ? 5 : group == 64 ? 6 : 7, Y, ldy);
     return hipGetLastError();
 }
-// More rows to a wavefront: the tokens go through LDS less often; more workgroups and wavefronts along k: more codes on their way. (One token, bf16, R and W 1 and 8, 2 and 8,
-// 2 and 4: 1024 x 8192 3.6, 4.0, 4.7 us; 4096 x 4096 4.4, 3.8, 4.1; 11008 x 4096 7.9, 6.9, 6.8; 16384 x 8192 in 32 bits 20.0, 18.0, 15.8.)
+// More rows to a wavefront: the tokens go through LDS less often; more workgroups and wavefronts along k: more codes on their way. (One
+// token, bf16, R and W 1 and 8, 2 and 8, 2 and 4: 1024 x 8192 3.6, 4.0, 4.7 us; 4096 x 4096 4.4, 3.8, 4.1; 11008 x 4096 7.9, 6.9, 6.8;
+// 16384 x 8192 in 32 bits 20.0, 18.0, 15.8.)
 template <int TYPE, int T>
 hipError_t launch_typed(int64_t t, int64_t n, int64_t k, int group, const void* X, int64_t ldx, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds,
                         void* Y, int64_t ldy, hipStream_t st) {

@@ -1,5 +1,5 @@
-// C ABI of the operators on weight matrices: argument checks, workspace layout and kernel sequencing. What computes is in
-// q4.hip, q4_few.hip, orthogonalize.hip and nt_product.h.
+// C ABI of the operators on weight matrices: argument checks, workspace layout, choice and sequencing of kernels. What computes is in
+// q4.hip, q4_token.hip, q4_few.hip, q4_tile.hip, orthogonalize.hip, orthogonalize_small.hip and nt_product.h.
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
@@ -31,7 +31,8 @@ ozimmu_status_t check_q4(int64_t k, int group, const void* codes, int64_t ldq, c
     return OZIMMU_OK;
 }
 
-// Room for the sums of shared tiles (nt_choose): at most 32 workgroups share one, four slabs at least to each, and no product takes more than kPartialBytes.
+// Room for the sums of shared tiles (nt_choose): at most 32 workgroups share one, four slabs at least to each, and no product takes more
+// than kPartialBytes.
 size_t partial_room(int64_t batch, int64_t m, int64_t n, int64_t slabs) {
     const int64_t parts = std::min<int64_t>(32, slabs / 4);
     if (parts < 2) return 0;
@@ -39,7 +40,8 @@ size_t partial_room(int64_t batch, int64_t m, int64_t n, int64_t slabs) {
     return bytes < (double)kPartialBytes ? (size_t)bytes : kPartialBytes;
 }
 
-// The operands of a product with many tokens in the workspace: V (t rows of `inner` values) and the weights (`outer` rows). 32-bit types take two slices.
+// The operands of a product with many tokens in the workspace: V (t rows of `inner` values) and the weights (`outer` rows). 32-bit types
+// take two slices.
 struct Operands {
     int64_t inner, outer, ld;
     size_t off_v, off_w, off_ev, off_ew, off_partial, partial, total;
@@ -64,21 +66,25 @@ Operands operands(int64_t t, int64_t n, int64_t k, int group, int type, bool gra
     o.total = off;
     return o;
 }
-// How Y = X W^T is computed: for one token or two on the vector units (q4_token.hip); by passes over the codes on the matrix cores, 16 or 32 tokens each
-// (q4_few.hip); tile by tile, the weights' operand made on the way (q4_tile.hip, 16-bit types); or as an operand of the weights and the tiled product
-// (nt_product.h), which gradients take always.
+// How Y = X W^T is computed: for one token or two on the vector units (q4_token.hip); by passes over the codes on the matrix cores, 16 or
+// 32 tokens each (q4_few.hip); tile by tile, the weights' operand made on the way (q4_tile.hip, 16-bit types); or as an operand of the
+// weights and the tiled product (nt_product.h), which gradients take always.
 //
-// One token through rows of 512 positions and more is faster on the vector units everywhere, two tokens but for wide layers in bf16 (two, passes and vector units, us:
-// 2048 x 2048 4.5, 3.4; 4096 x 11008 bf16 8.7, 12.1, 32 bits 18.5, 12.0; 16384 x 8192 bf16 18.3, 22.7; one through 512 x 256 2.5, 2.9). From there on the choice is by
-// an estimate of each, in us. 256 workgroups of the passes (32 rows of weights and 32 tokens; 64 and 16 in 32 bits, 32 and 16 with groups of 32) are a round, whose time grows with k. A tile's walk
-// takes half a microsecond a slab of 64 positions (twice that the large ones) until the chip has more than one workgroup for a compute unit. The product takes a walk
-// along k, the operand's bytes, dearer once no cache holds them, and its own operations. Fitted to 24 to 2048 tokens through fifteen layers from 20000 x 64 and
-// 1000 x 333 to 16384 x 8192, where the choices take 0.6 % more than the best ones do on average, 24 % at most. Times of passes, tiles, large tiles, product:
-// bf16 2048 x 2048, 64 tokens 6.7, 18.5, 33.0, 17.0, 512 23.5, 19.4, 33.5, 20.0; 8192 x 4096, 64 19.4, 34.0, 61.9, 38.7, 256 67.5, 44.5, 62.5, 47.4, 1024 250, 137, 94,
-// 78; 16384 x 8192, 128 122, 86, 121, 160, 512 453, 278, 185, 237; 32 bits 16384 x 8192, 128 234, -, -, 316; 8192 x 4096, 384 194, -, -, 111.
+// One token through rows of 512 positions and more is faster on the vector units everywhere, two tokens but for wide layers in bf16 (two,
+// passes and vector units, us: 2048 x 2048 4.5, 3.4; 4096 x 11008 bf16 8.7, 12.1, 32 bits 18.5, 12.0; 16384 x 8192 bf16 18.3, 22.7; one
+// through 512 x 256 2.5, 2.9). From there on the choice is by an estimate of each, in us. 256 workgroups of the passes (32 rows of weights
+// and 32 tokens; 64 and 16 in 32 bits, 32 and 16 with groups of 32) are a round, whose time grows with k. A tile's walk takes half a
+// microsecond a slab of 64 positions (twice that the large ones) until the chip has more than one workgroup for a compute unit. The product
+// takes a walk along k, the operand's bytes, dearer once no cache holds them, and its own operations. Fitted to 24 to 2048 tokens through
+// fifteen layers from 20000 x 64 and 1000 x 333 to 16384 x 8192, where the choices take 0.9 % more than the best ones do on average, 21 %
+// at most (1024 tokens, 16384 x 8192: large tiles 382, product 317), and 28 % with groups of 32 in 32 bits. Times of passes, tiles, large
+// tiles, product: bf16 2048 x 2048, 64 tokens 7.0, 19.4, 33.7, 17.3, 512 23.4, 20.2, 34.2, 20.4; 8192 x 4096, 64 19.4, 35.3, 62.8, 39.2,
+// 256 67.7, 47.3, 64.4, 49.6, 1024 254, 147, 103, 84; 16384 x 8192, 128 119, 88, 123, 156, 512 439, 295, 198, 238; 32 bits 16384 x 8192,
+// 128 226, -, -, 319; 8192 x 4096, 384 191, -, -, 116.
 //
-// With more tokens the answer turns to the product once and stays, so that a workspace serves fewer tokens too: every estimate rises with the tokens at least as
-// the product's does. (The passes are held against the product of their round's first tokens; `more` is added to the tiles' flat part.)
+// With more tokens the answer turns to the product once and stays, so that a workspace serves fewer tokens too: every estimate rises with
+// the tokens at least as the product's does. (The passes are held against the product of their round's first tokens; `more` is added to the
+// tiles' flat part.)
 enum class Way { token, passes, tiles, large_tiles, product };
 Way way_of(int64_t t, int64_t n, int64_t k, int group, int type, bool gradient) {
     if (gradient) return Way::product;
@@ -130,11 +136,11 @@ ozimmu_status_t q4_product(bool gradient, int64_t t, int64_t n, int64_t k, int g
     unsigned short* w = reinterpret_cast<unsigned short*>(base + o.off_w);
     int* ew = reinterpret_cast<int*>(base + o.off_ew);
     int* ev = reinterpret_cast<int*>(base + o.off_ev);
-    NtArgs a{};
     unsigned short* v = reinterpret_cast<unsigned short*>(base + o.off_v);
     // rows of 16-bit values that the kernel can read as they lie need no copy
     const bool in_place = type != OZIMMU_F32 && inner % kSlabValues == 0 && ldv < kMaxInPlaceLd && rows_aligned16(V, ldv, 2);
     hipError_t e = launch_operands(t, n, k, group, type, codes, ldq, scales, lds, gradient, w, ew, V, ldv, in_place ? nullptr : v, ev, o.ld, st);
+    NtArgs a{};
     a.P = in_place ? static_cast<const unsigned short*>(V) : v;
     a.ldp = in_place ? ldv : o.ld;
     a.Q = w;
@@ -158,8 +164,8 @@ ozimmu_status_t q4_product(bool gradient, int64_t t, int64_t n, int64_t k, int g
     return hip_status(e);
 }
 
-// Buffers of the orthogonal update, all in two slices: X as rows along the longer side, its transpose twice (one is read while the next is written), A
-// and the polynomial.
+// Buffers of the orthogonal update, all in two slices: X as rows along the longer side, its transpose twice (one is read while the next is
+// written), A and the polynomial.
 struct OrthLayout {
     int64_t r, l;              // shorter and longer side
     int64_t ld_x, ld_t;        // values per row: along the longer side, along the shorter one
@@ -204,14 +210,15 @@ NarrowLayout narrow_layout(int64_t batch, int64_t m, int64_t n) {
     o.total = off;
     return o;
 }
-// A shorter side of up to 64: panels, two launches a step, up to the length where one workgroup's sum of their parts takes what that saves (us, products and panels: 64 x 257 82
-// and 48, 64 x 1024 90 and 56, 64 x 4096 125 and 75, 32 x 8192 122 and 99, 64 x 16384 151 and 157; 64 of 64 x 1024 157 and 100).
+// A shorter side of up to 64: panels, two launches a step, up to the length where one workgroup's sum of their parts takes what that saves
+// (us, products and panels: 64 x 257 82 and 48, 64 x 1024 90 and 56, 64 x 4096 125 and 75, 32 x 8192 122 and 99, 64 x 16384 151 and 157; 64
+// of 64 x 1024 157 and 100).
 bool narrow_update(int64_t m, int64_t n) { return std::min(m, n) <= kSmallShorter && std::max(m, n) <= kNarrowLonger; }
 
 bool small_update(int64_t m, int64_t n) { return std::min(m, n) <= kSmallShorter && std::max(m, n) <= kSmallLonger; }
 
-// The power of two that slices of fp16 hold the iterates under: the largest up to 2^14 with which nothing overflows. The singular
-// values start at most at one, p(x) = a x + b x^3 + c x^5 takes [0, r] into [0, max |p|], and no element of X, A = X X^T or a + b A + c A^2 is
+// The power of two that slices of fp16 hold the iterates under: the largest up to 2^14 with which nothing overflows. The singular values
+// start at most at one, p(x) = a x + b x^3 + c x^5 takes [0, r] into [0, max |p|], and no element of X, A = X X^T or a + b A + c A^2 is
 // larger than its matrix's norm. -1: there is none, or a < 1: small values would shrink towards the 2^-25 that the slices leave of it.
 int slice_shift(int steps, double a, double b, double c) {
     if (!(a >= 1.0)) return -1;

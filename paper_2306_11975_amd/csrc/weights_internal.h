@@ -10,8 +10,8 @@
 
 namespace ozimmu {
 
-// A matrix of 16-bit values as the product kernel reads it: rows along the inner dimension, in slabs of 64 values (128 bytes). With one slice a slab
-// is 64 positions; with two it is 32 positions of the first slice and the same 32 of the second (value = first + second).
+// A matrix of 16-bit values as the product kernel reads it: rows along the inner dimension, in slabs of 64 values (128 bytes). With one
+// slice a slab is 64 positions; with two it is 32 positions of the first slice and the same 32 of the second (value = first + second).
 constexpr int kSlabValues = 64;
 
 // C = P Q^T on the 16-bit matrix cores (both operands rows along the inner dimension), with what becomes of the sums.
@@ -58,8 +58,9 @@ hipError_t launch_q4_split(int64_t n, int64_t k, int group, const void* W, int t
 // The weights s c as a typed matrix.
 hipError_t launch_q4_expand(int64_t n, int64_t k, int group, const uint8_t* codes, int64_t ldq, const void* scales, int type,
                             int64_t lds, void* W, int64_t ldw, hipStream_t st);
-// The operands of a product of many tokens, rows of ld values: the weights (`columns`: their columns) and, where v_out is not null, the rows of V. 16-bit types: one
-// slice, padded to slabs. OZIMMU_F32: two slices of fp16 scaled by 2^-exponent: one exponent per row, for columns of W one per group.
+// The operands of a product of many tokens, rows of ld values: the weights (`columns`: their columns) and, where v_out is not null, the
+// rows of V. 16-bit types: one slice, padded to slabs. OZIMMU_F32: two slices of fp16 scaled by 2^-exponent: one exponent per row, for
+// columns of W one per group.
 hipError_t launch_operands(int64_t t, int64_t n, int64_t k, int group, int type, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds, bool columns,
                            unsigned short* w_out, int* w_exps, const void* V, int64_t ldv, unsigned short* v_out, int* v_exps, int64_t ld, hipStream_t st);
 // Zeros into a typed matrix.
@@ -71,7 +72,8 @@ hipError_t launch_q4_token(int64_t t, int64_t n, int64_t k, int group, const voi
 hipError_t launch_q4_few(int64_t t, int64_t n, int64_t k, int group, const void* X, int type, int64_t ldx, const uint8_t* codes,
                          int64_t ldq, const void* scales, int64_t lds, void* Y, int64_t ldy, hipStream_t st);
 
-// q4_tile.hip: Y = X W^T of 16-bit types and k >= 8 for more tokens, the operand of the weights made tile by tile (64 x 64, or `large`: 128 x 128)
+// q4_tile.hip: Y = X W^T of 16-bit types and k >= 8 for more tokens, the operand of the weights made tile by tile (64 x 64, or `large`: 128
+// x 128)
 hipError_t launch_q4_tiles(bool large, int64_t t, int64_t n, int64_t k, int group, const void* X, int type, int64_t ldx, const uint8_t* codes, int64_t ldq,
                            const void* scales, int64_t lds, void* Y, int64_t ldy, hipStream_t st);
 
@@ -90,8 +92,8 @@ constexpr int64_t kSmallShorter = 64, kSmallLonger = 256;
 hipError_t launch_orthogonalize_small(int64_t batch, int64_t m, int64_t n, const void* G, int type, int64_t ldg, int64_t stride_g, void* X, int64_t ldx,
                                       int64_t stride_x, int steps, double a, double b, double c, double eps, int shift, hipStream_t st);
 
-// The same for longer ones, in panels of kNarrowPanel positions: `images` holds kNarrowPanel * 256 bytes and `sums` 64 * 64 values for every panel of every matrix, `factors` 64 * 64 * 4 bytes
-// for every matrix
+// The same for longer ones, in panels of kNarrowPanel positions: `images` holds kNarrowPanel * 256 bytes and `sums` 64 * 64 values for
+// every panel of every matrix, `factors` 64 * 64 * 4 bytes for every matrix
 constexpr int kNarrowPanel = 128;
 constexpr int64_t kNarrowLonger = 8192;
 hipError_t launch_orthogonalize_narrow(int64_t batch, int64_t m, int64_t n, const void* G, int type, int64_t ldg, int64_t stride_g, void* X, int64_t ldx,

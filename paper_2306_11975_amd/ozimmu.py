@@ -598,6 +598,7 @@ def orthogonalize_workspace_bytes(batch: int, m: int, n: int) -> int:
 
 
 def alloc_orthogonalize_workspace(batch: int, m: int, n: int, dtype=None, device="cuda"):
+    """A uint8 tensor of the size that orthogonalize asks for. (`dtype`, the matrices' type, does not change it; it may be given as to alloc_q4_workspace.)"""
     import torch
 
     return torch.empty(max(orthogonalize_workspace_bytes(batch, m, n), WORKSPACE_ALIGN), dtype=torch.uint8, device=device)
