@@ -58,7 +58,11 @@ typedef enum {
 } ozimmu_status_t;
 
 /* Types of the matrices that the operators on weights take (the FP64 products take doubles only). */
-typedef enum { OZIMMU_F32 = 0, OZIMMU_BF16 = 1, OZIMMU_F16 = 2 } ozimmu_type_t;
+typedef enum { OZIMMU_F32 = 0, OZIMMU_BF16 = 1, OZIMMU_F16 = 2,
+               OZIMMU_E4M3 = 3,      /* codes of the operators in 8-bit floating point; no other takes it */
+               OZIMMU_E8M0 = 4       /* their scales: a byte b for 2^(b - 127), 255 for NaN */
+} ozimmu_type_t;
+typedef enum { OZIMMU_SOFTMAX = 0, OZIMMU_SIGMOID = 1 } ozimmu_score_t;      /* of ozimmu_route */
 
 #define OZIMMU_MAX_SLICES 16
 #define OZIMMU_SLICE_BITS 7          /* Table 2: INT8-INT32 keeps 7 magnitude bits per slice */
@@ -71,6 +75,8 @@ typedef enum { OZIMMU_F32 = 0, OZIMMU_BF16 = 1, OZIMMU_F16 = 2 } ozimmu_type_t;
 #define OZIMMU_MAX_LD 16777216       /* largest distance between rows (2^24 values, bytes of codes) that the four-bit operators take */
 #define OZIMMU_MAX_BATCH 65535       /* matrices in one ozimmu_orthogonalize */
 #define OZIMMU_MAX_STEPS 64          /* of its iteration */
+#define OZIMMU_MAX_EXPERTS 1024      /* of the operators over experts */
+#define OZIMMU_MAX_CHOICES 32        /* experts chosen for a token */
 #define OZIMMU_WORKSPACE_ALIGN 256
 #define OZIMMU_STATIC_SCRATCH_BYTES 67108864   /* 64 MiB: the built-in scratch of ozimmu_dgemm_static */
 
@@ -427,6 +433,108 @@ ozimmu_status_t ozimmu_orthogonalize(int64_t batch, int64_t m, int64_t n, ozimmu
                                      int64_t ldg, int64_t stride_g, void* X, int64_t ldx, int64_t stride_x, int steps,
                                      double a, double b, double c, double eps, void* workspace, size_t workspace_bytes,
                                      void* stream);
+
+/*
+ * Products in 8-bit floating point. A matrix is cut into blocks of block_rows x 128 (block_rows 1: tokens, 128: weights). With amax the
+ * largest finite magnitude of a block,
+ *     e = the least integer in [-127, 127] with amax <= 448 2^e,   c = x 2^-e rounded to e4m3 (nearest, ties to even);
+ * x 2^-e is exact, so a code is rounded once and stands for c 2^e. An infinity or a NaN has the code of a NaN and no part in amax.
+ * Layout:
+ *   codes   a byte each; a row has ozimmu_f8_geometry's row_bytes = 128 ceil(k / 128) bytes, zeros beyond position k (the products read them;
+ *           ozimmu_f8_split writes them). ldq (bytes between rows) is at least that and a multiple of 16; codes are 16-byte aligned.
+ *   scales  ceil(n / block_rows) rows. OZIMMU_E8M0: a byte e + 127 for each 128 positions; a row has scale_bytes = 4 ceil(k / 512) bytes, of which
+ *           those beyond the last block are ignored (the cut writes zeros); lds is a multiple of four, the array four-byte aligned.
+ *           OZIMMU_F32 (weights only, made elsewhere): any 32-bit values, lds >= ceil(k / 128).
+ * ozimmu_f8_split cuts W (n x k; `type`, ldw values between rows). ozimmu_f8_expand writes the values c s as `type`; with 32-bit scales the
+ * product is rounded to 32 bits first.
+ *
+ * ozimmu_f8_gemm:        Y = X W^T      X: t x k, cut by 1 x 128; W: n x k codes by 128 x 128; Y: rows x n
+ * ozimmu_f8_gemm_grad:   dX = dY W      dY: rows x n, cut by 1 x 128; dX: rows x k
+ * ozimmu_f8_weight_grad: dW = dY^T X    both cut along the tokens, in runs of 128 that have one scale for each column; dW: n x k
+ * X, dY: `type`; the call cuts them into its workspace. With type OZIMMU_E4M3 the first two take codes that ozimmu_f8_split has cut
+ * (block_rows 1), with their scales x_scales (OZIMMU_E8M0; else null). Results: any of the three wide types, rounded once from sums in 32 bits.
+ *
+ * Over experts (experts >= 1; 0: one product, rows = t, offsets and source null): W holds `experts` matrices, one behind the other (n rows of
+ * codes and ceil(n / 128) rows of scales each); rows offsets[e] to offsets[e + 1] of Y, dY and dX belong to expert e (offsets: experts + 1
+ * values on the device, from 0, not falling; values outside [0, rows] are taken as the nearest within, and ranges that fall as empty). Rows
+ * outside all ranges are left as they were. source: `rows` values on the device (or null, with rows = t): row r of Y (gemm) or dY (weight_grad)
+ * goes with row source[r] of X; one outside [0, t) stands for a row of zeros. dW: experts x n x k (lddw between all rows), zeros for an expert
+ * without rows; its runs of 128 tokens begin with the expert's first row.
+ *
+ * Errors of the sums: results of 32 bits, and all results of calls with few rows (up to 32 to an expert or in all, by sizes; not the weights'
+ * gradient), are sums of exact products in 32 bits. 16-bit results of more rows, and of weights' gradients, come from matrix cores that
+ * drop, within eight products, what is below 2^-13 of the largest of them: at most 2^-12 of the sum of their magnitudes, 2^-16 where terms are
+ * alike. So a row's last bits may differ with the number of rows beside it. A NaN gives NaN in the results that it goes into and no others.
+ * An empty inner dimension gives zeros; no rows: nothing to do but for dW, which is zeros. With `source`, codes of X take less than
+ * 4 GiB (OZIMMU_ERR_BAD_LD). Outputs must not overlap inputs or the workspace. Everything is in a fixed order: equal calls give equal bits.
+ * workspace: ozimmu_f8_workspace_bytes(...) bytes for the operator (0, 1, 2: gemm, gemm_grad, weight_grad) and the same sizes and `type`,
+ * OZIMMU_WORKSPACE_ALIGN-aligned; may be null where that is 0; one for t and rows serves fewer. Errors: OZIMMU_ERR_BAD_DIM (sizes, experts,
+ * block_rows), _BAD_TYPE, _BAD_LD, _NULL, _MISALIGNED, _WORKSPACE.
+ */
+ozimmu_status_t ozimmu_f8_geometry(int64_t k, int64_t* row_bytes, int64_t* scale_bytes);
+ozimmu_status_t ozimmu_f8_split(int64_t n, int64_t k, int block_rows, ozimmu_type_t type, const void* W, int64_t ldw,
+                                uint8_t* codes, int64_t ldq, uint8_t* scales, int64_t lds, void* stream);
+ozimmu_status_t ozimmu_f8_expand(int64_t n, int64_t k, int block_rows, const uint8_t* codes, int64_t ldq,
+                                 ozimmu_type_t scale_type, const void* scales, int64_t lds, ozimmu_type_t type, void* W,
+                                 int64_t ldw, void* stream);
+ozimmu_status_t ozimmu_f8_workspace_bytes(int op, int64_t t, int64_t rows, int64_t n, int64_t k, int64_t experts,
+                                          ozimmu_type_t type, size_t* bytes);
+ozimmu_status_t ozimmu_f8_gemm(int64_t t, int64_t rows, int64_t n, int64_t k, int64_t experts, ozimmu_type_t type,
+                               const void* X, int64_t ldx, const uint8_t* x_scales, int64_t ldxs, const uint8_t* codes,
+                               int64_t ldq, ozimmu_type_t scale_type, const void* scales, int64_t lds, const int* offsets,
+                               const int* source, ozimmu_type_t out_type, void* Y, int64_t ldy, void* workspace,
+                               size_t workspace_bytes, void* stream);
+ozimmu_status_t ozimmu_f8_gemm_grad(int64_t rows, int64_t n, int64_t k, int64_t experts, ozimmu_type_t type, const void* dY,
+                                    int64_t lddy, const uint8_t* dy_scales, int64_t lddys, const uint8_t* codes, int64_t ldq,
+                                    ozimmu_type_t scale_type, const void* scales, int64_t lds, const int* offsets,
+                                    ozimmu_type_t out_type, void* dX, int64_t lddx, void* workspace, size_t workspace_bytes,
+                                    void* stream);
+ozimmu_status_t ozimmu_f8_weight_grad(int64_t t, int64_t rows, int64_t n, int64_t k, int64_t experts, ozimmu_type_t type,
+                                      const void* dY, int64_t lddy, const void* X, int64_t ldx, const int* offsets,
+                                      const int* source, ozimmu_type_t out_type, void* dW, int64_t lddw, void* workspace,
+                                      size_t workspace_bytes, void* stream);
+
+/*
+ * The choice of experts. For each token, from its logits l (t x experts, row-major, ldl values between rows):
+ *     s = softmax(l) or 1 / (1 + exp(-l)),   choice values v = s + bias   (bias: `experts` 32-bit values, or null);
+ * the experts form `groups` runs of equal length, a group's value is the sum of its two largest choice values (of its one), and of the
+ * top_groups best groups the `top` best experts are chosen, best first; ties go to the lowest index. Choice values are compared in 64 bits.
+ *     weights w_j = scale s_j,  with `renormalize` w_j = scale s_j / (sum of the chosen s)   (sigmoid: + 1e-20),
+ * go into indices and weights (t x top, contiguous). A logit (or bias) of -inf takes its expert out of the choice: it counts for nothing in its
+ * group. Where fewer than `top` can be chosen the rest are index -1 with weight 0. A row with a NaN (for softmax, or a logit of +inf) has
+ * indices -1 and weights NaN, so that it goes to no expert and stays visible.
+ *
+ * ozimmu_route_grad: dlogits (t x experts, `type`) from the gradient of the weights (32-bit, t x top) and the choice, which counts as
+ * constant. Indices outside [0, experts) count for nothing; a row without others gets zeros; of an index that stands twice both count.
+ *
+ * ozimmu_expert_order: the t x top pairs sorted by expert, within one as they come. offsets (experts + 1): expert e's pairs are rows
+ * offsets[e] to offsets[e + 1]; source (t top): the token of each row, -1 behind the last; place (t x top): the row of each pair, -1 for
+ * an index outside [0, experts). workspace: ozimmu_expert_order_workspace_bytes bytes (null where that is 0).
+ *
+ * ozimmu_expert_combine:       Y[i] = sum_j weights[i][j] O[place[i][j]]   (O: rows x n, Y: t x n, `type`; weights null: ones), summed
+ *                              in 32 bits in order and rounded once; a place outside [0, rows) counts as a row of zeros.
+ * ozimmu_expert_combine_grad:  dO[place[i][j]] = weights[i][j] dY[i],  dweights[i][j] = <dY[i], O[place[i][j]]> (0 without a row). Rows of
+ *                              dO that have no pair are left as they were; places must not repeat.
+ * With weights null, ozimmu_expert_combine is the gradient of taking rows by `source`.
+ *
+ * Empty dimensions: nothing to do (offsets and source of ozimmu_expert_order are written all the same). top in 1 .. OZIMMU_MAX_CHOICES, experts
+ * in 1 .. OZIMMU_MAX_EXPERTS, top <= experts for the choice and its gradient, groups divides experts, top_groups <= groups, scale finite, at
+ * most 2^27 pairs: else OZIMMU_ERR_BAD_DIM. score: OZIMMU_ERR_BAD_TYPE. Outputs must not overlap inputs or each other.
+ */
+ozimmu_status_t ozimmu_route(int64_t t, int64_t experts, int top, ozimmu_type_t type, const void* logits, int64_t ldl,
+                             const float* bias, ozimmu_score_t score, int groups, int top_groups, int renormalize, double scale,
+                             int* indices, float* weights, void* stream);
+ozimmu_status_t ozimmu_route_grad(int64_t t, int64_t experts, int top, ozimmu_type_t type, const void* logits, int64_t ldl,
+                                  const int* indices, const float* dweights, ozimmu_score_t score, int renormalize, double scale,
+                                  void* dlogits, int64_t lddl, void* stream);
+ozimmu_status_t ozimmu_expert_order_workspace_bytes(int64_t t, int top, int64_t experts, size_t* bytes);
+ozimmu_status_t ozimmu_expert_order(int64_t t, int top, int64_t experts, const int* indices, int* offsets, int* source,
+                                    int* place, void* workspace, size_t workspace_bytes, void* stream);
+ozimmu_status_t ozimmu_expert_combine(int64_t t, int top, int64_t rows, int64_t n, ozimmu_type_t type, const void* O, int64_t ldo,
+                                      const int* place, const float* weights, void* Y, int64_t ldy, void* stream);
+ozimmu_status_t ozimmu_expert_combine_grad(int64_t t, int top, int64_t rows, int64_t n, ozimmu_type_t type, const void* dY,
+                                           int64_t lddy, const void* O, int64_t ldo, const int* place, const float* weights,
+                                           void* dO, int64_t lddo, float* dweights, void* stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,159 @@
+// Device helpers for 8-bit floating point (e4m3: sign, four bits of exponent, three of fraction; 448 is the largest value, 0x7f a NaN, no
+// infinities) under power-of-two scales, and for rows sorted by expert (gfx950 only).
+#pragma once
+
+#include "eight_internal.h"
+#include "half_common.h"
+
+namespace ozimmu {
+namespace {
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef int v2i __attribute__((ext_vector_type(2)));
+
+// Byte e + 127 of the least e in [-127, 127] with top <= 448 2^e, for the bits of a finite top >= 0: 448 is 1.75 2^8, so the exponent goes up
+// where the fraction exceeds that of 1.75.
+__device__ __forceinline__ int scale_byte(unsigned top) { return max(0, (int)((top + 0x1fffffu) >> 23) - 8); }
+// The magnitude's bits where it is finite, else 0.
+__device__ __forceinline__ unsigned finite_bits(float x) {
+    const unsigned a = __float_as_uint(x) & 0x7fffffffu;
+    return a < 0x7f800000u ? a : 0u;
+}
+// Four codes as a word. x 2^-e is exact, or far below the least code; the conversion rounds to nearest, ties to even. What is not finite
+// becomes a NaN.
+__device__ __forceinline__ unsigned code4(const float* x, int e) {
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        y[i] = __builtin_amdgcn_ldexpf(x[i], -e);
+        y[i] = __builtin_fabsf(x[i]) < __builtin_inff() ? y[i] : __builtin_nanf("");
+    }
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+}
+// The values of a word of codes.
+__device__ __forceinline__ void values4(unsigned w, float (&x)[4]) {
+    x[0] = __builtin_amdgcn_cvt_f32_fp8((int)w, 0);
+    x[1] = __builtin_amdgcn_cvt_f32_fp8((int)w, 1);
+    x[2] = __builtin_amdgcn_cvt_f32_fp8((int)w, 2);
+    x[3] = __builtin_amdgcn_cvt_f32_fp8((int)w, 3);
+}
+// Sixteen codes as fp16, which holds each of them.
+__device__ __forceinline__ void halves16(const v4u& w, v8h& first, v8h& second) {
+    typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+    v2h h[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        h[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w[i], 1.0f, false);
+        h[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w[i], 1.0f, true);
+    }
+    first = v8h{h[0][0], h[0][1], h[1][0], h[1][1], h[2][0], h[2][1], h[3][0], h[3][1]};
+    second = v8h{h[4][0], h[4][1], h[5][0], h[5][1], h[6][0], h[6][1], h[7][0], h[7][1]};
+}
+
+// A scale of the weights as significand and exponent byte: value = m 2^(byte - 127). Bytes: m = 1. A NaN or infinity: byte 255.
+template <bool WIDE>
+__device__ __forceinline__ void scale_parts(const void* scales, int64_t at, float& m, int& byte) {
+    if constexpr (WIDE) {
+        const unsigned b = __float_as_uint(static_cast<const float*>(scales)[at]);
+        byte = (int)(b >> 23 & 255u);
+        if (byte == 0) {   // subnormal: fraction 2^-126
+            byte = 1;
+            m = __builtin_amdgcn_ldexpf((float)(b & 0x7fffffu), -23);
+        } else {
+            m = __uint_as_float((b & 0x7fffffu) | 0x3f800000u);
+        }
+        m = b >> 31 ? -m : m;
+    } else {
+        byte = static_cast<const uint8_t*>(scales)[at];
+        m = 1.0f;
+    }
+    if (byte == 255) m = __builtin_nanf("");
+}
+
+// ---- rows sorted by expert
+
+__device__ __forceinline__ int wave_scan(int x) {   // inclusive sum over the lanes before and this one
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(x, d);
+        x += lane >= d ? y : 0;
+    }
+    return x;
+}
+// Rows of expert e, whatever the offsets hold: none runs backwards or leaves [0, rows].
+__device__ __forceinline__ void expert_rows(const int* offsets, int e, int rows, int& first, int& count) {
+    first = min(max(offsets[e], 0), rows);
+    count = max(min(offsets[e + 1], rows) - first, 0);
+}
+// Which unit (of `unit` rows; counted in multiples of `to` for each expert) number `index` is, over all experts in order. Every lane of a
+// wavefront calls it with the same arguments. `total` receives the number of units.
+struct Segment {
+    int expert, first, count;   // its rows
+    int unit;                   // the unit's number within the expert
+    int before;                 // units of the experts before it
+};
+template <class F>
+__device__ __forceinline__ int over_experts(const int* offsets, int experts, int rows, int unit, int to, F&& f) {
+    const int lane = threadIdx.x & 63;
+    int base = 0;
+    for (int e0 = 0; e0 < experts; e0 += 64) {
+        const int e = e0 + lane;
+        int first = 0, count = 0;
+        if (e < experts) expert_rows(offsets, e, rows, first, count);
+        int units = (count + unit - 1) / unit;
+        units = (units + to - 1) / to * to;
+        const int sum = wave_scan(units);
+        f(e, first, count, units, base + sum - units);
+        base += __builtin_amdgcn_readlane(sum, 63);
+    }
+    return base;
+}
+__device__ __forceinline__ int count_units(const int* offsets, int experts, int rows, int unit) {
+    return over_experts(offsets, experts, rows, unit, 1, [](int, int, int, int, int) {});
+}
+__device__ __forceinline__ bool find_unit(const int* offsets, int experts, int rows, int unit, int to, int index, Segment& s) {
+    bool found = false;
+    over_experts(offsets, experts, rows, unit, to, [&](int e, int first, int count, int units, int before) {
+        const unsigned long long here = __builtin_amdgcn_ballot_w64(index >= before && index < before + units);
+        if (here) {
+            const int l = __builtin_ctzll(here);
+            s.expert = __builtin_amdgcn_readlane(e, l);
+            s.first = __builtin_amdgcn_readlane(first, l);
+            s.count = __builtin_amdgcn_readlane(count, l);
+            s.before = __builtin_amdgcn_readlane(before, l);
+            s.unit = index - s.before;
+            found = true;
+        }
+    });
+    return found;
+}
+
+// R[row][col .. col + 3], rounded once to the result's type; zeros where the row has no source.
+template <int TYPE>
+__device__ __forceinline__ void store_four_as(const F8Args& a, int64_t row, int col, const v4f& v, bool there) {
+    typedef typename Elem<TYPE>::raw raw;
+    typedef raw raw4 __attribute__((ext_vector_type(4)));
+    raw* at = static_cast<raw*>(a.out) + row * a.ldo + col;
+    raw4 x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = Elem<TYPE>::store(there ? v[e] : 0.f);
+    if ((reinterpret_cast<uintptr_t>(at) & (sizeof(raw4) - 1)) == 0 && col + 4 <= a.n)
+        *reinterpret_cast<raw4*>(at) = x;
+    else
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col + e < a.n) at[e] = x[e];
+}
+__device__ __forceinline__ void store_four(const F8Args& a, int64_t row, int col, const v4f& v, bool there) {
+    if (a.out_type == OZIMMU_F32)
+        store_four_as<OZIMMU_F32>(a, row, col, v, there);
+    else if (a.out_type == OZIMMU_BF16)
+        store_four_as<OZIMMU_BF16>(a, row, col, v, there);
+    else
+        store_four_as<OZIMMU_F16>(a, row, col, v, there);
+}
+
+}  // namespace
+}  // namespace ozimmu

@@ -1,0 +1,314 @@
+// The cut into 8-bit floating point, its inverse, and the transposed operands of gradients (gfx950).
+//
+// A block of 1 x 128 or 128 x 128 values has the scale 2^e, e the least integer in [-127, 127] with max |x| <= 448 2^e over its finite values;
+// the codes are RNE(x 2^-e) in e4m3. x 2^-e is exact, so a code is rounded once. Everything here is one pass over memory.
+#include <algorithm>
+
+#include "f8_common.h"
+
+namespace ozimmu {
+namespace {
+
+constexpr int kThreads = 256;
+
+template <int TYPE>
+struct Eight {   // eight consecutive values as they lie
+    v4u raw[TYPE == OZIMMU_F32 ? 2 : 1];
+};
+template <int TYPE>
+__device__ __forceinline__ void load8(const typename Elem<TYPE>::raw* row, int64_t at, int64_t len, Eight<TYPE>& x) {
+    typedef typename Elem<TYPE>::raw raw;
+    if (at + 8 <= len) {
+        x.raw[0] = *reinterpret_cast<const v4u_any*>(row + at);
+        if constexpr (TYPE == OZIMMU_F32) x.raw[1] = *reinterpret_cast<const v4u_any*>(row + at + 4);
+    } else {
+        raw r[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[e] = at + e < len ? row[at + e] : raw(0);
+        x = __builtin_bit_cast(Eight<TYPE>, r);
+    }
+}
+template <int TYPE>
+__device__ __forceinline__ void floats(const Eight<TYPE>& x, float (&f)[8]) {
+    if constexpr (TYPE == OZIMMU_F32) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(x.raw[e >> 2][e & 3]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            f[2 * e] = Elem<TYPE>::load((unsigned short)(x.raw[0][e] & 0xffffu));
+            f[2 * e + 1] = Elem<TYPE>::load((unsigned short)(x.raw[0][e] >> 16));
+        }
+    }
+}
+__device__ __forceinline__ unsigned top8(const float (&f)[8]) {
+    unsigned t = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t = max(t, finite_bits(f[e]));
+    return t;
+}
+__device__ __forceinline__ unsigned max16(unsigned x) {   // over sixteen neighbouring lanes, in all of them
+    x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, true));
+    x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, true));
+    x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xF, 0xF, true));
+    return max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xF, 0xF, true));
+}
+
+// Runs of a row: a wavefront takes 512 positions of kRows rows, eight to a lane, sixteen lanes to a run.
+constexpr int kRows = 4;
+template <int TYPE>
+__launch_bounds__(kThreads)
+__global__ void f8_split_rows_kernel(int64_t n, int64_t k, const void* W, int64_t ldw, uint8_t* codes, int64_t ldq, uint8_t* scales, int64_t lds, int chunks, int64_t items) {
+    typedef typename Elem<TYPE>::raw raw;
+    const int lane = threadIdx.x & 63;
+    const int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (item >= items) return;
+    const int64_t row0 = item / chunks * kRows, at = (item % chunks) * 512 + lane * 8;
+    Eight<TYPE> x[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) load8<TYPE>(static_cast<const raw*>(W) + min(row0 + r, n - 1) * ldw, at, k, x[r]);
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        if (row0 + r >= n) break;
+        float f[8];
+        floats<TYPE>(x[r], f);
+        const int byte = scale_byte(max16(top8(f)));
+        if (at < ((k + 127) & ~int64_t(127))) *reinterpret_cast<v2u*>(codes + (row0 + r) * ldq + at) = v2u{code4(f, byte - 127), code4(f + 4, byte - 127)};
+        const unsigned four = (unsigned)__builtin_amdgcn_readlane(byte, 0) | (unsigned)__builtin_amdgcn_readlane(byte, 16) << 8 |
+                              (unsigned)__builtin_amdgcn_readlane(byte, 32) << 16 | (unsigned)__builtin_amdgcn_readlane(byte, 48) << 24;
+        if (lane == 0) *reinterpret_cast<unsigned*>(scales + (row0 + r) * lds + (item % chunks) * 4) = four;
+    }
+}
+
+// Blocks: a workgroup each; a thread holds eight positions of every sixteenth row.
+template <int TYPE>
+__launch_bounds__(kThreads)
+__global__ void f8_split_blocks_kernel(int64_t n, int64_t k, const void* W, int64_t ldw, uint8_t* codes, int64_t ldq, uint8_t* scales, int64_t lds, int groups) {
+    typedef typename Elem<TYPE>::raw raw;
+    __shared__ unsigned tops[kThreads / 64];
+    const int64_t row0 = (int64_t)(blockIdx.x / groups) * 128;
+    const int group = blockIdx.x % groups;
+    const int64_t at = (int64_t)group * 128 + (threadIdx.x & 15) * 8;
+    const int r0 = threadIdx.x >> 4;
+    Eight<TYPE> x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) load8<TYPE>(static_cast<const raw*>(W) + min(row0 + r0 + 16 * i, n - 1) * ldw, at, k, x[i]);
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {   // (rows beyond the last repeat it)
+        float f[8];
+        floats<TYPE>(x[i], f);
+        top = max(top, top8(f));
+    }
+    top = max16(top);
+    top = max(max((unsigned)__builtin_amdgcn_readlane((int)top, 0), (unsigned)__builtin_amdgcn_readlane((int)top, 16)),
+              max((unsigned)__builtin_amdgcn_readlane((int)top, 32), (unsigned)__builtin_amdgcn_readlane((int)top, 48)));
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();
+    const int byte = scale_byte(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (row0 + r0 + 16 * i >= n) break;
+        float f[8];
+        floats<TYPE>(x[i], f);
+        *reinterpret_cast<v2u*>(codes + (row0 + r0 + 16 * i) * ldq + at) = v2u{code4(f, byte - 127), code4(f + 4, byte - 127)};
+    }
+    if (threadIdx.x == 0) {
+        uint8_t* s = scales + (row0 >> 7) * lds;
+        s[group] = (uint8_t)byte;
+        if (group == groups - 1)
+            for (int g = groups; g < ((groups + 3) & ~3); ++g) s[g] = 0;
+    }
+}
+
+// Values: eight positions to a thread.
+template <int TYPE, bool WIDE>
+__launch_bounds__(kThreads)
+__global__ void f8_expand_kernel(int64_t k, int shift, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds, void* W, int64_t ldw, int per_row, int64_t items) {
+    typedef typename Elem<TYPE>::raw raw;
+    const int64_t item = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (item >= items) return;
+    const int64_t row = item / per_row, at = (item % per_row) * 8;
+    const v2u c = *reinterpret_cast<const v2u*>(codes + row * ldq + at);
+    float m, f[8];
+    int byte;
+    scale_parts<WIDE>(scales, (row >> shift) * lds + (at >> 7), m, byte);
+    values4(c[0], *reinterpret_cast<float(*)[4]>(f));
+    values4(c[1], *reinterpret_cast<float(*)[4]>(f + 4));
+    raw r[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = Elem<TYPE>::store(__builtin_amdgcn_ldexpf(f[e] * m, byte - 127));
+    raw* out = static_cast<raw*>(W) + row * ldw + at;
+    if (at + 8 <= k) {
+        *reinterpret_cast<v4u_any*>(out) = *reinterpret_cast<const v4u*>(r);
+        if constexpr (TYPE == OZIMMU_F32) *reinterpret_cast<v4u_any*>(out + 4) = *reinterpret_cast<const v4u*>(r + 4);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (at + e < k) out[e] = r[e];
+    }
+}
+
+// Transposed weights: a workgroup turns a block of 128 x 128 in LDS, four by four bytes to a thread.
+template <bool WIDE>
+__launch_bounds__(kThreads)
+__global__ void f8_transpose_kernel(int64_t n, int64_t k, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds, uint8_t* codes_t, void* scales_t, int64_t ld_t, int64_t lds_t, int nb,
+                                    int kb) {
+    __shared__ unsigned block[128][33];
+    const int64_t expert = blockIdx.x / ((int64_t)nb * kb);
+    const int in = (int)(blockIdx.x - expert * nb * kb), bn = in / kb, bk = in % kb;
+    const uint8_t* from = codes + (expert * n + (int64_t)bn * 128) * ldq + (int64_t)bk * 128;
+    const int rows = (int)min<int64_t>(128, n - (int64_t)bn * 128), cols = (int)min<int64_t>(128, k - (int64_t)bk * 128);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = (threadIdx.x >> 3) + 32 * i, p = threadIdx.x & 7;
+        v4u x = {0, 0, 0, 0};
+        if (r < rows) x = *reinterpret_cast<const v4u*>(from + r * ldq + p * 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) block[r][p * 4 + e] = x[e];
+    }
+    __syncthreads();
+    uint8_t* to = codes_t + (expert * k + (int64_t)bk * 128) * ld_t + (int64_t)bn * 128;
+    const int r4 = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int c4 = (threadIdx.x >> 5) + 8 * i;
+        unsigned x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = block[4 * r4 + e][c4];
+        const unsigned a = __builtin_amdgcn_perm(x[1], x[0], 0x05010400u), b = __builtin_amdgcn_perm(x[3], x[2], 0x05010400u);   // bytes 0 and 1 of each pair
+        const unsigned c = __builtin_amdgcn_perm(x[1], x[0], 0x07030602u), d = __builtin_amdgcn_perm(x[3], x[2], 0x07030602u);   // bytes 2 and 3
+        const unsigned y[4] = {__builtin_amdgcn_perm(b, a, 0x05040100u), __builtin_amdgcn_perm(b, a, 0x07060302u), __builtin_amdgcn_perm(d, c, 0x05040100u),
+                               __builtin_amdgcn_perm(d, c, 0x07060302u)};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (4 * c4 + e < cols) *reinterpret_cast<unsigned*>(to + (int64_t)(4 * c4 + e) * ld_t + 4 * r4) = y[e];
+    }
+    if (threadIdx.x == 0) {
+        const int64_t at = (expert * nb + bn) * lds + bk, at_t = (expert * kb + bk) * lds_t + bn;
+        if constexpr (WIDE)
+            static_cast<float*>(scales_t)[at_t] = static_cast<const float*>(scales)[at];
+        else
+            static_cast<uint8_t*>(scales_t)[at_t] = static_cast<const uint8_t*>(scales)[at];
+    }
+}
+
+// Runs along the tokens: a workgroup takes 128 tokens of an expert and 64 columns; a thread holds eight columns of four neighbouring tokens,
+// whose codes are a word of the transposed row.
+template <int TYPE>
+__launch_bounds__(kThreads)
+__global__ void f8_cut_tokens_kernel(int t, int rows, int64_t n, int experts, const int* offsets, const int* source, const void* V, int64_t ldv, uint8_t* codes, int64_t ld, uint8_t* scales,
+                                     int64_t lds, int tiles) {
+    typedef typename Elem<TYPE>::raw raw;
+    __shared__ unsigned tops[kThreads / 64][64];
+    __shared__ unsigned turned[64][33];
+    const int run = blockIdx.x / tiles, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t col0 = (int64_t)(blockIdx.x % tiles) * 64;
+    int first = 0, count = rows, unit = run;
+    if (experts) {
+        Segment s;
+        if (!find_unit(offsets, experts, rows, 128, 4, run, s)) return;
+        first = s.first;
+        count = s.count;
+        unit = s.unit;
+    }
+    if (unit * 128 >= count) return;
+    const int token0 = unit * 128 + (threadIdx.x >> 3) * 4;   // within the expert's
+    const int64_t at = col0 + (threadIdx.x & 7) * 8;
+    float f[4][8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        int64_t row = first + min(token0 + i, count - 1);
+        bool there = token0 + i < count;
+        if (source) {
+            const int s = source[row];
+            there = there && (unsigned)s < (unsigned)t;
+            row = there ? s : 0;
+        }
+        Eight<TYPE> x;
+        load8<TYPE>(static_cast<const raw*>(V) + row * ldv, at, n, x);
+        floats<TYPE>(x, f[i]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[i][e] = there ? f[i][e] : 0.f;
+    }
+    unsigned top[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        top[e] = max(max(finite_bits(f[0][e]), finite_bits(f[1][e])), max(finite_bits(f[2][e]), finite_bits(f[3][e])));
+#pragma unroll
+        for (int d = 8; d < 64; d <<= 1) top[e] = max(top[e], (unsigned)__shfl_xor((int)top[e], d));
+        if (lane < 8) tops[wave][lane * 8 + e] = top[e];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int c = (threadIdx.x & 7) * 8 + e;
+        const int byte = scale_byte(max(max(tops[0][c], tops[1][c]), max(tops[2][c], tops[3][c])));
+        const float x[4] = {f[0][e], f[1][e], f[2][e], f[3][e]};
+        turned[c][threadIdx.x >> 3] = code4(x, byte - 127);
+    }
+    if (threadIdx.x < 64 && col0 + threadIdx.x < n)
+        scales[(col0 + threadIdx.x) * lds + run] = (uint8_t)scale_byte(max(max(tops[0][threadIdx.x], tops[1][threadIdx.x]), max(tops[2][threadIdx.x], tops[3][threadIdx.x])));
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int c = (threadIdx.x >> 3) + 32 * i, p = (threadIdx.x & 7) * 4;
+        if (col0 + c < n) *reinterpret_cast<v4u*>(codes + (col0 + c) * ld + (int64_t)run * 128 + p * 4) = v4u{turned[c][p], turned[c][p + 1], turned[c][p + 2], turned[c][p + 3]};
+    }
+}
+
+template <class F>
+hipError_t by_type(int type, F&& f) {
+    switch (type) {
+        case OZIMMU_F32: f(std::integral_constant<int, OZIMMU_F32>{}); break;
+        case OZIMMU_BF16: f(std::integral_constant<int, OZIMMU_BF16>{}); break;
+        default: f(std::integral_constant<int, OZIMMU_F16>{}); break;
+    }
+    return hipGetLastError();
+}
+bool too_many(int64_t workgroups) { return workgroups <= 0 || workgroups > INT32_MAX; }
+
+}  // namespace
+
+hipError_t launch_f8_split(int64_t n, int64_t k, int block_rows, const void* W, int type, int64_t ldw, uint8_t* codes, int64_t ldq, uint8_t* scales, int64_t lds, hipStream_t st) {
+    const int64_t chunks = (k + 511) / 512, items = (n + kRows - 1) / kRows * chunks, groups = f8_groups(k);
+    const int64_t grid = block_rows == 1 ? (items + 3) / 4 : (n + 127) / 128 * groups;
+    if (too_many(grid)) return hipErrorInvalidConfiguration;
+    return by_type(type, [&](auto kind) {
+        constexpr int T = decltype(kind)::value;
+        if (block_rows == 1)
+            f8_split_rows_kernel<T><<<dim3((unsigned)grid), dim3(kThreads), 0, st>>>(n, k, W, ldw, codes, ldq, scales, lds, (int)chunks, items);
+        else
+            f8_split_blocks_kernel<T><<<dim3((unsigned)grid), dim3(kThreads), 0, st>>>(n, k, W, ldw, codes, ldq, scales, lds, (int)groups);
+    });
+}
+
+hipError_t launch_f8_expand(int64_t n, int64_t k, int block_rows, const uint8_t* codes, int64_t ldq, int scale_type, const void* scales, int64_t lds, void* W, int type, int64_t ldw, hipStream_t st) {
+    const int64_t per_row = (k + 7) / 8, items = n * per_row, grid = (items + kThreads - 1) / kThreads;
+    if (too_many(grid)) return hipErrorInvalidConfiguration;
+    return by_type(type, [&](auto kind) {
+        constexpr int T = decltype(kind)::value;
+        auto kernel = scale_type == OZIMMU_F32 ? f8_expand_kernel<T, true> : f8_expand_kernel<T, false>;
+        kernel<<<dim3((unsigned)grid), dim3(kThreads), 0, st>>>(k, block_rows == 1 ? 0 : 7, codes, ldq, scales, lds, W, ldw, (int)per_row, items);
+    });
+}
+
+hipError_t launch_f8_transpose(int64_t experts, int64_t n, int64_t k, const uint8_t* codes, int64_t ldq, int scale_type, const void* scales, int64_t lds, uint8_t* codes_t, void* scales_t,
+                               hipStream_t st) {
+    const int64_t nb = f8_groups(n), kb = f8_groups(k), grid = experts * nb * kb;
+    if (too_many(grid)) return hipErrorInvalidConfiguration;
+    auto kernel = scale_type == OZIMMU_F32 ? f8_transpose_kernel<true> : f8_transpose_kernel<false>;
+    kernel<<<dim3((unsigned)grid), dim3(kThreads), 0, st>>>(n, k, codes, ldq, scales, lds, codes_t, scales_t, f8_row_bytes(n), f8_scale_bytes(n), (int)nb, (int)kb);
+    return hipGetLastError();
+}
+
+hipError_t launch_f8_cut_tokens(int64_t t, int64_t rows, int64_t n, int64_t experts, const int* offsets, const int* source, const void* V, int type, int64_t ldv, uint8_t* codes, int64_t ld,
+                                uint8_t* scales, int64_t lds, hipStream_t st) {
+    const int64_t tiles = (n + 63) / 64, grid = ld / 128 * tiles;
+    if (too_many(grid)) return hipErrorInvalidConfiguration;
+    return by_type(type, [&](auto kind) {
+        f8_cut_tokens_kernel<decltype(kind)::value><<<dim3((unsigned)grid), dim3(kThreads), 0, st>>>((int)t, (int)rows, n, (int)experts, offsets, source, V, ldv, codes, ld, scales, lds, (int)tiles);
+    });
+}
+
+}  // namespace ozimmu

@@ -1,0 +1,376 @@
+// R = P Q^T for codes in 8-bit floating point, tile by tile (gfx950). Rows of both operands run along the inner dimension, in slabs of 128
+// positions (128 bytes) that have one scale each.
+//
+// A workgroup owns a BM x BN tile. Slabs come into LDS by direct loads, swizzled and double-buffered as in nt_product.h (16-byte piece c of row
+// r lies at place c ^ (r % 8)); a lane's fragment of a slab is pieces lane / 16 and lane / 16 + 4 of row lane % 16, of either operand alike, so
+// that positions meet. Two ways of multiplying:
+//   16-bit results: v_mfma_scale_f32_16x16x128_f8f6f4, which takes a power-of-two scale for every row and 32 positions: a slab is one
+//     instruction and its scales cost nothing. Within eight products it drops what is below 2^-13 of the largest of them; the sums are 32-bit.
+//   32-bit results (EXACT): the codes become fp16, which holds each of them, four MFMAs a slab, at half the rate; a slab's sum is scaled and
+//     added to the tile's on the vector units.
+// Scales of the weights in 32 bits (WIDE): their exponents go the way of the bytes, their significands are multiplied on the vector units.
+// A lane's scales of four slabs are one word.
+//
+// Over experts the tiles are counted on the GPU from the offsets: every wavefront scans them once. The launch is as large as they could make
+// it; what is left over ends at once.
+#pragma once
+
+#include <algorithm>
+
+#include "f8_common.h"
+
+namespace ozimmu {
+namespace {
+
+// How the tiles are dealt: the first `whole` to a workgroup each, the others to `parts` each, with part_slabs (a multiple of four) slabs.
+struct F8Plan {
+    int tiles_m, tiles_n, whole, parts, part_slabs;
+};
+
+// Where a tile lies. false: there is no such tile.
+struct F8Tile {
+    int expert, first, count, row0, col0;   // rows first .. first + count are the expert's; row0 from there on
+    int slab0, slabs, before;               // `before`: slab from which the expert's runs begin (along_rows)
+};
+template <int BM, int BN>
+__device__ __forceinline__ bool f8_tile(const F8Args& a, const F8Plan& p, int block, F8Tile& t) {
+    t.expert = t.first = t.before = t.slab0 = 0;
+    t.count = a.rows;
+    t.slabs = a.slabs;
+    int tm, tn;
+    if (a.along_rows) {
+        const int one = p.tiles_m * p.tiles_n;
+        t.expert = block / one;
+        tile_of_logical(block - t.expert * one, p.tiles_m, p.tiles_n, tm, tn);
+        if (a.experts) {
+            int rows_first, rows_count;
+            expert_rows(a.offsets, t.expert, a.t, rows_first, rows_count);
+            t.slabs = (rows_count + 127) >> 7;
+            over_experts(a.offsets, a.experts, a.t, 128, 4, [&](int e, int, int, int, int before) {
+                const unsigned long long here = __builtin_amdgcn_ballot_w64(e == t.expert);
+                if (here) t.before = __builtin_amdgcn_readlane(before, __builtin_ctzll(here));
+            });
+        }
+    } else if (a.experts) {
+        const int units = count_units(a.offsets, a.experts, a.rows, BM), total = units * p.tiles_n;
+        int first, count;
+        xcd_tile_range(block & 7, total, first, count);
+        if ((block >> 3) >= count) return false;
+        tile_of_logical(first + (block >> 3), units, p.tiles_n, tm, tn);
+        Segment s;
+        if (!find_unit(a.offsets, a.experts, a.rows, BM, 1, tm, s)) return false;
+        t.expert = s.expert;
+        t.first = s.first;
+        t.count = s.count;
+        tm = s.unit;
+    } else {
+        int tile;
+        if (block >= p.whole) {
+            const int b = block - p.whole, part = b % p.parts;
+            tile = p.whole + b / p.parts;
+            t.slab0 = part * p.part_slabs;
+            t.slabs = min(p.part_slabs, a.slabs - t.slab0);
+        } else {
+            int first, count;
+            xcd_tile_range(block & 7, p.whole, first, count);
+            tile = first + (block >> 3);
+        }
+        tile_of_logical(tile, p.tiles_m, p.tiles_n, tm, tn);
+    }
+    t.row0 = tm * BM;
+    t.col0 = tn * BN;
+    return true;
+}
+
+enum F8Walk { kF8ReadOnTime, kF8FirstReadsAhead };
+
+template <int BM, int BN, int WM, int WN, int WALK, bool EXACT, bool WIDE, bool Q_ROWS>
+__launch_bounds__(WM * WN * 64)
+__global__ void f8_product_kernel(F8Args a, F8Plan plan) {
+    static_assert(!(WIDE && Q_ROWS) && BN / WN <= 128);
+    constexpr int W = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
+    constexpr int LP = BM / 8 / W, LQ = BN / 8 / W;   // direct loads per wavefront and slab
+    constexpr unsigned kStage = (BM + BN) * 128;
+    constexpr int SQ = Q_ROWS ? NI : 1;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    F8Tile t;
+    if (!f8_tile<BM, BN>(a, plan, blockIdx.x, t)) return;
+    const int slabs = t.slabs;
+
+    // operands: P's rows from `first` on (or by source), Q's from the expert's first
+    const int64_t p_row = a.along_rows ? t.row0 : a.source ? 0 : (int64_t)t.first + t.row0;
+    const int64_t q_row = a.along_rows ? t.col0 : (int64_t)t.expert * a.n + t.col0;
+    const int64_t slab_first = t.before + t.slab0;
+    const uint8_t* P = a.P + p_row * a.ldp + slab_first * 128;
+    const uint8_t* Q = a.Q + q_row * a.ldq + slab_first * 128;
+    auto row_of = [&](int r) {   // row of P, from p_row, of row r of the tile
+        r = min(r, t.count - 1 - t.row0);
+        if (!a.source || a.along_rows) return r;
+        const int s = a.source[t.first + t.row0 + r];
+        return (unsigned)s < (unsigned)a.t ? s : 0;
+    };
+    const unsigned piece = ((lane & 7) ^ (lane >> 3)) * 16;
+    unsigned voff_p[LP], voff_q[LQ];
+#pragma unroll
+    for (int i = 0; i < LP; ++i) voff_p[i] = (unsigned)row_of((wave * LP + i) * 8 + (lane >> 3)) * (unsigned)a.ldp + piece;
+#pragma unroll
+    for (int i = 0; i < LQ; ++i) voff_q[i] = (unsigned)min((wave * LQ + i) * 8 + (lane >> 3), a.n - 1 - t.col0) * (unsigned)a.ldq + piece;
+    const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds);
+    auto load = [&](int i, int slab, int stage) {
+        const unsigned at = lds0 + stage * kStage;
+        if (i < LP)
+            dma_load16<0>(P + (int64_t)slab * 128, voff_p[i], at + (wave * LP + i) * 1024);
+        else
+            dma_load16<0>(Q + (int64_t)slab * 128, voff_q[i - LP], at + BM * 128 + (wave * LQ + i - LP) * 1024);
+    };
+
+    const int wm = wave / WN, wn = wave % WN;
+    const unsigned frag0 = (lane & 15) * 128 + (((lane >> 4) ^ (lane & 7)) * 16);
+    const unsigned frag1 = (lane & 15) * 128 + ((((lane >> 4) + 4) ^ (lane & 7)) * 16);
+
+    // scales: words of four slabs
+    const uint8_t* SP = a.sp + p_row * a.ldsp + slab_first;
+    unsigned voff_sp[MI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) voff_sp[i] = (unsigned)row_of(wm * (BM / WM) + 16 * i + (lane & 15)) * (unsigned)a.ldsp;
+    const uint8_t* SQB = nullptr;
+    const float* SQF = nullptr;
+    unsigned voff_sq[SQ] = {};
+    if constexpr (Q_ROWS) {
+        SQB = static_cast<const uint8_t*>(a.sq) + q_row * a.ldsq + slab_first;
+#pragma unroll
+        for (int j = 0; j < NI; ++j) voff_sq[j] = (unsigned)min(wn * (BN / WN) + 16 * j + (lane & 15), a.n - 1 - t.col0) * (unsigned)a.ldsq;
+    } else {
+        const int64_t at = ((int64_t)t.expert * ((a.n + 127) >> 7) + min((t.col0 + wn * (BN / WN)) >> 7, (a.n - 1) >> 7)) * a.ldsq + slab_first;
+        if constexpr (WIDE)
+            SQF = static_cast<const float*>(a.sq) + at;
+        else
+            SQB = static_cast<const uint8_t*>(a.sq) + at;
+    }
+    unsigned sp[MI], sq[SQ];
+    float sig = 1.0f;
+    auto scales = [&](int slab) {   // those of `slab` and, for words, the three behind it
+        if ((slab & 3) == 0) {
+#pragma unroll
+            for (int i = 0; i < MI; ++i) sp[i] = *reinterpret_cast<const unsigned*>(SP + slab + voff_sp[i]);
+            if constexpr (!WIDE)
+#pragma unroll
+                for (int j = 0; j < SQ; ++j) sq[j] = *reinterpret_cast<const unsigned*>(SQB + slab + voff_sq[j]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < MI; ++i) sp[i] >>= 8;
+            if constexpr (!WIDE)
+#pragma unroll
+                for (int j = 0; j < SQ; ++j) sq[j] >>= 8;
+        }
+        if constexpr (WIDE) {
+            int byte;
+            scale_parts<true>(SQF, slab, sig, byte);
+            sq[0] = (unsigned)byte;
+        }
+    };
+
+    v4f acc[MI][NI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+
+    struct Operand {
+        v4u a, b;
+    };
+    auto read = [&](Operand& x, const unsigned char* at) {
+        x.a = *reinterpret_cast<const v4u*>(at + frag0);
+        x.b = *reinterpret_cast<const v4u*>(at + frag1);
+    };
+    auto both = [](const Operand& x) { return v8i{(int)x.a[0], (int)x.a[1], (int)x.a[2], (int)x.a[3], (int)x.b[0], (int)x.b[1], (int)x.b[2], (int)x.b[3]}; };
+    auto row_of_products = [&](int i, const Operand& p, const Operand (&q)[NI]) {
+        if constexpr (EXACT) {
+            v8h ph[4];
+            halves16(p.a, ph[0], ph[1]);
+            halves16(p.b, ph[2], ph[3]);
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                v8h qh[4];
+                halves16(q[j].a, qh[0], qh[1]);
+                halves16(q[j].b, qh[2], qh[3]);
+                v4f part = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int h = 0; h < 4; ++h) part = __builtin_amdgcn_mfma_f32_16x16x32_f16(qh[h], ph[h], part, 0, 0, 0);
+                // (a word of Q_ROWS is the lane's own row of Q; the sums are of its columns 4 (lane / 16) + 0 .. 3)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int byte = (int)((Q_ROWS ? (unsigned)__shfl((int)sq[j], (lane >> 4) * 4 + e) : sq[0]) & 255u);
+                    float x = part[e];
+                    if constexpr (WIDE) x *= sig;
+                    x = __builtin_amdgcn_ldexpf(x, (int)(sp[i] & 255u) + byte - 254);
+                    acc[i][j][e] += byte == 255 ? __builtin_nanf("") : x;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                if constexpr (WIDE) {
+                    const v4f part = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(both(q[j]), both(p), v4f{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, (int)sq[0], 0, (int)sp[i]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(part[e], sig, acc[i][j][e]);
+                } else {
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(both(q[j]), both(p), acc[i][j], 0, 0, 0, (int)sq[Q_ROWS ? j : 0], 0, (int)sp[i]);
+                }
+            }
+        }
+    };
+
+    if (slabs > 0) {
+#pragma unroll
+        for (int l = 0; l < LP + LQ; ++l) load(l, 0, 0);
+        if constexpr (WALK == kF8FirstReadsAhead) {
+            // As nt_product.h: behind the first barrier nobody reads the other stage any more, and its loads go out between the first rows of
+            // MFMAs; behind the second they have landed, and the next slab's first fragments are read under the last MFMAs.
+            static_assert(MI >= 4);
+            Operand q[2][NI], p[2];
+            auto first_reads = [&](int stage, int to) {
+                const unsigned char* at_p = lds + stage * kStage + wm * (BM / WM) * 128;
+                const unsigned char* at_q = lds + stage * kStage + BM * 128 + wn * (BN / WN) * 128;
+#pragma unroll
+                for (int j = 0; j < NI; ++j) read(q[to][j], at_q + j * 2048);
+                read(p[0], at_p);
+            };
+            constexpr int kLoadRows = MI / 2;
+            auto step = [&](int slab, auto odd) {
+                constexpr int now = decltype(odd)::value;
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                scales(slab);
+                const bool more = slab + 1 < slabs;
+                const unsigned char* at_p = lds + now * kStage + wm * (BM / WM) * 128;
+                static_for<0, MI>([&](auto row) {
+                    constexpr int i = decltype(row)::value;
+                    const Operand x = p[i & 1];
+                    if constexpr (i + 1 < MI) read(p[(i + 1) & 1], at_p + (i + 1) * 2048);
+                    if constexpr (i < kLoadRows) {
+                        if (more)
+#pragma unroll
+                            for (int l = (LP + LQ) * i / kLoadRows; l < (LP + LQ) * (i + 1) / kLoadRows; ++l) load(l, slab + 1, now ^ 1);
+                    }
+                    if constexpr (i + 1 == MI) {
+                        if (more) {
+                            asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+                            first_reads(now ^ 1, now ^ 1);
+                        }
+                    }
+                    row_of_products(i, x, q[now]);
+                });
+            };
+            asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+            first_reads(0, 0);
+            int slab = 0;
+            for (; slab + 1 < slabs; slab += 2) {
+                step(slab, std::integral_constant<int, 0>{});
+                step(slab + 1, std::integral_constant<int, 1>{});
+            }
+            if (slab < slabs) step(slab, std::integral_constant<int, 0>{});
+        } else {
+            for (int slab = 0; slab < slabs; ++slab) {
+                // the slab has landed and this wavefront's reads of the other stage are done; behind the barrier, everyone's
+                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                const int stage = slab & 1;
+                scales(slab);
+                if (slab + 1 < slabs)
+#pragma unroll
+                    for (int l = 0; l < LP + LQ; ++l) load(l, slab + 1, stage ^ 1);
+                const unsigned char* at_p = lds + stage * kStage + wm * (BM / WM) * 128;
+                const unsigned char* at_q = lds + stage * kStage + BM * 128 + wn * (BN / WN) * 128;
+                Operand q[NI];
+#pragma unroll
+                for (int j = 0; j < NI; ++j) read(q[j], at_q + j * 2048);
+#pragma unroll
+                for (int i = 0; i < MI; ++i) {
+                    Operand p;
+                    read(p, at_p + i * 2048);
+                    row_of_products(i, p, q);
+                }
+            }
+        }
+    }
+    // The compiler may move the last MFMAs down to where their results are stored, under a condition that lanes differ in; the instruction
+    // takes its operands from all lanes. So the sums are complete here.
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) asm volatile("" : "+v"(acc[i][j]));
+
+    // ---- results: lane holds R[row][col .. col + 3]
+    if (!a.along_rows && !a.experts && (int)blockIdx.x >= plan.whole) {
+        v4f* to = reinterpret_cast<v4f*>(a.partial) + (int64_t)(blockIdx.x - plan.whole) * (MI * NI * W * 64) + threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) to[(i * NI + j) * (W * 64)] = acc[i][j];
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        const int r = t.row0 + wm * (BM / WM) + 16 * i + (lane & 15);
+        if (r >= t.count) continue;
+        bool there = true;
+        if (a.source && !a.along_rows) there = (unsigned)a.source[t.first + r] < (unsigned)a.t;
+        const int64_t row = a.along_rows ? (int64_t)t.expert * a.rows + r : (int64_t)t.first + r;
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            const int c = t.col0 + wn * (BN / WN) + 16 * j + (lane >> 4) * 4;
+            if (c < a.n) store_four(a, row, c, acc[i][j], there);
+        }
+    }
+}
+
+// The shared tiles: parts added up in order, a workgroup for a 16 x 16 result of each wavefront.
+template <int BM, int BN, int WM, int WN>
+__launch_bounds__(WM * WN * 64)
+__global__ void f8_join_kernel(F8Args a, F8Plan plan) {
+    constexpr int W = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
+    const int i = blockIdx.y / NI, j = blockIdx.y % NI;
+    int tm, tn;
+    tile_of_logical(plan.whole + blockIdx.x, plan.tiles_m, plan.tiles_n, tm, tn);
+    const v4f* from = reinterpret_cast<const v4f*>(a.partial) + ((int64_t)blockIdx.x * plan.parts * (MI * NI) + blockIdx.y) * (W * 64) + threadIdx.x;
+    v4f sum = from[0];
+    for (int p = 1; p < plan.parts; ++p) {
+        const v4f x = from[(int64_t)p * (MI * NI * W * 64)];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += x[e];
+    }
+    const int r = tm * BM + wm * (BM / WM) + (lane & 15) + 16 * i, c = tn * BN + wn * (BN / WN) + (lane >> 4) * 4 + 16 * j;
+    if (r < a.rows && c < a.n) store_four(a, r, c, sum, true);
+}
+
+template <int BM, int BN, int WM, int WN, int WALK, bool EXACT, bool WIDE, bool Q_ROWS>
+hipError_t launch_f8_shape(const F8Args& a, const F8Plan& plan, int64_t grid, hipStream_t st) {
+    constexpr auto kernel = f8_product_kernel<BM, BN, WM, WN, WALK, EXACT, WIDE, Q_ROWS>;
+    constexpr int bytes = 2 * (BM + BN) * 128;
+    if (grid <= 0 || grid > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (hipError_t e = allow_dynamic_lds<kernel>(bytes); e != hipSuccess) return e;
+    kernel<<<dim3((unsigned)grid), dim3(WM * WN * 64), bytes, st>>>(a, plan);
+    const int rest = a.experts || a.along_rows ? 0 : plan.tiles_m * plan.tiles_n - plan.whole;
+    if (rest) f8_join_kernel<BM, BN, WM, WN><<<dim3((unsigned)rest, BM / WM / 16 * (BN / WN / 16)), dim3(WM * WN * 64), 0, st>>>(a, plan);
+    return hipGetLastError();
+}
+
+template <int BM, int BN, int WM, int WN, int WALK, bool EXACT>
+hipError_t launch_f8_tile(const F8Args& a, F8Plan plan, hipStream_t st) {
+    plan.tiles_m = (a.rows + BM - 1) / BM;
+    plan.tiles_n = (a.n + BN - 1) / BN;
+    int64_t grid;
+    if (a.along_rows)
+        grid = (int64_t)plan.tiles_m * plan.tiles_n * std::max(a.experts, 1);
+    else if (a.experts)
+        grid = pad_to(((int64_t)plan.tiles_m + std::min(a.experts, a.rows)) * plan.tiles_n, 8);
+    else
+        grid = plan.whole + ((int64_t)plan.tiles_m * plan.tiles_n - plan.whole) * plan.parts;
+    if (a.along_rows) return launch_f8_shape<BM, BN, WM, WN, WALK, EXACT, false, true>(a, plan, grid, st);
+    if (a.scale_type == OZIMMU_F32) return launch_f8_shape<BM, BN, WM, WN, WALK, EXACT, true, false>(a, plan, grid, st);
+    return launch_f8_shape<BM, BN, WM, WN, WALK, EXACT, false, false>(a, plan, grid, st);
+}
+
+}  // namespace
+}  // namespace ozimmu

@@ -13,7 +13,8 @@ _LIB_PATH = Path(__file__).resolve().parent / "libozimmu.so"
 
 (OK, ERR_BAD_DIM, ERR_BAD_LD, ERR_BAD_SLICES, ERR_NULL, ERR_WORKSPACE, ERR_HIP, ERR_NOT_IMPLEMENTED,
  ERR_TOO_LARGE, ERR_BAD_TYPE, ERR_BAD_POLYNOMIAL, ERR_MISALIGNED) = range(12)
-F32, BF16, F16 = range(3)            # ozimmu_type_t
+F32, BF16, F16, E4M3, E8M0 = range(5)            # ozimmu_type_t
+SOFTMAX, SIGMOID = range(2)          # ozimmu_score_t
 MAX_SLICES = 16
 ROW_ALIGN = 128
 K_ALIGN = 32
@@ -30,6 +31,9 @@ EXPORTS = (
     "ozimmu_dgemm_auto", "ozimmu_dgemm_blas_auto", "ozimmu_zgemm_blas_auto",
     "ozimmu_q4_geometry", "ozimmu_q4_split", "ozimmu_q4_expand", "ozimmu_q4_workspace_bytes", "ozimmu_q4_gemm", "ozimmu_q4_gemm_grad",
     "ozimmu_orthogonalize_workspace_bytes", "ozimmu_orthogonalize",
+    "ozimmu_f8_geometry", "ozimmu_f8_split", "ozimmu_f8_expand", "ozimmu_f8_workspace_bytes", "ozimmu_f8_gemm", "ozimmu_f8_gemm_grad",
+    "ozimmu_f8_weight_grad", "ozimmu_route", "ozimmu_route_grad", "ozimmu_expert_order_workspace_bytes", "ozimmu_expert_order",
+    "ozimmu_expert_combine", "ozimmu_expert_combine_grad",
 )
 PROBE_EXPORTS = ("ozimmu_probe_int8_mfma",)      # include/ozimmu_probe.h: measurement utility, not the product path
 
@@ -130,6 +134,24 @@ def lib() -> ctypes.CDLL:
         L.ozimmu_orthogonalize_workspace_bytes.argtypes = [i64, i64, i64, ctypes.POINTER(sz)]
         L.ozimmu_orthogonalize.restype = i32
         L.ozimmu_orthogonalize.argtypes = [i64, i64, i64, i32, vp, i64, i64, vp, i64, i64, i32] + [ctypes.c_double] * 4 + [vp, sz, vp]
+        for name, args in {
+            "f8_geometry": [i64, ctypes.POINTER(i64), ctypes.POINTER(i64)],
+            "f8_split": [i64, i64, i32, i32, vp, i64, vp, i64, vp, i64, vp],
+            "f8_expand": [i64, i64, i32, vp, i64, i32, vp, i64, i32, vp, i64, vp],
+            "f8_workspace_bytes": [i32, i64, i64, i64, i64, i64, i32, ctypes.POINTER(sz)],
+            "f8_gemm": [i64, i64, i64, i64, i64, i32, vp, i64, vp, i64, vp, i64, i32, vp, i64, vp, vp, i32, vp, i64, vp, sz, vp],
+            "f8_gemm_grad": [i64, i64, i64, i64, i32, vp, i64, vp, i64, vp, i64, i32, vp, i64, vp, i32, vp, i64, vp, sz, vp],
+            "f8_weight_grad": [i64, i64, i64, i64, i64, i32, vp, i64, vp, i64, vp, vp, i32, vp, i64, vp, sz, vp],
+            "route": [i64, i64, i32, i32, vp, i64, vp, i32, i32, i32, i32, ctypes.c_double, vp, vp, vp],
+            "route_grad": [i64, i64, i32, i32, vp, i64, vp, vp, i32, i32, ctypes.c_double, vp, i64, vp],
+            "expert_order_workspace_bytes": [i64, i32, i64, ctypes.POINTER(sz)],
+            "expert_order": [i64, i32, i64, vp, vp, vp, vp, vp, sz, vp],
+            "expert_combine": [i64, i32, i64, i64, i32, vp, i64, vp, vp, vp, i64, vp],
+            "expert_combine_grad": [i64, i32, i64, i64, i32, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp],
+        }.items():
+            f = getattr(L, "ozimmu_" + name)
+            f.restype = i32
+            f.argtypes = args
         dp = ctypes.POINTER(ctypes.c_double)
         L.ozimmu_probe_int8_mfma.restype = i32
         L.ozimmu_probe_int8_mfma.argtypes = [i32, i32, i32, dp, dp]
@@ -617,6 +639,273 @@ def orthogonalize(G, X, workspace, steps: int = 5, coefficients=(3.4445, -4.7750
     a, b, c = coefficients
     _call(lib().ozimmu_orthogonalize, stream, (G, X, workspace), batch, m, n, _type_of(G.dtype), G.data_ptr(), *ld["g"], X.data_ptr(), *ld["x"], int(steps),
           float(a), float(b), float(c), float(eps), _ptr(workspace), _size(workspace))
+
+
+def f8_geometry(k: int):
+    """(bytes of a row of codes, bytes of a row of scales) of a matrix of k columns in 8-bit floating point (see ozimmu.h)."""
+    row_bytes_, scale_bytes_ = ctypes.c_int64(), ctypes.c_int64()
+    _check(lib().ozimmu_f8_geometry(k, ctypes.byref(row_bytes_), ctypes.byref(scale_bytes_)))
+    return row_bytes_.value, scale_bytes_.value
+
+
+def f8_row_bytes(k: int) -> int:
+    return f8_geometry(k)[0]
+
+
+def f8_scale_bytes(k: int) -> int:
+    return f8_geometry(k)[1]
+
+
+_byte_types = _scale_types = None
+
+
+def _f8_types():
+    global _byte_types, _scale_types
+    if _torch is None:
+        _load_torch()
+    _byte_types = (_torch.uint8, _torch.float8_e4m3fn)
+    _scale_types = {_torch.uint8: E8M0, _torch.float8_e8m0fnu: E8M0, _torch.float32: F32}
+
+
+def _f8_matrix(what: str, codes, scales, n: int, k: int, block_rows: int):
+    """Checks codes and scales of an n x k matrix; (codes' row stride, scales' type, scales' row stride)."""
+    if _byte_types is None:
+        _f8_types()
+    row_bytes_, groups = (k + 127) // 128 * 128, (k + 127) // 128
+    rows, cols, ldq = _rows(codes)
+    if rows != n or cols < row_bytes_ or codes.dtype not in _byte_types:
+        raise ValueError(f"{what}: expected {n} rows of at least {row_bytes_} codes (uint8 or float8_e4m3fn)")
+    kind = _scale_types.get(scales.dtype)
+    srows, scols, lds = _rows(scales)
+    most = groups if kind == F32 else (groups + 3) // 4 * 4
+    if kind is None or srows != -(-n // block_rows) or scols < most:
+        raise ValueError(f"{what}' scales: expected {-(-n // block_rows)} rows of at least {most} (float8_e8m0fnu or uint8: multiples of four) or {groups} (float32)")
+    return (ldq if n > 1 else row_bytes_), kind, (lds if srows > 1 else most)
+
+
+def f8_split(W, codes, scales, block_rows: int = 128, stream=None) -> None:
+    """W (n x k; float32, bfloat16 or float16) into codes (n x f8_row_bytes(k); uint8 or float8_e4m3fn) and scales (ceil(n / block_rows) x
+    f8_scale_bytes(k); uint8 or float8_e8m0fnu), in blocks of block_rows (1: tokens, 128: weights) x 128."""
+    n, k, ldw = _rows(W)
+    _expect(block_rows in (1, 128), "block_rows: expected 1 or 128")
+    ldq, kind, lds = _f8_matrix("codes", codes, scales, n, k, block_rows)
+    _expect(kind == E8M0, "the cut makes scales of a byte (uint8 or float8_e8m0fnu)")
+    _call(lib().ozimmu_f8_split, stream, (W, codes, scales), n, k, block_rows, _type_of(W.dtype), W.data_ptr(), ldw, codes.data_ptr(), ldq, scales.data_ptr(), lds)
+
+
+def f8_expand(codes, scales, W, block_rows: int = 128, stream=None) -> None:
+    """The values that codes and scales stand for, into W (n x k; float32, bfloat16 or float16)."""
+    n, k, ldw = _rows(W)
+    _expect(block_rows in (1, 128), "block_rows: expected 1 or 128")
+    ldq, kind, lds = _f8_matrix("codes", codes, scales, n, k, block_rows)
+    _call(lib().ozimmu_f8_expand, stream, (W, codes, scales), n, k, block_rows, codes.data_ptr(), ldq, kind, scales.data_ptr(), lds, _type_of(W.dtype), W.data_ptr(), ldw)
+
+
+_F8_OPS = {"gemm": 0, "grad": 1, "weight_grad": 2}
+
+
+def f8_workspace_bytes(op: str, t: int, n: int, k: int, dtype, rows=None, experts: int = 0) -> int:
+    """Workspace of f8_gemm ("gemm"), f8_gemm_grad ("grad") or f8_weight_grad ("weight_grad"): t tokens, rows of Y and dY (experts; t without
+    them), and the type of X and dY."""
+    if _byte_types is None:
+        _f8_types()
+    _expect(op in _F8_OPS, "op: expected gemm, grad or weight_grad")
+    out = ctypes.c_size_t()
+    kind = E4M3 if dtype in _byte_types else _type_of(dtype)
+    _check(lib().ozimmu_f8_workspace_bytes(_F8_OPS[op], t, t if rows is None else rows, n, k, experts, kind, ctypes.byref(out)))
+    return out.value
+
+
+def alloc_f8_workspace(op: str, t: int, n: int, k: int, dtype, rows=None, experts: int = 0, device="cuda"):
+    """A uint8 tensor of the size that the operator asks for; it serves fewer tokens and rows too."""
+    import torch
+
+    return torch.empty(max(f8_workspace_bytes(op, t, n, k, dtype, rows, experts), WORKSPACE_ALIGN), dtype=torch.uint8, device=device)
+
+
+def _ints(t, count: int, what: str) -> int:
+    if t.dtype is not _torch.int32 or t.numel() != count or not t.is_contiguous():
+        raise ValueError(f"{what}: expected {count} contiguous int32 values")
+    return t.data_ptr()
+
+
+def _floats(t, count: int, what: str) -> int:
+    if t.dtype is not _torch.float32 or t.numel() != count or not t.is_contiguous():
+        raise ValueError(f"{what}: expected {count} contiguous float32 values")
+    return t.data_ptr()
+
+
+def _by_expert(t, offsets):
+    """A tensor of one more dimension over the experts, as the rows of all of them; (it, experts)."""
+    if offsets is None:
+        return t, 0
+    if t.dim() != 3 or (t.shape[0] > 1 and t.shape[1] > 0 and t.stride(0) != t.stride(1) * t.shape[1]) or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError("over experts, weights, scales and weights' gradients have three dimensions, the experts' rows one behind the other")
+    rows = t.shape[0] * t.shape[1]
+    return t.as_strided((rows, t.shape[2]), (t.stride(1) if t.shape[1] > 1 else t.stride(0) if t.shape[0] > 1 else max(t.shape[2], 1), 1)), t.shape[0]
+
+
+def _f8_product(gradient, V, codes, scales, R, workspace, v_scales, offsets, source, stream):
+    if _byte_types is None:
+        _f8_types()
+    t, inner, ldv = _rows(V)
+    rows, outer, ldr = _rows(R)
+    codes, experts = _by_expert(codes, offsets)
+    scales, experts_s = _by_expert(scales, offsets)
+    if V.dtype in _byte_types:
+        _expect(v_scales is not None, "codes of tokens need their scales")
+        # the width of codes is padded: the other sizes tell it
+        inner = codes.shape[0] // max(experts, 1) if gradient else min(inner, codes.shape[1])
+        kind = E4M3
+    else:
+        _expect(v_scales is None, "only codes have scales")
+        kind = _type_of(V.dtype)
+    n, k = (inner, outer) if gradient else (outer, inner)
+    if experts != experts_s or codes.shape[0] != n * max(experts, 1):
+        raise ValueError(f"codes: expected {n} rows" + (" for each expert" if experts else ""))
+    each = -(-n // 128)
+    row_bytes_, groups = (k + 127) // 128 * 128, (k + 127) // 128
+    qrows, cols, ldq = _rows(codes)
+    skind = _scale_types.get(scales.dtype)
+    srows, scols, lds = _rows(scales)
+    most = groups if skind == F32 else (groups + 3) // 4 * 4
+    if cols < row_bytes_ or codes.dtype not in _byte_types:
+        raise ValueError(f"codes: expected rows of at least {row_bytes_} codes (uint8 or float8_e4m3fn)")
+    if skind is None or srows != each * max(experts, 1) or scols < most:
+        raise ValueError(f"scales: expected {each} rows" + (" for each expert" if experts else "") + f" of at least {most} (float8_e8m0fnu or uint8: multiples of four) or {groups} (float32)")
+    vs, ldvs = None, 0
+    if kind == E4M3:
+        ldv_, _, ldvs = _f8_matrix("tokens", V, v_scales, t, inner, 1)
+        _expect(v_scales.dtype is not _torch.float32, "scales of tokens are bytes")
+        vs, ldv = v_scales.data_ptr(), ldv_
+    if gradient or source is None:
+        _expect(rows == t, "tokens and result must have the same number of rows")
+    tail = (_type_of(R.dtype), R.data_ptr(), ldr, None if workspace is None else workspace.data_ptr(), _size(workspace))
+    po = None if offsets is None else _ints(offsets, experts + 1, "offsets")
+    ps = None if source is None else _ints(source, rows, "source")
+    if qrows <= 1:
+        ldq = row_bytes_
+    if srows <= 1:
+        lds = most
+    tensors = (V, codes, scales, R, workspace, v_scales, offsets, source)
+    if gradient:
+        _call(lib().ozimmu_f8_gemm_grad, stream, tensors, rows, n, k, experts, kind, V.data_ptr(), ldv, vs, ldvs, codes.data_ptr(), ldq, skind, scales.data_ptr(), lds, po, *tail)
+    else:
+        _call(lib().ozimmu_f8_gemm, stream, tensors, t, rows, n, k, experts, kind, V.data_ptr(), ldv, vs, ldvs, codes.data_ptr(), ldq, skind, scales.data_ptr(), lds, po, ps, *tail)
+
+
+def f8_gemm(X, codes, scales, Y, workspace=None, x_scales=None, offsets=None, source=None, stream=None) -> None:
+    """Y = X W^T for weights in 8-bit floating point (X: t x k, Y: rows x n, each float32, bfloat16 or float16). X is cut in the call, or given
+    as codes with x_scales (f8_split with block_rows 1). Over experts: codes and scales with a first dimension of experts, offsets (experts + 1,
+    int32): the rows of Y of each, and source (rows, int32): the row of X for each row of Y (without it X has the rows of Y)."""
+    _f8_product(False, X, codes, scales, Y, workspace, x_scales, offsets, source, stream)
+
+
+def f8_gemm_grad(dY, codes, scales, dX, workspace, dy_scales=None, offsets=None, stream=None) -> None:
+    """dX = dY W for weights in 8-bit floating point (dY: rows x n, dX: rows x k): the gradient of f8_gemm's result, on its way to X. Over
+    experts dX has the rows of dY: expert_combine without weights adds those of a token."""
+    _f8_product(True, dY, codes, scales, dX, workspace, dy_scales, offsets, None, stream)
+
+
+def f8_weight_grad(dY, X, dW, workspace, offsets=None, source=None, stream=None) -> None:
+    """dW = dY^T X in 8-bit floating point, cut along the tokens (dY: rows x n, X: t x k of one type, dW: n x k). Over experts: dW with a
+    first dimension of experts, offsets and source as for f8_gemm."""
+    if _byte_types is None:
+        _f8_types()
+    rows, n, lddy = _rows(dY)
+    t, k, ldx = _rows(X)
+    flat, experts = _by_expert(dW, offsets)
+    wrows, cols, lddw = _rows(flat)
+    _expect(dY.dtype == X.dtype, "dY and X must have one type")
+    _expect(wrows == n * max(experts, 1) and cols == k, f"dW: expected {n} x {k}" + (" for each expert" if experts else ""))
+    if source is None:
+        _expect(rows == t, "dY and X must have the same number of rows")
+    po = None if offsets is None else _ints(offsets, experts + 1, "offsets")
+    ps = None if source is None else _ints(source, rows, "source")
+    _call(lib().ozimmu_f8_weight_grad, stream, (dY, X, dW, workspace, offsets, source), t, rows, n, k, experts, _type_of(X.dtype), dY.data_ptr(), lddy, X.data_ptr(), ldx, po, ps,
+          _type_of(dW.dtype), dW.data_ptr(), lddw, _ptr(workspace), _size(workspace))
+
+
+_SCORES = {"softmax": SOFTMAX, "sigmoid": SIGMOID}
+
+
+def _pairs(indices, what: str):
+    if indices.dim() != 2:
+        raise ValueError(f"{what}: expected a row for each token")
+    return indices.shape
+
+
+def route(logits, indices, weights, bias=None, score: str = "softmax", groups: int = 1, top_groups: int = 1, renormalize: bool = True, scale: float = 1.0,
+          stream=None) -> None:
+    """The best experts of each token and their weights (see ozimmu.h). logits: t x experts (float32, bfloat16 or float16); indices (int32)
+    and weights (float32): t x top, contiguous; bias: experts, float32, for the choice alone."""
+    t, experts, ldl = _rows(logits)
+    rows, top = _pairs(indices, "indices")
+    _expect(rows == t and score in _SCORES, "logits and indices must have the same number of rows, and the score is softmax or sigmoid")
+    kind = _type_of(logits.dtype)
+    _call(lib().ozimmu_route, stream, (logits, indices, weights, bias), t, experts, top, kind, logits.data_ptr(), ldl, None if bias is None else _floats(bias, experts, "bias"),
+          _SCORES[score], groups, top_groups, int(bool(renormalize)), float(scale), _ints(indices, t * top, "indices"), _floats(weights, t * top, "weights"))
+
+
+def route_grad(logits, indices, dweights, dlogits, score: str = "softmax", renormalize: bool = True, scale: float = 1.0, stream=None) -> None:
+    """The gradient of the logits (dlogits: their shape and type) from that of route's weights; the choice counts as constant."""
+    t, experts, ldl = _rows(logits)
+    rows, top = _pairs(indices, "indices")
+    drows, dcols, lddl = _rows(dlogits)
+    _expect(rows == t and score in _SCORES, "logits and indices must have the same number of rows, and the score is softmax or sigmoid")
+    _expect((drows, dcols) == (t, experts) and dlogits.dtype == logits.dtype, "dlogits must have the shape and type of the logits")
+    kind = _type_of(logits.dtype)
+    _call(lib().ozimmu_route_grad, stream, (logits, indices, dweights, dlogits), t, experts, top, kind, logits.data_ptr(), ldl, _ints(indices, t * top, "indices"),
+          _floats(dweights, t * top, "dweights"), _SCORES[score], int(bool(renormalize)), float(scale), dlogits.data_ptr(), lddl)
+
+
+def expert_order_workspace_bytes(t: int, top: int, experts: int) -> int:
+    out = ctypes.c_size_t()
+    _check(lib().ozimmu_expert_order_workspace_bytes(t, top, experts, ctypes.byref(out)))
+    return out.value
+
+
+def alloc_expert_order_workspace(t: int, top: int, experts: int, device="cuda"):
+    """A uint8 tensor of the size that expert_order asks for; it serves fewer tokens too."""
+    import torch
+
+    return torch.empty(max(expert_order_workspace_bytes(t, top, experts), WORKSPACE_ALIGN), dtype=torch.uint8, device=device)
+
+
+def expert_order(indices, experts: int, offsets, source, place, workspace=None, stream=None) -> None:
+    """The (token, choice) pairs of indices (t x top) sorted by expert: offsets (experts + 1), source (t top: the token of each row) and
+    place (t x top: the row of each pair, -1 for an index that is no expert). All int32."""
+    if _torch is None:
+        _load_torch()
+    t, top = _pairs(indices, "indices")
+    _call(lib().ozimmu_expert_order, stream, (indices, offsets, source, place, workspace), t, top, experts, _ints(indices, t * top, "indices"), _ints(offsets, experts + 1, "offsets"),
+          _ints(source, t * top, "source"), _ints(place, t * top, "place"), _ptr(workspace), _size(workspace))
+
+
+def expert_combine(O, place, weights, Y, stream=None) -> None:
+    """Y[i] = sum over j of weights[i, j] O[place[i, j]] (O: rows x n, Y: t x n of one type; place, weights: t x top; weights None: ones, which
+    gives the gradient of taking rows by `source`)."""
+    if _torch is None:
+        _load_torch()
+    rows, n, ldo = _rows(O)
+    t, cols, ldy = _rows(Y)
+    prow, top = _pairs(place, "place")
+    _expect(prow == t and cols == n and O.dtype == Y.dtype, "O and Y must have one type and width, place and Y the same number of rows")
+    _call(lib().ozimmu_expert_combine, stream, (O, place, weights, Y), t, top, rows, n, _type_of(O.dtype), O.data_ptr(), ldo, _ints(place, t * top, "place"),
+          None if weights is None else _floats(weights, t * top, "weights"), Y.data_ptr(), ldy)
+
+
+def expert_combine_grad(dY, O, place, weights, dO, dweights, stream=None) -> None:
+    """The gradients of expert_combine: dO (rows x n; rows without a pair are left alone) and dweights (t x top, float32)."""
+    if _torch is None:
+        _load_torch()
+    t, n, lddy = _rows(dY)
+    rows, cols, ldo = _rows(O)
+    drows, dcols, lddo = _rows(dO)
+    prow, top = _pairs(place, "place")
+    _expect(prow == t and cols == n and (drows, dcols) == (rows, n) and O.dtype == dY.dtype == dO.dtype, "dY, O and dO must have one type and width, dO the rows of O, place those of dY")
+    _call(lib().ozimmu_expert_combine_grad, stream, (dY, O, place, weights, dO, dweights), t, top, rows, n, _type_of(O.dtype), dY.data_ptr(), lddy, O.data_ptr(), ldo,
+          _ints(place, t * top, "place"), _floats(weights, t * top, "weights"), dO.data_ptr(), lddo, _floats(dweights, t * top, "dweights"))
 
 
 def probe_int8_mfma(pattern: int, shape: int = 0, iters: int = 200000):
