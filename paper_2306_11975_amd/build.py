@@ -18,7 +18,7 @@ BLAS_CLIENT = PKG / "blas_client"     # plain rocBLAS/hipBLAS program the interp
 
 SOURCES = ["split.hip", "gemm.hip", "gemm_real.hip", "gemm_dd.hip", "gemm_complex.hip", "gate.hip", "gate_many.hip", "small.hip", "small_complex.hip", "probes.hip", "static_scratch.hip", "api.cpp",
            "nt_product.hip", "nt_product_two.hip", "q4.hip", "q4_few.hip", "q4_token.hip", "q4_tile.hip", "orthogonalize.hip", "orthogonalize_small.hip", "weights.cpp",
-           "f8_cut.hip", "f8_few.hip", "f8_product.hip", "f8_product_exact.hip", "route.hip", "experts.hip", "eight.cpp"]
+           "f8_cut.hip", "f8_few.hip", "f8_product.hip", "f8_product_exact.hip", "f8_large.hip", "route.hip", "experts.hip", "eight.cpp"]
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-ffp-contract=off", "-Wall", f"-I{INCLUDE}", f"-I{CSRC}"]
 # device code: gfx950 only; packed-FP32 instruction selection is switched off on the test machines
 DEVICE = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
@@ -32,7 +32,7 @@ def hipcc() -> str:
 
 
 # translation units whose kernels write M0 in inline assembly (the LDS base of the direct loads)
-USES_M0 = ("gemm_real.hip", "gemm_dd.hip", "gemm_complex.hip", "nt_product.hip", "nt_product_two.hip", "f8_product.hip", "f8_product_exact.hip")
+USES_M0 = ("gemm_real.hip", "gemm_dd.hip", "gemm_complex.hip", "nt_product.hip", "nt_product_two.hip", "f8_product.hip", "f8_product_exact.hip", "f8_large.hip")
 # of those, the ones whose MFMAs the compiler issues (and keeps apart by itself)
 PLAIN_MFMA = ("nt_product.hip", "nt_product_two.hip", "f8_product.hip", "f8_product_exact.hip")
 

@@ -40,10 +40,20 @@ bool ws_ok(const void* ws, size_t bytes, size_t needed) { return needed == 0 || 
 
 enum { kGemm = 0, kGemmGrad = 1, kWeightGrad = 2 };
 
+// Few rows: straight from memory, 16 rows of tokens at a time, without a cut of its own (f8_few.hip). Cut and tiles take two launches, about
+// 2.3 us more, but stream the weights through LDS by whole lines and read the tokens once for every 64 columns: us (16-bit results) few rows, tiles:
+// 2048 x 2048 1 token 4.4, 8.7, 32 5.2, 8.9, 128 11.0, 10.4; 8192 x 4096 1 token 9.5, 13.2, 16 12.4, 13.4, 32 19.6, 13.6; 16384 x 8192 1 token
+// 27, 26; 64 experts of 2048 x 2048 with 128 rows 59, 44; 8 of 1000 x 640 with 64 rows 4.8, 7.5. The limit is where they meet, in weights read. (The
+// answer turns once as rows grow, so that a workspace serves fewer.)
+bool few_rows(int64_t rows, int64_t n, int64_t k, int64_t experts) {
+    const int64_t tiles = experts ? rows / 16 + std::min(experts, rows) : (rows + 15) / 16;
+    return (double)tiles * (double)n * (double)k <= 33554432.0;
+}
+
 // What a call keeps in its workspace: the cut rows (P), for gradients the transposed weights or the cut columns of X (Q).
 struct Layout {
     int64_t ldp, ldsp, ldq, ldsq;
-    size_t off_p, off_sp, off_q, off_sq, total;
+    size_t off_p, off_sp, off_q, off_sq, off_partial, partial, total;
 };
 Layout layout(int op, int64_t t, int64_t rows, int64_t n, int64_t k, int64_t experts, int type) {
     Layout o{};
@@ -61,7 +71,7 @@ Layout layout(int op, int64_t t, int64_t rows, int64_t n, int64_t k, int64_t exp
         const int64_t inner = op == kGemm ? k : n;
         o.ldp = f8_row_bytes(inner);
         o.ldsp = f8_scale_bytes(inner);
-        if (type != OZIMMU_E4M3) {
+        if (type != OZIMMU_E4M3 && !few_rows(rows, n, k, experts)) {
             o.off_p = take((op == kGemm ? t : rows) * o.ldp);
             o.off_sp = take((op == kGemm ? t : rows) * o.ldsp);
         }
@@ -72,6 +82,9 @@ Layout layout(int op, int64_t t, int64_t rows, int64_t n, int64_t k, int64_t exp
             o.off_sq = take(e * f8_groups(k) * o.ldsq * 4);
         }
     }
+    if (experts == 0 && !(op != kWeightGrad && few_rows(rows, n, k, experts)))
+        o.partial = op == kWeightGrad ? f8_partial_room(n, k, f8_groups(rows)) : f8_partial_room(rows, op == kGemm ? n : k, f8_groups(op == kGemm ? k : n));
+    o.off_partial = take((int64_t)o.partial);
     o.total = off;
     return o;
 }
@@ -87,12 +100,12 @@ ozimmu_status_t check_experts(int64_t t, int64_t rows, int64_t experts, const in
     return misaligned(offsets, 4) || (source && misaligned(source, 4)) ? OZIMMU_ERR_MISALIGNED : OZIMMU_OK;
 }
 
-// Few rows to an expert: the kernel that reads the weights once for every sixteen of them.
-bool few_rows(int64_t rows, int64_t experts) { return rows <= 16 * std::max<int64_t>(experts, 1); }
-
-hipError_t product(const F8Args& a, hipStream_t st) {
-    if (!a.along_rows && few_rows(a.rows, a.experts)) return launch_f8_few(a, st);
-    return a.out_type == OZIMMU_F32 ? launch_f8_tiles_exact(a, st) : launch_f8_tiles(a, st);
+// `few`: as few_rows has it (never for weights' gradients, whose codes lie in the workspace)
+hipError_t product(const F8Args& a, bool few, hipStream_t st) {
+    if (few) return launch_f8_few(a, st);
+    const F8Choice c = choose_f8_tile(a);
+    if (a.out_type == OZIMMU_F32) return launch_f8_tiles_exact(a, c, st);
+    return c.shape == kF8Tile256 ? launch_f8_large(a, st) : launch_f8_tiles(a, c, st);
 }
 
 ozimmu_status_t f8_product(int op, int64_t t, int64_t rows, int64_t n, int64_t k, int64_t experts, int type, const void* V, int64_t ldv, const uint8_t* v_scales, int64_t ldvs,
@@ -131,7 +144,12 @@ ozimmu_status_t f8_product(int op, int64_t t, int64_t rows, int64_t n, int64_t k
     a.out = R;
     a.out_type = out_type;
     a.ldo = ldr;
-    if (inner == 0 || t == 0) return hip_status(product(a, st));   // zeros
+    a.V = V;
+    a.v_type = type;
+    a.ldv = ldv;
+    a.k = inner;
+    const bool few = few_rows(rows, n, k, experts);
+    if (inner == 0 || t == 0) return hip_status(launch_f8_few(a, st));   // zeros
     a.slabs = (int)f8_groups(inner);
     hipError_t e = hipSuccess;
     if (type == OZIMMU_E4M3) {
@@ -139,7 +157,7 @@ ozimmu_status_t f8_product(int op, int64_t t, int64_t rows, int64_t n, int64_t k
         a.ldp = ldv;
         a.sp = v_scales;
         a.ldsp = ldvs;
-    } else {
+    } else if (!few) {
         a.P = base + o.off_p;
         a.ldp = o.ldp;
         a.sp = base + o.off_sp;
@@ -158,7 +176,9 @@ ozimmu_status_t f8_product(int op, int64_t t, int64_t rows, int64_t n, int64_t k
         a.ldsq = o.ldsq;
         if (e == hipSuccess) e = launch_f8_transpose(std::max<int64_t>(experts, 1), n, k, codes, ldq, scale_type, scales, lds, base + o.off_q, base + o.off_sq, st);
     }
-    if (e == hipSuccess) e = product(a, st);
+    if (o.partial) a.partial = reinterpret_cast<float*>(base + o.off_partial);
+    a.partial_bytes = o.partial;
+    if (e == hipSuccess) e = product(a, few, st);
     return hip_status(e);
 }
 
@@ -172,6 +192,74 @@ ozimmu_status_t check_pairs(int64_t t, int top) {
 }
 
 }  // namespace
+
+namespace ozimmu {
+
+// Room for the sums of shared tiles: at most eight workgroups to a tile, four slabs at least to each.
+size_t f8_partial_room(int64_t rows, int64_t n, int64_t slabs) {
+    const int64_t parts = std::min<int64_t>(8, slabs / 4);
+    if (parts < 2) return 0;
+    const double bytes = (double)pad_to(rows, 128) * (double)pad_to(n, 128) * (double)parts * sizeof(float);
+    return bytes < (double)kPartialBytes ? (size_t)bytes : kPartialBytes;
+}
+
+// By an estimate, in us: of a round of tiles, what the fullest compute unit takes for a slab, from `alone` (one workgroup) to `full` (`slots` / 256),
+// and what a round takes beside its slabs. Fitted to 35 products with 16-bit results and 14 with 32-bit ones, 64 to 16384 rows, 16 to 64 slabs, dense
+// and over 8 to 128 experts. 4096 x 4096 x 4096 by tiles of 256, 128, 64 x 128, 64, 32 x 64: 60, 76, 88, 119, 147; 1024 x 4096 x 4096: 42, 31, 26, 33,
+// 44; 512 x 2048 x 2048: 24, 16, 11, 9.1, 8.8; 8192 rows of 64 experts, 1024 x 1024: 25, 30, 28, 30, -. Over experts a tile's rows end with the
+// expert's: half a tile is counted for each.
+F8Choice choose_f8_tile(const F8Args& a) {
+    struct Shape {
+        int rows, cols, slots;
+        double alone, full, round, call;
+    };
+    static const Shape half[kF8Shapes] = {{256, 256, 256, 0.95, 1.5, 10.0, 5.0}, {128, 128, 512, 0.80, 1.10, 3.5, 3.0}, {64, 128, 768, 0.62, 0.87, 3.2, 2.5}, {64, 64, 1280, 0.38, 1.13, 1.3, 2.0},
+                                          {32, 64, 1536, 0.38, 0.83, 1.0, 2.0}};
+    static const Shape wide[kF8Shapes] = {{256, 256, 0, 0.0, 0.0, 0.0, 0.0}, {128, 128, 512, 1.5, 2.3, 4.0, 3.0}, {64, 128, 768, 0.9, 1.95, 3.0, 2.5}, {64, 64, 1024, 0.58, 1.43, 1.3, 2.0},
+                                          {32, 64, 1536, 0.50, 1.25, 1.0, 2.0}};
+    F8Choice best{kF8Tile64, 1, 1, a.slabs};
+    double best_us = 1e30;
+    for (int i = 0; i < kF8Shapes; ++i) {
+        const Shape& s = a.out_type == OZIMMU_F32 ? wide[i] : half[i];
+        if (s.slots == 0 || (i == kF8Tile256 && a.scale_type == OZIMMU_F32)) continue;
+        const double columns = (double)((a.n + s.cols - 1) / s.cols), tiles_m = (double)((a.rows + s.rows - 1) / s.rows), used = (double)std::min(a.experts, a.along_rows ? a.t : a.rows);
+        double all = tiles_m * columns, slabs = (double)a.slabs;
+        if (a.experts && a.along_rows) {
+            all *= used;
+            slabs = used > 0.0 ? (double)a.t / 128.0 / used + 0.5 : 0.0;
+        } else if (a.experts) {
+            all = std::max((double)a.rows / s.rows + 0.5 * used, used) * columns;
+        }
+        if (all > (double)(INT32_MAX / 64)) continue;
+        auto round_us = [&](double workgroups, double walk) {
+            if (workgroups <= 0.0) return 0.0;
+            const double most = (double)(s.slots / 256), deepest = std::ceil(workgroups / 256.0);
+            const double share = most > 1.0 ? (deepest - 1.0) / (most - 1.0) : workgroups / 256.0;
+            return s.round + walk * (s.alone + (s.full - s.alone) * share);
+        };
+        const double rounds = std::floor(all / s.slots), rest = all - rounds * s.slots;
+        const double whole_us = s.call + rounds * round_us(s.slots, slabs) + round_us(rest, slabs);
+        if (whole_us < best_us) {
+            best_us = whole_us;
+            best = F8Choice{i, (int)(a.experts ? 0.0 : all), 1, a.slabs};
+        }
+        if (a.experts || !a.partial || rest <= 0.0 || i == kF8Tile256) continue;
+        // the tiles of a last round that is not full may be shared, at the price of their sums' way through memory and of a launch
+        for (int parts = 2; parts <= 8 && rest * parts <= s.slots; ++parts) {
+            const int walk = (int)pad_to((a.slabs + parts - 1) / parts, 4), taken = (a.slabs + walk - 1) / walk;
+            const double bytes = rest * parts * s.rows * s.cols * sizeof(float);
+            if (taken != parts || bytes > (double)a.partial_bytes) continue;
+            const double us = s.call + rounds * round_us(s.slots, slabs) + round_us(rest * parts, walk) + 2.5 + 2.0 * bytes / 4.0e6;
+            if (us < best_us) {
+                best_us = us;
+                best = F8Choice{i, (int)(rounds * s.slots), parts, walk};
+            }
+        }
+    }
+    return best;
+}
+
+}  // namespace ozimmu
 
 extern "C" {
 
@@ -255,8 +343,10 @@ ozimmu_status_t ozimmu_f8_weight_grad(int64_t t, int64_t rows, int64_t n, int64_
     a.ldo = lddw;
     if (empty) {
         a.t = 0;   // no rows, so no slabs
-        return hip_status(product(a, st));
+        return hip_status(product(a, false, st));
     }
+    if (o.partial) a.partial = reinterpret_cast<float*>(base + o.off_partial);
+    a.partial_bytes = o.partial;
     a.slabs = (int)f8_groups(rows);
     a.P = base + o.off_p;
     a.sp = base + o.off_sp;
@@ -268,7 +358,7 @@ ozimmu_status_t ozimmu_f8_weight_grad(int64_t t, int64_t rows, int64_t n, int64_
     a.ldsq = o.ldsq;
     hipError_t e = launch_f8_cut_tokens(rows, rows, n, experts, offsets, nullptr, dY, type, lddy, base + o.off_p, o.ldp, base + o.off_sp, o.ldsp, st);
     if (e == hipSuccess) e = launch_f8_cut_tokens(t, rows, k, experts, offsets, source, X, type, ldx, base + o.off_q, o.ldq, base + o.off_sq, o.ldsq, st);
-    if (e == hipSuccess) e = product(a, st);
+    if (e == hipSuccess) e = product(a, false, st);
     return hip_status(e);
 }
 

@@ -30,7 +30,10 @@ hipError_t launch_f8_cut_tokens(int64_t t, int64_t rows, int64_t n, int64_t expe
 
 // R = P Q^T for codes under scales. P: rows (tokens), Q: rows (outputs), both along the inner dimension in slabs of 128 bytes.
 struct F8Args {
-    const uint8_t* P;
+    const void* V;            // launch_f8_few: the rows as they came (v_type, ldv values apart, k of them; OZIMMU_E4M3: codes, with sp)
+    int v_type;
+    int64_t ldv, k;
+    const uint8_t* P;         // the others: their codes
     const uint8_t* sp;        // a byte for each row and slab
     const uint8_t* Q;
     const void* sq;           // bytes or 32-bit values for 128 rows and a slab (q_rows: bytes for each row)
@@ -50,9 +53,18 @@ struct F8Args {
 };
 // f8_few.hip: few rows to an expert, codes straight from memory
 hipError_t launch_f8_few(const F8Args& a, hipStream_t st);
-// f8_product.hip, f8_product_exact.hip: tiles
-hipError_t launch_f8_tiles(const F8Args& a, hipStream_t st);
-hipError_t launch_f8_tiles_exact(const F8Args& a, hipStream_t st);
+// Which tile a product takes, and how its last round of tiles is shared along the inner dimension (the first `whole` tiles are not).
+enum F8Shape { kF8Tile256, kF8Tile128, kF8Tile64x128, kF8Tile64, kF8Tile32x64, kF8Shapes };
+struct F8Choice {
+    int shape, whole, parts, part_slabs;
+};
+F8Choice choose_f8_tile(const F8Args& a);
+size_t f8_partial_room(int64_t rows, int64_t n, int64_t slabs);
+// f8_large.hip: tiles of 256 x 256, 16-bit results, scales of a byte
+hipError_t launch_f8_large(const F8Args& a, hipStream_t st);
+// f8_product.hip, f8_product_exact.hip: smaller tiles; results of 16 bits, of 32
+hipError_t launch_f8_tiles(const F8Args& a, const F8Choice& c, hipStream_t st);
+hipError_t launch_f8_tiles_exact(const F8Args& a, const F8Choice& c, hipStream_t st);
 
 // route.hip
 struct RouteArgs {

@@ -31,6 +31,42 @@ __device__ __forceinline__ unsigned code4(const float* x, int e) {
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
     return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
 }
+template <int TYPE>
+struct Eight {   // eight consecutive values as they lie
+    v4u raw[TYPE == OZIMMU_F32 ? 2 : 1];
+};
+template <int TYPE>
+__device__ __forceinline__ void load8(const typename Elem<TYPE>::raw* row, int64_t at, int64_t len, Eight<TYPE>& x) {
+    typedef typename Elem<TYPE>::raw raw;
+    if (at + 8 <= len) {
+        x.raw[0] = *reinterpret_cast<const v4u_any*>(row + at);
+        if constexpr (TYPE == OZIMMU_F32) x.raw[1] = *reinterpret_cast<const v4u_any*>(row + at + 4);
+    } else {
+        raw r[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[e] = at + e < len ? row[at + e] : raw(0);
+        x = __builtin_bit_cast(Eight<TYPE>, r);
+    }
+}
+template <int TYPE>
+__device__ __forceinline__ void floats(const Eight<TYPE>& x, float (&f)[8]) {
+    if constexpr (TYPE == OZIMMU_F32) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(x.raw[e >> 2][e & 3]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            f[2 * e] = Elem<TYPE>::load((unsigned short)(x.raw[0][e] & 0xffffu));
+            f[2 * e + 1] = Elem<TYPE>::load((unsigned short)(x.raw[0][e] >> 16));
+        }
+    }
+}
+__device__ __forceinline__ unsigned top8(const float (&f)[8]) {
+    unsigned t = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t = max(t, finite_bits(f[e]));
+    return t;
+}
 // The values of a word of codes.
 __device__ __forceinline__ void values4(unsigned w, float (&x)[4]) {
     x[0] = __builtin_amdgcn_cvt_f32_fp8((int)w, 0);
@@ -52,23 +88,24 @@ __device__ __forceinline__ void halves16(const v4u& w, v8h& first, v8h& second) 
 }
 
 // A scale of the weights as significand and exponent byte: value = m 2^(byte - 127). Bytes: m = 1. A NaN or infinity: byte 255.
+__device__ __forceinline__ void scale_parts(unsigned bits, float& m, int& byte) {   // of 32 bits
+    byte = (int)(bits >> 23 & 255u);
+    m = __uint_as_float((bits & 0x7fffffu) | 0x3f800000u);
+    if (byte == 0) {   // subnormal: fraction 2^-126
+        byte = 1;
+        m = __builtin_amdgcn_ldexpf((float)(bits & 0x7fffffu), -23);
+    }
+    m = bits >> 31 ? -m : m;
+    if (byte == 255) m = __builtin_nanf("");
+}
 template <bool WIDE>
 __device__ __forceinline__ void scale_parts(const void* scales, int64_t at, float& m, int& byte) {
     if constexpr (WIDE) {
-        const unsigned b = __float_as_uint(static_cast<const float*>(scales)[at]);
-        byte = (int)(b >> 23 & 255u);
-        if (byte == 0) {   // subnormal: fraction 2^-126
-            byte = 1;
-            m = __builtin_amdgcn_ldexpf((float)(b & 0x7fffffu), -23);
-        } else {
-            m = __uint_as_float((b & 0x7fffffu) | 0x3f800000u);
-        }
-        m = b >> 31 ? -m : m;
+        scale_parts(static_cast<const unsigned*>(scales)[at], m, byte);
     } else {
         byte = static_cast<const uint8_t*>(scales)[at];
-        m = 1.0f;
+        m = byte == 255 ? __builtin_nanf("") : 1.0f;
     }
-    if (byte == 255) m = __builtin_nanf("");
 }
 
 // ---- rows sorted by expert

@@ -11,42 +11,6 @@ namespace {
 
 constexpr int kThreads = 256;
 
-template <int TYPE>
-struct Eight {   // eight consecutive values as they lie
-    v4u raw[TYPE == OZIMMU_F32 ? 2 : 1];
-};
-template <int TYPE>
-__device__ __forceinline__ void load8(const typename Elem<TYPE>::raw* row, int64_t at, int64_t len, Eight<TYPE>& x) {
-    typedef typename Elem<TYPE>::raw raw;
-    if (at + 8 <= len) {
-        x.raw[0] = *reinterpret_cast<const v4u_any*>(row + at);
-        if constexpr (TYPE == OZIMMU_F32) x.raw[1] = *reinterpret_cast<const v4u_any*>(row + at + 4);
-    } else {
-        raw r[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) r[e] = at + e < len ? row[at + e] : raw(0);
-        x = __builtin_bit_cast(Eight<TYPE>, r);
-    }
-}
-template <int TYPE>
-__device__ __forceinline__ void floats(const Eight<TYPE>& x, float (&f)[8]) {
-    if constexpr (TYPE == OZIMMU_F32) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(x.raw[e >> 2][e & 3]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            f[2 * e] = Elem<TYPE>::load((unsigned short)(x.raw[0][e] & 0xffffu));
-            f[2 * e + 1] = Elem<TYPE>::load((unsigned short)(x.raw[0][e] >> 16));
-        }
-    }
-}
-__device__ __forceinline__ unsigned top8(const float (&f)[8]) {
-    unsigned t = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) t = max(t, finite_bits(f[e]));
-    return t;
-}
 __device__ __forceinline__ unsigned max16(unsigned x) {   // over sixteen neighbouring lanes, in all of them
     x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, true));
     x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, true));

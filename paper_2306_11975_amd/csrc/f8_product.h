@@ -27,64 +27,62 @@ struct F8Plan {
     int tiles_m, tiles_n, whole, parts, part_slabs;
 };
 
-// Where a tile lies. false: there is no such tile.
+// A workgroup's items: tiles, and parts of those that are shared. Every XCD has a contiguous run of them (tile_of_block).
 struct F8Tile {
     int expert, first, count, row0, col0;   // rows first .. first + count are the expert's; row0 from there on
     int slab0, slabs, before;               // `before`: slab from which the expert's runs begin (along_rows)
+    int shared;                             // number among the shared parts, or -1
 };
+template <int BM>
+__device__ __forceinline__ int f8_items(const F8Args& a, const F8Plan& p) {
+    const int tiles = p.tiles_m * p.tiles_n;
+    if (a.along_rows && a.experts) return a.experts * tiles;
+    if (a.experts) return count_units(a.offsets, a.experts, a.rows, BM) * p.tiles_n;
+    return p.whole + (tiles - p.whole) * p.parts;
+}
 template <int BM, int BN>
-__device__ __forceinline__ bool f8_tile(const F8Args& a, const F8Plan& p, int block, F8Tile& t) {
+__device__ __forceinline__ F8Tile f8_tile(const F8Args& a, const F8Plan& p, int items, int item) {
+    F8Tile t;
     t.expert = t.first = t.before = t.slab0 = 0;
     t.count = a.rows;
     t.slabs = a.slabs;
+    t.shared = -1;
     int tm, tn;
-    if (a.along_rows) {
+    if (a.along_rows && a.experts) {
         const int one = p.tiles_m * p.tiles_n;
-        t.expert = block / one;
-        tile_of_logical(block - t.expert * one, p.tiles_m, p.tiles_n, tm, tn);
-        if (a.experts) {
-            int rows_first, rows_count;
-            expert_rows(a.offsets, t.expert, a.t, rows_first, rows_count);
-            t.slabs = (rows_count + 127) >> 7;
-            over_experts(a.offsets, a.experts, a.t, 128, 4, [&](int e, int, int, int, int before) {
-                const unsigned long long here = __builtin_amdgcn_ballot_w64(e == t.expert);
-                if (here) t.before = __builtin_amdgcn_readlane(before, __builtin_ctzll(here));
-            });
-        }
+        t.expert = item / one;
+        tile_of_logical(item - t.expert * one, p.tiles_m, p.tiles_n, tm, tn);
+        int rows_first, rows_count;
+        expert_rows(a.offsets, t.expert, a.t, rows_first, rows_count);
+        t.slabs = (rows_count + 127) >> 7;
+        over_experts(a.offsets, a.experts, a.t, 128, 4, [&](int e, int, int, int, int before) {
+            const unsigned long long here = __builtin_amdgcn_ballot_w64(e == t.expert);
+            if (here) t.before = __builtin_amdgcn_readlane(before, __builtin_ctzll(here));
+        });
     } else if (a.experts) {
-        const int units = count_units(a.offsets, a.experts, a.rows, BM), total = units * p.tiles_n;
-        int first, count;
-        xcd_tile_range(block & 7, total, first, count);
-        if ((block >> 3) >= count) return false;
-        tile_of_logical(first + (block >> 3), units, p.tiles_n, tm, tn);
-        Segment s;
-        if (!find_unit(a.offsets, a.experts, a.rows, BM, 1, tm, s)) return false;
+        tile_of_logical(item, items / p.tiles_n, p.tiles_n, tm, tn);
+        Segment s{};
+        find_unit(a.offsets, a.experts, a.rows, BM, 1, tm, s);
         t.expert = s.expert;
         t.first = s.first;
         t.count = s.count;
         tm = s.unit;
     } else {
-        int tile;
-        if (block >= p.whole) {
-            const int b = block - p.whole, part = b % p.parts;
-            tile = p.whole + b / p.parts;
-            t.slab0 = part * p.part_slabs;
+        int tile = item;
+        if (item >= p.whole) {
+            t.shared = item - p.whole;
+            tile = p.whole + t.shared / p.parts;
+            t.slab0 = t.shared % p.parts * p.part_slabs;
             t.slabs = min(p.part_slabs, a.slabs - t.slab0);
-        } else {
-            int first, count;
-            xcd_tile_range(block & 7, p.whole, first, count);
-            tile = first + (block >> 3);
         }
         tile_of_logical(tile, p.tiles_m, p.tiles_n, tm, tn);
     }
     t.row0 = tm * BM;
     t.col0 = tn * BN;
-    return true;
+    return t;
 }
 
-enum F8Walk { kF8ReadOnTime, kF8FirstReadsAhead };
-
-template <int BM, int BN, int WM, int WN, int WALK, bool EXACT, bool WIDE, bool Q_ROWS>
+template <int BM, int BN, int WM, int WN, bool EXACT, bool WIDE, bool Q_ROWS>
 __launch_bounds__(WM * WN * 64)
 __global__ void f8_product_kernel(F8Args a, F8Plan plan) {
     static_assert(!(WIDE && Q_ROWS) && BN / WN <= 128);
@@ -94,8 +92,11 @@ __global__ void f8_product_kernel(F8Args a, F8Plan plan) {
     constexpr int SQ = Q_ROWS ? NI : 1;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    F8Tile t;
-    if (!f8_tile<BM, BN>(a, plan, blockIdx.x, t)) return;
+    const int items = f8_items<BM>(a, plan);
+    int item, mine;
+    xcd_tile_range(blockIdx.x & 7, items, item, mine);
+    if ((int)(blockIdx.x >> 3) >= mine) return;
+    const F8Tile t = f8_tile<BM, BN>(a, plan, items, item + (blockIdx.x >> 3));
     const int slabs = t.slabs;
 
     // operands: P's rows from `first` on (or by source), Q's from the expert's first
@@ -148,15 +149,30 @@ __global__ void f8_product_kernel(F8Args a, F8Plan plan) {
         else
             SQB = static_cast<const uint8_t*>(a.sq) + at;
     }
-    unsigned sp[MI], sq[SQ];
+    // The words of the next four slabs are asked for a slab ahead, with the direct loads, whose wait they share.
+    unsigned sp[MI], sq[SQ], sp_next[MI], sq_next[WIDE ? 4 : SQ];
     float sig = 1.0f;
-    auto scales = [&](int slab) {   // those of `slab` and, for words, the three behind it
+    auto request_scales = [&](int slab) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) sp_next[i] = *reinterpret_cast<const unsigned*>(SP + slab + voff_sp[i]);
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) sq_next[s] = __float_as_uint(SQF[min(slab + s, slabs - 1)]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < SQ; ++j) sq_next[j] = *reinterpret_cast<const unsigned*>(SQB + slab + voff_sq[j]);
+        }
+    };
+    auto next_scales = [&]() {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) sp[i] = sp_next[i];
+        if constexpr (!WIDE)
+#pragma unroll
+            for (int j = 0; j < SQ; ++j) sq[j] = sq_next[j];
+    };
+    auto scales = [&](int slab) {   // those of `slab` in the low bytes
         if ((slab & 3) == 0) {
-#pragma unroll
-            for (int i = 0; i < MI; ++i) sp[i] = *reinterpret_cast<const unsigned*>(SP + slab + voff_sp[i]);
-            if constexpr (!WIDE)
-#pragma unroll
-                for (int j = 0; j < SQ; ++j) sq[j] = *reinterpret_cast<const unsigned*>(SQB + slab + voff_sq[j]);
+            next_scales();
         } else {
 #pragma unroll
             for (int i = 0; i < MI; ++i) sp[i] >>= 8;
@@ -166,9 +182,11 @@ __global__ void f8_product_kernel(F8Args a, F8Plan plan) {
         }
         if constexpr (WIDE) {
             int byte;
-            scale_parts<true>(SQF, slab, sig, byte);
+            const unsigned w = (slab & 2) ? (slab & 1) ? sq_next[3] : sq_next[2] : (slab & 1) ? sq_next[1] : sq_next[0];
+            scale_parts(w, sig, byte);
             sq[0] = (unsigned)byte;
         }
+        if ((slab & 3) == 3 && slab + 1 < slabs) request_scales(slab + 1);
     };
 
     v4f acc[MI][NI];
@@ -225,71 +243,25 @@ __global__ void f8_product_kernel(F8Args a, F8Plan plan) {
     if (slabs > 0) {
 #pragma unroll
         for (int l = 0; l < LP + LQ; ++l) load(l, 0, 0);
-        if constexpr (WALK == kF8FirstReadsAhead) {
-            // As nt_product.h: behind the first barrier nobody reads the other stage any more, and its loads go out between the first rows of
-            // MFMAs; behind the second they have landed, and the next slab's first fragments are read under the last MFMAs.
-            static_assert(MI >= 4);
-            Operand q[2][NI], p[2];
-            auto first_reads = [&](int stage, int to) {
-                const unsigned char* at_p = lds + stage * kStage + wm * (BM / WM) * 128;
-                const unsigned char* at_q = lds + stage * kStage + BM * 128 + wn * (BN / WN) * 128;
+        request_scales(0);
+        for (int slab = 0; slab < slabs; ++slab) {
+            // the slab has landed and this wavefront's reads of the other stage are done; behind the barrier, everyone's
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            const int stage = slab & 1;
+            scales(slab);
+            if (slab + 1 < slabs)
 #pragma unroll
-                for (int j = 0; j < NI; ++j) read(q[to][j], at_q + j * 2048);
-                read(p[0], at_p);
-            };
-            constexpr int kLoadRows = MI / 2;
-            auto step = [&](int slab, auto odd) {
-                constexpr int now = decltype(odd)::value;
-                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                scales(slab);
-                const bool more = slab + 1 < slabs;
-                const unsigned char* at_p = lds + now * kStage + wm * (BM / WM) * 128;
-                static_for<0, MI>([&](auto row) {
-                    constexpr int i = decltype(row)::value;
-                    const Operand x = p[i & 1];
-                    if constexpr (i + 1 < MI) read(p[(i + 1) & 1], at_p + (i + 1) * 2048);
-                    if constexpr (i < kLoadRows) {
-                        if (more)
+                for (int l = 0; l < LP + LQ; ++l) load(l, slab + 1, stage ^ 1);
+            const unsigned char* at_p = lds + stage * kStage + wm * (BM / WM) * 128;
+            const unsigned char* at_q = lds + stage * kStage + BM * 128 + wn * (BN / WN) * 128;
+            Operand q[NI];
 #pragma unroll
-                            for (int l = (LP + LQ) * i / kLoadRows; l < (LP + LQ) * (i + 1) / kLoadRows; ++l) load(l, slab + 1, now ^ 1);
-                    }
-                    if constexpr (i + 1 == MI) {
-                        if (more) {
-                            asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-                            first_reads(now ^ 1, now ^ 1);
-                        }
-                    }
-                    row_of_products(i, x, q[now]);
-                });
-            };
-            asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-            first_reads(0, 0);
-            int slab = 0;
-            for (; slab + 1 < slabs; slab += 2) {
-                step(slab, std::integral_constant<int, 0>{});
-                step(slab + 1, std::integral_constant<int, 1>{});
-            }
-            if (slab < slabs) step(slab, std::integral_constant<int, 0>{});
-        } else {
-            for (int slab = 0; slab < slabs; ++slab) {
-                // the slab has landed and this wavefront's reads of the other stage are done; behind the barrier, everyone's
-                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                const int stage = slab & 1;
-                scales(slab);
-                if (slab + 1 < slabs)
+            for (int j = 0; j < NI; ++j) read(q[j], at_q + j * 2048);
 #pragma unroll
-                    for (int l = 0; l < LP + LQ; ++l) load(l, slab + 1, stage ^ 1);
-                const unsigned char* at_p = lds + stage * kStage + wm * (BM / WM) * 128;
-                const unsigned char* at_q = lds + stage * kStage + BM * 128 + wn * (BN / WN) * 128;
-                Operand q[NI];
-#pragma unroll
-                for (int j = 0; j < NI; ++j) read(q[j], at_q + j * 2048);
-#pragma unroll
-                for (int i = 0; i < MI; ++i) {
-                    Operand p;
-                    read(p, at_p + i * 2048);
-                    row_of_products(i, p, q);
-                }
+            for (int i = 0; i < MI; ++i) {
+                Operand p;
+                read(p, at_p + i * 2048);
+                row_of_products(i, p, q);
             }
         }
     }
@@ -298,11 +270,11 @@ __global__ void f8_product_kernel(F8Args a, F8Plan plan) {
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int j = 0; j < NI; ++j) asm volatile("" : "+v"(acc[i][j]));
+        for (int j = 0; j < NI; ++j) asm volatile("" : "+a"(acc[i][j]));
 
     // ---- results: lane holds R[row][col .. col + 3]
-    if (!a.along_rows && !a.experts && (int)blockIdx.x >= plan.whole) {
-        v4f* to = reinterpret_cast<v4f*>(a.partial) + (int64_t)(blockIdx.x - plan.whole) * (MI * NI * W * 64) + threadIdx.x;
+    if (t.shared >= 0) {
+        v4f* to = reinterpret_cast<v4f*>(a.partial) + (int64_t)t.shared * (MI * NI * W * 64) + threadIdx.x;
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -344,32 +316,35 @@ __global__ void f8_join_kernel(F8Args a, F8Plan plan) {
     if (r < a.rows && c < a.n) store_four(a, r, c, sum, true);
 }
 
-template <int BM, int BN, int WM, int WN, int WALK, bool EXACT, bool WIDE, bool Q_ROWS>
+// Items of a product, at most (over experts the offsets tell how many), by eights.
+template <int BM, int BN>
+int64_t f8_most_items(const F8Args& a, F8Plan& plan) {
+    plan.tiles_m = (a.rows + BM - 1) / BM;
+    plan.tiles_n = (a.n + BN - 1) / BN;
+    const int64_t tiles = (int64_t)plan.tiles_m * plan.tiles_n;
+    if (a.along_rows && a.experts) return pad_to(tiles * a.experts, 8);
+    if (a.experts) return pad_to(tiles + (int64_t)std::min(a.experts, a.rows) * plan.tiles_n, 8);
+    return pad_to(plan.whole + (tiles - plan.whole) * plan.parts, 8);
+}
+
+template <int BM, int BN, int WM, int WN, bool EXACT, bool WIDE, bool Q_ROWS>
 hipError_t launch_f8_shape(const F8Args& a, const F8Plan& plan, int64_t grid, hipStream_t st) {
-    constexpr auto kernel = f8_product_kernel<BM, BN, WM, WN, WALK, EXACT, WIDE, Q_ROWS>;
+    constexpr auto kernel = f8_product_kernel<BM, BN, WM, WN, EXACT, WIDE, Q_ROWS>;
     constexpr int bytes = 2 * (BM + BN) * 128;
-    if (grid <= 0 || grid > INT32_MAX) return hipErrorInvalidConfiguration;
     if (hipError_t e = allow_dynamic_lds<kernel>(bytes); e != hipSuccess) return e;
     kernel<<<dim3((unsigned)grid), dim3(WM * WN * 64), bytes, st>>>(a, plan);
-    const int rest = a.experts || a.along_rows ? 0 : plan.tiles_m * plan.tiles_n - plan.whole;
+    const int rest = a.experts ? 0 : plan.tiles_m * plan.tiles_n - plan.whole;
     if (rest) f8_join_kernel<BM, BN, WM, WN><<<dim3((unsigned)rest, BM / WM / 16 * (BN / WN / 16)), dim3(WM * WN * 64), 0, st>>>(a, plan);
     return hipGetLastError();
 }
 
-template <int BM, int BN, int WM, int WN, int WALK, bool EXACT>
+template <int BM, int BN, int WM, int WN, bool EXACT>
 hipError_t launch_f8_tile(const F8Args& a, F8Plan plan, hipStream_t st) {
-    plan.tiles_m = (a.rows + BM - 1) / BM;
-    plan.tiles_n = (a.n + BN - 1) / BN;
-    int64_t grid;
-    if (a.along_rows)
-        grid = (int64_t)plan.tiles_m * plan.tiles_n * std::max(a.experts, 1);
-    else if (a.experts)
-        grid = pad_to(((int64_t)plan.tiles_m + std::min(a.experts, a.rows)) * plan.tiles_n, 8);
-    else
-        grid = plan.whole + ((int64_t)plan.tiles_m * plan.tiles_n - plan.whole) * plan.parts;
-    if (a.along_rows) return launch_f8_shape<BM, BN, WM, WN, WALK, EXACT, false, true>(a, plan, grid, st);
-    if (a.scale_type == OZIMMU_F32) return launch_f8_shape<BM, BN, WM, WN, WALK, EXACT, true, false>(a, plan, grid, st);
-    return launch_f8_shape<BM, BN, WM, WN, WALK, EXACT, false, false>(a, plan, grid, st);
+    const int64_t grid = f8_most_items<BM, BN>(a, plan);
+    if (grid <= 0 || grid > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (a.along_rows) return launch_f8_shape<BM, BN, WM, WN, EXACT, false, true>(a, plan, grid, st);
+    if (a.scale_type == OZIMMU_F32) return launch_f8_shape<BM, BN, WM, WN, EXACT, true, false>(a, plan, grid, st);
+    return launch_f8_shape<BM, BN, WM, WN, EXACT, false, false>(a, plan, grid, st);
 }
 
 }  // namespace

@@ -3,12 +3,14 @@
 
 namespace ozimmu {
 
-hipError_t launch_f8_tiles(const F8Args& a, hipStream_t st) {
-    F8Plan plan{};
-    plan.parts = 1;
-    plan.part_slabs = a.slabs;
-    plan.whole = (int)(((int64_t)(a.rows + 127) / 128) * ((a.n + 127) / 128));
-    return launch_f8_tile<128, 128, 2, 2, kF8ReadOnTime, false>(a, plan, st);
+hipError_t launch_f8_tiles(const F8Args& a, const F8Choice& c, hipStream_t st) {
+    const F8Plan plan{0, 0, c.whole, c.parts, c.part_slabs};
+    switch (c.shape) {
+        case kF8Tile128: return launch_f8_tile<128, 128, 2, 2, false>(a, plan, st);
+        case kF8Tile64x128: return launch_f8_tile<64, 128, 2, 2, false>(a, plan, st);
+        case kF8Tile64: return launch_f8_tile<64, 64, 2, 2, false>(a, plan, st);
+        default: return launch_f8_tile<32, 64, 2, 2, false>(a, plan, st);
+    }
 }
 
 }  // namespace ozimmu

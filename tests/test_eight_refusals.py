@@ -76,6 +76,7 @@ def test_workspace_sizes():
             assert sizes == sorted(sizes)       # a workspace serves fewer tokens than it was made for
             sizes = [size(op, 500, n, k, torch.float16, rows=r, experts=37) for r in [*range(0, 1300, 3), 4096, 10 ** 5]]
             assert sizes == sorted(sizes)
+    assert size("gemm", 16, 2048, 2048, torch.bfloat16) == size("gemm", 1, 8192, 4096, torch.float32) == 0      # cut on the way
     assert size("gemm", 300, 1000, 4000, torch.uint8) <= size("gemm", 300, 1000, 4000, torch.float32)
     assert size("gemm", 300, 1000, 4000, torch.float32) >= 300 * 4096
     assert size("grad", 300, 1000, 4000, torch.float8_e4m3fn) >= 4000 * 1024
@@ -99,6 +100,7 @@ def test_workspace_sizes():
 
 DIM, TYPE, LD, NULL, MIS, WS = oz.ERR_BAD_DIM, oz.ERR_BAD_TYPE, oz.ERR_BAD_LD, oz.ERR_NULL, oz.ERR_MISALIGNED, oz.ERR_WORKSPACE
 OVER = dict(experts=3, offsets=FAKE)
+LARGE = dict(n=8192, k=8192, ldq=8192, lds=64)      # weights that take a workspace with these rows
 
 
 @pytest.mark.parametrize("call,bad,code", [
@@ -111,7 +113,7 @@ OVER = dict(experts=3, offsets=FAKE)
     (gemm, dict(source=FAKE), DIM), (gemm, dict(experts=3), NULL), (gemm, dict(t=50, **OVER), DIM), (gemm, dict(experts=3, offsets=ODD), MIS), (gemm, dict(source=ODD, **OVER), MIS),
     (gemm, dict(type_=4), TYPE), (gemm, dict(stype=2), TYPE), (gemm, dict(out=3), TYPE), (gemm, dict(ldx=63), LD), (gemm, dict(ldy=7), LD), (gemm, dict(ldq=64), LD), (gemm, dict(lds=2), LD),
     (gemm, dict(X=None), NULL), (gemm, dict(Y=None), NULL), (gemm, dict(codes=None), NULL), (gemm, dict(scales=None), NULL), (gemm, dict(X=ODD), MIS), (gemm, dict(Y=ODD), MIS),
-    (gemm, dict(ws=None), WS), (gemm, dict(size=100), WS), (gemm, dict(ws=ctypes.c_void_p(4096 + 16)), WS), (gemm, dict(type_=3, ldx=128, xs=None, ldxs=4), NULL),
+    (gemm, dict(ws=None, ldx=8192, ldy=8192, **LARGE), WS), (gemm, dict(size=100, ldx=8192, ldy=8192, **LARGE), WS), (gemm, dict(ws=ctypes.c_void_p(4096 + 16), ldx=8192, ldy=8192, **LARGE), WS), (gemm, dict(type_=3, ldx=128, xs=None, ldxs=4), NULL),
     (gemm, dict(type_=3, ldx=64, xs=FAKE, ldxs=4), LD), (gemm, dict(type_=3, ldx=128, xs=FAKE, ldxs=2), LD), (gemm, dict(type_=3, ldx=128, xs=ODD, ldxs=4), MIS),
     (gemm, dict(t=MAX, k=1024, ldx=1024, ldq=1024, source=FAKE, **OVER), LD), (gemm, dict(type_=3, t=MAX, ldx=1024, xs=FAKE, ldxs=4, source=FAKE, **OVER), LD),
     (grad, dict(rows=-1), DIM), (grad, dict(type_=5), TYPE), (grad, dict(stype=1), TYPE), (grad, dict(lddy=7), LD), (grad, dict(lddx=63), LD), (grad, dict(dY=None), NULL), (grad, dict(ws=None), WS),
