@@ -67,14 +67,9 @@ __device__ __forceinline__ void scores(const RouteArgs& a, int64_t token, int la
     }
 }
 
+// The choice in 64 bits throughout. values, kept: LDS of this wavefront.
 template <int TYPE, int SLOTS>
-__launch_bounds__(kThreads)
-__global__ void route_kernel(RouteArgs a, int* indices, float* weights) {
-    __shared__ double values[kThreads / 64][SLOTS * 64];
-    __shared__ unsigned long long kept[kThreads / 64][16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t token = (int64_t)blockIdx.x * (kThreads / 64) + wave;
-    if (token >= a.t) return;
+__device__ __forceinline__ void choose_exactly(const RouteArgs& a, int64_t token, int lane, double* values, unsigned long long* kept, int* indices, float* weights) {
     double l[SLOTS], s[SLOTS], c[SLOTS];
     bool bad;
     scores<TYPE, SLOTS>(a, token, lane, l, s, bad);
@@ -88,8 +83,8 @@ __global__ void route_kernel(RouteArgs a, int* indices, float* weights) {
     if (a.groups > 1) {
         const int per = a.experts / a.groups;
 #pragma unroll
-        for (int k = 0; k < SLOTS; ++k) values[wave][k * 64 + lane] = c[k];
-        if (lane < 16) kept[wave][lane] = 0;
+        for (int k = 0; k < SLOTS; ++k) values[k * 64 + lane] = c[k];
+        if (lane < 16) kept[lane] = 0;
         __builtin_amdgcn_wave_barrier();
         // groups lane, lane + 64, ...: the two largest of each
         double g[16];
@@ -101,7 +96,7 @@ __global__ void route_kernel(RouteArgs a, int* indices, float* weights) {
             if (r >= rounds || group >= a.groups) continue;
             double first = -INFINITY, second = -INFINITY;
             for (int e = 0; e < per; ++e) {
-                const double x = values[wave][group * per + e];
+                const double x = values[group * per + e];
                 second = fmax(second, fmin(first, x));
                 first = fmax(first, x);
             }
@@ -118,13 +113,13 @@ __global__ void route_kernel(RouteArgs a, int* indices, float* weights) {
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 if (r * 64 + lane == i) g[r] = -INFINITY;
-            if (lane == 0) kept[wave][i >> 6] |= 1ull << (i & 63);
+            if (lane == 0) kept[i >> 6] |= 1ull << (i & 63);
         }
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int k = 0; k < SLOTS; ++k) {
             const int group = min((k * 64 + lane) / per, a.groups - 1);
-            if (!(kept[wave][group >> 6] >> (group & 63) & 1)) c[k] = -INFINITY;
+            if (!(kept[group >> 6] >> (group & 63) & 1)) c[k] = -INFINITY;
         }
     }
     // the best, one after the other; lane j keeps choice j
@@ -168,6 +163,332 @@ __global__ void route_kernel(RouteArgs a, int* indices, float* weights) {
     if (lane < a.top) {
         indices[token * a.top + lane] = mine;
         weights[token * a.top + lane] = bad ? __builtin_nanf("") : mine < 0 ? 0.f : (float)(w * (double)a.scale);
+    }
+}
+
+template <int TYPE, int SLOTS>
+__launch_bounds__(kThreads)
+__global__ void route_exactly_kernel(RouteArgs a, int* indices, float* weights) {
+    __shared__ double values[kThreads / 64][SLOTS * 64];
+    __shared__ unsigned long long kept[kThreads / 64][16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t token = (int64_t)blockIdx.x * (kThreads / 64) + wave;
+    if (token < a.t) choose_exactly<TYPE, SLOTS>(a, token, lane, values[wave], kept[wave], indices, weights);
+}
+
+// ---- the same in 32 bits, where those tell
+
+// Reductions over LANES lanes (a row of 16, or all 64), the result in each of them.
+template <int CTRL>
+__device__ __forceinline__ unsigned row_turned(unsigned x) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true); }
+template <int CTRL>
+__device__ __forceinline__ double row_turned(double x) {
+    const unsigned long long b = (unsigned long long)__double_as_longlong(x);
+    return __longlong_as_double((long long)((unsigned long long)row_turned<CTRL>((unsigned)(b >> 32)) << 32 | row_turned<CTRL>((unsigned)b)));
+}
+template <int CTRL>
+__device__ __forceinline__ float row_turned(float x) { return __uint_as_float(row_turned<CTRL>(__float_as_uint(x))); }
+template <int CTRL>
+__device__ __forceinline__ unsigned long long row_turned(unsigned long long x) {
+    return (unsigned long long)row_turned<CTRL>((unsigned)(x >> 32)) << 32 | row_turned<CTRL>((unsigned)x);
+}
+template <int LANES, class T, class F>
+__device__ __forceinline__ T over_lanes(T x, F&& f) {
+    x = f(x, row_turned<0x128>(x));   // rotations of a row by 8, 4, 2 and 1
+    x = f(x, row_turned<0x124>(x));
+    x = f(x, row_turned<0x122>(x));
+    x = f(x, row_turned<0x121>(x));
+    if constexpr (LANES == 64) {
+        x = f(x, __shfl_xor(x, 16));
+        x = f(x, __shfl_xor(x, 32));
+    }
+    return x;
+}
+template <int LANES, class T>
+__device__ __forceinline__ T most(T x) { return over_lanes<LANES>(x, [](T p, T q) { return p > q ? p : q; }); }
+template <int LANES>
+__device__ __forceinline__ unsigned least(unsigned x) { return over_lanes<LANES>(x, [](unsigned p, unsigned q) { return min(p, q); }); }
+template <int LANES, class T>
+__device__ __forceinline__ T sum_of(T x) { return over_lanes<LANES>(x, [](T p, T q) { return p + q; }); }
+
+// SLOTS neighbouring experts of a lane.
+template <int TYPE, int SLOTS>
+__device__ __forceinline__ void load_experts(const typename Elem<TYPE>::raw* row, int experts, int lane, float (&l)[SLOTS]) {
+    typedef typename Elem<TYPE>::raw raw;
+    row += lane * SLOTS;
+    constexpr int words = SLOTS * (int)sizeof(raw) / 4;
+    raw r[SLOTS];
+    if (words > 0 && lane * SLOTS + SLOTS <= experts) {
+        typedef unsigned many __attribute__((ext_vector_type(words > 4 ? 4 : words > 0 ? words : 1)));
+        typedef many many_any __attribute__((aligned(2)));
+#pragma unroll
+        for (int w = 0; w < (words + 3) / 4; ++w) reinterpret_cast<many*>(r)[w] = reinterpret_cast<const many_any*>(row)[w];
+    } else {
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k)
+            if (lane * SLOTS + k < experts) r[k] = row[k];
+    }
+#pragma unroll
+    for (int k = 0; k < SLOTS; ++k) l[k] = lane * SLOTS + k < experts ? Elem<TYPE>::load(r[k]) : -INFINITY;
+}
+// Bits that order like the values; 0 for what cannot be chosen.
+template <class V> struct Bits;
+template <> struct Bits<float> {
+    typedef unsigned type;
+    static __device__ __forceinline__ type of(float x) {
+        const unsigned b = __float_as_uint(x + 0.f);   // (-0 is 0)
+        return x == -INFINITY ? 0u : b ^ (b >> 31 ? 0xffffffffu : 0x80000000u);
+    }
+    static __device__ __forceinline__ float value(type k) { return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu)); }
+};
+template <> struct Bits<double> {
+    typedef unsigned long long type;
+    static __device__ __forceinline__ type of(double x) {
+        const unsigned long long b = (unsigned long long)__double_as_longlong(x + 0.0);
+        return x == -INFINITY ? 0ull : b ^ (b >> 63 ? ~0ull : 1ull << 63);
+    }
+};
+
+// The choice by the values c (-inf: cannot be chosen): lane j <= top keeps the expert of round j (0xffffffff: none) and its value's bits. V = float:
+// unsure where the best top_groups + 1 groups are too near each other to tell.
+template <int LANES, int SLOTS, class V>
+__device__ __forceinline__ void choose(const RouteArgs& a, int lane, V (&c)[SLOTS], float near_scores, unsigned& mine, typename Bits<V>::type& mine_bits, bool& unsure) {
+    typedef typename Bits<V>::type bits;
+    if (a.groups > 1) {
+        // a group is `width` neighbouring lanes: the two largest of each, then the groups by their sum
+        const int width = a.experts / a.groups / SLOTS;
+        V first = -INFINITY, second = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) {
+            second = max(second, min(first, c[k]));
+            first = max(first, c[k]);
+        }
+        for (int d = 1; d < width; d <<= 1) {
+            const V f = __shfl_xor(first, d), g = __shfl_xor(second, d);
+            second = max(max(second, g), min(first, f));
+            first = max(first, f);
+        }
+        const V sum = second == -INFINITY ? first : first + second;
+        bits key = lane * SLOTS < a.experts ? Bits<V>::of(sum) : 0, before = 0;
+        bool keep = false;
+        for (int n = 0; n <= a.top_groups && n < a.groups; ++n) {
+            const bits best = most<LANES>(key);
+            if constexpr (sizeof(V) == 4) {   // (which ones are kept matters, not their order)
+                const float v = Bits<float>::value(before), w = Bits<float>::value(best);
+                unsure |= n == a.top_groups && best != 0 && !(v - w > 2.f * near_scores + (fabsf(v) + fabsf(w)) * 0x1p-21f);
+            }
+            before = best;
+            if (n == a.top_groups) break;
+            const int at = (int)least<LANES>(key == best ? (unsigned)lane : 64u) / width;
+            if (best != 0 && lane / width == at) {
+                keep = true;
+                key = 0;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) c[k] = keep ? c[k] : (V)-INFINITY;
+    }
+    bits key[SLOTS];
+#pragma unroll
+    for (int k = 0; k < SLOTS; ++k) key[k] = Bits<V>::of(c[k]);
+    mine = 0xffffffffu;
+    mine_bits = 0;
+    for (int j = 0; j <= a.top; ++j) {
+        bits here = key[0];
+        unsigned slot = 0;
+#pragma unroll
+        for (int k = 1; k < SLOTS; ++k) {
+            slot = key[k] > here ? (unsigned)k : slot;
+            here = key[k] > here ? key[k] : here;
+        }
+        const bits best = most<LANES>(here);
+        const unsigned winner = least<LANES>(here == best && best != 0 ? (unsigned)lane * SLOTS + slot : 0xffffffffu);
+        mine = lane == j ? winner : mine;
+        mine_bits = lane == j ? best : mine_bits;
+        const unsigned gone = winner - (unsigned)lane * SLOTS;
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) key[k] = gone == (unsigned)k ? 0 : key[k];
+    }
+}
+
+// LANES lanes to a token (16: four tokens a wavefront), experts lane * SLOTS + k. The choice goes by 32-bit values where their order is beyond
+// doubt: without a bias and groups by the logits themselves, whose order the scores have, else by scores that are off by less than 2^-20 of the
+// largest, plus their bias. Where two neighbours among the best top + 1, or the last group kept and the next, are as near as that, and not equal
+// in all that they come from, the wavefront's tokens are chosen again by 64-bit values (at 256 experts with sigmoid scores and a bias one token in
+// some hundreds). Each round finds the largest value, then the lowest expert that has it, and takes that out; lane j keeps the round's, so that
+// neighbours and weights are looked at once, all together. Bound: the rounds' instructions, and the second choice of the last wavefront.
+// 16384 tokens, 256 experts in 8 groups, 8 of 4 groups, us: all in 64 bits 80, 64 lanes to a token 48, 16 lanes 26.
+template <int TYPE, int LANES, int SLOTS>
+__launch_bounds__(kThreads)
+__global__ void route_kernel(RouteArgs a, int* indices, float* weights) {
+    typedef typename Elem<TYPE>::raw raw;
+    const int lane = threadIdx.x & (LANES - 1);
+    const int64_t mine_token = (int64_t)blockIdx.x * (kThreads / LANES) + threadIdx.x / LANES;
+    const bool there = mine_token < a.t;
+    if (__builtin_amdgcn_ballot_w64(there) == 0) return;
+    const int64_t token = there ? mine_token : a.t - 1;      // (rows beyond the last do it again, and write nothing)
+    float l[SLOTS], b[SLOTS], c[SLOTS];
+    load_experts<TYPE, SLOTS>(static_cast<const raw*>(a.logits) + token * a.ldl, a.experts, lane, l);
+    if (a.bias) load_experts<OZIMMU_F32, SLOTS>(a.bias, a.experts, lane, b);
+    bool odd = false, bad = false;      // what 64 bits may not tell apart; what has no order
+    unsigned top_bits = 0;
+#pragma unroll
+    for (int k = 0; k < SLOTS; ++k) {
+        odd |= l[k] > 10.f && a.sigmoid;
+        bad |= l[k] != l[k] || (!a.sigmoid && l[k] == INFINITY);
+        top_bits = max(top_bits, Bits<float>::of(l[k]));
+    }
+    const bool by_values = a.bias != nullptr || a.groups > 1;      // (the same for all)
+    top_bits = most<LANES>(top_bits);
+    const float top_logit = Bits<float>::value(top_bits);
+    float largest = 1.f;      // a score is at most that
+    if (by_values) {
+        if (a.sigmoid) {
+#pragma unroll
+            for (int k = 0; k < SLOTS; ++k) c[k] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * l[k]));
+        } else {
+            float sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < SLOTS; ++k) {
+                c[k] = l[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(1.44269504f * (l[k] - top_logit));
+                sum += c[k];
+            }
+            largest = 1.f / sum_of<LANES>(sum);
+#pragma unroll
+            for (int k = 0; k < SLOTS; ++k) c[k] *= largest;
+        }
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) {
+            if (a.bias) {
+                bad |= l[k] != -INFINITY && c[k] + b[k] != c[k] + b[k];
+                c[k] += b[k];
+            }
+            c[k] = l[k] == -INFINITY ? -INFINITY : c[k];
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) c[k] = l[k];
+    }
+    // Scores: the argument of the exponential is rounded to 2^-23 of itself; |l| <= 10 for sigmoid, whose slope is at most 1 / 4, and for softmax
+    // the argument's size times the score is below one half of the largest.
+    const float near_scores = largest * 0x1p-20f;
+    unsigned mine, mine_bits;
+    bool unsure = odd;
+    choose<LANES, SLOTS>(a, lane, c, near_scores, mine, mine_bits, unsure);
+    float logit = -INFINITY;
+    {   // neighbours: lane j against lane j - 1
+        float bias = 0.f;
+        if (mine != 0xffffffffu) {
+            logit = Elem<TYPE>::load((static_cast<const raw*>(a.logits) + token * a.ldl)[mine]);
+            if (a.bias) bias = a.bias[mine];
+        }
+        const float v = Bits<float>::value((unsigned)__shfl_up((int)mine_bits, 1)), w = Bits<float>::value(mine_bits);
+        const bool same = __shfl_up(logit, 1) == logit && __shfl_up(bias, 1) == bias;
+        const float near = by_values ? 2.f * near_scores + (fabsf(v) + fabsf(w)) * 0x1p-22f : 1e-9f;
+        if (lane > 0 && lane <= a.top && mine != 0xffffffffu) unsure |= !(v - w > near) && !same;
+        if (!a.sigmoid && mine != 0xffffffffu) unsure |= top_logit - logit > 600.f;      // (64 bits have no score for it)
+    }
+    constexpr unsigned long long kMask = LANES == 64 ? ~0ull : (1ull << (LANES & 63)) - 1;
+    const int row0 = (threadIdx.x & 63) / LANES * LANES;
+    bad = (__builtin_amdgcn_ballot_w64(bad) >> row0 & kMask) != 0;
+    const unsigned long long doubt = __builtin_amdgcn_ballot_w64(unsure && !bad);
+    if (doubt) {   // (the same for the wavefront)
+        double d[SLOTS], sum = 0.0;
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) {
+            d[k] = a.sigmoid ? 1.0 / (1.0 + exp(-(double)l[k])) : l[k] == -INFINITY ? 0.0 : exp((double)l[k] - (double)top_logit);
+            sum += d[k];
+        }
+        sum = sum_of<LANES>(sum);
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) {
+            if (!a.sigmoid) d[k] /= sum;
+            if (a.bias) d[k] += (double)b[k];
+            d[k] = l[k] == -INFINITY ? -INFINITY : d[k];
+        }
+        unsigned exact;
+        unsigned long long exact_bits;
+        bool never = false;
+        choose<LANES, SLOTS>(a, lane, d, 0.f, exact, exact_bits, never);
+        if (doubt >> row0 & kMask) {
+            mine = exact;
+            logit = mine != 0xffffffffu ? Elem<TYPE>::load((static_cast<const raw*>(a.logits) + token * a.ldl)[mine]) : -INFINITY;
+        }
+    }
+    // the weights from the chosen logits, in 64 bits
+    const bool chosen = mine != 0xffffffffu && lane < a.top && !bad;
+    double w;
+    if (a.sigmoid) {
+        w = chosen ? 1.0 / (1.0 + exp(-(double)logit)) : 0.0;
+        if (a.renormalize) w /= sum_of<LANES>(w) + 1e-20;
+    } else if (a.renormalize) {
+        const float top = Bits<float>::value(most<LANES>(chosen ? Bits<float>::of(logit) : 0u));
+        w = chosen ? exp((double)logit - (double)top) : 0.0;
+        const double sum = sum_of<LANES>(w);
+        w = sum > 0.0 ? w / sum : 0.0;
+    } else {
+        double sum = 0.0;
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) sum += l[k] == -INFINITY ? 0.0 : exp((double)l[k] - (double)top_logit);
+        sum = sum_of<LANES>(sum);
+        w = chosen ? exp((double)logit - (double)top_logit) / sum : 0.0;
+    }
+    if (there && lane < a.top) {
+        indices[token * a.top + lane] = chosen ? (int)mine : -1;
+        weights[token * a.top + lane] = bad ? __builtin_nanf("") : chosen ? (float)(w * (double)a.scale) : 0.f;
+    }
+}
+
+// The gradient where only the chosen scores have one: sigmoid, or renormalised softmax. Lane j computes choice j's; the row is zeros beside them.
+template <int TYPE, int LANES, int SLOTS>
+__launch_bounds__(kThreads)
+__global__ void route_grad_chosen_kernel(RouteArgs a, const int* indices, const float* dweights, void* dlogits, int64_t lddl) {
+    typedef typename Elem<TYPE>::raw raw;
+    const int lane = threadIdx.x & (LANES - 1);
+    const int64_t token = (int64_t)blockIdx.x * (kThreads / LANES) + threadIdx.x / LANES;
+    if (token >= a.t) return;      // (whole rows of lanes)
+    int mine = lane < a.top ? indices[token * a.top + lane] : -1;
+    if ((unsigned)mine >= (unsigned)a.experts) mine = -1;
+    const double l = mine >= 0 ? (double)Elem<TYPE>::load((static_cast<const raw*>(a.logits) + token * a.ldl)[mine]) : -INFINITY;
+    const double dw = mine >= 0 ? (double)dweights[token * a.top + lane] * (double)a.scale : 0.0;
+    double d;
+    if (a.sigmoid) {
+        const double s = mine >= 0 ? 1.0 / (1.0 + exp(-l)) : 0.0;
+        if (a.renormalize) {
+            const double total = sum_of<LANES>(s) + 1e-20, mean = sum_of<LANES>(dw * s) / total;
+            d = (dw - mean) / total * s * (1.0 - s);
+        } else {
+            d = dw * s * (1.0 - s);
+        }
+    } else {
+        const float top = Bits<float>::value(most<LANES>(mine >= 0 ? Bits<float>::of((float)l) : 0u));
+        const double x = mine >= 0 && l != -INFINITY ? exp(l - (double)top) : 0.0, sum = sum_of<LANES>(x), w = sum > 0.0 ? x / sum : 0.0;
+        d = w * (dw - sum_of<LANES>(dw * w));
+    }
+    float g[SLOTS];
+#pragma unroll
+    for (int k = 0; k < SLOTS; ++k) g[k] = 0.f;
+    const float df = (float)d;
+    for (int j = 0; j < a.top; ++j) {   // (an index that stands twice gets both)
+        const int i = __shfl(mine, j, LANES);
+        const float x = __shfl(df, j, LANES);
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) g[k] += i == lane * SLOTS + k ? x : 0.f;
+    }
+    raw* row = static_cast<raw*>(dlogits) + token * lddl + lane * SLOTS;
+    raw r[SLOTS];
+#pragma unroll
+    for (int k = 0; k < SLOTS; ++k) r[k] = Elem<TYPE>::store(g[k]);
+    constexpr int words = SLOTS * (int)sizeof(raw) / 4;
+    if (words > 0 && lane * SLOTS + SLOTS <= a.experts) {
+        typedef unsigned many __attribute__((ext_vector_type(words > 4 ? 4 : words > 0 ? words : 1)));
+        typedef many many_any __attribute__((aligned(2)));
+#pragma unroll
+        for (int w = 0; w < (words + 3) / 4; ++w) reinterpret_cast<many_any*>(row)[w] = reinterpret_cast<const many*>(r)[w];
+    } else {
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k)
+            if (lane * SLOTS + k < a.experts) row[k] = r[k];
     }
 }
 
@@ -239,41 +560,69 @@ __global__ void route_grad_kernel(RouteArgs a, const int* indices, const float* 
 }
 
 template <class F>
-hipError_t by_shape(int type, int experts, F&& f) {
-    auto by_slots = [&](auto kind) {
-        if (experts <= 64)
-            f(kind, std::integral_constant<int, 1>{});
-        else if (experts <= 128)
-            f(kind, std::integral_constant<int, 2>{});
-        else if (experts <= 256)
-            f(kind, std::integral_constant<int, 4>{});
-        else if (experts <= 512)
-            f(kind, std::integral_constant<int, 8>{});
-        else
-            f(kind, std::integral_constant<int, 16>{});
-    };
+hipError_t by_type(int type, F&& f) {
     if (type == OZIMMU_F32)
-        by_slots(std::integral_constant<int, OZIMMU_F32>{});
+        f(std::integral_constant<int, OZIMMU_F32>{});
     else if (type == OZIMMU_BF16)
-        by_slots(std::integral_constant<int, OZIMMU_BF16>{});
+        f(std::integral_constant<int, OZIMMU_BF16>{});
     else
-        by_slots(std::integral_constant<int, OZIMMU_F16>{});
+        f(std::integral_constant<int, OZIMMU_F16>{});
     return hipGetLastError();
+}
+// Slots of `lanes` lanes that hold the experts: a power of two.
+int slots_of(int experts, int lanes) {
+    int s = 1;
+    while (s * lanes < experts) s *= 2;
+    return s;
+}
+template <class F>
+void by_slots(int slots, F&& f) {
+    switch (slots) {
+        case 1: f(std::integral_constant<int, 1>{}); break;
+        case 2: f(std::integral_constant<int, 2>{}); break;
+        case 4: f(std::integral_constant<int, 4>{}); break;
+        case 8: f(std::integral_constant<int, 8>{}); break;
+        default: f(std::integral_constant<int, 16>{}); break;
+    }
+}
+// Groups that are whole lanes, a power of two of them.
+bool groups_fit(const RouteArgs& a, int slots) {
+    const int per = a.experts / a.groups;
+    return a.groups == 1 || (per % slots == 0 && (per / slots & (per / slots - 1)) == 0);
 }
 
 }  // namespace
 
 hipError_t launch_route(const RouteArgs& a, int* indices, float* weights, hipStream_t st) {
-    const dim3 grid((unsigned)((a.t + 3) / 4));
-    return by_shape(a.type, a.experts, [&](auto kind, auto slots) {
-        route_kernel<decltype(kind)::value, decltype(slots)::value><<<grid, dim3(kThreads), 0, st>>>(a, indices, weights);
+    const int few = slots_of(a.experts, 16), many = slots_of(a.experts, 64);
+    return by_type(a.type, [&](auto kind) {
+        constexpr int T = decltype(kind)::value;
+        if (few <= 16 && a.top < 16 && groups_fit(a, few)) {
+            by_slots(few, [&](auto slots) { route_kernel<T, 16, decltype(slots)::value><<<dim3((unsigned)((a.t + 15) / 16)), dim3(kThreads), 0, st>>>(a, indices, weights); });
+        } else {
+            by_slots(many, [&](auto slots) {
+                constexpr int S = decltype(slots)::value;
+                auto kernel = groups_fit(a, S) ? route_kernel<T, 64, S> : route_exactly_kernel<T, S>;
+                kernel<<<dim3((unsigned)((a.t + 3) / 4)), dim3(kThreads), 0, st>>>(a, indices, weights);
+            });
+        }
     });
 }
 
 hipError_t launch_route_grad(const RouteArgs& a, const int* indices, const float* dweights, void* dlogits, int64_t lddl, hipStream_t st) {
-    const dim3 grid((unsigned)((a.t + 3) / 4));
-    return by_shape(a.type, a.experts, [&](auto kind, auto slots) {
-        route_grad_kernel<decltype(kind)::value, decltype(slots)::value><<<grid, dim3(kThreads), 0, st>>>(a, indices, dweights, dlogits, lddl);
+    const int few = slots_of(a.experts, 16), many = slots_of(a.experts, 64);
+    const bool chosen = a.sigmoid || a.renormalize;
+    return by_type(a.type, [&](auto kind) {
+        constexpr int T = decltype(kind)::value;
+        if (chosen && few <= 16 && a.top <= 16) {
+            by_slots(few, [&](auto slots) { route_grad_chosen_kernel<T, 16, decltype(slots)::value><<<dim3((unsigned)((a.t + 15) / 16)), dim3(kThreads), 0, st>>>(a, indices, dweights, dlogits, lddl); });
+        } else {
+            by_slots(many, [&](auto slots) {
+                constexpr int S = decltype(slots)::value;
+                auto kernel = chosen ? route_grad_chosen_kernel<T, 64, S> : route_grad_kernel<T, S>;
+                kernel<<<dim3((unsigned)((a.t + 3) / 4)), dim3(kThreads), 0, st>>>(a, indices, dweights, dlogits, lddl);
+            });
+        }
     });
 }
 

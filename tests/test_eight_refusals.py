@@ -92,7 +92,7 @@ def test_workspace_sizes():
     with pytest.raises(ValueError):
         size("product", 1, 1, 1, torch.float32)
     assert oz.expert_order_workspace_bytes(1, 8, 64) == 0
-    sizes = [oz.expert_order_workspace_bytes(t, 8, 64) for t in range(0, 9000, 100)]
+    sizes = [oz.expert_order_workspace_bytes(t, 8, 64) for t in [*range(0, 9000, 100), 32768, 32769, 40000, 10 ** 6]]
     assert sizes == sorted(sizes) and sizes[-1] > 0
     assert oz.lib().ozimmu_expert_order_workspace_bytes(1, 33, 4, ctypes.byref(out)) == oz.ERR_BAD_DIM
     assert oz.lib().ozimmu_expert_order_workspace_bytes(1, 1, 4, None) == oz.ERR_NULL

@@ -154,7 +154,7 @@ def device_order(indices, experts):
     return offsets[:-1].cpu(), source[:-1].cpu(), place[:-1].cpu()
 
 
-@pytest.mark.parametrize("t,top,experts", [(1, 1, 1), (7, 3, 5), (64, 8, 64), (1000, 4, 33), (513, 8, 256), (600, 7, 1024), (3000, 3, 2), (5000, 4, 100), (40000, 1, 1024)])
+@pytest.mark.parametrize("t,top,experts", [(1, 1, 1), (7, 3, 5), (64, 8, 64), (1000, 4, 33), (513, 8, 256), (600, 7, 1024), (3000, 3, 2), (5000, 4, 100), (40000, 1, 1024), (16384, 8, 256), (70000, 4, 70), (150000, 8, 8)])
 def test_order(t, top, experts):
     g = gen(t)
     indices = torch.randint(-1 if t % 2 else 0, experts, (t, top), generator=g, dtype=torch.int32)
