@@ -456,7 +456,7 @@ ozimmu_status_t ozimmu_orthogonalize(int64_t batch, int64_t m, int64_t n, ozimmu
  *
  * Over experts (experts >= 1; 0: one product, rows = t, offsets and source null): W holds `experts` matrices, one behind the other (n rows of
  * codes and ceil(n / 128) rows of scales each); rows offsets[e] to offsets[e + 1] of Y, dY and dX belong to expert e (offsets: experts + 1
- * values on the device, from 0, not falling; values outside [0, rows] are taken as the nearest within, and ranges that fall as empty). Rows
+ * values on the device, not falling, within [0, rows]; one that falls is taken as the largest before it, one outside as the nearest within). Rows
  * outside all ranges are left as they were. source: `rows` values on the device (or null, with rows = t): row r of Y (gemm) or dY (weight_grad)
  * goes with row source[r] of X; one outside [0, t) stands for a row of zeros. dW: experts x n x k (lddw between all rows), zeros for an expert
  * without rows; its runs of 128 tokens begin with the expert's first row.

@@ -19,17 +19,15 @@ __device__ __forceinline__ unsigned finite_bits(float x) {
     const unsigned a = __float_as_uint(x) & 0x7fffffffu;
     return a < 0x7f800000u ? a : 0u;
 }
-// Four codes as a word. x 2^-e is exact, or far below the least code; the conversion rounds to nearest, ties to even. What is not finite
-// becomes a NaN.
-__device__ __forceinline__ unsigned code4(const float* x, int e) {
-    float y[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        y[i] = __builtin_amdgcn_ldexpf(x[i], -e);
-        y[i] = __builtin_fabsf(x[i]) < __builtin_inff() ? y[i] : __builtin_nanf("");
-    }
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+// Four codes as a word, under the scale of a byte. The conversion takes the scale's exponent: x 2^-e is exact, or far below the least code, and is
+// rounded once, to nearest, ties to even. What is not finite becomes a NaN.
+typedef short v2s __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ unsigned code4(const float* x, int byte) {
+    const float scale = __uint_as_float((unsigned)byte << 23);
+    v2s w = {0, 0};
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[0], x[1], scale, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[2], x[3], scale, true);
+    return __builtin_bit_cast(unsigned, w);
 }
 template <int TYPE>
 struct Eight {   // eight consecutive values as they lie
@@ -61,10 +59,47 @@ __device__ __forceinline__ void floats(const Eight<TYPE>& x, float (&f)[8]) {
         }
     }
 }
-__device__ __forceinline__ unsigned top8(const float (&f)[8]) {
-    unsigned t = 0;
+// Codes of eight values as they lie.
+template <int TYPE>
+__device__ __forceinline__ v2u code8(const Eight<TYPE>& x, int byte) {
+    const float scale = __uint_as_float((unsigned)byte << 23);
+    v2u out;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) t = max(t, finite_bits(f[e]));
+    for (int h = 0; h < 2; ++h) {
+        v2s w = {0, 0};
+        const unsigned first = x.raw[0][2 * h], second = x.raw[0][2 * h + 1];   // (a bit cast of a vector's element takes element 0)
+        if constexpr (TYPE == OZIMMU_F32) {
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, __uint_as_float(x.raw[h][0]), __uint_as_float(x.raw[h][1]), scale, false);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, __uint_as_float(x.raw[h][2]), __uint_as_float(x.raw[h][3]), scale, true);
+        } else if constexpr (TYPE == OZIMMU_BF16) {
+            typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(v2b, first), scale, false);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(v2b, second), scale, true);
+        } else {
+            typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, __builtin_bit_cast(v2h, first), scale, false);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, __builtin_bit_cast(v2h, second), scale, true);
+        }
+        out[h] = __builtin_bit_cast(unsigned, w);
+    }
+    return out;
+}
+// The largest finite magnitude's bits (of 32-bit floats) among eight values as they lie.
+template <int TYPE>
+__device__ __forceinline__ unsigned top8(const Eight<TYPE>& x) {
+    unsigned t = 0;
+    if constexpr (TYPE == OZIMMU_BF16) {   // bits order like magnitudes: the halves of the words each for themselves
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const unsigned low = x.raw[0][e] << 16 & 0x7fffffffu, high = x.raw[0][e] & 0x7fff0000u;
+            t = max(t, max(low < 0x7f800000u ? low : 0u, high < 0x7f800000u ? high : 0u));
+        }
+    } else {
+        float f[8];
+        floats<TYPE>(x, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t = max(t, finite_bits(f[e]));
+    }
     return t;
 }
 // The values of a word of codes.
@@ -119,13 +154,9 @@ __device__ __forceinline__ int wave_scan(int x) {   // inclusive sum over the la
     }
     return x;
 }
-// Rows of expert e, whatever the offsets hold: none runs backwards or leaves [0, rows].
-__device__ __forceinline__ void expert_rows(const int* offsets, int e, int rows, int& first, int& count) {
-    first = min(max(offsets[e], 0), rows);
-    count = max(min(offsets[e + 1], rows) - first, 0);
-}
-// Which unit (of `unit` rows; counted in multiples of `to` for each expert) number `index` is, over all experts in order. Every lane of a
-// wavefront calls it with the same arguments. `total` receives the number of units.
+// The experts' rows, whatever the offsets hold: an offset is taken as at least the largest before it and within [0, rows], so that no two
+// experts share rows. Units are of `unit` rows, counted in multiples of `to` for each expert. Every lane of a wavefront calls these with the same
+// arguments.
 struct Segment {
     int expert, first, count;   // its rows
     int unit;                   // the unit's number within the expert
@@ -134,11 +165,25 @@ struct Segment {
 template <class F>
 __device__ __forceinline__ int over_experts(const int* offsets, int experts, int rows, int unit, int to, F&& f) {
     const int lane = threadIdx.x & 63;
-    int base = 0;
+    int base = 0, least = 0;
     for (int e0 = 0; e0 < experts; e0 += 64) {
         const int e = e0 + lane;
-        int first = 0, count = 0;
-        if (e < experts) expert_rows(offsets, e, rows, first, count);
+        int first = rows, end = rows;
+        if (e < experts) {
+            first = min(max(offsets[e], 0), rows);
+            end = min(max(offsets[e + 1], 0), rows);
+        }
+        if (__builtin_amdgcn_ballot_w64(end < first || first < least)) {   // some fall: the largest so far instead
+            first = max(first, least);
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int y = __shfl_up(first, d);
+                first = lane >= d ? max(first, y) : first;
+            }
+            end = max(first, end);
+        }
+        least = __builtin_amdgcn_readlane(end, 63);
+        const int count = e < experts ? end - first : 0;
         int units = (count + unit - 1) / unit;
         units = (units + to - 1) / to * to;
         const int sum = wave_scan(units);

@@ -22,25 +22,22 @@ __device__ __forceinline__ unsigned max16(unsigned x) {   // over sixteen neighb
 constexpr int kRows = 4;
 template <int TYPE>
 __launch_bounds__(kThreads)
-__global__ void f8_split_rows_kernel(int64_t n, int64_t k, const void* W, int64_t ldw, uint8_t* codes, int64_t ldq, uint8_t* scales, int64_t lds, int chunks, int64_t items) {
+__global__ void f8_split_rows_kernel(int64_t n, int64_t k, const void* W, int64_t ldw, uint8_t* codes, int64_t ldq, uint8_t* scales, int64_t lds) {
     typedef typename Elem<TYPE>::raw raw;
     const int lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (item >= items) return;
-    const int64_t row0 = item / chunks * kRows, at = (item % chunks) * 512 + lane * 8;
+    const int64_t row0 = ((int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kRows, at = (int64_t)blockIdx.y * 512 + lane * 8;
+    if (row0 >= n) return;
     Eight<TYPE> x[kRows];
 #pragma unroll
     for (int r = 0; r < kRows; ++r) load8<TYPE>(static_cast<const raw*>(W) + min(row0 + r, n - 1) * ldw, at, k, x[r]);
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
         if (row0 + r >= n) break;
-        float f[8];
-        floats<TYPE>(x[r], f);
-        const int byte = scale_byte(max16(top8(f)));
-        if (at < ((k + 127) & ~int64_t(127))) *reinterpret_cast<v2u*>(codes + (row0 + r) * ldq + at) = v2u{code4(f, byte - 127), code4(f + 4, byte - 127)};
+        const int byte = scale_byte(max16(top8<TYPE>(x[r])));
+        if (at < ((k + 127) & ~int64_t(127))) *reinterpret_cast<v2u*>(codes + (row0 + r) * ldq + at) = code8<TYPE>(x[r], byte);
         const unsigned four = (unsigned)__builtin_amdgcn_readlane(byte, 0) | (unsigned)__builtin_amdgcn_readlane(byte, 16) << 8 |
                               (unsigned)__builtin_amdgcn_readlane(byte, 32) << 16 | (unsigned)__builtin_amdgcn_readlane(byte, 48) << 24;
-        if (lane == 0) *reinterpret_cast<unsigned*>(scales + (row0 + r) * lds + (item % chunks) * 4) = four;
+        if (lane == 0) *reinterpret_cast<unsigned*>(scales + (row0 + r) * lds + (int64_t)blockIdx.y * 4) = four;
     }
 }
 
@@ -59,11 +56,7 @@ __global__ void f8_split_blocks_kernel(int64_t n, int64_t k, const void* W, int6
     for (int i = 0; i < 8; ++i) load8<TYPE>(static_cast<const raw*>(W) + min(row0 + r0 + 16 * i, n - 1) * ldw, at, k, x[i]);
     unsigned top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {   // (rows beyond the last repeat it)
-        float f[8];
-        floats<TYPE>(x[i], f);
-        top = max(top, top8(f));
-    }
+    for (int i = 0; i < 8; ++i) top = max(top, top8<TYPE>(x[i]));   // (rows beyond the last repeat it)
     top = max16(top);
     top = max(max((unsigned)__builtin_amdgcn_readlane((int)top, 0), (unsigned)__builtin_amdgcn_readlane((int)top, 16)),
               max((unsigned)__builtin_amdgcn_readlane((int)top, 32), (unsigned)__builtin_amdgcn_readlane((int)top, 48)));
@@ -73,9 +66,7 @@ __global__ void f8_split_blocks_kernel(int64_t n, int64_t k, const void* W, int6
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         if (row0 + r0 + 16 * i >= n) break;
-        float f[8];
-        floats<TYPE>(x[i], f);
-        *reinterpret_cast<v2u*>(codes + (row0 + r0 + 16 * i) * ldq + at) = v2u{code4(f, byte - 127), code4(f + 4, byte - 127)};
+        *reinterpret_cast<v2u*>(codes + (row0 + r0 + 16 * i) * ldq + at) = code8<TYPE>(x[i], byte);
     }
     if (threadIdx.x == 0) {
         uint8_t* s = scales + (row0 >> 7) * lds;
@@ -85,42 +76,51 @@ __global__ void f8_split_blocks_kernel(int64_t n, int64_t k, const void* W, int6
     }
 }
 
-// Values: eight positions to a thread.
+// Values: a wavefront takes 512 positions of kRows rows, eight to a lane.
 template <int TYPE, bool WIDE>
 __launch_bounds__(kThreads)
-__global__ void f8_expand_kernel(int64_t k, int shift, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds, void* W, int64_t ldw, int per_row, int64_t items) {
+__global__ void f8_expand_kernel(int64_t n, int64_t k, int shift, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds, void* W, int64_t ldw) {
     typedef typename Elem<TYPE>::raw raw;
-    const int64_t item = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (item >= items) return;
-    const int64_t row = item / per_row, at = (item % per_row) * 8;
-    const v2u c = *reinterpret_cast<const v2u*>(codes + row * ldq + at);
-    float m, f[8];
-    int byte;
-    scale_parts<WIDE>(scales, (row >> shift) * lds + (at >> 7), m, byte);
-    values4(c[0], *reinterpret_cast<float(*)[4]>(f));
-    values4(c[1], *reinterpret_cast<float(*)[4]>(f + 4));
-    raw r[8];
+    const int lane = threadIdx.x & 63;
+    const int64_t row0 = ((int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kRows, at = (int64_t)blockIdx.y * 512 + lane * 8;
+    if (row0 >= n || at >= k) return;
+    v2u c[kRows];
+    float m[kRows];
+    int byte[kRows];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = Elem<TYPE>::store(__builtin_amdgcn_ldexpf(f[e] * m, byte - 127));
-    raw* out = static_cast<raw*>(W) + row * ldw + at;
-    if (at + 8 <= k) {
-        *reinterpret_cast<v4u_any*>(out) = *reinterpret_cast<const v4u*>(r);
-        if constexpr (TYPE == OZIMMU_F32) *reinterpret_cast<v4u_any*>(out + 4) = *reinterpret_cast<const v4u*>(r + 4);
-    } else {
+    for (int i = 0; i < kRows; ++i) {
+        const int64_t row = min(row0 + i, n - 1);
+        c[i] = *reinterpret_cast<const v2u*>(codes + row * ldq + at);
+        scale_parts<WIDE>(scales, (row >> shift) * lds + (at >> 7), m[i], byte[i]);
+    }
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (at + e < k) out[e] = r[e];
+    for (int i = 0; i < kRows; ++i) {
+        if (row0 + i >= n) break;
+        float f[8];
+        values4(c[i][0], *reinterpret_cast<float(*)[4]>(f));
+        values4(c[i][1], *reinterpret_cast<float(*)[4]>(f + 4));
+        raw r[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[e] = Elem<TYPE>::store(__builtin_amdgcn_ldexpf(f[e] * m[i], byte[i] - 127));
+        raw* out = static_cast<raw*>(W) + (row0 + i) * ldw + at;
+        if (at + 8 <= k) {
+            *reinterpret_cast<v4u_any*>(out) = *reinterpret_cast<const v4u*>(r);
+            if constexpr (TYPE == OZIMMU_F32) *reinterpret_cast<v4u_any*>(out + 4) = *reinterpret_cast<const v4u*>(r + 4);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (at + e < k) out[e] = r[e];
+        }
     }
 }
 
 // Transposed weights: a workgroup turns a block of 128 x 128 in LDS, four by four bytes to a thread.
 template <bool WIDE>
 __launch_bounds__(kThreads)
-__global__ void f8_transpose_kernel(int64_t n, int64_t k, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds, uint8_t* codes_t, void* scales_t, int64_t ld_t, int64_t lds_t, int nb,
-                                    int kb) {
+__global__ void f8_transpose_kernel(int64_t n, int64_t k, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds, uint8_t* codes_t, void* scales_t, int64_t ld_t, int64_t lds_t) {
     __shared__ unsigned block[128][33];
-    const int64_t expert = blockIdx.x / ((int64_t)nb * kb);
-    const int in = (int)(blockIdx.x - expert * nb * kb), bn = in / kb, bk = in % kb;
+    const int64_t expert = blockIdx.z;
+    const int bn = blockIdx.y, bk = blockIdx.x, nb = gridDim.y, kb = gridDim.x;
     const uint8_t* from = codes + (expert * n + (int64_t)bn * 128) * ldq + (int64_t)bk * 128;
     const int rows = (int)min<int64_t>(128, n - (int64_t)bn * 128), cols = (int)min<int64_t>(128, k - (int64_t)bk * 128);
 #pragma unroll
@@ -209,7 +209,7 @@ __global__ void f8_cut_tokens_kernel(int t, int rows, int64_t n, int experts, co
         const int c = (threadIdx.x & 7) * 8 + e;
         const int byte = scale_byte(max(max(tops[0][c], tops[1][c]), max(tops[2][c], tops[3][c])));
         const float x[4] = {f[0][e], f[1][e], f[2][e], f[3][e]};
-        turned[c][threadIdx.x >> 3] = code4(x, byte - 127);
+        turned[c][threadIdx.x >> 3] = code4(x, byte);
     }
     if (threadIdx.x < 64 && col0 + threadIdx.x < n)
         scales[(col0 + threadIdx.x) * lds + run] = (uint8_t)scale_byte(max(max(tops[0][threadIdx.x], tops[1][threadIdx.x]), max(tops[2][threadIdx.x], tops[3][threadIdx.x])));
@@ -235,34 +235,32 @@ bool too_many(int64_t workgroups) { return workgroups <= 0 || workgroups > INT32
 }  // namespace
 
 hipError_t launch_f8_split(int64_t n, int64_t k, int block_rows, const void* W, int type, int64_t ldw, uint8_t* codes, int64_t ldq, uint8_t* scales, int64_t lds, hipStream_t st) {
-    const int64_t chunks = (k + 511) / 512, items = (n + kRows - 1) / kRows * chunks, groups = f8_groups(k);
-    const int64_t grid = block_rows == 1 ? (items + 3) / 4 : (n + 127) / 128 * groups;
-    if (too_many(grid)) return hipErrorInvalidConfiguration;
+    const int64_t groups = f8_groups(k), blocks = (n + 127) / 128 * groups;
+    const dim3 rows((unsigned)((n + 4 * kRows - 1) / (4 * kRows)), (unsigned)((k + 511) / 512));
+    if (too_many(blocks)) return hipErrorInvalidConfiguration;
     return by_type(type, [&](auto kind) {
         constexpr int T = decltype(kind)::value;
         if (block_rows == 1)
-            f8_split_rows_kernel<T><<<dim3((unsigned)grid), dim3(kThreads), 0, st>>>(n, k, W, ldw, codes, ldq, scales, lds, (int)chunks, items);
+            f8_split_rows_kernel<T><<<rows, dim3(kThreads), 0, st>>>(n, k, W, ldw, codes, ldq, scales, lds);
         else
-            f8_split_blocks_kernel<T><<<dim3((unsigned)grid), dim3(kThreads), 0, st>>>(n, k, W, ldw, codes, ldq, scales, lds, (int)groups);
+            f8_split_blocks_kernel<T><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(n, k, W, ldw, codes, ldq, scales, lds, (int)groups);
     });
 }
 
 hipError_t launch_f8_expand(int64_t n, int64_t k, int block_rows, const uint8_t* codes, int64_t ldq, int scale_type, const void* scales, int64_t lds, void* W, int type, int64_t ldw, hipStream_t st) {
-    const int64_t per_row = (k + 7) / 8, items = n * per_row, grid = (items + kThreads - 1) / kThreads;
-    if (too_many(grid)) return hipErrorInvalidConfiguration;
+    const dim3 grid((unsigned)((n + 4 * kRows - 1) / (4 * kRows)), (unsigned)((k + 511) / 512));
     return by_type(type, [&](auto kind) {
         constexpr int T = decltype(kind)::value;
         auto kernel = scale_type == OZIMMU_F32 ? f8_expand_kernel<T, true> : f8_expand_kernel<T, false>;
-        kernel<<<dim3((unsigned)grid), dim3(kThreads), 0, st>>>(k, block_rows == 1 ? 0 : 7, codes, ldq, scales, lds, W, ldw, (int)per_row, items);
+        kernel<<<grid, dim3(kThreads), 0, st>>>(n, k, block_rows == 1 ? 0 : 7, codes, ldq, scales, lds, W, ldw);
     });
 }
 
 hipError_t launch_f8_transpose(int64_t experts, int64_t n, int64_t k, const uint8_t* codes, int64_t ldq, int scale_type, const void* scales, int64_t lds, uint8_t* codes_t, void* scales_t,
                                hipStream_t st) {
-    const int64_t nb = f8_groups(n), kb = f8_groups(k), grid = experts * nb * kb;
-    if (too_many(grid)) return hipErrorInvalidConfiguration;
+    const dim3 grid((unsigned)f8_groups(k), (unsigned)f8_groups(n), (unsigned)experts);
     auto kernel = scale_type == OZIMMU_F32 ? f8_transpose_kernel<true> : f8_transpose_kernel<false>;
-    kernel<<<dim3((unsigned)grid), dim3(kThreads), 0, st>>>(n, k, codes, ldq, scales, lds, codes_t, scales_t, f8_row_bytes(n), f8_scale_bytes(n), (int)nb, (int)kb);
+    kernel<<<grid, dim3(kThreads), 0, st>>>(n, k, codes, ldq, scales, lds, codes_t, scales_t, f8_row_bytes(n), f8_scale_bytes(n));
     return hipGetLastError();
 }
 

@@ -52,12 +52,11 @@ __device__ __forceinline__ F8Tile f8_tile(const F8Args& a, const F8Plan& p, int 
         const int one = p.tiles_m * p.tiles_n;
         t.expert = item / one;
         tile_of_logical(item - t.expert * one, p.tiles_m, p.tiles_n, tm, tn);
-        int rows_first, rows_count;
-        expert_rows(a.offsets, t.expert, a.t, rows_first, rows_count);
-        t.slabs = (rows_count + 127) >> 7;
-        over_experts(a.offsets, a.experts, a.t, 128, 4, [&](int e, int, int, int, int before) {
+        over_experts(a.offsets, a.experts, a.t, 128, 4, [&](int e, int, int count, int, int before) {
             const unsigned long long here = __builtin_amdgcn_ballot_w64(e == t.expert);
-            if (here) t.before = __builtin_amdgcn_readlane(before, __builtin_ctzll(here));
+            if (!here) return;
+            t.slabs = (__builtin_amdgcn_readlane(count, __builtin_ctzll(here)) + 127) >> 7;
+            t.before = __builtin_amdgcn_readlane(before, __builtin_ctzll(here));
         });
     } else if (a.experts) {
         tile_of_logical(item, items / p.tiles_n, p.tiles_n, tm, tn);

@@ -746,52 +746,59 @@ def _by_expert(t, offsets):
 
 
 def _f8_product(gradient, V, codes, scales, R, workspace, v_scales, offsets, source, stream):
+    # (Checked in one place, attributes read once: a token's call waits for every microsecond spent here.)
     if _byte_types is None:
         _f8_types()
     t, inner, ldv = _rows(V)
     rows, outer, ldr = _rows(R)
-    codes, experts = _by_expert(codes, offsets)
-    scales, experts_s = _by_expert(scales, offsets)
-    if V.dtype in _byte_types:
-        _expect(v_scales is not None, "codes of tokens need their scales")
-        # the width of codes is padded: the other sizes tell it
-        inner = codes.shape[0] // max(experts, 1) if gradient else min(inner, codes.shape[1])
-        kind = E4M3
-    else:
-        _expect(v_scales is None, "only codes have scales")
-        kind = _type_of(V.dtype)
-    n, k = (inner, outer) if gradient else (outer, inner)
-    if experts != experts_s or codes.shape[0] != n * max(experts, 1):
-        raise ValueError(f"codes: expected {n} rows" + (" for each expert" if experts else ""))
-    each = -(-n // 128)
-    row_bytes_, groups = (k + 127) // 128 * 128, (k + 127) // 128
+    experts = 0
+    if offsets is not None:
+        codes, experts = _by_expert(codes, offsets)
+        scales, experts_s = _by_expert(scales, offsets)
+        if experts != experts_s:
+            raise ValueError("codes and scales must have the same number of experts")
     qrows, cols, ldq = _rows(codes)
-    skind = _scale_types.get(scales.dtype)
     srows, scols, lds = _rows(scales)
-    most = groups if skind == F32 else (groups + 3) // 4 * 4
-    if cols < row_bytes_ or codes.dtype not in _byte_types:
-        raise ValueError(f"codes: expected rows of at least {row_bytes_} codes (uint8 or float8_e4m3fn)")
-    if skind is None or srows != each * max(experts, 1) or scols < most:
-        raise ValueError(f"scales: expected {each} rows" + (" for each expert" if experts else "") + f" of at least {most} (float8_e8m0fnu or uint8: multiples of four) or {groups} (float32)")
+    each = experts or 1
     vs, ldvs = None, 0
-    if kind == E4M3:
-        ldv_, _, ldvs = _f8_matrix("tokens", V, v_scales, t, inner, 1)
-        _expect(v_scales.dtype is not _torch.float32, "scales of tokens are bytes")
-        vs, ldv = v_scales.data_ptr(), ldv_
-    if gradient or source is None:
-        _expect(rows == t, "tokens and result must have the same number of rows")
-    tail = (_type_of(R.dtype), R.data_ptr(), ldr, None if workspace is None else workspace.data_ptr(), _size(workspace))
-    po = None if offsets is None else _ints(offsets, experts + 1, "offsets")
-    ps = None if source is None else _ints(source, rows, "source")
+    kind = _types.get(V.dtype)
+    if kind is None:
+        if V.dtype not in _byte_types:
+            _type_of(V.dtype)       # raises
+        _expect(v_scales is not None and v_scales.dtype is not _torch.float32, "codes of tokens need their scales, which are bytes")
+        kind = E4M3
+        # the width of codes is padded: the other sizes tell it
+        inner = qrows // each if gradient else min(inner, cols)
+        ldv, _, ldvs = _f8_matrix("tokens", V, v_scales, t, inner, 1)
+        vs = v_scales.data_ptr()
+    elif v_scales is not None:
+        raise ValueError("only codes have scales")
+    n, k = (inner, outer) if gradient else (outer, inner)
+    groups = (k + 127) // 128
+    if qrows != n * each or cols < 128 * groups or codes.dtype not in _byte_types:
+        raise ValueError(f"codes: expected {n} rows" + (" for each expert" if experts else "") + f" of at least {128 * groups} codes (uint8 or float8_e4m3fn)")
+    skind = _scale_types.get(scales.dtype)
+    most = groups if skind == F32 else (groups + 3) // 4 * 4
+    if skind is None or srows != (n + 127) // 128 * each or scols < most:
+        raise ValueError(f"scales: expected {(n + 127) // 128} rows" + (" for each expert" if experts else "") + f" of at least {most} (float8_e8m0fnu or uint8: multiples of four) or {groups} (float32)")
+    if rows != t and (gradient or source is None):
+        raise ValueError("tokens and result must have the same number of rows")
+    out = _types.get(R.dtype)
+    if out is None:
+        _type_of(R.dtype)           # raises
     if qrows <= 1:
-        ldq = row_bytes_
+        ldq = 128 * groups
     if srows <= 1:
         lds = most
-    tensors = (V, codes, scales, R, workspace, v_scales, offsets, source)
+    ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), _size(workspace))
+    po = None if offsets is None else _ints(offsets, experts + 1, "offsets")
     if gradient:
-        _call(lib().ozimmu_f8_gemm_grad, stream, tensors, rows, n, k, experts, kind, V.data_ptr(), ldv, vs, ldvs, codes.data_ptr(), ldq, skind, scales.data_ptr(), lds, po, *tail)
+        _call(lib().ozimmu_f8_gemm_grad, stream, (V, codes, scales, R, workspace, v_scales, offsets), rows, n, k, experts, kind, V.data_ptr(), ldv, vs, ldvs, codes.data_ptr(), ldq, skind,
+              scales.data_ptr(), lds, po, out, R.data_ptr(), ldr, ws, size)
     else:
-        _call(lib().ozimmu_f8_gemm, stream, tensors, t, rows, n, k, experts, kind, V.data_ptr(), ldv, vs, ldvs, codes.data_ptr(), ldq, skind, scales.data_ptr(), lds, po, ps, *tail)
+        ps = None if source is None else _ints(source, rows, "source")
+        _call(lib().ozimmu_f8_gemm, stream, (V, codes, scales, R, workspace, v_scales, offsets, source), t, rows, n, k, experts, kind, V.data_ptr(), ldv, vs, ldvs, codes.data_ptr(), ldq, skind,
+              scales.data_ptr(), lds, po, ps, out, R.data_ptr(), ldr, ws, size)
 
 
 def f8_gemm(X, codes, scales, Y, workspace=None, x_scales=None, offsets=None, source=None, stream=None) -> None:

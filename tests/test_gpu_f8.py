@@ -355,23 +355,23 @@ def test_experts_wide_scales(counts):
 
 @pytest.mark.parametrize("few", [True, False])
 def test_offsets_that_leave_their_range(few):
-    """Ranges that fall are empty, values outside are taken as the nearest within; nothing outside the ranges is written."""
+    """An offset is at least the largest before it, and within the rows; nothing outside the ranges is written."""
     n, k, t = 40, 128, 30 if few else 200
+    n = n if few else 6000
     g = gen(2)
     X, W = small_integers((t, k), g), torch.stack([small_integers((n, k), g) for _ in range(4)])
     cut_w = [device_cut(w.to(F32)) for w in W]
     codes, scales = torch.stack([c for c, _ in cut_w]), torch.stack([s for _, s in cut_w])
-    offsets = torch.tensor([-5, 10, 7, 20, t + 1000], dtype=torch.int32, device=DEV)
-    want = torch.full((t, n), 77.0, dtype=torch.float64)
-    want[:10] = X[:10] @ W[0].t()
-    want[7:20] = X[7:20] @ W[2].t()      # (rows 7 to 10 belong to two experts; the later one or the earlier)
-    want[20:] = X[20:] @ W[3].t()
-    got = product("gemm", X.to(BF16), codes, scales, (t, n), BF16, offsets=offsets).cpu()
-    w = round_to(want, BF16)
-    keep = [i for i in range(t) if not 7 <= i < 10]
-    assert torch.equal(got[keep], w[keep])
-    other = round_to(X[7:10] @ W[0].t(), BF16)
-    assert all(torch.equal(got[i], w[i]) or torch.equal(got[i], other[i - 7]) for i in range(7, 10))
+    dY = small_integers((t, n), g)
+    for given, taken in (([-5, 10, 7, 20, t + 1000], [0, 10, 10, 20, t]), ([3, 8, 2, 1, 9], [3, 8, 8, 8, 9]), ([t + 7, 5, 6, 7, 8], [t] * 5), ([-9, -8, -7, 4, -1], [0, 0, 0, 4, 4])):
+        offsets = torch.tensor(given, dtype=torch.int32, device=DEV)
+        want, wantx, wantw = torch.full((t, n), 77.0, dtype=torch.float64), torch.full((t, k), 77.0, dtype=torch.float64), torch.zeros(4, n, k, dtype=torch.float64)
+        for e in range(4):
+            a, b = taken[e], taken[e + 1]
+            want[a:b], wantx[a:b], wantw[e] = X[a:b] @ W[e].t(), dY[a:b] @ W[e], dY[a:b].t() @ X[a:b]
+        assert torch.equal(product("gemm", X.to(BF16), codes, scales, (t, n), BF16, offsets=offsets).cpu(), round_to(want, BF16))
+        assert torch.equal(product("grad", dY.to(BF16), codes, scales, (t, k), BF16, offsets=offsets).cpu(), round_to(wantx, BF16))
+        assert torch.equal(weight_product(dY.to(BF16), X.to(BF16), BF16, 4, offsets=offsets).cpu(), round_to(wantw, BF16))
 
 
 def test_other_stream_and_graph():
