@@ -162,7 +162,7 @@ ozimmu_status_t f8_product(int op, int64_t t, int64_t rows, int64_t n, int64_t k
         a.ldp = o.ldp;
         a.sp = base + o.off_sp;
         a.ldsp = o.ldsp;
-        e = launch_f8_split(t, inner, 1, V, type, ldv, base + o.off_p, o.ldp, base + o.off_sp, o.ldsp, st);
+        if (op == kGemm) e = launch_f8_split(t, inner, 1, V, type, ldv, base + o.off_p, o.ldp, base + o.off_sp, o.ldsp, st);
     }
     if (op == kGemm) {
         a.Q = codes;
@@ -174,7 +174,9 @@ ozimmu_status_t f8_product(int op, int64_t t, int64_t rows, int64_t n, int64_t k
         a.ldq = o.ldq;
         a.sq = base + o.off_sq;
         a.ldsq = o.ldsq;
-        if (e == hipSuccess) e = launch_f8_transpose(std::max<int64_t>(experts, 1), n, k, codes, ldq, scale_type, scales, lds, base + o.off_q, base + o.off_sq, st);
+        const bool cut = type != OZIMMU_E4M3 && !few;
+        e = launch_f8_gradient_operands(std::max<int64_t>(experts, 1), n, k, codes, ldq, scale_type, scales, lds, base + o.off_q, base + o.off_sq, rows, V, type, ldv,
+                                        cut ? base + o.off_p : nullptr, base + o.off_sp, st);
     }
     if (o.partial) a.partial = reinterpret_cast<float*>(base + o.off_partial);
     a.partial_bytes = o.partial;
@@ -356,8 +358,8 @@ ozimmu_status_t ozimmu_f8_weight_grad(int64_t t, int64_t rows, int64_t n, int64_
     a.sq = base + o.off_sq;
     a.ldq = o.ldq;
     a.ldsq = o.ldsq;
-    hipError_t e = launch_f8_cut_tokens(rows, rows, n, experts, offsets, nullptr, dY, type, lddy, base + o.off_p, o.ldp, base + o.off_sp, o.ldsp, st);
-    if (e == hipSuccess) e = launch_f8_cut_tokens(t, rows, k, experts, offsets, source, X, type, ldx, base + o.off_q, o.ldq, base + o.off_sq, o.ldsq, st);
+    const F8Columns dy{dY, lddy, n, (int)rows, nullptr, base + o.off_p, base + o.off_sp}, x{X, ldx, k, (int)t, source, base + o.off_q, base + o.off_sq};
+    hipError_t e = launch_f8_cut_tokens(rows, experts, offsets, type, dy, x, o.ldsp, st);
     if (e == hipSuccess) e = product(a, false, st);
     return hip_status(e);
 }

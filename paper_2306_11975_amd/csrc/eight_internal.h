@@ -19,14 +19,20 @@ inline int64_t most_token_runs(int64_t rows, int64_t experts) { return pad_to(f8
 // Blocks of block_rows (1 or 128) x 128 of W.
 hipError_t launch_f8_split(int64_t n, int64_t k, int block_rows, const void* W, int type, int64_t ldw, uint8_t* codes, int64_t ldq, uint8_t* scales, int64_t lds, hipStream_t st);
 hipError_t launch_f8_expand(int64_t n, int64_t k, int block_rows, const uint8_t* codes, int64_t ldq, int scale_type, const void* scales, int64_t lds, void* W, int type, int64_t ldw, hipStream_t st);
-// Codes and scales of the transposed weights (blocks of 128 x 128), expert by expert: rows of pad_to(n, 128) bytes, and scales (of the type that
-// they have) in rows of f8_scale_bytes(n) values.
-hipError_t launch_f8_transpose(int64_t experts, int64_t n, int64_t k, const uint8_t* codes, int64_t ldq, int scale_type, const void* scales, int64_t lds, uint8_t* codes_t, void* scales_t,
-                               hipStream_t st);
-// V (rows x n) cut along its rows' direction, in runs of 128 tokens that begin with every expert (experts 0: one), transposed: codes n x ld,
-// scales n x lds.
-hipError_t launch_f8_cut_tokens(int64_t t, int64_t rows, int64_t n, int64_t experts, const int* offsets, const int* source, const void* V, int type, int64_t ldv, uint8_t* codes, int64_t ld,
-                                uint8_t* scales, int64_t lds, hipStream_t st);
+// The operands of a gradient dY W: codes and scales of the transposed weights (blocks of 128 x 128), expert by expert, in rows of pad_to(n, 128)
+// bytes, and scales (of the type that they have) in rows of f8_scale_bytes(n) values; and, where v_codes is not null, V (rows x n) cut by 1 x 128.
+hipError_t launch_f8_gradient_operands(int64_t experts, int64_t n, int64_t k, const uint8_t* codes, int64_t ldq, int scale_type, const void* scales, int64_t lds, uint8_t* codes_t,
+                                       void* scales_t, int64_t rows, const void* V, int type, int64_t ldv, uint8_t* v_codes, uint8_t* v_scales, hipStream_t st);
+// The operands of a weights' gradient: rows of V (by source, of t) cut along their direction, in runs of 128 that begin with every expert (experts
+// 0: one), transposed: codes n x 128 runs, scales n x runs.
+struct F8Columns {
+    const void* V;
+    int64_t ldv, n;
+    int t;
+    const int* source;
+    uint8_t *codes, *scales;
+};
+hipError_t launch_f8_cut_tokens(int64_t rows, int64_t experts, const int* offsets, int type, const F8Columns& dy, const F8Columns& x, int64_t runs, hipStream_t st);
 
 // R = P Q^T for codes under scales. P: rows (tokens), Q: rows (outputs), both along the inner dimension in slabs of 128 bytes.
 struct F8Args {

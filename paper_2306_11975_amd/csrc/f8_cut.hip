@@ -21,11 +21,10 @@ __device__ __forceinline__ unsigned max16(unsigned x) {   // over sixteen neighb
 // Runs of a row: a wavefront takes 512 positions of kRows rows, eight to a lane, sixteen lanes to a run.
 constexpr int kRows = 4;
 template <int TYPE>
-__launch_bounds__(kThreads)
-__global__ void f8_split_rows_kernel(int64_t n, int64_t k, const void* W, int64_t ldw, uint8_t* codes, int64_t ldq, uint8_t* scales, int64_t lds) {
+__device__ __forceinline__ void split_rows(int64_t n, int64_t k, const void* W, int64_t ldw, uint8_t* codes, int64_t ldq, uint8_t* scales, int64_t lds, int64_t block, int64_t chunk) {
     typedef typename Elem<TYPE>::raw raw;
     const int lane = threadIdx.x & 63;
-    const int64_t row0 = ((int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kRows, at = (int64_t)blockIdx.y * 512 + lane * 8;
+    const int64_t row0 = (block * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kRows, at = chunk * 512 + lane * 8;
     if (row0 >= n) return;
     Eight<TYPE> x[kRows];
 #pragma unroll
@@ -37,8 +36,13 @@ __global__ void f8_split_rows_kernel(int64_t n, int64_t k, const void* W, int64_
         if (at < ((k + 127) & ~int64_t(127))) *reinterpret_cast<v2u*>(codes + (row0 + r) * ldq + at) = code8<TYPE>(x[r], byte);
         const unsigned four = (unsigned)__builtin_amdgcn_readlane(byte, 0) | (unsigned)__builtin_amdgcn_readlane(byte, 16) << 8 |
                               (unsigned)__builtin_amdgcn_readlane(byte, 32) << 16 | (unsigned)__builtin_amdgcn_readlane(byte, 48) << 24;
-        if (lane == 0) *reinterpret_cast<unsigned*>(scales + (row0 + r) * lds + (int64_t)blockIdx.y * 4) = four;
+        if (lane == 0) *reinterpret_cast<unsigned*>(scales + (row0 + r) * lds + chunk * 4) = four;
     }
+}
+template <int TYPE>
+__launch_bounds__(kThreads)
+__global__ void f8_split_rows_kernel(int64_t n, int64_t k, const void* W, int64_t ldw, uint8_t* codes, int64_t ldq, uint8_t* scales, int64_t lds) {
+    split_rows<TYPE>(n, k, W, ldw, codes, ldq, scales, lds, blockIdx.x, blockIdx.y);
 }
 
 // Blocks: a workgroup each; a thread holds eight positions of every sixteenth row.
@@ -114,25 +118,51 @@ __global__ void f8_expand_kernel(int64_t n, int64_t k, int shift, const uint8_t*
     }
 }
 
-// Transposed weights: a workgroup turns a block of 128 x 128 in LDS, four by four bytes to a thread.
-template <bool WIDE>
+// Transposed weights: a workgroup turns a block of 128 x 128 in LDS, four by four bytes to a thread. The rows of a gradient are cut in the same launch,
+// by the workgroups behind those.
+struct Turn {
+    int64_t n, k;
+    const uint8_t* codes;
+    int64_t ldq;
+    const void* scales;
+    int64_t lds;
+    uint8_t* codes_t;
+    void* scales_t;
+    int64_t ld_t, lds_t;
+    int nb, kb, blocks;
+};
+struct Rows {
+    int64_t n, k;
+    const void* V;
+    int64_t ldv;
+    uint8_t* codes;
+    int64_t ld;
+    uint8_t* scales;
+    int64_t lds;
+    int chunks;
+};
+template <int TYPE, bool WIDE>
 __launch_bounds__(kThreads)
-__global__ void f8_transpose_kernel(int64_t n, int64_t k, const uint8_t* codes, int64_t ldq, const void* scales, int64_t lds, uint8_t* codes_t, void* scales_t, int64_t ld_t, int64_t lds_t) {
+__global__ void f8_gradient_operands_kernel(Turn t, Rows v) {
     __shared__ unsigned block[128][33];
-    const int64_t expert = blockIdx.z;
-    const int bn = blockIdx.y, bk = blockIdx.x, nb = gridDim.y, kb = gridDim.x;
-    const uint8_t* from = codes + (expert * n + (int64_t)bn * 128) * ldq + (int64_t)bk * 128;
-    const int rows = (int)min<int64_t>(128, n - (int64_t)bn * 128), cols = (int)min<int64_t>(128, k - (int64_t)bk * 128);
+    if ((int)blockIdx.x >= t.blocks) {
+        const int b = blockIdx.x - t.blocks;
+        split_rows<TYPE>(v.n, v.k, v.V, v.ldv, v.codes, v.ld, v.scales, v.lds, b / v.chunks, b % v.chunks);
+        return;
+    }
+    const int line = blockIdx.x / t.kb, bk = blockIdx.x - line * t.kb, expert = line / t.nb, bn = line - expert * t.nb;
+    const uint8_t* from = t.codes + (expert * t.n + (int64_t)bn * 128) * t.ldq + (int64_t)bk * 128;
+    const int rows = (int)min<int64_t>(128, t.n - (int64_t)bn * 128), cols = (int)min<int64_t>(128, t.k - (int64_t)bk * 128);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int r = (threadIdx.x >> 3) + 32 * i, p = threadIdx.x & 7;
         v4u x = {0, 0, 0, 0};
-        if (r < rows) x = *reinterpret_cast<const v4u*>(from + r * ldq + p * 16);
+        if (r < rows) x = *reinterpret_cast<const v4u*>(from + r * t.ldq + p * 16);
 #pragma unroll
         for (int e = 0; e < 4; ++e) block[r][p * 4 + e] = x[e];
     }
     __syncthreads();
-    uint8_t* to = codes_t + (expert * k + (int64_t)bk * 128) * ld_t + (int64_t)bn * 128;
+    uint8_t* to = t.codes_t + (expert * t.k + (int64_t)bk * 128) * t.ld_t + (int64_t)bn * 128;
     const int r4 = threadIdx.x & 31;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -146,28 +176,35 @@ __global__ void f8_transpose_kernel(int64_t n, int64_t k, const uint8_t* codes, 
                                __builtin_amdgcn_perm(d, c, 0x07060302u)};
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (4 * c4 + e < cols) *reinterpret_cast<unsigned*>(to + (int64_t)(4 * c4 + e) * ld_t + 4 * r4) = y[e];
+            if (4 * c4 + e < cols) *reinterpret_cast<unsigned*>(to + (int64_t)(4 * c4 + e) * t.ld_t + 4 * r4) = y[e];
     }
     if (threadIdx.x == 0) {
-        const int64_t at = (expert * nb + bn) * lds + bk, at_t = (expert * kb + bk) * lds_t + bn;
+        const int64_t at = ((int64_t)expert * t.nb + bn) * t.lds + bk, at_t = ((int64_t)expert * t.kb + bk) * t.lds_t + bn;
         if constexpr (WIDE)
-            static_cast<float*>(scales_t)[at_t] = static_cast<const float*>(scales)[at];
+            static_cast<float*>(t.scales_t)[at_t] = static_cast<const float*>(t.scales)[at];
         else
-            static_cast<uint8_t*>(scales_t)[at_t] = static_cast<const uint8_t*>(scales)[at];
+            static_cast<uint8_t*>(t.scales_t)[at_t] = static_cast<const uint8_t*>(t.scales)[at];
     }
 }
 
 // Runs along the tokens: a workgroup takes 128 tokens of an expert and 64 columns; a thread holds eight columns of four neighbouring tokens,
 // whose codes are a word of the transposed row.
+// Both operands of a weights' gradient in one launch.
 template <int TYPE>
 __launch_bounds__(kThreads)
-__global__ void f8_cut_tokens_kernel(int t, int rows, int64_t n, int experts, const int* offsets, const int* source, const void* V, int64_t ldv, uint8_t* codes, int64_t ld, uint8_t* scales,
-                                     int64_t lds, int tiles) {
+__global__ void f8_cut_tokens_kernel(int rows, int experts, const int* offsets, F8Columns dy, F8Columns x, int runs) {
     typedef typename Elem<TYPE>::raw raw;
+    const int dy_tiles = (int)((dy.n + 63) / 64), first_x = runs * dy_tiles;
+    const bool second = (int)blockIdx.x >= first_x;
+    const int tiles = second ? (int)((x.n + 63) / 64) : dy_tiles, number = second ? blockIdx.x - first_x : blockIdx.x, t = second ? x.t : dy.t;
+    const int64_t n = second ? x.n : dy.n, ldv = second ? x.ldv : dy.ldv, ld = (int64_t)runs * 128, lds = runs;
+    const int* source = second ? x.source : dy.source;
+    const void* V = second ? x.V : dy.V;
+    uint8_t *codes = second ? x.codes : dy.codes, *scales = second ? x.scales : dy.scales;
     __shared__ unsigned tops[kThreads / 64][64];
     __shared__ unsigned turned[64][33];
-    const int run = blockIdx.x / tiles, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t col0 = (int64_t)(blockIdx.x % tiles) * 64;
+    const int run = number / tiles, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t col0 = (int64_t)(number % tiles) * 64;
     int first = 0, count = rows, unit = run;
     if (experts) {
         Segment s;
@@ -256,21 +293,23 @@ hipError_t launch_f8_expand(int64_t n, int64_t k, int block_rows, const uint8_t*
     });
 }
 
-hipError_t launch_f8_transpose(int64_t experts, int64_t n, int64_t k, const uint8_t* codes, int64_t ldq, int scale_type, const void* scales, int64_t lds, uint8_t* codes_t, void* scales_t,
-                               hipStream_t st) {
-    const dim3 grid((unsigned)f8_groups(k), (unsigned)f8_groups(n), (unsigned)experts);
-    auto kernel = scale_type == OZIMMU_F32 ? f8_transpose_kernel<true> : f8_transpose_kernel<false>;
-    kernel<<<grid, dim3(kThreads), 0, st>>>(n, k, codes, ldq, scales, lds, codes_t, scales_t, f8_row_bytes(n), f8_scale_bytes(n));
-    return hipGetLastError();
+hipError_t launch_f8_gradient_operands(int64_t experts, int64_t n, int64_t k, const uint8_t* codes, int64_t ldq, int scale_type, const void* scales, int64_t lds, uint8_t* codes_t,
+                                       void* scales_t, int64_t rows, const void* V, int type, int64_t ldv, uint8_t* v_codes, uint8_t* v_scales, hipStream_t st) {
+    const int64_t nb = f8_groups(n), kb = f8_groups(k), blocks = experts * nb * kb, chunks = (n + 511) / 512, cuts = v_codes ? (rows + 4 * kRows - 1) / (4 * kRows) * chunks : 0;
+    if (too_many(blocks + cuts)) return hipErrorInvalidConfiguration;
+    const Turn t{n, k, codes, ldq, scales, lds, codes_t, scales_t, f8_row_bytes(n), f8_scale_bytes(n), (int)nb, (int)kb, (int)blocks};
+    const Rows v{rows, n, V, ldv, v_codes, f8_row_bytes(n), v_scales, f8_scale_bytes(n), (int)chunks};
+    return by_type(type, [&](auto kind) {
+        constexpr int T = decltype(kind)::value;
+        auto kernel = scale_type == OZIMMU_F32 ? f8_gradient_operands_kernel<T, true> : f8_gradient_operands_kernel<T, false>;
+        kernel<<<dim3((unsigned)(blocks + cuts)), dim3(kThreads), 0, st>>>(t, v);
+    });
 }
 
-hipError_t launch_f8_cut_tokens(int64_t t, int64_t rows, int64_t n, int64_t experts, const int* offsets, const int* source, const void* V, int type, int64_t ldv, uint8_t* codes, int64_t ld,
-                                uint8_t* scales, int64_t lds, hipStream_t st) {
-    const int64_t tiles = (n + 63) / 64, grid = ld / 128 * tiles;
+hipError_t launch_f8_cut_tokens(int64_t rows, int64_t experts, const int* offsets, int type, const F8Columns& dy, const F8Columns& x, int64_t runs, hipStream_t st) {
+    const int64_t grid = runs * ((dy.n + 63) / 64 + (x.n + 63) / 64);
     if (too_many(grid)) return hipErrorInvalidConfiguration;
-    return by_type(type, [&](auto kind) {
-        f8_cut_tokens_kernel<decltype(kind)::value><<<dim3((unsigned)grid), dim3(kThreads), 0, st>>>((int)t, (int)rows, n, (int)experts, offsets, source, V, ldv, codes, ld, scales, lds, (int)tiles);
-    });
+    return by_type(type, [&](auto kind) { f8_cut_tokens_kernel<decltype(kind)::value><<<dim3((unsigned)grid), dim3(kThreads), 0, st>>>((int)rows, (int)experts, offsets, dy, x, (int)runs); });
 }
 
 }  // namespace ozimmu
