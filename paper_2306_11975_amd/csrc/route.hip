@@ -455,8 +455,8 @@ __global__ void route_grad_chosen_kernel(RouteArgs a, const int* indices, const 
     if (a.sigmoid) {
         const double s = mine >= 0 ? 1.0 / (1.0 + exp(-l)) : 0.0;
         if (a.renormalize) {
-            const double total = sum_of<LANES>(s) + 1e-20, mean = sum_of<LANES>(dw * s) / total;
-            d = (dw - mean) / total * s * (1.0 - s);
+            const double total = sum_of<LANES>(s) + 1e-20, w = s / total;      // (one choice: w is 1 and the gradient 0, not a rounding)
+            d = (dw - sum_of<LANES>(dw * w)) / total * s * (1.0 - s);
         } else {
             d = dw * s * (1.0 - s);
         }
@@ -492,6 +492,7 @@ __global__ void route_grad_chosen_kernel(RouteArgs a, const int* indices, const 
     }
 }
 
+// That of softmax scores as they are: every logit has one, -s (sum of the chosen scores' gradients times the scores), and the chosen ones s dw beside it.
 template <int TYPE, int SLOTS>
 __launch_bounds__(kThreads)
 __global__ void route_grad_kernel(RouteArgs a, const int* indices, const float* dweights, void* dlogits, int64_t lddl) {
@@ -505,41 +506,17 @@ __global__ void route_grad_kernel(RouteArgs a, const int* indices, const float* 
     int mine = lane < a.top ? indices[token * a.top + lane] : -1;
     if ((unsigned)mine >= (unsigned)a.experts) mine = -1;
     const double dw = mine >= 0 ? (double)dweights[token * a.top + lane] * (double)a.scale : 0.0;
-    double score = 0.0, logit = -INFINITY;
+    double score = 0.0;
     for (int j = 0; j < a.top; ++j) {   // lane j's choice: its score
         const int i = __shfl(mine, j);
         if (i < 0) continue;
-        double sc = 0.0, lg = 0.0;
+        double sc = 0.0;
 #pragma unroll
-        for (int k = 0; k < SLOTS; ++k)
-            if (k == (i >> 6)) {
-                sc = s[k];
-                lg = l[k];
-            }
+        for (int k = 0; k < SLOTS; ++k) sc = k == (i >> 6) ? s[k] : sc;
         sc = __shfl(sc, i & 63);
-        lg = __shfl(lg, i & 63);
-        if (lane == j) {
-            score = sc;
-            logit = lg;
-        }
+        score = lane == j ? sc : score;
     }
-    // d: what goes to the chosen logit; for softmax scores that are not renormalised, every logit receives -s (sum of score gradients times scores)
-    double d, all = 0.0;
-    if (a.renormalize) {
-        if (a.sigmoid) {
-            const double total = wave_sum(score) + 1e-20, mean = wave_sum(dw * score) / total;
-            d = (dw - mean) / total * score * (1.0 - score);
-        } else {
-            const double top = wave_max(logit);
-            const double x = mine >= 0 ? exp(logit - top) : 0.0, sum = wave_sum(x), w = sum > 0.0 ? x / sum : 0.0;
-            d = w * (dw - wave_sum(dw * w));
-        }
-    } else if (a.sigmoid) {
-        d = dw * score * (1.0 - score);
-    } else {
-        d = dw * score;
-        all = wave_sum(d);
-    }
+    const double d = dw * score, all = wave_sum(d);
     const bool any = __builtin_amdgcn_ballot_w64(mine >= 0) != 0;
 #pragma unroll
     for (int k = 0; k < SLOTS; ++k) g[k] = any && all != 0.0 ? -s[k] * all : 0.0;
@@ -548,8 +525,7 @@ __global__ void route_grad_kernel(RouteArgs a, const int* indices, const float* 
         const double x = __shfl(d, j);
         if (i < 0) continue;
 #pragma unroll
-        for (int k = 0; k < SLOTS; ++k)
-            if (k * 64 + lane == i) g[k] += x;
+        for (int k = 0; k < SLOTS; ++k) g[k] += k * 64 + lane == i ? x : 0.0;
     }
     raw* row = static_cast<raw*>(dlogits) + token * lddl;
 #pragma unroll

@@ -144,6 +144,14 @@ def test_route_gradient(t, experts, top, renormalize, score, dt):
         assert ((got[:, e].double() - slope).abs() <= slope.abs() * half_step(dt) + size[:, 0] * 1e-6 + torch.finfo(dt).smallest_normal * half_step(dt)).all()
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_gradient_of_one_choice_is_zero(score):
+    """One renormalised weight is 1 whatever the logits are."""
+    logits = torch.randn(200, 24, generator=gen(1))
+    indices, _ = route64(logits, 1, score=score)
+    assert not device_grad(logits, indices, torch.randn(200, 1, generator=gen(2)), score=score).any()
+
+
 # ---------------------------------------------------------------- order
 def device_order(indices, experts):
     t, top = indices.shape
