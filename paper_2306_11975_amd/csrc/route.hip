@@ -69,7 +69,7 @@ __device__ __forceinline__ void scores(const RouteArgs& a, int64_t token, int la
 
 // The choice in 64 bits throughout. values, kept: LDS of this wavefront.
 template <int TYPE, int SLOTS>
-__device__ __forceinline__ void choose_exactly(const RouteArgs& a, int64_t token, int lane, double* values, unsigned long long* kept, int* indices, float* weights) {
+__device__ __forceinline__ void route_exactly(const RouteArgs& a, int64_t token, int lane, double* values, unsigned long long* kept, int* indices, float* weights) {
     double l[SLOTS], s[SLOTS], c[SLOTS];
     bool bad;
     scores<TYPE, SLOTS>(a, token, lane, l, s, bad);
@@ -173,7 +173,7 @@ __global__ void route_exactly_kernel(RouteArgs a, int* indices, float* weights) 
     __shared__ unsigned long long kept[kThreads / 64][16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t token = (int64_t)blockIdx.x * (kThreads / 64) + wave;
-    if (token < a.t) choose_exactly<TYPE, SLOTS>(a, token, lane, values[wave], kept[wave], indices, weights);
+    if (token < a.t) route_exactly<TYPE, SLOTS>(a, token, lane, values[wave], kept[wave], indices, weights);
 }
 
 // ---- the same in 32 bits, where those tell
@@ -249,75 +249,129 @@ template <> struct Bits<double> {
     }
 };
 
-// The choice by the values c (-inf: cannot be chosen): lane j <= top keeps the expert of round j (0xffffffff: none) and its value's bits. V = float:
-// unsure where the best top_groups + 1 groups are too near each other to tell.
-template <int LANES, int SLOTS, class V>
-__device__ __forceinline__ void choose(const RouteArgs& a, int lane, V (&c)[SLOTS], float near_scores, unsigned& mine, typename Bits<V>::type& mine_bits, bool& unsure) {
+// A group is `width` neighbouring lanes. From each lane's two largest values (-inf: none): whether its group is one of the best top_groups, by the
+// sum of its two. V = float: unsure where the last group kept and the next are too near each other to tell.
+template <int LANES, class V>
+__device__ __forceinline__ bool in_best_groups(const RouteArgs& a, int lane, bool there, int width, V first, V second, float near_scores, bool& unsure) {
     typedef typename Bits<V>::type bits;
-    if (a.groups > 1) {
-        // a group is `width` neighbouring lanes: the two largest of each, then the groups by their sum
-        const int width = a.experts / a.groups / SLOTS;
-        V first = -INFINITY, second = -INFINITY;
-#pragma unroll
-        for (int k = 0; k < SLOTS; ++k) {
-            second = max(second, min(first, c[k]));
-            first = max(first, c[k]);
-        }
-        for (int d = 1; d < width; d <<= 1) {
-            const V f = __shfl_xor(first, d), g = __shfl_xor(second, d);
-            second = max(max(second, g), min(first, f));
-            first = max(first, f);
-        }
-        const V sum = second == -INFINITY ? first : first + second;
-        bits key = lane * SLOTS < a.experts ? Bits<V>::of(sum) : 0, before = 0;
-        bool keep = false;
-        for (int n = 0; n <= a.top_groups && n < a.groups; ++n) {
-            const bits best = most<LANES>(key);
-            if constexpr (sizeof(V) == 4) {   // (which ones are kept matters, not their order)
-                const float v = Bits<float>::value(before), w = Bits<float>::value(best);
-                unsure |= n == a.top_groups && best != 0 && !(v - w > 2.f * near_scores + (fabsf(v) + fabsf(w)) * 0x1p-21f);
-            }
-            before = best;
-            if (n == a.top_groups) break;
-            const int at = (int)least<LANES>(key == best ? (unsigned)lane : 64u) / width;
-            if (best != 0 && lane / width == at) {
-                keep = true;
-                key = 0;
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < SLOTS; ++k) c[k] = keep ? c[k] : (V)-INFINITY;
+    for (int d = 1; d < width; d <<= 1) {
+        const V f = __shfl_xor(first, d), g = __shfl_xor(second, d);
+        second = max(max(second, g), min(first, f));
+        first = max(first, f);
     }
-    bits key[SLOTS];
+    const V sum = second == -INFINITY ? first : first + second;
+    bits key = there ? Bits<V>::of(sum) : 0, before = 0;
+    bool keep = false;
+    for (int n = 0; n <= a.top_groups && n < a.groups; ++n) {
+        const bits best = most<LANES>(key);
+        if constexpr (sizeof(V) == 4) {   // (which ones are kept matters, not their order)
+            const float v = Bits<float>::value(before), w = Bits<float>::value(best);
+            unsure |= n == a.top_groups && best != 0 && !(v - w > 2.f * near_scores + (fabsf(v) + fabsf(w)) * 0x1p-21f);
+        }
+        before = best;
+        if (n == a.top_groups) break;
+        const int at = (int)least<LANES>(key == best ? (unsigned)lane : 64u) / width;
+        if (best != 0 && lane / width == at) {
+            keep = true;
+            key = 0;
+        }
+    }
+    return keep;
+}
+template <int SLOTS, class V>
+__device__ __forceinline__ void two_largest(const V (&c)[SLOTS], V& first, V& second) {
+    first = second = -INFINITY;
 #pragma unroll
-    for (int k = 0; k < SLOTS; ++k) key[k] = Bits<V>::of(c[k]);
-    mine = 0xffffffffu;
-    mine_bits = 0;
-    for (int j = 0; j <= a.top; ++j) {
-        bits here = key[0];
+    for (int k = 0; k < SLOTS; ++k) {
+        second = max(second, min(first, c[k]));
+        first = max(first, c[k]);
+    }
+}
+
+// Lane j < top keeps the expert of round j (0xffffffff: none), the one with the largest value, of equals the lowest.
+template <int LANES, int SLOTS>
+__device__ __forceinline__ unsigned choose_exactly(const RouteArgs& a, int lane, const double (&c)[SLOTS]) {
+    unsigned long long key[SLOTS];
+    unsigned mine = 0xffffffffu;
+#pragma unroll
+    for (int k = 0; k < SLOTS; ++k) key[k] = Bits<double>::of(c[k]);
+    for (int j = 0; j < a.top; ++j) {
+        unsigned long long here = key[0];
         unsigned slot = 0;
 #pragma unroll
         for (int k = 1; k < SLOTS; ++k) {
             slot = key[k] > here ? (unsigned)k : slot;
             here = key[k] > here ? key[k] : here;
         }
-        const bits best = most<LANES>(here);
+        const unsigned long long best = most<LANES>(here);
         const unsigned winner = least<LANES>(here == best && best != 0 ? (unsigned)lane * SLOTS + slot : 0xffffffffu);
         mine = lane == j ? winner : mine;
-        mine_bits = lane == j ? best : mine_bits;
         const unsigned gone = winner - (unsigned)lane * SLOTS;
 #pragma unroll
         for (int k = 0; k < SLOTS; ++k) key[k] = gone == (unsigned)k ? 0 : key[k];
     }
+    return mine;
 }
+
+// A sorting network: pairs of places, the larger value to the first (merges of odd and even halves).
+template <int N>
+struct Network {
+    int first[80], second[80], count;
+    constexpr Network() : first(), second(), count(0) {
+        for (int p = 1; p < N; p *= 2)
+            for (int k = p; k >= 1; k /= 2)
+                for (int j = k % p; j <= N - 1 - k; j += 2 * k)
+                    for (int i = 0; i < k && i + j + k < N; ++i)
+                        if ((i + j) / (2 * p) == (i + j + k) / (2 * p)) {
+                            first[count] = i + j;
+                            second[count++] = i + j + k;
+                        }
+    }
+};
+// The same by 32-bit values, whose last bits (those of SLOTS - 1) make room for the slot: each lane sorts its keys once, and a round takes the
+// largest of their heads; the winner's move up.
+template <int LANES, int SLOTS>
+struct Sorted {
+    static constexpr unsigned kSlot = SLOTS - 1;
+    unsigned key[SLOTS];
+    __device__ __forceinline__ explicit Sorted(const float (&c)[SLOTS]) {
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) {
+            const unsigned b = Bits<float>::of(c[k]);
+            key[k] = b == 0 ? 0 : (b & ~kSlot) | (kSlot - k);
+        }
+        constexpr Network<SLOTS> network;
+        static_for<0, network.count>([&](auto n) {
+            constexpr Network<SLOTS> w;
+            constexpr int i = w.first[decltype(n)::value], j = w.second[decltype(n)::value];
+            const unsigned high = max(key[i], key[j]), low = min(key[i], key[j]);
+            key[i] = high;
+            key[j] = low;
+        });
+    }
+    // The expert (0xffffffff: none) and its value's bits.
+    __device__ __forceinline__ unsigned next(int lane, unsigned& best) {
+        const unsigned here = key[0] & ~kSlot;
+        best = most<LANES>(here);
+        const unsigned expert = (unsigned)lane * SLOTS + (kSlot - (key[0] & kSlot));
+        const unsigned winner = least<LANES>(here == best && best != 0 ? expert : 0xffffffffu);
+        const bool won = winner == expert && best != 0;
+#pragma unroll
+        for (int k = 0; k + 1 < SLOTS; ++k) key[k] = won ? key[k + 1] : key[k];
+        key[SLOTS - 1] = won ? 0 : key[SLOTS - 1];
+        return winner;
+    }
+};
 
 // LANES lanes to a token (16: four tokens a wavefront), experts lane * SLOTS + k. The choice goes by 32-bit values where their order is beyond
 // doubt: without a bias and groups by the logits themselves, whose order the scores have, else by scores that are off by less than 2^-20 of the
-// largest, plus their bias. Where two neighbours among the best top + 1, or the last group kept and the next, are as near as that, and not equal
-// in all that they come from, the wavefront's tokens are chosen again by 64-bit values (at 256 experts with sigmoid scores and a bias one token in
-// some hundreds). Each round finds the largest value, then the lowest expert that has it, and takes that out; lane j keeps the round's, so that
-// neighbours and weights are looked at once, all together. Bound: the rounds' instructions, and the second choice of the last wavefront.
-// 16384 tokens, 256 experts in 8 groups, 8 of 4 groups, us: all in 64 bits 80, 64 lanes to a token 48, 16 lanes 26.
+// largest, plus their bias. Where two neighbours among the best top + 1 are as near as that, and not equal in all that they come from, those
+// top + 1 are put in order by their 64-bit values (at 256 experts with sigmoid scores and a bias one token in some hundreds); where the last
+// group kept and the next are as near (one token in some ten thousands), the groups by the 64-bit values of their best; where those top + 1 need
+// not hold all that are that near, or the sum of all scores would be needed, the wavefront's tokens are chosen again from all 64-bit values. Each round finds the largest value, then the lowest expert that has it, and takes that out; lane j keeps the
+// round's, so that neighbours and weights are looked at once, all together. Bound: the rounds' instructions.
+// 16384 tokens, 256 experts in 8 groups, 8 of 4 groups, us: all in 64 bits 80, 64 lanes to a token 48, 16 lanes 26, the lanes' keys sorted 24,
+// and 64-bit values of the few in doubt 17.
 template <int TYPE, int LANES, int SLOTS>
 __launch_bounds__(kThreads)
 __global__ void route_kernel(RouteArgs a, int* indices, float* weights) {
@@ -336,10 +390,10 @@ __global__ void route_kernel(RouteArgs a, int* indices, float* weights) {
     for (int k = 0; k < SLOTS; ++k) {
         odd |= l[k] > 10.f && a.sigmoid;
         bad |= l[k] != l[k] || (!a.sigmoid && l[k] == INFINITY);
-        top_bits = max(top_bits, Bits<float>::of(l[k]));
+        if (!a.sigmoid) top_bits = max(top_bits, Bits<float>::of(l[k]));
     }
     const bool by_values = a.bias != nullptr || a.groups > 1;      // (the same for all)
-    top_bits = most<LANES>(top_bits);
+    if (!a.sigmoid) top_bits = most<LANES>(top_bits);
     const float top_logit = Bits<float>::value(top_bits);
     float largest = 1.f;      // a score is at most that
     if (by_values) {
@@ -372,27 +426,100 @@ __global__ void route_kernel(RouteArgs a, int* indices, float* weights) {
     // Scores: the argument of the exponential is rounded to 2^-23 of itself; |l| <= 10 for sigmoid, whose slope is at most 1 / 4, and for softmax
     // the argument's size times the score is below one half of the largest.
     const float near_scores = largest * 0x1p-20f;
-    unsigned mine, mine_bits;
-    bool unsure = odd;
-    choose<LANES, SLOTS>(a, lane, c, near_scores, mine, mine_bits, unsure);
-    float logit = -INFINITY;
+    // (the values' last bits are gone; and logits nearer than 1e-9 may have one score in 64 bits)
+    auto apart = [&](float v, float w) { return v - w > (by_values ? 2.f * near_scores : 1e-9f) + (fabsf(v) + fabsf(w)) * 0x1p-18f; };
+    bool unsure = false, all = odd;     // neighbours too near; only the choice among all experts will tell
+    const int width = a.groups > 1 ? a.experts / a.groups / SLOTS : 1;
+    const bool some = lane * SLOTS < a.experts;
+    if (a.groups > 1) {
+        float first, second;
+        two_largest(c, first, second);
+        bool near_groups = false, keep = in_best_groups<LANES>(a, lane, some, width, first, second, near_scores, near_groups);
+        if (!a.sigmoid) {
+            all |= near_groups;
+        } else if (__builtin_amdgcn_ballot_w64(near_groups)) {
+            // the groups by 64-bit values of those that may be the two largest of their lane
+            const float border = second == INFINITY ? second : second - (2.f * near_scores + fabsf(second) * 0x1p-21f);
+            unsigned left = 0;
+#pragma unroll
+            for (int k = 0; k < SLOTS; ++k) left |= c[k] > -INFINITY && c[k] >= border ? 1u << k : 0u;
+            double first64 = -INFINITY, second64 = -INFINITY;
+            while (__builtin_amdgcn_ballot_w64(left != 0)) {
+                const unsigned slot = (unsigned)__builtin_ctz(left | 1u << 31);
+                float logit = 0.f, bias = 0.f;
+#pragma unroll
+                for (int k = 0; k < SLOTS; ++k) {
+                    logit = slot == (unsigned)k ? l[k] : logit;
+                    if (a.bias) bias = slot == (unsigned)k ? b[k] : bias;
+                }
+                const double value = left ? 1.0 / (1.0 + exp(-(double)logit)) + (double)bias : -INFINITY;
+                second64 = max(second64, min(first64, value));
+                first64 = max(first64, value);
+                left &= left - 1;
+            }
+            keep = in_best_groups<LANES>(a, lane, some, width, first64, second64, 0.f, near_groups);
+        }
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) c[k] = keep ? c[k] : -INFINITY;
+    }
+    Sorted<LANES, SLOTS> sorted(c);
+    unsigned mine = 0xffffffffu, mine_bits = 0;
+    for (int j = 0; j <= a.top; ++j) {      // (lane top: the best that is not chosen)
+        unsigned best;
+        const unsigned winner = sorted.next(lane, best);
+        mine = lane == j ? winner : mine;
+        mine_bits = lane == j ? best : mine_bits;
+    }
+    float logit = -INFINITY, bias = 0.f;
     {   // neighbours: lane j against lane j - 1
-        float bias = 0.f;
         if (mine != 0xffffffffu) {
             logit = Elem<TYPE>::load((static_cast<const raw*>(a.logits) + token * a.ldl)[mine]);
             if (a.bias) bias = a.bias[mine];
         }
         const float v = Bits<float>::value((unsigned)__shfl_up((int)mine_bits, 1)), w = Bits<float>::value(mine_bits);
         const bool same = __shfl_up(logit, 1) == logit && __shfl_up(bias, 1) == bias;
-        const float near = by_values ? 2.f * near_scores + (fabsf(v) + fabsf(w)) * 0x1p-22f : 1e-9f;
-        if (lane > 0 && lane <= a.top && mine != 0xffffffffu) unsure |= !(v - w > near) && !same;
-        if (!a.sigmoid && mine != 0xffffffffu) unsure |= top_logit - logit > 600.f;      // (64 bits have no score for it)
+        // (of equals the lowest came first; but behind the last chosen and its equal there may be a larger one yet, unless the values' lost
+        // bits were zeros)
+        const bool in_order = same && (lane < a.top || (TYPE != OZIMMU_F32 && !by_values));
+        if (lane > 0 && lane <= a.top && mine != 0xffffffffu) unsure |= !apart(v, w) && !in_order;
+        if (!a.sigmoid && mine != 0xffffffffu) all |= top_logit - logit > 600.f;      // (64 bits have no score for it)
     }
     constexpr unsigned long long kMask = LANES == 64 ? ~0ull : (1ull << (LANES & 63)) - 1;
     const int row0 = (threadIdx.x & 63) / LANES * LANES;
     bad = (__builtin_amdgcn_ballot_w64(bad) >> row0 & kMask) != 0;
     const unsigned long long doubt = __builtin_amdgcn_ballot_w64(unsure && !bad);
     if (doubt) {   // (the same for the wavefront)
+        // Where the one behind them is clearly less than the last chosen, the chosen are among these top + 1. Softmax with a bias or groups
+        // needs the sum over all for their values.
+        unsigned next_bits;
+        sorted.next(lane, next_bits);
+        const float last = Bits<float>::value((unsigned)__shfl((int)mine_bits, row0 + a.top - 1));
+        const bool mine_doubt = (doubt >> row0 & kMask) != 0;
+        all |= mine_doubt && ((!a.sigmoid && by_values) || (next_bits != 0 && !apart(last, Bits<float>::value(next_bits))));
+        double d = -INFINITY;
+        if (mine != 0xffffffffu) d = a.sigmoid ? 1.0 / (1.0 + exp(-(double)logit)) + (double)bias : (double)logit;
+        int before = 0;
+        for (int j = 0; j <= a.top; ++j) {
+            const double other = __shfl(d, row0 + j);
+            before += other > d || (other == d && (unsigned)__shfl((int)mine, row0 + j) < mine);
+            all |= mine_doubt && !a.sigmoid && other != d && fabs(other - d) < 1e-9;
+        }
+        unsigned sure = 0xffffffffu;
+        float of_sure = -INFINITY;
+        for (int j = 0; j <= a.top; ++j) {
+            const bool at = __shfl(mine != 0xffffffffu ? before : -1, row0 + j) == lane;
+            const unsigned expert = (unsigned)__shfl((int)mine, row0 + j);
+            const float value = __shfl(logit, row0 + j);
+            sure = at ? expert : sure;
+            of_sure = at ? value : of_sure;
+        }
+        if (mine_doubt) {
+            mine = sure;
+            logit = of_sure;
+        }
+    }
+    const unsigned long long rest = __builtin_amdgcn_ballot_w64(all && !bad);
+    if (rest) {
         double d[SLOTS], sum = 0.0;
 #pragma unroll
         for (int k = 0; k < SLOTS; ++k) {
@@ -406,11 +533,16 @@ __global__ void route_kernel(RouteArgs a, int* indices, float* weights) {
             if (a.bias) d[k] += (double)b[k];
             d[k] = l[k] == -INFINITY ? -INFINITY : d[k];
         }
-        unsigned exact;
-        unsigned long long exact_bits;
-        bool never = false;
-        choose<LANES, SLOTS>(a, lane, d, 0.f, exact, exact_bits, never);
-        if (doubt >> row0 & kMask) {
+        if (a.groups > 1) {
+            double first, second;
+            bool never = false;
+            two_largest(d, first, second);
+            const bool keep = in_best_groups<LANES>(a, lane, some, width, first, second, 0.f, never);
+#pragma unroll
+            for (int k = 0; k < SLOTS; ++k) d[k] = keep ? d[k] : -INFINITY;
+        }
+        const unsigned exact = choose_exactly<LANES, SLOTS>(a, lane, d);
+        if (rest >> row0 & kMask) {
             mine = exact;
             logit = mine != 0xffffffffu ? Elem<TYPE>::load((static_cast<const raw*>(a.logits) + token * a.ldl)[mine]) : -INFINITY;
         }

@@ -79,6 +79,65 @@ def test_route_ties_and_neighbours(score):
     assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts,top,groups,top_groups", [(16, 2, 1, 1), (64, 8, 1, 1), (256, 8, 8, 4), (256, 15, 1, 1), (512, 16, 1, 1), (1024, 32, 1, 1)])
+def test_route_few_neighbours(experts, top, groups, top_groups, score):
+    """Most of many tokens are clear; some have two or more experts too near for 32 bits among the chosen, at the border and just behind it."""
+    t = 2000
+    g = gen(experts + top)
+    logits = torch.randn(t, experts, generator=g)
+    bias = (torch.randn(experts, generator=g) * 0.1).bfloat16().float()
+    for b in (None, bias):
+        l = logits.clone()
+        p = route64(l, experts if groups == 1 and experts <= 32 else min(32, experts), score=score, bias=b, groups=groups, top_groups=top_groups)[0].long()
+        for first, count in ((0, 2), (top - 1, 2), (top - 2, 2), (top - 1, 3), (top - 2, 4), (0, min(32, experts))):
+            rows = torch.arange(t)[first + 7 * count::61]
+            chosen = p[rows][:, first:first + count]
+            chosen = chosen[:, (chosen >= 0).all(dim=0)]
+            if b is None:        # the same logit but for a few units
+                at = l[rows, chosen[:, 0]][:, None]
+                l[rows[:, None], chosen] = at * (1 + torch.randint(-3, 4, chosen.shape, generator=g) * 2.0 ** -23)
+            elif score == "sigmoid":   # the same sum of score and bias but for what the rounding of the logit leaves
+                value = torch.sigmoid(l[rows, chosen[:, 0]].double())[:, None] + b.double()[chosen[:, :1]]
+                l[rows[:, None], chosen] = torch.logit((value - b.double()[chosen]).clamp(0.05, 0.95)).float()
+        how = dict(score=score, bias=b, groups=groups, top_groups=top_groups)
+        got, weights = device_route(l, top, **how)
+        want, w = route64(l, top, **how)
+        assert torch.equal(got, want)
+        check_weights(weights, w)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts,groups,top_groups", [(64, 8, 4), (256, 8, 4), (256, 64, 1), (512, 4, 3), (1024, 8, 2)])
+def test_route_few_near_groups(experts, groups, top_groups, score):
+    """Some of many tokens have groups whose sums of two are too near for 32 bits, the two among several that are nearly as large; and biases that
+    always or never choose an expert."""
+    t, top, per = 1000, 4, experts // groups
+    g = gen(experts)
+    logits = torch.randn(t, experts, generator=g)
+    bias = (torch.randn(experts, generator=g) * 0.1).bfloat16().float()
+    never = bias.clone()
+    never[::5], never[3::11] = -INF, INF
+    for b in (None, bias, never):
+        l = logits.clone()
+        by_group, value = l.view(t, groups, per), torch.zeros(per) if b is None else b.view(groups, per)
+        for i in range(0, t, 29):
+            first, second = torch.randperm(groups, generator=g)[:2].tolist()
+            order = by_group[i, first].topk(min(3, per)).values
+            if b is None or score == "softmax":
+                by_group[i, second, :len(order)] = order * (1 + torch.randint(-2, 3, order.shape, generator=g) * 2.0 ** -23)
+            else:
+                shift = (value[first] - value[second]).nan_to_num(0.0, 0.0, 0.0).double()
+                by_group[i, second] = torch.logit((torch.sigmoid(by_group[i, first].double()) + shift).clamp(0.02, 0.98)).float()
+            if i % 2:      # more than two in a group
+                by_group[i, first, :3] = by_group[i, first].max() * (1 + torch.randint(-2, 3, by_group[i, first, :3].shape, generator=g) * 2.0 ** -23)
+        how = dict(score=score, bias=b, groups=groups, top_groups=top_groups)
+        got, weights = device_route(l, top, **how)
+        want, w = route64(l, top, **how)
+        assert torch.equal(got, want)
+        check_weights(weights, w)
+
+
 @pytest.mark.parametrize("dt", TYPES)
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("groups,top_groups", [(1, 1), (4, 2)])
