@@ -104,6 +104,7 @@ ozimmu_status_t check_experts(int64_t t, int64_t rows, int64_t experts, const in
 hipError_t product(const F8Args& a, bool few, hipStream_t st) {
     if (few) return launch_f8_few(a, st);
     const F8Choice c = choose_f8_tile(a);
+    if (c.shape == kF8Shapes) return hipErrorInvalidConfiguration;
     if (a.out_type == OZIMMU_F32) return launch_f8_tiles_exact(a, c, st);
     return c.shape == kF8Tile256 ? launch_f8_large(a, st) : launch_f8_tiles(a, c, st);
 }
@@ -219,7 +220,7 @@ F8Choice choose_f8_tile(const F8Args& a) {
                                           {32, 64, 1536, 0.38, 0.83, 1.0, 2.0}};
     static const Shape wide[kF8Shapes] = {{256, 256, 0, 0.0, 0.0, 0.0, 0.0}, {128, 128, 512, 1.5, 2.3, 4.0, 3.0}, {64, 128, 768, 0.9, 1.95, 3.0, 2.5}, {64, 64, 1024, 0.58, 1.43, 1.3, 2.0},
                                           {32, 64, 1536, 0.50, 1.25, 1.0, 2.0}};
-    F8Choice best{kF8Tile64, 1, 1, a.slabs};
+    F8Choice best{kF8Shapes, 0, 1, a.slabs};      // (none: more tiles than a launch has)
     double best_us = 1e30;
     for (int i = 0; i < kF8Shapes; ++i) {
         const Shape& s = a.out_type == OZIMMU_F32 ? wide[i] : half[i];

@@ -116,6 +116,7 @@ __global__ void f8_few_kernel(F8Args a, int tiles_n) {
                 scale_parts<WIDE>(a.sq, sq + slab0 + s, m, byte);
                 v4u codes[2];
                 e = (int)ep[s];
+                if (TYPE == OZIMMU_E4M3 && e == 255) m = __builtin_nanf("");
                 cut_slab<TYPE>(x[s], codes, e);
                 v8h h[4];
                 halves16(codes[0], h[0], h[1]);

@@ -207,6 +207,8 @@ __global__ void f8_product_kernel(F8Args a, F8Plan plan) {
             v8h ph[4];
             halves16(p.a, ph[0], ph[1]);
             halves16(p.b, ph[2], ph[3]);
+            // (a byte of 255 is a NaN: the sums of two others end at 254; columns that were cut here have none)
+            const int sp_now = (int)(sp[i] & 255u), e_p = Q_ROWS || sp_now < 255 ? sp_now : 512;
 #pragma unroll
             for (int j = 0; j < NI; ++j) {
                 v8h qh[4];
@@ -221,8 +223,9 @@ __global__ void f8_product_kernel(F8Args a, F8Plan plan) {
                     const int byte = (int)((Q_ROWS ? (unsigned)__shfl((int)sq[j], (lane >> 4) * 4 + e) : sq[0]) & 255u);
                     float x = part[e];
                     if constexpr (WIDE) x *= sig;
-                    x = __builtin_amdgcn_ldexpf(x, (int)(sp[i] & 255u) + byte - 254);
-                    acc[i][j][e] += byte == 255 ? __builtin_nanf("") : x;
+                    const int exponent = e_p + (Q_ROWS || byte < 255 ? byte : 512) - 254;
+                    x = __builtin_amdgcn_ldexpf(x, exponent);
+                    acc[i][j][e] += !Q_ROWS && exponent > 254 ? __builtin_nanf("") : x;
                 }
             }
         } else {

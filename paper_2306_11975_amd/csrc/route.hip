@@ -1,4 +1,5 @@
-// The choice of experts for each token, and its gradient (gfx950). A wavefront takes a token; lane l holds experts l, l + 64, ...
+// The choice of experts for each token, and its gradient (gfx950). First the form that computes everything in 64 bits, a wavefront to a token, lane l
+// with experts l, l + 64, ...: it serves groups that do not fill whole lanes. Below it the one that goes by 32 bits wherever those tell.
 //
 // Scores s: softmax or sigmoid of the logits. Choice values s + bias; of `groups` equal runs of experts the top_groups best stay, a group's
 // value being the sum of its two largest choice values; of what stays the `top` best are chosen, ties going to the lowest index. Scores and

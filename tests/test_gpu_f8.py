@@ -263,6 +263,24 @@ def test_nan_stays_in_its_row(t, dt):
     assert got[:, 128:].isnan().all() and torch.equal(got[:, :128], clean[:, :128])
 
 
+@pytest.mark.parametrize("t", [5, 150, 2100])
+@pytest.mark.parametrize("dt", [BF16, F32])
+def test_nan_scale_of_a_token(t, dt):
+    """A byte of 255 among the scales of given codes is a NaN for its row, whatever the other scale is."""
+    n, k = 2300, 700
+    codes, scales = device_cut(weights(n, k, 2))
+    xc, xs = device_cut(torch.randn(t, k, generator=gen(1)), 1)
+    clean, got = torch.empty(t, n, dtype=dt, device=DEV), torch.empty(t, n, dtype=dt, device=DEV)
+    ws = oz.alloc_f8_workspace("gemm", t, n, k, torch.uint8)
+    oz.f8_gemm(xc, codes, scales, clean, ws, x_scales=xs)
+    xs[2, 4], scales[0, 4] = 255, 0
+    xs[3, 4] = 254
+    oz.f8_gemm(xc, codes, scales, got, ws, x_scales=xs)
+    assert got[2].isnan().all() and not got[[i for i in range(t) if i != 2]].isnan().any()
+    rest = [i for i in range(t) if i not in (2, 3)]
+    assert torch.equal(got[rest][:, 128:], clean[rest][:, 128:])
+
+
 @pytest.mark.parametrize("t", [5, 150])
 @pytest.mark.parametrize("dt", [BF16, F32])
 def test_scales_far_apart(t, dt):
