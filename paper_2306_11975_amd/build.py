@@ -1,9 +1,11 @@
 """Build libozimmu.so (HIP, gfx950) in-tree with hipcc. Run: python -m paper_2306_11975_amd.build"""
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 from pathlib import Path
 
@@ -14,6 +16,7 @@ OBJ = PKG / "_build"
 LIB = PKG / "libozimmu.so"
 EXAMPLE = PKG / "example_dgemm"       # stand-alone C++ user of the C ABI (csrc/example_dgemm.cpp)
 PRELOAD = PKG / "libozimmu_preload.so"  # interposer for the vendor DGEMM/ZGEMM symbols (csrc/preload.cpp)
+CALLS = PKG / "_calls.so"             # Python's calls of the operators that a token waits for (csrc/calls.cpp; torch's headers)
 BLAS_CLIENT = PKG / "blas_client"     # plain rocBLAS/hipBLAS program the interposer is tried on (csrc/blas_client.cpp)
 
 SOURCES = ["split.hip", "gemm.hip", "gemm_real.hip", "gemm_dd.hip", "gemm_complex.hip", "gate.hip", "gate_many.hip", "small.hip", "small_complex.hip", "probes.hip", "static_scratch.hip", "api.cpp",
@@ -90,15 +93,35 @@ def _compile(src: str) -> Path:
     return obj
 
 
+def _compile_calls() -> Path:
+    """The object of the Python module; it is linked against torch's libraries, which are loaded when it is."""
+    torch = Path(importlib.util.find_spec("torch").submodule_search_locations[0])
+    obj = OBJ / "calls.cpp.o"
+    subprocess.run([hipcc(), "-O2", "-std=c++17", "-fPIC", "-Wall", f"-I{INCLUDE}", f"-I{torch / 'include'}", f"-I{torch / 'include/torch/csrc/api/include'}",
+                    f"-I{sysconfig.get_paths()['include']}", "-c", str(CSRC / "calls.cpp"), "-o", str(obj)], check=True)
+    return obj
+
+
+def _link_calls(obj: Path) -> None:
+    torch = Path(importlib.util.find_spec("torch").submodule_search_locations[0])
+    tmp = CALLS.with_suffix(f".tmp{os.getpid()}.so")
+    subprocess.run([hipcc(), "-shared", str(obj), f"-L{PKG}", "-lozimmu", f"-L{torch / 'lib'}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN", "-o", str(tmp)],
+                   check=True)
+    os.replace(tmp, CALLS)
+
+
 def build(verbose: bool = True) -> Path:
     """Compile every translation unit and link the shared library (always recompiles)."""
     OBJ.mkdir(exist_ok=True)
-    with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        calls = ex.submit(_compile_calls)
         objs = list(ex.map(_compile, SOURCES))
+        calls = calls.result()
     tmp = LIB.with_suffix(f".tmp{os.getpid()}.so")
     cmd = [hipcc(), "-shared", "-fPIC", "--offload-arch=gfx950", *map(str, objs), "-o", str(tmp)]
     subprocess.run(cmd, check=True)
     os.replace(tmp, LIB)
+    _link_calls(calls)
     # the stand-alone example links against the library it was just built next to
     tmp_ex = EXAMPLE.with_suffix(f".tmp{os.getpid()}")
     subprocess.run([hipcc(), "-O2", "-std=c++17", f"-I{INCLUDE}", str(CSRC / "example_dgemm.cpp"), f"-L{PKG}", "-lozimmu",

@@ -656,49 +656,39 @@ def f8_scale_bytes(k: int) -> int:
     return f8_geometry(k)[1]
 
 
-_byte_types = _scale_types = None
+_native = None
 
 
-def _f8_types():
-    global _byte_types, _scale_types
-    if _torch is None:
-        _load_torch()
-    _byte_types = (_torch.uint8, _torch.float8_e4m3fn)
-    _scale_types = {_torch.uint8: E8M0, _torch.float8_e8m0fnu: E8M0, _torch.float32: F32}
-
-
-def _f8_matrix(what: str, codes, scales, n: int, k: int, block_rows: int):
-    """Checks codes and scales of an n x k matrix; (codes' row stride, scales' type, scales' row stride)."""
-    if _byte_types is None:
-        _f8_types()
-    row_bytes_, groups = (k + 127) // 128 * 128, (k + 127) // 128
-    rows, cols, ldq = _rows(codes)
-    if rows != n or cols < row_bytes_ or codes.dtype not in _byte_types:
-        raise ValueError(f"{what}: expected {n} rows of at least {row_bytes_} codes (uint8 or float8_e4m3fn)")
-    kind = _scale_types.get(scales.dtype)
-    srows, scols, lds = _rows(scales)
-    most = groups if kind == F32 else (groups + 3) // 4 * 4
-    if kind is None or srows != -(-n // block_rows) or scols < most:
-        raise ValueError(f"{what}' scales: expected {-(-n // block_rows)} rows of at least {most} (float8_e8m0fnu or uint8: multiples of four) or {groups} (float32)")
-    return (ldq if n > 1 else row_bytes_), kind, (lds if srows > 1 else most)
+def _calls():
+    """The module whose functions check tensors and call the library in one step (csrc/calls.cpp): a token's call waits for every microsecond spent
+    on the host."""
+    global _native
+    if _native is None:
+        lib()
+        if _torch is None:
+            _load_torch()
+        try:
+            from . import _calls as module
+        except ImportError as e:
+            raise RuntimeError(f"{Path(__file__).parent / '_calls.so'} is missing or was built for another torch: build it with "
+                               "`python -m paper_2306_11975_amd.build`") from e
+        _native = module
+    return _native
 
 
 def f8_split(W, codes, scales, block_rows: int = 128, stream=None) -> None:
     """W (n x k; float32, bfloat16 or float16) into codes (n x f8_row_bytes(k); uint8 or float8_e4m3fn) and scales (ceil(n / block_rows) x
     f8_scale_bytes(k); uint8 or float8_e8m0fnu), in blocks of block_rows (1: tokens, 128: weights) x 128."""
-    n, k, ldw = _rows(W)
-    _expect(block_rows in (1, 128), "block_rows: expected 1 or 128")
-    ldq, kind, lds = _f8_matrix("codes", codes, scales, n, k, block_rows)
-    _expect(kind == E8M0, "the cut makes scales of a byte (uint8 or float8_e8m0fnu)")
-    _call(lib().ozimmu_f8_split, stream, (W, codes, scales), n, k, block_rows, _type_of(W.dtype), W.data_ptr(), ldw, codes.data_ptr(), ldq, scales.data_ptr(), lds)
+    code = (_native or _calls()).f8_split(W, codes, scales, block_rows, stream)
+    if code:
+        _check(code)
 
 
 def f8_expand(codes, scales, W, block_rows: int = 128, stream=None) -> None:
     """The values that codes and scales stand for, into W (n x k; float32, bfloat16 or float16)."""
-    n, k, ldw = _rows(W)
-    _expect(block_rows in (1, 128), "block_rows: expected 1 or 128")
-    ldq, kind, lds = _f8_matrix("codes", codes, scales, n, k, block_rows)
-    _call(lib().ozimmu_f8_expand, stream, (W, codes, scales), n, k, block_rows, codes.data_ptr(), ldq, kind, scales.data_ptr(), lds, _type_of(W.dtype), W.data_ptr(), ldw)
+    code = (_native or _calls()).f8_expand(codes, scales, W, block_rows, stream)
+    if code:
+        _check(code)
 
 
 _F8_OPS = {"gemm": 0, "grad": 1, "weight_grad": 2}
@@ -707,11 +697,11 @@ _F8_OPS = {"gemm": 0, "grad": 1, "weight_grad": 2}
 def f8_workspace_bytes(op: str, t: int, n: int, k: int, dtype, rows=None, experts: int = 0) -> int:
     """Workspace of f8_gemm ("gemm"), f8_gemm_grad ("grad") or f8_weight_grad ("weight_grad"): t tokens, rows of Y and dY (experts; t without
     them), and the type of X and dY."""
-    if _byte_types is None:
-        _f8_types()
+    if _torch is None:
+        _load_torch()
     _expect(op in _F8_OPS, "op: expected gemm, grad or weight_grad")
     out = ctypes.c_size_t()
-    kind = E4M3 if dtype in _byte_types else _type_of(dtype)
+    kind = E4M3 if dtype in (_torch.uint8, _torch.float8_e4m3fn) else _type_of(dtype)
     _check(lib().ozimmu_f8_workspace_bytes(_F8_OPS[op], t, t if rows is None else rows, n, k, experts, kind, ctypes.byref(out)))
     return out.value
 
@@ -723,147 +713,55 @@ def alloc_f8_workspace(op: str, t: int, n: int, k: int, dtype, rows=None, expert
     return torch.empty(max(f8_workspace_bytes(op, t, n, k, dtype, rows, experts), WORKSPACE_ALIGN), dtype=torch.uint8, device=device)
 
 
-def _ints(t, count: int, what: str) -> int:
-    if t.dtype is not _torch.int32 or t.numel() != count or not t.is_contiguous():
-        raise ValueError(f"{what}: expected {count} contiguous int32 values")
-    return t.data_ptr()
-
-
-def _floats(t, count: int, what: str) -> int:
-    if t.dtype is not _torch.float32 or t.numel() != count or not t.is_contiguous():
-        raise ValueError(f"{what}: expected {count} contiguous float32 values")
-    return t.data_ptr()
-
-
-def _by_expert(t, offsets):
-    """A tensor of one more dimension over the experts, as the rows of all of them; (it, experts)."""
-    if offsets is None:
-        return t, 0
-    if t.dim() != 3 or (t.shape[0] > 1 and t.shape[1] > 0 and t.stride(0) != t.stride(1) * t.shape[1]) or (t.shape[2] > 1 and t.stride(2) != 1):
-        raise ValueError("over experts, weights, scales and weights' gradients have three dimensions, the experts' rows one behind the other")
-    rows = t.shape[0] * t.shape[1]
-    return t.as_strided((rows, t.shape[2]), (t.stride(1) if t.shape[1] > 1 else t.stride(0) if t.shape[0] > 1 else max(t.shape[2], 1), 1)), t.shape[0]
-
-
-def _f8_product(gradient, V, codes, scales, R, workspace, v_scales, offsets, source, stream):
-    # (Checked in one place, attributes read once: a token's call waits for every microsecond spent here.)
-    if _byte_types is None:
-        _f8_types()
-    t, inner, ldv = _rows(V)
-    rows, outer, ldr = _rows(R)
-    experts = 0
-    if offsets is not None:
-        codes, experts = _by_expert(codes, offsets)
-        scales, experts_s = _by_expert(scales, offsets)
-        if experts != experts_s:
-            raise ValueError("codes and scales must have the same number of experts")
-    qrows, cols, ldq = _rows(codes)
-    srows, scols, lds = _rows(scales)
-    each = experts or 1
-    vs, ldvs = None, 0
-    kind = _types.get(V.dtype)
-    if kind is None:
-        if V.dtype not in _byte_types:
-            _type_of(V.dtype)       # raises
-        _expect(v_scales is not None and v_scales.dtype is not _torch.float32, "codes of tokens need their scales, which are bytes")
-        kind = E4M3
-        # the width of codes is padded: the other sizes tell it
-        inner = qrows // each if gradient else min(inner, cols)
-        ldv, _, ldvs = _f8_matrix("tokens", V, v_scales, t, inner, 1)
-        vs = v_scales.data_ptr()
-    elif v_scales is not None:
-        raise ValueError("only codes have scales")
-    n, k = (inner, outer) if gradient else (outer, inner)
-    groups = (k + 127) // 128
-    if qrows != n * each or cols < 128 * groups or codes.dtype not in _byte_types:
-        raise ValueError(f"codes: expected {n} rows" + (" for each expert" if experts else "") + f" of at least {128 * groups} codes (uint8 or float8_e4m3fn)")
-    skind = _scale_types.get(scales.dtype)
-    most = groups if skind == F32 else (groups + 3) // 4 * 4
-    if skind is None or srows != (n + 127) // 128 * each or scols < most:
-        raise ValueError(f"scales: expected {(n + 127) // 128} rows" + (" for each expert" if experts else "") + f" of at least {most} (float8_e8m0fnu or uint8: multiples of four) or {groups} (float32)")
-    if rows != t and (gradient or source is None):
-        raise ValueError("tokens and result must have the same number of rows")
-    out = _types.get(R.dtype)
-    if out is None:
-        _type_of(R.dtype)           # raises
-    if qrows <= 1:
-        ldq = 128 * groups
-    if srows <= 1:
-        lds = most
-    ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), _size(workspace))
-    po = None if offsets is None else _ints(offsets, experts + 1, "offsets")
-    if gradient:
-        _call(lib().ozimmu_f8_gemm_grad, stream, (V, codes, scales, R, workspace, v_scales, offsets), rows, n, k, experts, kind, V.data_ptr(), ldv, vs, ldvs, codes.data_ptr(), ldq, skind,
-              scales.data_ptr(), lds, po, out, R.data_ptr(), ldr, ws, size)
-    else:
-        ps = None if source is None else _ints(source, rows, "source")
-        _call(lib().ozimmu_f8_gemm, stream, (V, codes, scales, R, workspace, v_scales, offsets, source), t, rows, n, k, experts, kind, V.data_ptr(), ldv, vs, ldvs, codes.data_ptr(), ldq, skind,
-              scales.data_ptr(), lds, po, ps, out, R.data_ptr(), ldr, ws, size)
-
-
 def f8_gemm(X, codes, scales, Y, workspace=None, x_scales=None, offsets=None, source=None, stream=None) -> None:
     """Y = X W^T for weights in 8-bit floating point (X: t x k, Y: rows x n, each float32, bfloat16 or float16). X is cut in the call, or given
     as codes with x_scales (f8_split with block_rows 1). Over experts: codes and scales with a first dimension of experts, offsets (experts + 1,
     int32): the rows of Y of each, and source (rows, int32): the row of X for each row of Y (without it X has the rows of Y)."""
-    _f8_product(False, X, codes, scales, Y, workspace, x_scales, offsets, source, stream)
+    code = (_native or _calls()).f8_gemm(X, codes, scales, Y, workspace, x_scales, offsets, source, stream)
+    if code:
+        _check(code)
 
 
 def f8_gemm_grad(dY, codes, scales, dX, workspace, dy_scales=None, offsets=None, stream=None) -> None:
     """dX = dY W for weights in 8-bit floating point (dY: rows x n, dX: rows x k): the gradient of f8_gemm's result, on its way to X. Over
     experts dX has the rows of dY: expert_combine without weights adds those of a token."""
-    _f8_product(True, dY, codes, scales, dX, workspace, dy_scales, offsets, None, stream)
+    code = (_native or _calls()).f8_gemm_grad(dY, codes, scales, dX, workspace, dy_scales, offsets, stream)
+    if code:
+        _check(code)
 
 
 def f8_weight_grad(dY, X, dW, workspace, offsets=None, source=None, stream=None) -> None:
     """dW = dY^T X in 8-bit floating point, cut along the tokens (dY: rows x n, X: t x k of one type, dW: n x k). Over experts: dW with a
     first dimension of experts, offsets and source as for f8_gemm."""
-    if _byte_types is None:
-        _f8_types()
-    rows, n, lddy = _rows(dY)
-    t, k, ldx = _rows(X)
-    flat, experts = _by_expert(dW, offsets)
-    wrows, cols, lddw = _rows(flat)
-    _expect(dY.dtype == X.dtype, "dY and X must have one type")
-    _expect(wrows == n * max(experts, 1) and cols == k, f"dW: expected {n} x {k}" + (" for each expert" if experts else ""))
-    if source is None:
-        _expect(rows == t, "dY and X must have the same number of rows")
-    po = None if offsets is None else _ints(offsets, experts + 1, "offsets")
-    ps = None if source is None else _ints(source, rows, "source")
-    _call(lib().ozimmu_f8_weight_grad, stream, (dY, X, dW, workspace, offsets, source), t, rows, n, k, experts, _type_of(X.dtype), dY.data_ptr(), lddy, X.data_ptr(), ldx, po, ps,
-          _type_of(dW.dtype), dW.data_ptr(), lddw, _ptr(workspace), _size(workspace))
+    code = (_native or _calls()).f8_weight_grad(dY, X, dW, workspace, offsets, source, stream)
+    if code:
+        _check(code)
 
 
 _SCORES = {"softmax": SOFTMAX, "sigmoid": SIGMOID}
 
 
-def _pairs(indices, what: str):
-    if indices.dim() != 2:
-        raise ValueError(f"{what}: expected a row for each token")
-    return indices.shape
+def _score(name: str) -> int:
+    score = _SCORES.get(name)
+    if score is None:
+        raise ValueError("score: expected softmax or sigmoid")
+    return score
 
 
 def route(logits, indices, weights, bias=None, score: str = "softmax", groups: int = 1, top_groups: int = 1, renormalize: bool = True, scale: float = 1.0,
           stream=None) -> None:
     """The best experts of each token and their weights (see ozimmu.h). logits: t x experts (float32, bfloat16 or float16); indices (int32)
     and weights (float32): t x top, contiguous; bias: experts, float32, for the choice alone."""
-    t, experts, ldl = _rows(logits)
-    rows, top = _pairs(indices, "indices")
-    _expect(rows == t and score in _SCORES, "logits and indices must have the same number of rows, and the score is softmax or sigmoid")
-    kind = _type_of(logits.dtype)
-    _call(lib().ozimmu_route, stream, (logits, indices, weights, bias), t, experts, top, kind, logits.data_ptr(), ldl, None if bias is None else _floats(bias, experts, "bias"),
-          _SCORES[score], groups, top_groups, int(bool(renormalize)), float(scale), _ints(indices, t * top, "indices"), _floats(weights, t * top, "weights"))
+    code = (_native or _calls()).route(logits, indices, weights, bias, _score(score), groups, top_groups, renormalize, scale, stream)
+    if code:
+        _check(code)
 
 
 def route_grad(logits, indices, dweights, dlogits, score: str = "softmax", renormalize: bool = True, scale: float = 1.0, stream=None) -> None:
     """The gradient of the logits (dlogits: their shape and type) from that of route's weights; the choice counts as constant."""
-    t, experts, ldl = _rows(logits)
-    rows, top = _pairs(indices, "indices")
-    drows, dcols, lddl = _rows(dlogits)
-    _expect(rows == t and score in _SCORES, "logits and indices must have the same number of rows, and the score is softmax or sigmoid")
-    _expect((drows, dcols) == (t, experts) and dlogits.dtype == logits.dtype, "dlogits must have the shape and type of the logits")
-    kind = _type_of(logits.dtype)
-    _call(lib().ozimmu_route_grad, stream, (logits, indices, dweights, dlogits), t, experts, top, kind, logits.data_ptr(), ldl, _ints(indices, t * top, "indices"),
-          _floats(dweights, t * top, "dweights"), _SCORES[score], int(bool(renormalize)), float(scale), dlogits.data_ptr(), lddl)
+    code = (_native or _calls()).route_grad(logits, indices, dweights, dlogits, _score(score), renormalize, scale, stream)
+    if code:
+        _check(code)
 
 
 def expert_order_workspace_bytes(t: int, top: int, experts: int) -> int:
@@ -882,37 +780,24 @@ def alloc_expert_order_workspace(t: int, top: int, experts: int, device="cuda"):
 def expert_order(indices, experts: int, offsets, source, place, workspace=None, stream=None) -> None:
     """The (token, choice) pairs of indices (t x top) sorted by expert: offsets (experts + 1), source (t top: the token of each row) and
     place (t x top: the row of each pair, -1 for an index that is no expert). All int32."""
-    if _torch is None:
-        _load_torch()
-    t, top = _pairs(indices, "indices")
-    _call(lib().ozimmu_expert_order, stream, (indices, offsets, source, place, workspace), t, top, experts, _ints(indices, t * top, "indices"), _ints(offsets, experts + 1, "offsets"),
-          _ints(source, t * top, "source"), _ints(place, t * top, "place"), _ptr(workspace), _size(workspace))
+    code = (_native or _calls()).expert_order(indices, experts, offsets, source, place, workspace, stream)
+    if code:
+        _check(code)
 
 
 def expert_combine(O, place, weights, Y, stream=None) -> None:
     """Y[i] = sum over j of weights[i, j] O[place[i, j]] (O: rows x n, Y: t x n of one type; place, weights: t x top; weights None: ones, which
     gives the gradient of taking rows by `source`)."""
-    if _torch is None:
-        _load_torch()
-    rows, n, ldo = _rows(O)
-    t, cols, ldy = _rows(Y)
-    prow, top = _pairs(place, "place")
-    _expect(prow == t and cols == n and O.dtype == Y.dtype, "O and Y must have one type and width, place and Y the same number of rows")
-    _call(lib().ozimmu_expert_combine, stream, (O, place, weights, Y), t, top, rows, n, _type_of(O.dtype), O.data_ptr(), ldo, _ints(place, t * top, "place"),
-          None if weights is None else _floats(weights, t * top, "weights"), Y.data_ptr(), ldy)
+    code = (_native or _calls()).expert_combine(O, place, weights, Y, stream)
+    if code:
+        _check(code)
 
 
 def expert_combine_grad(dY, O, place, weights, dO, dweights, stream=None) -> None:
     """The gradients of expert_combine: dO (rows x n; rows without a pair are left alone) and dweights (t x top, float32)."""
-    if _torch is None:
-        _load_torch()
-    t, n, lddy = _rows(dY)
-    rows, cols, ldo = _rows(O)
-    drows, dcols, lddo = _rows(dO)
-    prow, top = _pairs(place, "place")
-    _expect(prow == t and cols == n and (drows, dcols) == (rows, n) and O.dtype == dY.dtype == dO.dtype, "dY, O and dO must have one type and width, dO the rows of O, place those of dY")
-    _call(lib().ozimmu_expert_combine_grad, stream, (dY, O, place, weights, dO, dweights), t, top, rows, n, _type_of(O.dtype), dY.data_ptr(), lddy, O.data_ptr(), ldo,
-          _ints(place, t * top, "place"), _floats(weights, t * top, "weights"), dO.data_ptr(), lddo, _floats(dweights, t * top, "dweights"))
+    code = (_native or _calls()).expert_combine_grad(dY, O, place, weights, dO, dweights, stream)
+    if code:
+        _check(code)
 
 
 def probe_int8_mfma(pattern: int, shape: int = 0, iters: int = 200000):

@@ -172,3 +172,17 @@ def test_binding_refusals():
     for call in wrong:      # (the last kind: everything fits but the device)
         with pytest.raises(ValueError):
             call()
+
+
+def test_binding_takes_tensors_and_numbers():
+    """What is no tensor, no number or no such score is refused as such; a call's own module refuses another count of arguments."""
+    W, codes, scales, i32 = torch.empty(200, 300), torch.empty(200, 384, dtype=torch.uint8), torch.empty(2, 4, dtype=torch.uint8), dict(dtype=torch.int32)
+    l, i, w = torch.empty(5, 8), torch.empty(5, 2, **i32), torch.empty(5, 2)
+    for call in (lambda: oz.f8_split(None, codes, scales), lambda: oz.f8_split(W, codes, [1]), lambda: oz.f8_gemm(W, codes, scales, W, workspace=3), lambda: oz.f8_split(W, codes, scales, "a"),
+                 lambda: oz.route(l, i, w, groups=1.5), lambda: oz.route(l, i, w, scale="a"), lambda: oz.expert_order(i, None, i, i, i), lambda: oz._calls().route(l, i, w)):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: oz.route(l[0], i, w), lambda: oz.route(l, i[0], w), lambda: oz.route(l, i, w, score=None), lambda: oz.expert_combine(l, i, w, l.to("meta")), lambda: oz.f8_split(W[None], codes, scales),
+                 lambda: oz.f8_weight_grad(l, l, torch.empty(8, 8), torch.empty(8, 8).t())):
+        with pytest.raises(ValueError):
+            call()

@@ -412,3 +412,40 @@ def test_layer_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(held[a], want[a]) for a in names)
+
+
+def test_stream_as_an_argument():
+    """Each call on a stream that is handed over gives what it gives on the current one."""
+    t, experts, top, n, k = 300, 16, 3, 200, 260
+    g = gen(5)
+    logits, X = torch.randn(t, experts, generator=g).to(DEV), torch.randn(t, k, generator=g).to(BF16).to(DEV)
+    W, dw = torch.randn(experts, n, k, generator=g).to(DEV), torch.randn(t, top, generator=g).to(DEV)
+    dY = torch.randn(t * top, n, generator=g).to(BF16).to(DEV)
+
+    def run(stream):
+        with torch.cuda.stream(torch.cuda.Stream() if stream is None else torch.cuda.current_stream()):
+            new = lambda *shape, dt=torch.int32: torch.zeros(*shape, dtype=dt, device=DEV)
+            i, w, dl = new(t, top), new(t, top, dt=F32), new(t, experts, dt=F32)
+            offsets, source, place = new(experts + 1), new(t * top), new(t, top)
+            codes, scales = new(experts, n, oz.f8_row_bytes(k), dt=torch.uint8), new(experts, 2, oz.f8_scale_bytes(k), dt=torch.uint8)
+            back, Y, dX = new(n, k, dt=BF16), new(t * top, n, dt=BF16), new(t * top, k, dt=BF16)
+            dW, out, dO, dweights = new(experts, n, k, dt=F32), new(t, n, dt=BF16), new(t * top, n, dt=BF16), new(t, top, dt=F32)
+            ws = {op: oz.alloc_f8_workspace(op, t, n, k, BF16, rows=t * top, experts=experts) for op in ("gemm", "grad", "weight_grad")}
+            order = oz.alloc_expert_order_workspace(t, top, experts)
+            torch.cuda.synchronize()
+            oz.route(logits, i, w, stream=stream)
+            oz.route_grad(logits, i, dw, dl, stream=stream)
+            oz.expert_order(i, experts, offsets, source, place, order, stream=stream)
+            for e in range(experts):
+                oz.f8_split(W[e], codes[e], scales[e], stream=stream)
+            oz.f8_expand(codes[1], scales[1], back, stream=stream)
+            oz.f8_gemm(X, codes, scales, Y, ws["gemm"], offsets=offsets, source=source, stream=stream)
+            oz.f8_gemm_grad(dY, codes, scales, dX, ws["grad"], offsets=offsets, stream=stream)
+            oz.f8_weight_grad(dY, X, dW, ws["weight_grad"], offsets=offsets, source=source, stream=stream)
+            oz.expert_combine(Y, place, w, out, stream=stream)
+            oz.expert_combine_grad(out, Y, place, w, dO, dweights, stream=stream)
+            torch.cuda.synchronize()
+        return i, w, dl, offsets, source, place, codes, scales, back, Y, dX, dW, out, dO, dweights
+
+    for a, b in zip(run(None), run(torch.cuda.Stream())):
+        assert torch.equal(a, b) and a.any()
