@@ -145,14 +145,13 @@ __device__ __forceinline__ void scale_parts(const void* scales, int64_t at, floa
 
 // ---- rows sorted by expert
 
-__device__ __forceinline__ int wave_scan(int x) {   // inclusive sum over the lanes before and this one
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(x, d);
-        x += lane >= d ? y : 0;
-    }
-    return x;
+__device__ __forceinline__ int wave_scan(int x) {   // inclusive sum over the lanes before and this one: within rows of sixteen, then the rows' last
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);
+    return x + __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
 }
 // The experts' rows, whatever the offsets hold: an offset is taken as at least the largest before it and within [0, rows], so that no two
 // experts share rows. Units are of `unit` rows, counted in multiples of `to` for each expert. Every lane of a wavefront calls these with the same

@@ -41,6 +41,17 @@ __device__ __forceinline__ float sum_read(float a) {
     asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(a));
     return v;
 }
+// Two values rounded to 16 bits, as a word.
+template <int TYPE>
+__device__ __forceinline__ unsigned two_as(float x, float y) {
+    typedef float v2f __attribute__((ext_vector_type(2)));
+    typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+    typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+    if constexpr (TYPE == OZIMMU_BF16)
+        return __builtin_bit_cast(unsigned, __builtin_convertvector(v2f{x, y}, v2b));
+    else
+        return __builtin_bit_cast(unsigned, __builtin_convertvector(v2f{x, y}, v2h));
+}
 // One word to a lane, as dma_load16.
 __device__ __forceinline__ void dma_load4(const void* gbase, unsigned voff, unsigned lds_addr) {
     asm volatile(
@@ -54,7 +65,9 @@ __device__ __forceinline__ void dma_load4(const void* gbase, unsigned voff, unsi
 
 constexpr int kLargeTile = 256;
 constexpr int kFree = 3, kLanded = 16;   // slots of a slab's 32 MFMAs (see below; 2 to 6 and 16 to 23 were within 4 %)
-constexpr unsigned kLargeStage = 2 * kLargeTile * 128, kLargeScales = 2 * kLargeStage, kLargeBytes = kLargeScales + 2 * 2 * kLargeTile * 4;
+constexpr unsigned kLargeStage = 2 * kLargeTile * 128, kLargeScales = 2 * kLargeStage, kLargeTurn = kLargeScales + 2 * 2 * kLargeTile * 4;
+// Each wavefront's 32 x 64 results on their way to memory; rows of 128 bytes, 16 apart, meet no bank twice.
+constexpr unsigned kTurnPitch = 144, kLargeBytes = kLargeTurn + 4 * 32 * kTurnPitch;
 
 template <bool Q_ROWS, int TYPE>
 __launch_bounds__(256)
@@ -188,6 +201,11 @@ __global__ void f8_large_kernel(F8Args a, F8Plan plan) {
         mfma_results_ready();
         // the next tile's first slabs come while this one's results go: behind the barrier nobody reads LDS, and nothing is on its way to it
         const F8Tile done = t;
+        unsigned no_source = 0;   // bit i: row 32 i + lane % 32 of this wavefront's has none (read before other loads and stores are on their way)
+        if (a.source && !a.along_rows)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                no_source |= (unsigned)a.source[done.first + min(done.row0 + wm * 128 + 32 * i + (lane & 31), done.count - 1)] >= (unsigned)a.t ? 1u << i : 0u;
         at_item += gridDim.x >> 3;
         const bool more = at_item < mine;
         if (more) {
@@ -196,7 +214,7 @@ __global__ void f8_large_kernel(F8Args a, F8Plan plan) {
             first_loads();
         }
 
-        // ---- results: lane holds R[row][col + 8 g + 4 (lane / 32) .. + 3], g = 0 .. 3
+        // ---- results: lane holds R[row][col + 8 g + 4 (lane / 32) .. + 3], g = 0 .. 3, of row lane % 32
         if (done.shared >= 0) {
             v4f* to = reinterpret_cast<v4f*>(a.partial) + (int64_t)done.shared * (B * B / 4) + threadIdx.x;
 #pragma unroll
@@ -209,44 +227,70 @@ __global__ void f8_large_kernel(F8Args a, F8Plan plan) {
                         __builtin_amdgcn_sched_barrier(0);
                     }
         } else {
+            // 32 x 64 at a time by way of LDS, so that stores are of whole lines; while a piece is read back the next is rounded.
+            unsigned char* const turn = lds + kLargeTurn + wave * (32 * kTurnPitch);
+            const int row0 = done.row0 + wm * 128, col0 = done.col0 + wn * 128;
+            const bool whole = row0 + 128 <= done.count && col0 + 128 <= a.n;
+            raw* const out = static_cast<raw*>(a.out) + ((a.along_rows ? (int64_t)done.expert * a.rows : (int64_t)done.first) + row0) * a.ldo + col0;
+            const unsigned lane_out = (unsigned)(lane >> 3) * (unsigned)a.ldo * sizeof(raw) + (lane & 7) * 16;
+            v4u piece[4], y[4];
+            auto round = [&](auto number) {
+                constexpr int i = decltype(number)::value / 2, half = decltype(number)::value % 2;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = done.row0 + wm * 128 + 32 * i + (lane & 31);
-                bool there = r < done.count;
-                if (a.source && !a.along_rows) there = there && (unsigned)a.source[done.first + min(r, done.count - 1)] < (unsigned)a.t;
-                const int64_t row = a.along_rows ? (int64_t)done.expert * a.rows + r : (int64_t)done.first + r;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < 2; ++j)
 #pragma unroll
                     for (int g = 0; g < 4; g += 2) {   // the halves of the wavefront exchange: eight columns to a lane
                         unsigned x[2][2];
 #pragma unroll
                         for (int f = 0; f < 2; ++f)
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const float v0 = sum_read(acc[i][j][4 * (g + f) + 2 * e]), v1 = sum_read(acc[i][j][4 * (g + f) + 2 * e + 1]);
-                                x[f][e] = there ? (unsigned)Elem<TYPE>::store(v0) | (unsigned)Elem<TYPE>::store(v1) << 16 : 0u;
-                            }
-                        v4u y;
+                            for (int e = 0; e < 2; ++e) x[f][e] = two_as<TYPE>(sum_read(acc[i][2 * half + j][4 * (g + f) + 2 * e]), sum_read(acc[i][2 * half + j][4 * (g + f) + 2 * e + 1]));
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             const auto z = __builtin_amdgcn_permlane32_swap(x[0][e], x[1][e], false, false);
-                            y[e] = z[0];
-                            y[2 + e] = z[1];
+                            piece[2 * j + g / 2][e] = z[0];
+                            piece[2 * j + g / 2][2 + e] = z[1];
                         }
-                        const int c = done.col0 + wn * 128 + 32 * j + 8 * (g + (lane >> 5));
-                        raw* out = static_cast<raw*>(a.out) + row * a.ldo + c;
-                        if (r < done.count && c + 8 <= a.n) {
-                            *reinterpret_cast<v4u_any*>(out) = y;
-                        } else if (r < done.count) {
+                    }
+                if (no_source >> i & 1)
 #pragma unroll
+                    for (int x = 0; x < 4; ++x) piece[x] = v4u{0, 0, 0, 0};
+            };
+            auto by_lds = [&]() {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) *reinterpret_cast<v4u*>(turn + (lane & 31) * kTurnPitch + (2 * x + (lane >> 5)) * 16) = piece[x];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) y[q] = *reinterpret_cast<const v4u*>(turn + (q * 8 + (lane >> 3)) * kTurnPitch + (lane & 7) * 16);
+            };
+            auto store = [&](auto number) {   // eight rows at a time
+                constexpr int i = decltype(number)::value / 2, half = decltype(number)::value % 2;
+                if (whole) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        *reinterpret_cast<v4u_any*>(reinterpret_cast<unsigned char*>(out + (int64_t)(32 * i + 8 * q) * a.ldo + 64 * half) + lane_out) = y[q];
+                } else {
+#pragma unroll 1
+                    for (int q = 0; q < 4; ++q) {
+                        const int r = 32 * i + q * 8 + (lane >> 3), c = 64 * half + (lane & 7) * 8;
+                        const raw* from = reinterpret_cast<const raw*>(turn + (q * 8 + (lane >> 3)) * kTurnPitch + (lane & 7) * 16);
+                        if (row0 + r >= done.count) continue;
+                        if (col0 + c + 8 <= a.n)
+                            *reinterpret_cast<v4u_any*>(out + (int64_t)r * a.ldo + c) = *reinterpret_cast<const v4u*>(from);
+                        else
+#pragma unroll 1
                             for (int e = 0; e < 8; ++e)
-                                if (c + e < a.n) out[e] = (raw)(y[e >> 1] >> (e & 1) * 16);
-                        }
-                        __builtin_amdgcn_sched_barrier(0);   // (all sums at once would take as many ordinary registers)
+                                if (col0 + c + e < a.n) out[(int64_t)r * a.ldo + c + e] = from[e];
                     }
                 }
-            }
+            };
+            static_for<0, 8>([&](auto number) {
+                round(number);
+                __builtin_amdgcn_sched_barrier(0);   // (all sums at once would take as many ordinary registers)
+                if constexpr (decltype(number)::value > 0) store(std::integral_constant<int, decltype(number)::value - 1>{});
+                by_lds();
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            store(std::integral_constant<int, 7>{});
         }
         if (!more) return;
     }
