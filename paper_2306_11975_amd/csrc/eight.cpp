@@ -40,14 +40,15 @@ bool ws_ok(const void* ws, size_t bytes, size_t needed) { return needed == 0 || 
 
 enum { kGemm = 0, kGemmGrad = 1, kWeightGrad = 2 };
 
-// Few rows: straight from memory, 16 rows of tokens at a time, without a cut of its own (f8_few.hip). Cut and tiles take two launches, about
-// 2.3 us more, but stream the weights through LDS by whole lines and read the tokens once for every 64 columns: us (16-bit results) few rows, tiles:
-// 2048 x 2048 1 token 4.4, 8.7, 32 5.2, 8.9, 128 11.0, 10.4; 8192 x 4096 1 token 9.5, 13.2, 16 12.4, 13.4, 32 19.6, 13.6; 16384 x 8192 1 token
-// 27, 26; 64 experts of 2048 x 2048 with 128 rows 59, 44; 8 of 1000 x 640 with 64 rows 4.8, 7.5. The limit is where they meet, in weights read. (The
-// answer turns once as rows grow, so that a workspace serves fewer.)
+// Few rows: straight from memory, 16 rows of tokens at a time, without a cut of its own (f8_few.hip). Cut and tiles take two launches, but stream the
+// weights through LDS by whole lines and read the tokens once for every 64 columns. us, few rows against tiles, tokens and results of bf16:
+// 2048 x 2048 1 row 5.6, 9.4, 64 rows 9.7, 11.2, 128 19, 14; 4096 x 4096 16 rows 9.9, 13.3, 32 15.5, 13.2; 8192 x 4096 1 row 12.9, 13.5, 16 rows
+// 15.5, 14.5; 16 experts of 2048 x 1024 8 rows 8.6, 10.0, 64 rows 15.0, 11.8. 32 bits: 2048 x 2048 32 rows 8.6, 10.8, 64 13.1, 11.4; 8192 x 4096
+// 1 row 13.2, 14.8, 8 rows 17.1, 15.4. Given codes: 2048 x 2048 32 rows 5.6, 7.0, 64 7.8, 7.6. The limit is where they meet, in weights read; up to
+// four rows the tokens of a run cost little. (The answer turns once as rows grow, so that a workspace serves fewer.)
 bool few_rows(int64_t rows, int64_t n, int64_t k, int64_t experts) {
-    const int64_t tiles = experts ? rows / 16 + std::min(experts, rows) : (rows + 15) / 16;
-    return (double)tiles * (double)n * (double)k <= 33554432.0;
+    const double runs = experts ? (double)(rows / 16 + std::min(experts, rows)) : rows <= 4 ? 0.5 : (double)((rows + 15) / 16);
+    return runs * (double)n * (double)k <= 16777216.0;
 }
 
 // What a call keeps in its workspace: the cut rows (P), for gradients the transposed weights or the cut columns of X (Q).

@@ -13,8 +13,8 @@
 // 29 MFMAs after the last of them, 45 after the first. (All loads at once were 7 % slower: they stand in each other's way. Waiting at the slab's end
 // with one barrier: 4 %.) Past the end the last slab is fetched again, so that all waits are alike. Scales come by direct loads too, a word (four
 // slabs) to a row; the loop takes four slabs a round, and the instruction picks the byte. Workgroups stay for as many tiles as there are to each
-// compute unit: the next tile's first slabs come while this one's results go. 4096 x 8192 x 4096: 111 us, 2.47 PFLOP/s (a library product of 8-bit
-// matrices, without blocks' scales: 110); tile by tile with stores of 8 bytes 130; 128 x 128 tiles 150.
+// compute unit: the next tile's first slabs come while this one's results go. 4096 x 8192 x 4096: 106 us, 2.6 PFLOP/s (a library product of 8-bit
+// matrices, without blocks' scales: 110); tile by tile with stores of 8 bytes 130, of 32-byte pieces 111; 128 x 128 tiles 145.
 #pragma once
 
 #include "f8_product.h"
