@@ -461,8 +461,8 @@ ozimmu_status_t ozimmu_orthogonalize(int64_t batch, int64_t m, int64_t n, ozimmu
  * goes with row source[r] of X; one outside [0, t) stands for a row of zeros. dW: experts x n x k (lddw between all rows), zeros for an expert
  * without rows; its runs of 128 tokens begin with the expert's first row.
  *
- * Errors of the sums: results of 32 bits, and all results of calls with few rows (r n k <= 2^24, r the runs of 16 rows, one half for up to
- * four rows; over experts floor(rows / 16) and one more for each expert that can have rows; not the weights' gradient), are sums of exact
+ * Errors of the sums: results of 32 bits, and all results of calls with few rows (r n k <= 2^24, r the runs of 16 rows, one half where
+ * there is one; over experts floor(rows / 16) and one more for each expert that can have rows; not the weights' gradient), are sums of exact
  * products in 32 bits. 16-bit results of more rows, and of weights' gradients, come from matrix cores that drop, within eight products, what
  * is below 2^-13 of the largest of them: at most 2^-12 of the sum of their magnitudes, 2^-16 where terms are alike. So a row's last bits may
  * differ with the number of rows beside it. A NaN gives NaN in the results that it goes into and no others.

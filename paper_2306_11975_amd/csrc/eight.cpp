@@ -42,12 +42,12 @@ enum { kGemm = 0, kGemmGrad = 1, kWeightGrad = 2 };
 
 // Few rows: straight from memory, 16 rows of tokens at a time, without a cut of its own (f8_few.hip). Cut and tiles take two launches, but stream the
 // weights through LDS by whole lines and read the tokens once for every 64 columns. us, few rows against tiles, tokens and results of bf16:
-// 2048 x 2048 1 row 5.6, 9.4, 64 rows 9.7, 11.2, 128 19, 14; 4096 x 4096 16 rows 9.9, 13.3, 32 15.5, 13.2; 8192 x 4096 1 row 12.9, 13.5, 16 rows
-// 15.5, 14.5; 16 experts of 2048 x 1024 8 rows 8.6, 10.0, 64 rows 15.0, 11.8. 32 bits: 2048 x 2048 32 rows 8.6, 10.8, 64 13.1, 11.4; 8192 x 4096
-// 1 row 13.2, 14.8, 8 rows 17.1, 15.4. Given codes: 2048 x 2048 32 rows 5.6, 7.0, 64 7.8, 7.6. The limit is where they meet, in weights read; up to
-// four rows the tokens of a run cost little. (The answer turns once as rows grow, so that a workspace serves fewer.)
+// 2048 x 2048 1 row 5.6, 9.5, 64 rows 8.5, 11.2, 128 13.6, 13.6; 4096 x 4096 16 rows 9.8, 13.3, 32 12.6, 13.4, 64 22, 15; 8192 x 4096 1 row 10.4,
+// 13.6, 16 rows 12.6, 14.6, 32 22, 15; 16 experts of 2048 x 1024 8 rows 7.4, 10.2, 64 rows 12.5, 11.4. 32 bits: 2048 x 2048 64 rows 10.0, 11.4, 128 17,
+// 13; 8192 x 4096 16 rows 15.9, 15.6; 2048 x 8192 1 row 11.7, 13.3, 16 rows 21, 14. Given codes: 2048 x 2048 64 rows 7.1, 7.6; 8192 x 4096 16
+// rows 11.0, 11.3. The limit is where they meet, in weights read. (The answer turns once as rows grow, so that a workspace serves fewer.)
 bool few_rows(int64_t rows, int64_t n, int64_t k, int64_t experts) {
-    const double runs = experts ? (double)(rows / 16 + std::min(experts, rows)) : rows <= 4 ? 0.5 : (double)((rows + 15) / 16);
+    const double runs = experts ? (double)(rows / 16 + std::min(experts, rows)) : rows <= 16 ? 0.5 : (double)((rows + 15) / 16);
     return runs * (double)n * (double)k <= 16777216.0;
 }
 
@@ -72,7 +72,7 @@ Layout layout(int op, int64_t t, int64_t rows, int64_t n, int64_t k, int64_t exp
         const int64_t inner = op == kGemm ? k : n;
         o.ldp = f8_row_bytes(inner);
         o.ldsp = f8_scale_bytes(inner);
-        if (type != OZIMMU_E4M3 && !few_rows(rows, n, k, experts)) {
+        if (type != OZIMMU_E4M3 && (op == kGemmGrad || !few_rows(rows, n, k, experts))) {
             o.off_p = take((op == kGemm ? t : rows) * o.ldp);
             o.off_sp = take((op == kGemm ? t : rows) * o.ldsp);
         }
@@ -159,7 +159,7 @@ ozimmu_status_t f8_product(int op, int64_t t, int64_t rows, int64_t n, int64_t k
         a.ldp = ldv;
         a.sp = v_scales;
         a.ldsp = ldvs;
-    } else if (!few) {
+    } else if (op == kGemmGrad || !few) {      // (gradients: the cut goes with the turn of the weights)
         a.P = base + o.off_p;
         a.ldp = o.ldp;
         a.sp = base + o.off_sp;
@@ -176,7 +176,12 @@ ozimmu_status_t f8_product(int op, int64_t t, int64_t rows, int64_t n, int64_t k
         a.ldq = o.ldq;
         a.sq = base + o.off_sq;
         a.ldsq = o.ldsq;
-        const bool cut = type != OZIMMU_E4M3 && !few;
+        const bool cut = type != OZIMMU_E4M3;
+        if (cut) {
+            a.V = a.P;
+            a.v_type = OZIMMU_E4M3;
+            a.ldv = a.ldp;
+        }
         e = launch_f8_gradient_operands(std::max<int64_t>(experts, 1), n, k, codes, ldq, scale_type, scales, lds, base + o.off_q, base + o.off_sq, rows, V, type, ldv,
                                         cut ? base + o.off_p : nullptr, base + o.off_sp, st);
     }

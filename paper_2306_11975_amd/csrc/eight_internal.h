@@ -36,7 +36,7 @@ hipError_t launch_f8_cut_tokens(int64_t rows, int64_t experts, const int* offset
 
 // R = P Q^T for codes under scales. P: rows (tokens), Q: rows (outputs), both along the inner dimension in slabs of 128 bytes.
 struct F8Args {
-    const void* V;            // launch_f8_few: the rows as they came (v_type, ldv values apart, k of them; OZIMMU_E4M3: codes, with sp)
+    const void* V;            // launch_f8_few: the rows (v_type, ldv values apart, k of them: cut on the way; OZIMMU_E4M3: codes, with sp)
     int v_type;
     int64_t ldv, k;
     const uint8_t* P;         // the others: their codes
