@@ -85,7 +85,9 @@ __global__ void f8_large_kernel(F8Args a, F8Plan plan) {
     int slabs;
     const uint8_t *P, *Q, *SP, *SQ;
     unsigned voff_p[8], voff_q[8], voff_sp, voff_sq;
+    // (the lane number is formed anew outside the walk: what comes of it has no registers to wait in, and reloads would wait for loads and stores)
     auto take = [&](int item) {   // a tile's operands
+        const int lane = lane_here();
         t = f8_tile<B, B>(a, plan, items, item);
         slabs = t.slabs;
         const int64_t p_row = a.along_rows ? t.row0 : a.source ? 0 : (int64_t)t.first + t.row0;
@@ -201,6 +203,7 @@ __global__ void f8_large_kernel(F8Args a, F8Plan plan) {
         mfma_results_ready();
         // the next tile's first slabs come while this one's results go: behind the barrier nobody reads LDS, and nothing is on its way to it
         const F8Tile done = t;
+        const int lane = lane_here();
         unsigned no_source = 0;   // bit i: row 32 i + lane % 32 of this wavefront's has none (read before other loads and stores are on their way)
         if (a.source && !a.along_rows)
 #pragma unroll
@@ -215,83 +218,70 @@ __global__ void f8_large_kernel(F8Args a, F8Plan plan) {
         }
 
         // ---- results: lane holds R[row][col + 8 g + 4 (lane / 32) .. + 3], g = 0 .. 3, of row lane % 32
-        if (done.shared >= 0) {
-            v4f* to = reinterpret_cast<v4f*>(a.partial) + (int64_t)done.shared * (B * B / 4) + threadIdx.x;
+        // 32 x 64 at a time by way of LDS, so that stores are of whole lines; while a piece is read back the next is rounded.
+        unsigned char* const turn = lds + kLargeTurn + wave * (32 * kTurnPitch);
+        const int row0 = done.row0 + wm * 128, col0 = done.col0 + wn * 128;
+        const bool whole = row0 + 128 <= done.count && col0 + 128 <= a.n;
+        raw* const out = static_cast<raw*>(a.out) + ((a.along_rows ? (int64_t)done.expert * a.rows : (int64_t)done.first) + row0) * a.ldo + col0;
+        const unsigned lane_out = (unsigned)(lane >> 3) * (unsigned)a.ldo * sizeof(raw) + (lane & 7) * 16;
+        v4u piece[4], y[4];
+        auto round = [&](auto number) {
+            constexpr int i = decltype(number)::value / 2, half = decltype(number)::value % 2;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+                for (int g = 0; g < 4; g += 2) {   // the halves of the wavefront exchange: eight columns to a lane
+                    unsigned x[2][2];
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        to[((i * 4 + j) * 4 + g) * 256] = v4f{sum_read(acc[i][j][4 * g]), sum_read(acc[i][j][4 * g + 1]), sum_read(acc[i][j][4 * g + 2]), sum_read(acc[i][j][4 * g + 3])};
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-        } else {
-            // 32 x 64 at a time by way of LDS, so that stores are of whole lines; while a piece is read back the next is rounded.
-            unsigned char* const turn = lds + kLargeTurn + wave * (32 * kTurnPitch);
-            const int row0 = done.row0 + wm * 128, col0 = done.col0 + wn * 128;
-            const bool whole = row0 + 128 <= done.count && col0 + 128 <= a.n;
-            raw* const out = static_cast<raw*>(a.out) + ((a.along_rows ? (int64_t)done.expert * a.rows : (int64_t)done.first) + row0) * a.ldo + col0;
-            const unsigned lane_out = (unsigned)(lane >> 3) * (unsigned)a.ldo * sizeof(raw) + (lane & 7) * 16;
-            v4u piece[4], y[4];
-            auto round = [&](auto number) {
-                constexpr int i = decltype(number)::value / 2, half = decltype(number)::value % 2;
+                    for (int f = 0; f < 2; ++f)
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                        for (int e = 0; e < 2; ++e) x[f][e] = two_as<TYPE>(sum_read(acc[i][2 * half + j][4 * (g + f) + 2 * e]), sum_read(acc[i][2 * half + j][4 * (g + f) + 2 * e + 1]));
 #pragma unroll
-                    for (int g = 0; g < 4; g += 2) {   // the halves of the wavefront exchange: eight columns to a lane
-                        unsigned x[2][2];
-#pragma unroll
-                        for (int f = 0; f < 2; ++f)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) x[f][e] = two_as<TYPE>(sum_read(acc[i][2 * half + j][4 * (g + f) + 2 * e]), sum_read(acc[i][2 * half + j][4 * (g + f) + 2 * e + 1]));
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const auto z = __builtin_amdgcn_permlane32_swap(x[0][e], x[1][e], false, false);
-                            piece[2 * j + g / 2][e] = z[0];
-                            piece[2 * j + g / 2][2 + e] = z[1];
-                        }
-                    }
-                if (no_source >> i & 1)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) piece[x] = v4u{0, 0, 0, 0};
-            };
-            auto by_lds = [&]() {
-#pragma unroll
-                for (int x = 0; x < 4; ++x) *reinterpret_cast<v4u*>(turn + (lane & 31) * kTurnPitch + (2 * x + (lane >> 5)) * 16) = piece[x];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) y[q] = *reinterpret_cast<const v4u*>(turn + (q * 8 + (lane >> 3)) * kTurnPitch + (lane & 7) * 16);
-            };
-            auto store = [&](auto number) {   // eight rows at a time
-                constexpr int i = decltype(number)::value / 2, half = decltype(number)::value % 2;
-                if (whole) {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        *reinterpret_cast<v4u_any*>(reinterpret_cast<unsigned char*>(out + (int64_t)(32 * i + 8 * q) * a.ldo + 64 * half) + lane_out) = y[q];
-                } else {
-#pragma unroll 1
-                    for (int q = 0; q < 4; ++q) {
-                        const int r = 32 * i + q * 8 + (lane >> 3), c = 64 * half + (lane & 7) * 8;
-                        const raw* from = reinterpret_cast<const raw*>(turn + (q * 8 + (lane >> 3)) * kTurnPitch + (lane & 7) * 16);
-                        if (row0 + r >= done.count) continue;
-                        if (col0 + c + 8 <= a.n)
-                            *reinterpret_cast<v4u_any*>(out + (int64_t)r * a.ldo + c) = *reinterpret_cast<const v4u*>(from);
-                        else
-#pragma unroll 1
-                            for (int e = 0; e < 8; ++e)
-                                if (col0 + c + e < a.n) out[(int64_t)r * a.ldo + c + e] = from[e];
+                    for (int e = 0; e < 2; ++e) {
+                        const auto z = __builtin_amdgcn_permlane32_swap(x[0][e], x[1][e], false, false);
+                        piece[2 * j + g / 2][e] = z[0];
+                        piece[2 * j + g / 2][2 + e] = z[1];
                     }
                 }
-            };
-            static_for<0, 8>([&](auto number) {
-                round(number);
-                __builtin_amdgcn_sched_barrier(0);   // (all sums at once would take as many ordinary registers)
-                if constexpr (decltype(number)::value > 0) store(std::integral_constant<int, decltype(number)::value - 1>{});
-                by_lds();
-                __builtin_amdgcn_sched_barrier(0);
-            });
-            store(std::integral_constant<int, 7>{});
-        }
+            if (no_source >> i & 1)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) piece[x] = v4u{0, 0, 0, 0};
+        };
+        auto by_lds = [&]() {
+#pragma unroll
+            for (int x = 0; x < 4; ++x) *reinterpret_cast<v4u*>(turn + (lane & 31) * kTurnPitch + (2 * x + (lane >> 5)) * 16) = piece[x];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) y[q] = *reinterpret_cast<const v4u*>(turn + (q * 8 + (lane >> 3)) * kTurnPitch + (lane & 7) * 16);
+        };
+        auto store = [&](auto number) {   // eight rows at a time
+            constexpr int i = decltype(number)::value / 2, half = decltype(number)::value % 2;
+            if (whole) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *reinterpret_cast<v4u_any*>(reinterpret_cast<unsigned char*>(out + (int64_t)(32 * i + 8 * q) * a.ldo + 64 * half) + lane_out) = y[q];
+            } else {
+#pragma unroll 1
+                for (int q = 0; q < 4; ++q) {
+                    const int r = 32 * i + q * 8 + (lane >> 3), c = 64 * half + (lane & 7) * 8;
+                    const raw* from = reinterpret_cast<const raw*>(turn + (q * 8 + (lane >> 3)) * kTurnPitch + (lane & 7) * 16);
+                    if (row0 + r >= done.count) continue;
+                    if (col0 + c + 8 <= a.n)
+                        *reinterpret_cast<v4u_any*>(out + (int64_t)r * a.ldo + c) = *reinterpret_cast<const v4u*>(from);
+                    else
+#pragma unroll 1
+                        for (int e = 0; e < 8; ++e)
+                            if (col0 + c + e < a.n) out[(int64_t)r * a.ldo + c + e] = from[e];
+                }
+            }
+        };
+        static_for<0, 8>([&](auto number) {
+            round(number);
+            __builtin_amdgcn_sched_barrier(0);   // (all sums at once would take as many ordinary registers)
+            if constexpr (decltype(number)::value > 0) store(std::integral_constant<int, decltype(number)::value - 1>{});
+            by_lds();
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        store(std::integral_constant<int, 7>{});
         if (!more) return;
     }
 }
