@@ -216,12 +216,13 @@ template <int TYPE>
 __device__ __forceinline__ void store_four_as(const F8Args& a, int64_t row, int col, const v4f& v, bool there) {
     typedef typename Elem<TYPE>::raw raw;
     typedef raw raw4 __attribute__((ext_vector_type(4)));
+    typedef raw4 raw4_any __attribute__((aligned(sizeof(raw))));
     raw* at = static_cast<raw*>(a.out) + row * a.ldo + col;
     raw4 x;
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] = Elem<TYPE>::store(there ? v[e] : 0.f);
-    if ((reinterpret_cast<uintptr_t>(at) & (sizeof(raw4) - 1)) == 0 && col + 4 <= a.n)
-        *reinterpret_cast<raw4*>(at) = x;
+    if (col + 4 <= a.n)
+        *reinterpret_cast<raw4_any*>(at) = x;
     else
 #pragma unroll
         for (int e = 0; e < 4; ++e)
