@@ -211,6 +211,18 @@ __device__ __forceinline__ bool find_unit(const int* offsets, int experts, int r
     return found;
 }
 
+// Two values rounded to 16 bits, as a word.
+template <int TYPE>
+__device__ __forceinline__ unsigned two_as(float x, float y) {
+    typedef float v2f __attribute__((ext_vector_type(2)));
+    typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+    typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+    if constexpr (TYPE == OZIMMU_BF16)
+        return __builtin_bit_cast(unsigned, __builtin_convertvector(v2f{x, y}, v2b));
+    else
+        return __builtin_bit_cast(unsigned, __builtin_convertvector(v2f{x, y}, v2h));
+}
+
 // R[row][col .. col + 3], rounded once to the result's type; zeros where the row has no source.
 template <int TYPE>
 __device__ __forceinline__ void store_four_as(const F8Args& a, int64_t row, int col, const v4f& v, bool there) {

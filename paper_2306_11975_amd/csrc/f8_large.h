@@ -41,17 +41,6 @@ __device__ __forceinline__ float sum_read(float a) {
     asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(a));
     return v;
 }
-// Two values rounded to 16 bits, as a word.
-template <int TYPE>
-__device__ __forceinline__ unsigned two_as(float x, float y) {
-    typedef float v2f __attribute__((ext_vector_type(2)));
-    typedef __bf16 v2b __attribute__((ext_vector_type(2)));
-    typedef _Float16 v2h __attribute__((ext_vector_type(2)));
-    if constexpr (TYPE == OZIMMU_BF16)
-        return __builtin_bit_cast(unsigned, __builtin_convertvector(v2f{x, y}, v2b));
-    else
-        return __builtin_bit_cast(unsigned, __builtin_convertvector(v2f{x, y}, v2h));
-}
 // One word to a lane, as dma_load16.
 __device__ __forceinline__ void dma_load4(const void* gbase, unsigned voff, unsigned lds_addr) {
     asm volatile(
