@@ -5,7 +5,11 @@
 // r lies at place c ^ (r % 8)); a lane's fragment of a slab is pieces lane / 16 and lane / 16 + 4 of row lane % 16, of either operand alike, so
 // that positions meet. Two ways of multiplying:
 //   16-bit results: v_mfma_scale_f32_16x16x128_f8f6f4, which takes a power-of-two scale for every row and 32 positions: a slab is one
-//     instruction and its scales cost nothing. Within eight products it drops what is below 2^-13 of the largest of them; the sums are 32-bit.
+//     instruction and its scales cost nothing. It cuts each product toward zero to a multiple of 2^(E - 13), E the largest sum of two codes' exponents
+//     among eight neighbouring products (those of zeros apart; subnormal codes count with -6), and adds the eights up in 32 bits: measured, on every
+//     one of 2 10^5 random eights. For normally distributed values that is 2^-19 of the sum of magnitudes, 2^-10.2 of it at worst, 2^-7.2 beside
+//     subnormal codes. It is taken for 16-bit results alone, of values whose own rounding to codes lost up to 2^-4 of each, for two and a half times
+//     the speed; 32-bit results are the way to exact products.
 //   32-bit results (EXACT): the codes become fp16, which holds each of them, four MFMAs a slab, at half the rate; a slab's sum is scaled and
 //     added to the tile's on the vector units.
 // Scales of the weights in 32 bits (WIDE): their exponents go the way of the bytes, their significands are multiplied on the vector units.
