@@ -503,7 +503,8 @@ ozimmu_status_t ozimmu_f8_weight_grad(int64_t t, int64_t rows, int64_t n, int64_
  * The choice of experts. For each token, from its logits l (t x experts, row-major, ldl values between rows):
  *     s = softmax(l) or 1 / (1 + exp(-l)),   choice values v = s + bias   (bias: `experts` 32-bit values, or null);
  * the experts form `groups` runs of equal length, a group's value is the sum of its two largest choice values (of its one), and of the
- * top_groups best groups the `top` best experts are chosen, best first; ties go to the lowest index. Choice values are compared in 64 bits.
+ * top_groups best groups the `top` best experts are chosen, best first; ties go to the lowest index. Choice values are compared in 64 bits (where a
+ * sigmoid score is 0 for logits below -709.78).
  *     weights w_j = scale s_j,  with `renormalize` w_j = scale s_j / (sum of the chosen s)   (sigmoid: + 1e-20),
  * go into indices and weights (t x top, contiguous). A logit (or bias) of -inf takes its expert out of the choice: it counts for nothing in its
  * group. Where fewer than `top` can be chosen the rest are index -1 with weight 0. A row with a NaN (for softmax, or a logit of +inf) has

@@ -483,7 +483,8 @@ __global__ void route_kernel(RouteArgs a, int* indices, float* weights) {
         // bits were zeros)
         const bool in_order = same && (lane < a.top || (TYPE != OZIMMU_F32 && !by_values));
         if (lane > 0 && lane <= a.top && mine != 0xffffffffu) unsure |= !apart(v, w) && !in_order;
-        if (!a.sigmoid && mine != 0xffffffffu) all |= top_logit - logit > 600.f;      // (64 bits have no score for it)
+        // Scores that 64 bits do not tell apart: softmax has none so far below the largest; sigmoid's are 0 below -709.8, whatever the logit.
+        if (mine != 0xffffffffu) all |= a.sigmoid ? !by_values && logit < -700.f : top_logit - logit > 600.f;
     }
     constexpr unsigned long long kMask = LANES == 64 ? ~0ull : (1ull << (LANES & 63)) - 1;
     const int row0 = (threadIdx.x & 63) / LANES * LANES;
