@@ -251,7 +251,8 @@ template <> struct Bits<double> {
 };
 
 // A group is `width` neighbouring lanes. From each lane's two largest values (-inf: none): whether its group is one of the best top_groups, by the
-// sum of its two. V = float: unsure where the last group kept and the next are too near each other to tell.
+// sum of its two. V = float: unsure where a group that is kept and one that is not are too near each other to tell. What a sum may be off by: its two
+// values' roundings and its own, 2^-24 of each, which outlast the sum where the two cancel, and the two scores' errors.
 template <int LANES, class V>
 __device__ __forceinline__ bool in_best_groups(const RouteArgs& a, int lane, bool there, int width, V first, V second, float near_scores, bool& unsure) {
     typedef typename Bits<V>::type bits;
@@ -260,22 +261,24 @@ __device__ __forceinline__ bool in_best_groups(const RouteArgs& a, int lane, boo
         second = max(max(second, g), min(first, f));
         first = max(first, f);
     }
-    const V sum = second == -INFINITY ? first : first + second;
-    bits key = there ? Bits<V>::of(sum) : 0, before = 0;
+    const bool one = second == -INFINITY;
+    const V sum = one ? first : first + second;
+    bits key = there ? Bits<V>::of(sum) : 0;
     bool keep = false;
-    for (int n = 0; n <= a.top_groups && n < a.groups; ++n) {
+    for (int n = 0; n < a.top_groups; ++n) {
         const bits best = most<LANES>(key);
-        if constexpr (sizeof(V) == 4) {   // (which ones are kept matters, not their order)
-            const float v = Bits<float>::value(before), w = Bits<float>::value(best);
-            unsure |= n == a.top_groups && best != 0 && !(v - w > 2.f * near_scores + (fabsf(v) + fabsf(w)) * 0x1p-21f);
-        }
-        before = best;
-        if (n == a.top_groups) break;
         const int at = (int)least<LANES>(key == best ? (unsigned)lane : 64u) / width;
         if (best != 0 && lane / width == at) {
             keep = true;
             key = 0;
         }
+    }
+    if constexpr (sizeof(V) == 4) {   // which ones are kept matters, not their order: the least that a kept one may be against the most that another may
+        const float off = 2.f * near_scores + fabsf(first) * 0x1p-22f + (one ? 0.f : fabsf(second) * 0x1p-22f);
+        const bool beyond = !(fabsf(sum) < INFINITY);
+        const float low = first == INFINITY ? INFINITY : beyond ? -INFINITY : sum - off, high = beyond ? sum : sum + off;
+        const float kept = -most<LANES>(keep ? -low : -INFINITY), other = most<LANES>(key != 0 ? high : -INFINITY);
+        unsure |= !(kept > other) && other > -INFINITY;
     }
     return keep;
 }
