@@ -252,7 +252,8 @@ template <> struct Bits<double> {
 
 // A group is `width` neighbouring lanes. From each lane's two largest values (-inf: none): whether its group is one of the best top_groups, by the
 // sum of its two. V = float: unsure where a group that is kept and one that is not are too near each other to tell. What a sum may be off by: its two
-// values' roundings and its own, 2^-24 of each, which outlast the sum where the two cancel, and the two scores' errors.
+// values' roundings and its own, 2^-24 of each, which outlast the sum where the two cancel, and the two scores' errors. A sum beyond 32 bits tells
+// nothing but its sign.
 template <int LANES, class V>
 __device__ __forceinline__ bool in_best_groups(const RouteArgs& a, int lane, bool there, int width, V first, V second, float near_scores, bool& unsure) {
     typedef typename Bits<V>::type bits;
@@ -261,8 +262,10 @@ __device__ __forceinline__ bool in_best_groups(const RouteArgs& a, int lane, boo
         second = max(max(second, g), min(first, f));
         first = max(first, f);
     }
+    constexpr float kMost = 0x1.fffffep127f;
     const bool one = second == -INFINITY;
-    const V sum = one ? first : first + second;
+    V sum = one ? first : first + second;
+    if constexpr (sizeof(V) == 4) sum = one ? sum : max(sum, -kMost);      // (-inf is a group of which nothing can be chosen)
     bits key = there ? Bits<V>::of(sum) : 0;
     bool keep = false;
     for (int n = 0; n < a.top_groups; ++n) {
@@ -275,7 +278,7 @@ __device__ __forceinline__ bool in_best_groups(const RouteArgs& a, int lane, boo
     }
     if constexpr (sizeof(V) == 4) {   // which ones are kept matters, not their order: the least that a kept one may be against the most that another may
         const float off = 2.f * near_scores + fabsf(first) * 0x1p-22f + (one ? 0.f : fabsf(second) * 0x1p-22f);
-        const bool beyond = !(fabsf(sum) < INFINITY);
+        const bool beyond = !(fabsf(sum) < kMost);
         const float low = first == INFINITY ? INFINITY : beyond ? -INFINITY : sum - off, high = beyond ? sum : sum + off;
         const float kept = -most<LANES>(keep ? -low : -INFINITY), other = most<LANES>(key != 0 ? high : -INFINITY);
         unsure |= !(kept > other) && other > -INFINITY;

@@ -1,5 +1,7 @@
-"""The choice of experts where 32-bit values do not show which groups are best: those whose two largest values nearly cancel.
-Against the plain form in 64 bits."""
+"""The choice of experts where 32-bit values do not show which groups are best: those whose two largest values nearly cancel, or whose sum 32 bits do not
+hold. Against the plain form in 64 bits."""
+import math
+
 import pytest
 import torch
 
@@ -8,6 +10,8 @@ from paper_2306_11975_amd import ozimmu as oz
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
+INF = math.inf
+LOWEST = torch.finfo(F32).min
 
 
 def gen(seed):
@@ -52,3 +56,25 @@ def test_groups_whose_values_nearly_cancel(experts, groups, top_groups, size, sc
         bias[1] *= 0.5
         bias[2, 0] = bias[2, 0] + 1.0
     check(logits, 2, score=score, groups=groups, top_groups=top_groups, bias=bias.view(-1))
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts,groups,top_groups", GROUPS)
+def test_groups_under_the_lowest_bias(experts, groups, top_groups, score):
+    """The lowest bias of 32 bits, or one next to it, is no -inf: where too few groups are without it, the sum of two of them still takes part."""
+    t, per = 60, experts // groups
+    g = gen(experts + 1)
+    logits = torch.randn(t, experts, generator=g)
+    top = min(2 * per, 15)
+    for low in (LOWEST, -2e38, -1.8e38):
+        for free in {0, 1, max(0, top_groups - 1), top_groups, min(groups, top_groups + 1)}:
+            bias = torch.full((groups, per), low)
+            for n, group in enumerate(torch.randperm(groups, generator=g)[:free].tolist()):
+                bias[group] = 0.1 * torch.randn(per, generator=g)
+                if n == 1:
+                    bias[group, 1:] = low      # one of its experts is free
+            check(logits, top, score=score, groups=groups, top_groups=top_groups, bias=bias.view(-1))
+    bias = torch.where(torch.rand(experts, generator=g) < 0.3, torch.tensor(INF), 0.1 * torch.randn(experts, generator=g))
+    bias[::7] = -INF
+    check(logits, top, score=score, groups=groups, top_groups=top_groups, bias=bias)
+    check(logits, top, score=score, groups=groups, top_groups=top_groups, bias=torch.where(torch.rand(experts, generator=g) < 0.5, 3e38, -3e38))
