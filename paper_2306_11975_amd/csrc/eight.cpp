@@ -46,7 +46,8 @@ enum { kGemm = 0, kGemmGrad = 1, kWeightGrad = 2 };
 // 13.6, 16 rows 12.6, 14.6, 32 22, 15; 16 experts of 2048 x 1024 8 rows 7.4, 10.2, 64 rows 12.5, 11.4. 32 bits: 2048 x 2048 64 rows 10.0, 11.4, 128 17,
 // 13; 8192 x 4096 16 rows 15.9, 15.6; 2048 x 8192 1 row 11.7, 13.3, 16 rows 21, 14. Given codes: 2048 x 2048 64 rows 7.1, 7.6; 8192 x 4096 16
 // rows 11.0, 11.3. The limit is where they meet, in weights read. (The answer turns once as rows grow, so that a workspace serves fewer.)
-bool few_rows(int64_t rows, int64_t n, int64_t k, int64_t experts) {
+bool few_rows(int op, int64_t rows, int64_t n, int64_t k, int64_t experts, int type) {
+    if (op == kGemm && type == OZIMMU_E4M3) k = f8_row_bytes(k);      // (a caller may know codes' length by whole runs alone, when sizing the workspace or when calling)
     const double runs = experts ? (double)(rows / 16 + std::min(experts, rows)) : rows <= 16 ? 0.5 : (double)((rows + 15) / 16);
     return runs * (double)n * (double)k <= 16777216.0;
 }
@@ -72,7 +73,7 @@ Layout layout(int op, int64_t t, int64_t rows, int64_t n, int64_t k, int64_t exp
         const int64_t inner = op == kGemm ? k : n;
         o.ldp = f8_row_bytes(inner);
         o.ldsp = f8_scale_bytes(inner);
-        if (type != OZIMMU_E4M3 && (op == kGemmGrad || !few_rows(rows, n, k, experts))) {
+        if (type != OZIMMU_E4M3 && (op == kGemmGrad || !few_rows(op, rows, n, k, experts, type))) {
             o.off_p = take((op == kGemm ? t : rows) * o.ldp);
             o.off_sp = take((op == kGemm ? t : rows) * o.ldsp);
         }
@@ -83,7 +84,7 @@ Layout layout(int op, int64_t t, int64_t rows, int64_t n, int64_t k, int64_t exp
             o.off_sq = take(e * f8_groups(k) * o.ldsq * 4);
         }
     }
-    if (experts == 0 && !(op != kWeightGrad && few_rows(rows, n, k, experts)))
+    if (experts == 0 && !(op != kWeightGrad && few_rows(op, rows, n, k, experts, type)))
         o.partial = op == kWeightGrad ? f8_partial_room(n, k, f8_groups(rows)) : f8_partial_room(rows, op == kGemm ? n : k, f8_groups(op == kGemm ? k : n));
     o.off_partial = take((int64_t)o.partial);
     o.total = off;
@@ -150,7 +151,7 @@ ozimmu_status_t f8_product(int op, int64_t t, int64_t rows, int64_t n, int64_t k
     a.v_type = type;
     a.ldv = ldv;
     a.k = inner;
-    const bool few = few_rows(rows, n, k, experts);
+    const bool few = few_rows(op, rows, n, k, experts, type);
     if (inner == 0 || t == 0) return hip_status(launch_f8_few(a, st));   // zeros
     a.slabs = (int)f8_groups(inner);
     hipError_t e = hipSuccess;
