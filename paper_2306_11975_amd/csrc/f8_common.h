@@ -142,6 +142,18 @@ __device__ __forceinline__ void scale_parts(const void* scales, int64_t at, floa
         m = byte == 255 ? __builtin_nanf("") : 1.0f;
     }
 }
+// The scale itself; a NaN where it is not finite.
+template <bool WIDE>
+__device__ __forceinline__ float scale_value(const void* scales, int64_t at) {
+    unsigned bits;
+    if constexpr (WIDE) {
+        bits = static_cast<const unsigned*>(scales)[at];
+    } else {
+        const unsigned byte = static_cast<const uint8_t*>(scales)[at];
+        bits = byte ? byte << 23 : 0x400000u;
+    }
+    return (bits >> 23 & 255u) == 255u ? __builtin_nanf("") : __uint_as_float(bits);
+}
 
 // ---- rows sorted by expert
 

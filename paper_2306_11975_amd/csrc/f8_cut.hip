@@ -91,13 +91,12 @@ __global__ void f8_expand_kernel(int64_t n, int64_t k, int shift, const uint8_t*
     const int64_t row0 = ((int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kRows, at = (int64_t)blockIdx.y * 512 + lane * 8;
     if (row0 >= n || at >= k) return;
     v2u c[kRows];
-    float m[kRows];
-    int byte[kRows];
+    float s[kRows];      // (32 bits hold 2^-127, as a subnormal value, and a product with any scale is rounded once)
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
         const int64_t row = min(row0 + i, n - 1);
         c[i] = *reinterpret_cast<const v2u*>(codes + row * ldq + at);
-        scale_parts<WIDE>(scales, (row >> shift) * lds + (at >> 7), m[i], byte[i]);
+        s[i] = scale_value<WIDE>(scales, (row >> shift) * lds + (at >> 7));
     }
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
@@ -107,7 +106,11 @@ __global__ void f8_expand_kernel(int64_t n, int64_t k, int shift, const uint8_t*
         values4(c[i][1], *reinterpret_cast<float(*)[4]>(f + 4));
         raw r[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) r[e] = Elem<TYPE>::store(__builtin_amdgcn_ldexpf(f[e] * m[i], byte[i] - 127));
+        for (int e = 0; e < 8; ++e) {
+            float x = f[e] * s[i];
+            asm("" : "+v"(x));      // (in one instruction with the rounding to fp16 the product would not be rounded to 32 bits first)
+            r[e] = Elem<TYPE>::store(x);
+        }
         raw* out = static_cast<raw*>(W) + (row0 + i) * ldw + at;
         if (at + 8 <= k) {
             *reinterpret_cast<v4u_any*>(out) = *reinterpret_cast<const v4u*>(r);
