@@ -444,7 +444,7 @@ ozimmu_status_t ozimmu_orthogonalize(int64_t batch, int64_t m, int64_t n, ozimmu
  *           ozimmu_f8_split writes them). ldq (bytes between rows) is at least that and a multiple of 16; codes are 16-byte aligned.
  *   scales  ceil(n / block_rows) rows. OZIMMU_E8M0: a byte e + 127 for each 128 positions; a row has scale_bytes = 4 ceil(k / 512) bytes, of which
  *           those beyond the last block are ignored (the cut writes zeros); lds is a multiple of four, the array four-byte aligned.
- *           OZIMMU_F32 (weights only, made elsewhere): any 32-bit values, lds >= ceil(k / 128).
+ *           OZIMMU_F32 (weights only, made elsewhere): any 32-bit values, an infinity counting as a NaN; lds >= ceil(k / 128).
  * ozimmu_f8_split cuts W (n x k; `type`, ldw values between rows). ozimmu_f8_expand writes the values c s as `type`; with 32-bit scales the
  * product is rounded to 32 bits first.
  *
