@@ -238,7 +238,7 @@ __launch_bounds__(kThreads)
 __global__ void combine_grad_kernel(int top, int rows, int64_t n, const void* dY, int64_t lddy, const void* O, int64_t ldo, const int* place, const float* weights, void* dO, int64_t lddo,
                                     float* dweights, int64_t pairs) {
     const int lane = threadIdx.x & 63;
-    const int64_t pair = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t pair = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (pair >= pairs) return;
     const int64_t token = (unsigned)pair / (unsigned)top;
     const int row = place[pair];
@@ -304,8 +304,8 @@ hipError_t launch_expert_combine(int t, int top, int rows, int64_t n, int type, 
 
 hipError_t launch_expert_combine_grad(int t, int top, int rows, int64_t n, int type, const void* dY, int64_t lddy, const void* O, int64_t ldo, const int* place, const float* weights, void* dO,
                                       int64_t lddo, float* dweights, hipStream_t st) {
-    const int64_t pairs = (int64_t)t * top;
-    const dim3 grid((unsigned)((pairs + 3) / 4));
+    const int64_t pairs = (int64_t)t * top, blocks = (pairs + 3) / 4, across = std::min<int64_t>(blocks, 1 << 23);      // (2^32 threads are too many for one dimension)
+    const dim3 grid((unsigned)across, (unsigned)((blocks + across - 1) / across));
     return by_type(type, [&](auto kind) {
         combine_grad_kernel<decltype(kind)::value><<<grid, dim3(kThreads), 0, st>>>(top, rows, n, dY, lddy, O, ldo, place, weights, dO, lddo, dweights, pairs);
     });
