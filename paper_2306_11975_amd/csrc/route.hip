@@ -486,8 +486,8 @@ __global__ void route_kernel(RouteArgs a, int* indices, float* weights) {
         const float v = Bits<float>::value((unsigned)__shfl_up((int)mine_bits, 1)), w = Bits<float>::value(mine_bits);
         const bool same = __shfl_up(logit, 1) == logit && __shfl_up(bias, 1) == bias;
         // (of equals the lowest came first; but behind the last chosen and its equal there may be a larger one yet, unless the values' lost
-        // bits were zeros)
-        const bool in_order = same && (lane < a.top || (TYPE != OZIMMU_F32 && !by_values));
+        // bits were zeros, or one with the same score in 64 bits, unless the next value of the type is apart: 16-bit ones are, from 1e-6 on)
+        const bool in_order = same && (lane < a.top || (TYPE != OZIMMU_F32 && !by_values && fabsf(w) > 1e-6f));
         if (lane > 0 && lane <= a.top && mine != 0xffffffffu) unsure |= !apart(v, w) && !in_order;
         // Scores that 64 bits do not tell apart: softmax has none so far below the largest; sigmoid's are 0 below -709.8, whatever the logit.
         if (mine != 0xffffffffu) all |= a.sigmoid ? !by_values && logit < -700.f : top_logit - logit > 600.f;
