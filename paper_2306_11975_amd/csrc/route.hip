@@ -484,7 +484,8 @@ __global__ void route_kernel(RouteArgs a, int* indices, float* weights) {
             if (a.bias) bias = a.bias[mine];
         }
         const float v = Bits<float>::value((unsigned)__shfl_up((int)mine_bits, 1)), w = Bits<float>::value(mine_bits);
-        const bool same = __shfl_up(logit, 1) == logit && __shfl_up(bias, 1) == bias;
+        const float logit_before = __shfl_up(logit, 1), bias_before = __shfl_up(bias, 1);      // (of all lanes: behind a condition they would be of some)
+        const bool same = logit_before == logit && bias_before == bias;
         // (of equals the lowest came first; but behind the last chosen and its equal there may be a larger one yet, unless the values' lost
         // bits were zeros, or one with the same score in 64 bits, unless the next value of the type is apart: 16-bit ones are, from 1e-6 on)
         const bool in_order = same && (lane < a.top || (TYPE != OZIMMU_F32 && !by_values && fabsf(w) > 1e-6f));
@@ -509,7 +510,8 @@ __global__ void route_kernel(RouteArgs a, int* indices, float* weights) {
         int before = 0;
         for (int j = 0; j <= a.top; ++j) {
             const double other = __shfl(d, row0 + j);
-            before += other > d || (other == d && (unsigned)__shfl((int)mine, row0 + j) < mine);
+            const unsigned expert = (unsigned)__shfl((int)mine, row0 + j);
+            before += other > d || (other == d && expert < mine);
             all |= mine_doubt && !a.sigmoid && other != d && fabs(other - d) < 1e-9;
         }
         unsigned sure = 0xffffffffu;
