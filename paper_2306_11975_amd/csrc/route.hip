@@ -477,6 +477,8 @@ __global__ void route_kernel(RouteArgs a, int* indices, float* weights) {
         mine = lane == j ? winner : mine;
         mine_bits = lane == j ? best : mine_bits;
     }
+    constexpr unsigned long long kMask = LANES == 64 ? ~0ull : (1ull << (LANES & 63)) - 1;
+    const int row0 = (threadIdx.x & 63) / LANES * LANES;
     float logit = -INFINITY, bias = 0.f;
     {   // neighbours: lane j against lane j - 1
         if (mine != 0xffffffffu) {
@@ -487,14 +489,19 @@ __global__ void route_kernel(RouteArgs a, int* indices, float* weights) {
         const float logit_before = __shfl_up(logit, 1), bias_before = __shfl_up(bias, 1);      // (of all lanes: behind a condition they would be of some)
         const bool same = logit_before == logit && bias_before == bias;
         // (of equals the lowest came first; but behind the last chosen and its equal there may be a larger one yet, unless the values' lost
-        // bits were zeros, or one with the same score in 64 bits, unless the next value of the type is apart: 16-bit ones are, from 1e-6 on)
-        const bool in_order = same && (lane < a.top || (TYPE != OZIMMU_F32 && !by_values && fabsf(w) > 1e-6f));
+        // bits were zeros; and a smaller one with the same score in 64 bits, unless no other logit is that near: 16-bit ones are not, from 1e-6 on)
+        bool near_other = false;
+        if (TYPE != OZIMMU_F32 && !by_values && __builtin_amdgcn_ballot_w64(lane == a.top && same && fabsf(logit) <= 1e-6f)) {   // (the same for the wavefront)
+            const float last = __shfl(logit, row0 + a.top);
+#pragma unroll
+            for (int k = 0; k < SLOTS; ++k) near_other |= l[k] != last && fabsf(l[k] - last) < 2e-9f;
+            near_other = (__builtin_amdgcn_ballot_w64(near_other) >> row0 & kMask) != 0;
+        }
+        const bool in_order = same && (lane < a.top || (TYPE != OZIMMU_F32 && !by_values && !near_other));
         if (lane > 0 && lane <= a.top && mine != 0xffffffffu) unsure |= !apart(v, w) && !in_order;
         // Scores that 64 bits do not tell apart: softmax has none so far below the largest; sigmoid's are 0 below -709.8, whatever the logit.
         if (mine != 0xffffffffu) all |= a.sigmoid ? !by_values && logit < -700.f : top_logit - logit > 600.f;
     }
-    constexpr unsigned long long kMask = LANES == 64 ? ~0ull : (1ull << (LANES & 63)) - 1;
-    const int row0 = (threadIdx.x & 63) / LANES * LANES;
     bad = (__builtin_amdgcn_ballot_w64(bad) >> row0 & kMask) != 0;
     const unsigned long long doubt = __builtin_amdgcn_ballot_w64(unsure && !bad);
     if (doubt) {   // (the same for the wavefront)
