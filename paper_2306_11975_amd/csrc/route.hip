@@ -320,7 +320,7 @@ __device__ __forceinline__ unsigned choose_exactly(const RouteArgs& a, int lane,
     return mine;
 }
 
-// A sorting network: pairs of places, the larger value to the first (merges of odd and even halves).
+// A sorting network, Batcher's odd-even merge sort (1968): pairs of places, the larger value to the first.
 template <int N>
 struct Network {
     int first[80], second[80], count;
@@ -371,7 +371,7 @@ struct Sorted {
 };
 
 // LANES lanes to a token (16: four tokens a wavefront), experts lane * SLOTS + k. The choice goes by 32-bit values where their order is beyond
-// doubt: without a bias and groups by the logits themselves, whose order the scores have, else by scores that are off by less than 2^-20 of the
+// doubt: without a bias and groups by the logits themselves, whose order the scores have (sigmoid's down to -700), else by scores that are off by less than 2^-20 of the
 // largest, plus their bias. Where two neighbours among the best top + 1 are as near as that, and not equal in all that they come from, those
 // top + 1 are put in order by their 64-bit values (at 256 experts with sigmoid scores and a bias one token in some hundreds); where the last
 // group kept and the next are as near (one token in some ten thousands), the groups by the 64-bit values of their best; where those top + 1 need
